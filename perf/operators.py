@@ -1,0 +1,389 @@
+"""The norms around the expert layer, microscaled 4-bit quantisation and the experts in four bits, for timing: what a program
+that trains or serves a block h -> norm -> experts -> norm + residual calls beside the layer itself.
+
+A case's "op" is one of
+
+  norm_fwd   h' = alpha h + beta g u, u = the (normalised and weighted) output y of a block, and n = norm(h') of the next block
+  norm_bwd   its gradient in y, h, g and both weights, from the saved h' and the rows' 1/rms
+  mx4        values to microscaled 4 bits (e2m1, one power-of-two scale per 32 along the contraction) and back: tokens in their
+             rows, or weights [e, K, N] along K
+  experts    the experts' forward for serving: rows and activations in microscaled 4 bits against weights in them
+
+Sizes are those of workloads.py's configurations or generic.
+"""
+import math
+
+import torch
+
+own = False
+
+MX = 32                 # elements that share a scale
+EPS = 1e-6
+
+
+# --------------------------------------------------------------------------------------------------------- cases
+def _norm(op, T, d, dtype="bf16", residual="bf16", post_norm=True, w_post=True, gate=False, alpha=1.0, beta=1.0):
+    return dict(op=op, T=T, d=d, dtype=dtype, residual=residual, post_norm=post_norm, w_post=w_post, gate=gate, alpha=alpha, beta=beta)
+
+
+def _mx4(batch, rows, cols, dtype="bf16", along_rows=False):
+    return dict(op="mx4", batch=batch, rows=rows, cols=cols, dtype=dtype, along_rows=along_rows)
+
+
+def _experts(T, d, f, E, e_cnt, k, zipf):
+    return dict(op="experts", T=T, d=d, f=f, E=E, e_cnt=e_cnt, k=k, zipf=zipf)
+
+
+def listed():
+    cases = {
+        # one decode step of a small batch between two blocks: latency counts
+        "norm-fwd-decode-t4": _norm("norm_fwd", 4, 4096),
+        # an fp32 layer of a size that one debugs with, odd token count, hidden size off the tiles, no norm behind the block
+        "norm-fwd-fp32-t1500": _norm("norm_fwd", 1500, 520, "f32", "f32", post_norm=False, w_post=False, beta=0.5),
+        # a training step's tokens with the residual stream in fp32 and a gate on the block
+        "norm-fwd-t32768": _norm("norm_fwd", 32768, 7168, residual="f32", gate=True),
+        # one odd prompt's gradient at a hidden size that is no power of two
+        "norm-bwd-t2047": _norm("norm_bwd", 2047, 2880, gate=True, alpha=0.5),
+        # a training step's gradient
+        "norm-bwd-t16384": _norm("norm_bwd", 16384, 4096, residual="f32"),
+        # tokens of one odd prompt on their way to 4-bit experts
+        "mx4-tokens-t2047": _mx4(1, 2047, 2880),
+        # one weight tensor of a share, laid out along its contraction
+        "mx4-weights-16x4096x1536": _mx4(16, 4096, 1536, along_rows=True),
+        # a decode step of a few tokens: two or three experts with a row each
+        "experts-decode-t4": _experts(4, 4096, 1536, 128, 16, 8, 1.0),
+        # a decode step of a large serving batch on the largest share: reading 0.75 GB of weights
+        "experts-decode-t128": _experts(128, 7168, 2048, 256, 32, 8, 1.0),
+        # prefill of one prompt of odd length, contraction no multiple of the tiles
+        "experts-prefill-t2047": _experts(2047, 2880, 2880, 128, 16, 4, 1.0),
+        # few large experts, all local
+        "experts-prefill-8x14336": _experts(4096, 4096, 14336, 8, 8, 2, 0.3),
+        # a large prefill batch on the largest share
+        "experts-prefill-t16384": _experts(16384, 7168, 2048, 256, 32, 8, 1.0),
+    }
+    return [dict(case, name=name) for name, case in cases.items()]
+
+
+def _log_int(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def draw(rng):
+    op = rng.choice(("norm_fwd", "norm_bwd", "mx4", "mx4", "experts", "experts", "experts"))
+    if op in ("norm_fwd", "norm_bwd"):
+        dtype = rng.choice(("bf16", "bf16", "f32"))
+        return _norm(op, _log_int(rng, 1, 16384), 8 * _log_int(rng, 8, 896), dtype, "f32" if dtype == "f32" else rng.choice(("bf16", "f32")),
+                     post_norm=rng.random() < 0.7, w_post=rng.random() < 0.7, gate=rng.random() < 0.5,
+                     alpha=rng.choice((1.0, 0.5)), beta=rng.choice((1.0, 0.25)))
+    if op == "mx4":
+        dtype = rng.choice(("bf16", "bf16", "f32"))
+        if rng.random() < 0.5:
+            return _mx4(1, _log_int(rng, 1, 16384), 32 * _log_int(rng, 2, 224), dtype)
+        return _mx4(_log_int(rng, 1, 16), 32 * _log_int(rng, 2, 128), 32 * _log_int(rng, 2, 128), dtype, along_rows=True)
+    d, f, E, e_cnt, k = rng.choice(((2048, 768, 128, 16, 8), (2048, 1408, 64, 8, 4), (2880, 2880, 128, 16, 4), (4096, 1536, 128, 16, 8),
+                                    (7168, 2048, 256, 32, 8), (4096, 14336, 8, 8, 2), None, None)) or (0, 0, 0, 0, 0)
+    if not d:       # a share of no particular model
+        E = rng.choice((8, 16, 32, 64, 96, 128, 256))
+        d, f, e_cnt, k = 32 * rng.randrange(16, 161), 32 * rng.randrange(16, 129), max(4, E // rng.choice((1, 4, 8))), rng.choice((1, 2, 4, 8))
+    return _experts(_log_int(rng, 1, 4096), d, f, E, e_cnt, k, rng.choice((0.0, 0.5, 1.0)))
+
+
+# --------------------------------------------------------------------------------------------------------- inputs
+class _State:
+    pass
+
+
+def _dtype(name):
+    return torch.bfloat16 if name == "bf16" else torch.float32
+
+
+def _scale_shape(K, n):
+    """Scales of n rows of K elements: four 32-element blocks of a row are four bytes side by side."""
+    return ((K + 127) // 128, n, 4)
+
+
+def _pack(x):
+    """x [n, K] fp32 -> bytes [n, K/2] (even elements in the low half) and scales [ceil(K/128), n, 4], both uint8."""
+    n, K = x.shape
+    q, s = _mx4_parts(x)
+    mag = q.abs()
+    code = torch.where(mag < 2, 2 * mag, torch.where(mag < 4, mag + 2, mag / 2 + 4)).to(torch.uint8) + 8 * torch.signbit(q).to(torch.uint8)
+    code = code.reshape(n, K)
+    blocks = torch.zeros((n, 4 * ((K + 127) // 128)), dtype=torch.uint8, device=x.device)
+    blocks[:, :K // MX] = (s + 127).reshape(n, K // MX).to(torch.uint8)
+    return code[:, 0::2] | code[:, 1::2] << 4, blocks.reshape(n, -1, 4).transpose(0, 1).contiguous()
+
+
+def _rows_of(case):
+    """Rows of each local expert, the same for all inputs of a case (they are the outputs' shape): the top k of N(0,1) logits with
+    a popularity by rank, experts' ranks in a drawn order."""
+    E = case["E"]
+    g = torch.Generator(device="cuda").manual_seed(case["T"] + E)
+    rank = torch.randperm(E, generator=g, device="cuda") + 1
+    logits = torch.randn((case["T"], E), generator=g, device="cuda") - case["zipf"] * rank.float().log()
+    rows = torch.bincount(logits.topk(case["k"], dim=1).indices.reshape(-1), minlength=E)[:case["e_cnt"]]
+    if not int(rows.sum()):         # a share that none of the tokens reached would make no call
+        rows[0] = 1
+    return rows
+
+
+def prepare(case, seed):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    s = _State()
+    s.case = case
+    randn = lambda *shape: torch.randn(shape, generator=g, device="cuda")  # noqa: E731
+    empty = lambda *shape, dtype: torch.empty(shape, device="cuda", dtype=dtype)  # noqa: E731
+    if case["op"] in ("norm_fwd", "norm_bwd"):
+        T, d = case["T"], case["d"]
+        dt, rt = _dtype(case["dtype"]), _dtype(case["residual"])
+        s.y, s.h = (0.5 * randn(T, d)).to(dt), (2.0 * randn(T, d)).to(rt)
+        s.gate = torch.sigmoid(randn(T)) if case["gate"] else None
+        s.w_post = (1.0 + 0.1 * randn(d)).to(dt) if case["w_post"] else None
+        s.w_pre = (1.0 + 0.1 * randn(d)).to(dt)
+        s.h_out, s.n = empty(T, d, dtype=rt), empty(T, d, dtype=dt)
+        if case["op"] == "norm_bwd":
+            h, n, s.r_post, s.r_pre = _norm_fwd(s)
+            s.h_out.copy_(h)
+            del s.h
+            s.dn, s.dh_out = randn(T, d).to(dt), randn(T, d).to(rt)
+            s.dh, s.dy = empty(T, d, dtype=rt), empty(T, d, dtype=dt)
+            s.dgate = empty(T, dtype=torch.float32) if case["gate"] else None
+            s.dw_post, s.dw_pre = (empty(d, dtype=dt) if case["w_post"] else None), empty(d, dtype=dt)
+            s.ws = empty(_ws_norm(T, d), dtype=torch.uint8)
+    elif case["op"] == "mx4":
+        b, r, c = case["batch"], case["rows"], case["cols"]
+        dt = _dtype(case["dtype"])
+        # weights ~ N(0, 1/K); hidden states with channels of very different size
+        s.x = (randn(b, r, c) * r ** -0.5 if case["along_rows"] else randn(b, r, c) * torch.exp(randn(c))).to(dt)
+        n, K = (c, r) if case["along_rows"] else (r, c)
+        s.q, s.scales = empty(b, n, K // 2, dtype=torch.uint8), empty(b, *_scale_shape(K, n), dtype=torch.uint8)
+        s.values = empty(b, n, K, dtype=dt)
+    else:
+        d, f, e_cnt = case["d"], case["f"], case["e_cnt"]
+        rows = _rows_of(case)
+        s.rows = rows.tolist()
+        R = sum(s.rows)
+        s.offsets = torch.zeros(e_cnt + 1, dtype=torch.int32, device="cuda")
+        s.offsets[1:] = rows.cumsum(0)
+        cap = R + R // 20 + 8
+        s.xp = (randn(cap, d) * torch.exp(0.5 * randn(d))).to(torch.bfloat16)
+        s.w = {}
+        for name, n, K in (("w1", f, d), ("w3", f, d), ("w2", d, f)):
+            parts = [_pack((randn(n, K) * K ** -0.5).to(torch.bfloat16).float()) for _ in range(e_cnt)]
+            s.w[name] = torch.stack([p[0] for p in parts]), torch.stack([p[1] for p in parts])
+        s.o = empty(cap, d, dtype=torch.bfloat16)
+        s.ws = empty(_ws_experts(cap, d, f), dtype=torch.uint8)
+    return s
+
+
+def _ws_norm(T, d):
+    return 256 + 2 * 1024 * 4 * (d + 64)
+
+
+def _ws_experts(cap, d, f):
+    K = 256 * ((d + 255) // 256) + 256 * ((f + 255) // 256)
+    return (1 << 20) + (cap + 1) * K * 17 // 32
+
+
+# --------------------------------------------------------------------------------------------------------- plain forms
+def _rms(x):
+    return torch.rsqrt(x.square().mean(dim=1, keepdim=True) + EPS)
+
+
+def _norm_fwd(s):
+    case, y, h = s.case, s.y.float(), s.h.float()
+    r_post = _rms(y) if case["post_norm"] else None
+    u = y * r_post if case["post_norm"] else y
+    if s.w_post is not None:
+        u = u * s.w_post.float()
+    if s.gate is not None:
+        u = u * s.gate[:, None]
+    h = case["alpha"] * h + case["beta"] * u
+    r_pre = _rms(h)
+    return h, h * r_pre * s.w_pre.float(), None if r_post is None else r_post[:, 0], r_pre[:, 0]
+
+
+def _norm_bwd(s):
+    case, y, h, dn = s.case, s.y.float(), s.h_out.float(), s.dn.float()
+    r = s.r_pre[:, None]
+    t = dn * s.w_pre.float()
+    gh = s.dh_out.float() + r * t - h * r.pow(3) * (t * h).mean(dim=1, keepdim=True)
+    out = {"dh": (case["alpha"] * gh).to(s.dh.dtype), "dw_pre": (dn * h * r).sum(dim=0).to(s.dn.dtype)}
+    norm = y * s.r_post[:, None] if case["post_norm"] else y
+    u = norm if s.w_post is None else norm * s.w_post.float()
+    du = case["beta"] * gh
+    if s.gate is not None:
+        out["dgate"] = (du * u).sum(dim=1)
+        du = du * s.gate[:, None]
+    if s.w_post is not None:
+        out["dw_post"] = (du * norm).sum(dim=0).to(s.dn.dtype)
+        du = du * s.w_post.float()
+    if case["post_norm"]:
+        r = s.r_post[:, None]
+        du = r * du - y * r.pow(3) * (du * y).mean(dim=1, keepdim=True)
+    out["dy"] = du.to(s.dy.dtype)
+    return out
+
+
+def _mx4_parts(x):
+    """x [..., K] -> elements [..., K/32, 32] as values of e2m1, and the exponents [..., K/32, 1] of their scales."""
+    b = x.unflatten(-1, (-1, MX))
+    top = b.abs().amax(dim=-1, keepdim=True)
+    s = torch.where(top > 0, torch.frexp(top).exponent - 3, -127).clamp(-127, 127)
+    v = torch.ldexp(b, -s)
+    mag = v.abs()
+    step = torch.where(mag < 2, 0.5, torch.where(mag < 4, 1.0, 2.0))
+    return torch.copysign((torch.round(mag / step) * step).clamp(max=6.0), v), s
+
+
+def _mx4_values(x):
+    q, s = _mx4_parts(x)
+    return torch.ldexp(q, s).flatten(-2)
+
+
+def _weights(q, scales):
+    """Bytes [n, K/2] and scales [ceil(K/128), n, 4] -> values [n, K] in fp32."""
+    n, K = q.shape[0], 2 * q.shape[1]
+    table = torch.tensor([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0, -0.0, -0.5, -1.0, -1.5, -2.0, -3.0, -4.0, -6.0], device=q.device)
+    code = torch.stack((q & 15, q >> 4), dim=2).reshape(n, K)
+    s = scales.transpose(0, 1).reshape(n, -1)[:, :K // MX].int() - 127
+    return torch.ldexp(table[code.int()].unflatten(1, (-1, MX)), s[:, :, None]).flatten(1)
+
+
+def _experts_plain(s):
+    out, row = [], 0
+    for e, rows in enumerate(s.rows):           # experts differ in rows: one product after the other
+        if rows:
+            w1, w3, w2 = (_weights(s.w[name][0][e], s.w[name][1][e]) for name in ("w1", "w3", "w2"))
+            x = _mx4_values(s.xp[row:row + rows].float())
+            h1 = x @ w1.t()
+            a = h1 / (1 + torch.exp(-h1)) * (x @ w3.t())
+            out.append((_mx4_values(a) @ w2.t()).to(torch.bfloat16))
+            row += rows
+    return torch.cat(out)
+
+
+def _plain(s):
+    case = s.case
+    if case["op"] == "norm_fwd":
+        h, n, _, _ = _norm_fwd(s)
+        return {"h_out": h.to(s.h_out.dtype), "n": n.to(s.n.dtype)}
+    if case["op"] == "norm_bwd":
+        return _norm_bwd(s)
+    if case["op"] == "mx4":
+        x = s.x.transpose(1, 2) if case["along_rows"] else s.x
+        return {"values": _mx4_values(x.float()).to(s.x.dtype)}
+    return {"o": _experts_plain(s)}
+
+
+# --------------------------------------------------------------------------------------------------------- a pass
+def run(s):
+    if not own:
+        return _plain(s)
+    from paper_2605_11005_amd import binding as B
+    case = s.case
+    if case["op"] == "norm_fwd":
+        B.moe_block_norm_fwd(s.y, s.gate, s.w_post, case["post_norm"], s.h, s.w_pre, case["alpha"], case["beta"], EPS, s.h_out, s.n)
+        return {"h_out": s.h_out, "n": s.n}
+    if case["op"] == "norm_bwd":
+        B.moe_block_norm_bwd(s.y, s.gate, s.w_post, case["post_norm"], s.h_out, s.w_pre, s.r_post, s.r_pre, s.dh_out, s.dn,
+                             case["alpha"], case["beta"], s.dh, s.dy, s.dgate, s.dw_post, s.dw_pre, False, s.ws)
+        out = {"dh": s.dh, "dy": s.dy, "dgate": s.dgate, "dw_post": s.dw_post, "dw_pre": s.dw_pre}
+        return {name: t for name, t in out.items() if t is not None}
+    if case["op"] == "mx4":
+        B.moe_mx4_quantize(s.x, case["along_rows"], s.q, s.scales)
+        B.moe_mx4_dequantize(s.q, s.scales, s.values)
+        return {"values": s.values}
+    (q1, s1), (q3, s3), (q2, s2) = s.w["w1"], s.w["w3"], s.w["w2"]
+    B.moe_mx4_expert_fwd(s.xp, s.offsets, q1, s1, q3, s3, q2, s2, s.o, s.ws)
+    return {"o": s.o[:sum(s.rows)]}
+
+
+def _expected_rows(case):
+    """Expected rows of each expert of the layer, popularity taken as proportional to rank^-zipf and no expert above T rows."""
+    p = [r ** -case["zipf"] for r in range(1, case["E"] + 1)]
+    return [min(1.0, case["k"] * v / sum(p)) * case["T"] for v in p]
+
+
+def work(case):
+    """Inputs read once, outputs written once; of the experts' weights those of experts that have rows."""
+    size = {"bf16": 2, "f32": 4}
+    if case["op"] in ("norm_fwd", "norm_bwd"):
+        pair = size[case["dtype"]] + size[case["residual"]]
+        elements = case["T"] * case["d"]
+        fwd = case["op"] == "norm_fwd"
+        # forward: y, h -> h', n.  backward: y, h', dn, dh' -> dy, dh
+        return {"bytes": (2 * pair if fwd else 3 * pair) * elements + (4 * case["T"] if case["gate"] else 0), "flops": (10 if fwd else 25) * elements}
+    if case["op"] == "mx4":
+        elements = case["batch"] * case["rows"] * case["cols"]
+        return {"bytes": elements * (2 * size[case["dtype"]] + 17 / 32), "flops": 4 * elements}
+    rows = _expected_rows(case)
+    share = case["e_cnt"] / case["E"]
+    R, active = sum(rows) * share, sum(1 - math.exp(-r) for r in rows) * share
+    return {"bytes": active * 3 * case["d"] * case["f"] * 17 / 32 + R * case["d"] * 4, "flops": 6 * R * case["d"] * case["f"]}
+
+
+# --------------------------------------------------------------------------------------------------------- in 64 bits
+def _exact_norm(s, case):
+    y = s.y.double().requires_grad_()
+    g = torch.ones(case["T"], dtype=torch.float64, device="cuda") if s.gate is None else s.gate.double()
+    w_post = torch.ones(case["d"], dtype=torch.float64, device="cuda") if s.w_post is None else s.w_post.double()
+    w_pre = s.w_pre.double()
+    for t in (g, w_post, w_pre):
+        t.requires_grad_()
+
+    def branch():
+        u = y / (y.pow(2).sum(dim=1, keepdim=True) / case["d"] + EPS).sqrt() if case["post_norm"] else y
+        return case["beta"] * (g.unsqueeze(1) * (u * w_post))
+
+    def normed(h):
+        return h / (h.pow(2).sum(dim=1, keepdim=True) / case["d"] + EPS).sqrt() * w_pre
+
+    if case["op"] == "norm_fwd":
+        with torch.no_grad():
+            h = case["alpha"] * s.h.double() + branch()
+            return {"h_out": h, "n": normed(h)}
+    h = s.h_out.double().requires_grad_()
+    through, dw_pre = torch.autograd.grad(normed(h), (h, w_pre), s.dn.double())
+    gh = through + s.dh_out.double()
+    dy, dgate, dw_post = torch.autograd.grad(branch(), (y, g, w_post), gh)
+    out = {"dh": case["alpha"] * gh, "dy": dy, "dw_pre": dw_pre}
+    if s.gate is not None:
+        out["dgate"] = dgate
+    if s.w_post is not None:
+        out["dw_post"] = dw_post
+    return out
+
+
+def _exact_mx4(x):
+    """x [..., K] in 64 bits -> the nearest values of e2m1 times the block's scale; halfway to the even one of the eight."""
+    grid = torch.tensor([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0], dtype=torch.float64, device=x.device)
+    between = (grid[1:] + grid[:-1]) / 2
+    b = x.reshape(*x.shape[:-1], x.shape[-1] // MX, MX)
+    top = b.abs().max(dim=-1, keepdim=True).values
+    s = torch.floor(torch.log2(top.clamp(min=2.0 ** -140)))
+    s = torch.where(torch.exp2(s) > top, s - 1, torch.where(torch.exp2(s + 1) <= top, s + 1, s))       # (log2 rounds)
+    scale = torch.exp2((s - 2).clamp(-127, 127))
+    mag = (b / scale).abs()
+    at = torch.bucketize(mag, between)                          # halfway: the lower neighbour
+    up = (at < 7) & (mag == between[at.clamp(max=6)]) & (at % 2 == 1)
+    return (torch.sign(b) * grid[at + up.long()] * scale).reshape(x.shape)
+
+
+def exact(case, seed):
+    s = prepare(case, seed)
+    if case["op"] in ("norm_fwd", "norm_bwd"):
+        return _exact_norm(s, case)
+    if case["op"] == "mx4":
+        x = s.x.mT if case["along_rows"] else s.x
+        return {"values": torch.stack([_exact_mx4(m.double()) for m in x])}
+    o = torch.zeros((sum(s.rows), case["d"]), dtype=torch.float64, device="cuda")
+    row = 0
+    for e, rows in enumerate(s.rows):
+        if rows:
+            w1, w3, w2 = (_weights(s.w[name][0][e], s.w[name][1][e]).double() for name in ("w1", "w3", "w2"))
+            x = _exact_mx4(s.xp[row:row + rows].double())
+            h1 = x @ w1.mT
+            o[row:row + rows] = _exact_mx4(h1 * torch.sigmoid(h1) * (x @ w3.mT)) @ w2.mT
+            row += rows
+    return {"o": o}
