@@ -97,21 +97,24 @@ def _dtype(name):
     return torch.bfloat16 if name == "bf16" else torch.float32
 
 
-def _scale_shape(K, n):
-    """Scales of n rows of K elements: four 32-element blocks of a row are four bytes side by side."""
-    return ((K + 127) // 128, n, 4)
+def _tile_shapes(n, K):
+    """The library's layout of n rows of K elements in 4 bits: tiles of 16 rows by 128 elements, in them 32-element chunk, row, 16
+    bytes; scales of 16 rows by 512 elements, in them chunk of the 128, row, 128 of the 512.  What is past n or K is zero."""
+    return ((n + 15) // 16, (K + 127) // 128, 4, 16, 16), ((n + 15) // 16, (K + 511) // 512, 4, 16, 4)
 
 
 def _pack(x):
-    """x [n, K] fp32 -> bytes [n, K/2] (even elements in the low half) and scales [ceil(K/128), n, 4], both uint8."""
-    n, K = x.shape
+    """x [n, K] fp32 -> its tiles of bytes (even elements in the low half) and of scales, both uint8."""
+    (n, K), ((nt, kt, _, _, _), (_, st, _, _, _)) = x.shape, _tile_shapes(*x.shape)
     q, s = _mx4_parts(x)
     mag = q.abs()
     code = torch.where(mag < 2, 2 * mag, torch.where(mag < 4, mag + 2, mag / 2 + 4)).to(torch.uint8) + 8 * torch.signbit(q).to(torch.uint8)
-    code = code.reshape(n, K)
-    blocks = torch.zeros((n, 4 * ((K + 127) // 128)), dtype=torch.uint8, device=x.device)
-    blocks[:, :K // MX] = (s + 127).reshape(n, K // MX).to(torch.uint8)
-    return code[:, 0::2] | code[:, 1::2] << 4, blocks.reshape(n, -1, 4).transpose(0, 1).contiguous()
+    codes = torch.zeros((16 * nt, 128 * kt), dtype=torch.uint8, device=x.device)
+    codes[:n, :K] = code.flatten(1)
+    blocks = torch.zeros((16 * nt, 16 * st), dtype=torch.uint8, device=x.device)
+    blocks[:n, :K // MX] = (s + 127).flatten(1).to(torch.uint8)
+    data = codes[:, 0::2] | codes[:, 1::2] << 4
+    return (data.view(nt, 16, kt, 4, 16).permute(0, 2, 3, 1, 4).contiguous(), blocks.view(nt, 16, st, 4, 4).permute(0, 2, 4, 1, 3).contiguous())
 
 
 def _rows_of(case):
@@ -156,7 +159,7 @@ def prepare(case, seed):
         # weights ~ N(0, 1/K); hidden states with channels of very different size
         s.x = (randn(b, r, c) * r ** -0.5 if case["along_rows"] else randn(b, r, c) * torch.exp(randn(c))).to(dt)
         n, K = (c, r) if case["along_rows"] else (r, c)
-        s.q, s.scales = empty(b, n, K // 2, dtype=torch.uint8), empty(b, *_scale_shape(K, n), dtype=torch.uint8)
+        s.q, s.scales = (empty(b, *shape, dtype=torch.uint8) for shape in _tile_shapes(n, K))
         s.values = empty(b, n, K, dtype=dt)
     else:
         d, f, e_cnt = case["d"], case["f"], case["e_cnt"]
@@ -167,12 +170,12 @@ def prepare(case, seed):
         s.offsets[1:] = rows.cumsum(0)
         cap = R + R // 20 + 8
         s.xp = (randn(cap, d) * torch.exp(0.5 * randn(d))).to(torch.bfloat16)
-        s.w = {}
-        for name, n, K in (("w1", f, d), ("w3", f, d), ("w2", d, f)):
+        s.w, s.nk = {}, {"w1": (f, d), "w3": (f, d), "w2": (d, f)}
+        for name, (n, K) in s.nk.items():
             parts = [_pack((randn(n, K) * K ** -0.5).to(torch.bfloat16).float()) for _ in range(e_cnt)]
             s.w[name] = torch.stack([p[0] for p in parts]), torch.stack([p[1] for p in parts])
         s.o = empty(cap, d, dtype=torch.bfloat16)
-        s.ws = empty(_ws_experts(cap, d, f), dtype=torch.uint8)
+        s.ws = empty(_ws_experts(cap, d, f, e_cnt), dtype=torch.uint8)
     return s
 
 
@@ -180,9 +183,9 @@ def _ws_norm(T, d):
     return 256 + 2 * 1024 * 4 * (d + 64)
 
 
-def _ws_experts(cap, d, f):
-    K = 256 * ((d + 255) // 256) + 256 * ((f + 255) // 256)
-    return (1 << 20) + (cap + 1) * K * 17 // 32
+def _ws_experts(cap, d, f, e_cnt):
+    K = 512 * ((d + 511) // 512) + 512 * ((f + 511) // 512)
+    return (1 << 20) + (cap + 16 * e_cnt) * K * 17 // 32
 
 
 # --------------------------------------------------------------------------------------------------------- plain forms
@@ -241,12 +244,12 @@ def _mx4_values(x):
     return torch.ldexp(q, s).flatten(-2)
 
 
-def _weights(q, scales):
-    """Bytes [n, K/2] and scales [ceil(K/128), n, 4] -> values [n, K] in fp32."""
-    n, K = q.shape[0], 2 * q.shape[1]
+def _weights(q, scales, n, K):
+    """Tiles of bytes and of scales -> values [n, K] in fp32."""
     table = torch.tensor([0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0, -0.0, -0.5, -1.0, -1.5, -2.0, -3.0, -4.0, -6.0], device=q.device)
-    code = torch.stack((q & 15, q >> 4), dim=2).reshape(n, K)
-    s = scales.transpose(0, 1).reshape(n, -1)[:, :K // MX].int() - 127
+    q = q.permute(0, 3, 1, 2, 4).flatten(0, 1).flatten(1)[:n]
+    code = torch.stack((q & 15, q >> 4), dim=2).flatten(1)[:, :K]
+    s = scales.permute(0, 3, 1, 4, 2).flatten(0, 1).flatten(1)[:n, :K // MX].int() - 127
     return torch.ldexp(table[code.int()].unflatten(1, (-1, MX)), s[:, :, None]).flatten(1)
 
 
@@ -254,7 +257,7 @@ def _experts_plain(s):
     out, row = [], 0
     for e, rows in enumerate(s.rows):           # experts differ in rows: one product after the other
         if rows:
-            w1, w3, w2 = (_weights(s.w[name][0][e], s.w[name][1][e]) for name in ("w1", "w3", "w2"))
+            w1, w3, w2 = (_weights(s.w[name][0][e], s.w[name][1][e], *s.nk[name]) for name in ("w1", "w3", "w2"))
             x = _mx4_values(s.xp[row:row + rows].float())
             h1 = x @ w1.t()
             a = h1 / (1 + torch.exp(-h1)) * (x @ w3.t())
@@ -381,7 +384,7 @@ def exact(case, seed):
     row = 0
     for e, rows in enumerate(s.rows):
         if rows:
-            w1, w3, w2 = (_weights(s.w[name][0][e], s.w[name][1][e]).double() for name in ("w1", "w3", "w2"))
+            w1, w3, w2 = (_weights(s.w[name][0][e], s.w[name][1][e], *s.nk[name]).double() for name in ("w1", "w3", "w2"))
             x = _exact_mx4(s.xp[row:row + rows].double())
             h1 = x @ w1.mT
             o[row:row + rows] = _exact_mx4(h1 * torch.sigmoid(h1) * (x @ w3.mT)) @ w2.mT
