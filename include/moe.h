@@ -40,12 +40,14 @@ typedef void* moe_stream_t; /* hipStream_t */
 enum { MOE_OK = 0, MOE_EINVAL = 1, MOE_EUNSUPPORTED = 2, MOE_EWORKSPACE = 3, MOE_EHIP = 4 };
 enum { MOE_F32 = 0, MOE_BF16 = 1 };
 enum { MOE_GATE_SOFTMAX_RENORM = 0, MOE_GATE_SIGMOID_RENORM = 1, MOE_GATE_SOFTMAX = 2 };
-enum { MOE_WS_DISPATCH = 0, MOE_WS_EXPERT_FWD = 1, MOE_WS_EXPERT_BWD = 2, MOE_WS_ROUTER = 3 };
+enum { MOE_WS_DISPATCH = 0, MOE_WS_EXPERT_FWD = 1, MOE_WS_EXPERT_BWD = 2, MOE_WS_ROUTER = 3,
+       MOE_WS_BLOCK_NORM = 4, MOE_WS_MX4_EXPERT_FWD = 5 };
 
 /* Limits checked by the entry points (MOE_EUNSUPPORTED beyond them). */
 #define MOE_MAX_EXPERTS 1024 /* E */
 #define MOE_MAX_LOCAL 1024   /* e_cnt */
 #define MOE_MAX_TOPK 64      /* k */
+#define MOE_MAX_NORM_D 16384 /* d of moe_block_norm_fwd and _bwd */
 
 /*
  * moe_route -- top-k gating (MoE background section: a gate network selects the top-k
@@ -258,6 +260,85 @@ int moe_router_bwd(const void* x, const void* wr, const float* dlogits, int dtyp
                    moe_stream_t stream);
 
 /*
+ * The norms between two blocks (the layer sits between a norm in front of it and a residual sum behind it; a block may have a norm of its
+ * output as well).  One pass takes the residual stream over a block's output y to the next block's input:
+ *     u  = (post_norm ? y * r_post : y) * w_post          r_post[t] = (mean_c y[t,c]^2 + eps)^-1/2
+ *     h' = alpha * h + beta * gate[t] * u
+ *     n  = h' * r_pre * w_pre                             r_pre[t]  = (mean_c h'[t,c]^2 + eps)^-1/2
+ *
+ * moe_block_norm_fwd
+ *   y      [T,d] dtype      the block's output; NULL: there is none yet, h' = h (alpha, beta, gate, w_post and post_norm do not enter), for
+ *                           the norm in front of a model's first block
+ *   gate   [T] float        NULL: 1
+ *   w_post [d] dtype        NULL: 1.  With post_norm == 0 it is a scale per channel.
+ *   h      [T,d] res_dtype  the residual stream; res_dtype is dtype or MOE_F32
+ *   w_pre  [d] dtype        NULL: n is not formed (behind the last block)
+ *   h_out  [T,d] res_dtype  out: h', may be h itself; NULL: not stored.  NULL where y is.
+ *   n      [T,d] dtype      out, NULL exactly where w_pre is; may be y itself
+ *   r_post, r_pre [T] float out, what the backward needs; NULL: not stored
+ * Sums are fp32.  n is formed from h' before its rounding to res_dtype: it is rounded once.
+ *
+ * moe_block_norm_bwd -- the gradient, at the saved y, h' (h_out; h where y is NULL), r_post and r_pre:
+ *     gh = dh_out + r_pre (w_pre dn) - h' r_pre^3 mean_c(w_pre dn h')        dh = alpha gh
+ *     du = beta gate[t] gh                                                   dgate[t] = beta sum_c gh u
+ *     dy = post_norm ? r_post (w_post du) - y r_post^3 mean_c(w_post du y) : w_post du
+ *     dw_pre (+)= sum_t dn h' r_pre          dw_post (+)= sum_t du (post_norm ? y r_post : y)
+ *   dh_out [T,d] res_dtype  gradient of h' from further on; NULL: none.  dn [T,d] dtype: NULL exactly where w_pre is.  Not both NULL.
+ *   dh [T,d] res_dtype out, may be dh_out itself; dy [T,d] dtype out, may be y or dn itself, NULL exactly where y is; dgate [T] float
+ *   out; dw_post, dw_pre [d] dtype out, added to their contents with accumulate == 1.  dh, dgate, dw_post and dw_pre: NULL: not formed.
+ *   r_post is read where post_norm is set, r_pre where w_pre is given.
+ *   ws: moe_workspace_bytes(MOE_WS_BLOCK_NORM, dtype, T, 0, d, 0, 0, 0) bytes, 256-byte aligned.
+ * The column sums are fp32, formed over rows that T alone decides and added in a fixed order: results are bit-reproducible.
+ * Errors of both: EINVAL (NULL, negative sizes, unknown types, res_dtype neither dtype nor MOE_F32, eps not a positive number, outputs without their inputs),
+ * EUNSUPPORTED (bf16 with d % 8 != 0, fp32 with d % 4 != 0, d > MOE_MAX_NORM_D), EWORKSPACE.
+ */
+int moe_block_norm_fwd(const void* y, const float* gate, const void* w_post, int post_norm, const void* h, const void* w_pre,
+                       int dtype, int res_dtype, int T, int d, float alpha, float beta, float eps, void* h_out, void* n,
+                       float* r_post, float* r_pre, moe_stream_t stream);
+int moe_block_norm_bwd(const void* y, const float* gate, const void* w_post, int post_norm, const void* h_out, const void* w_pre,
+                       const float* r_post, const float* r_pre, const void* dh_out, const void* dn, int dtype, int res_dtype,
+                       int T, int d, float alpha, float beta, void* dh, void* dy, float* dgate, void* dw_post, void* dw_pre,
+                       int accumulate, void* ws, size_t ws_bytes, moe_stream_t stream);
+
+/*
+ * Microscaled 4-bit numbers (the OCP MX format of e2m1 elements with one e8m0 scale per 32): an element is 0, 1/2, 1, 3/2, 2, 3, 4, 6 or the
+ * negative of one, times a power of two that 32 elements along the contraction share.
+ *
+ * Layout.  n rows of K elements, K the contraction (weights: n output columns, K inputs), are kept in the order of the matrix instruction:
+ *   data    uint8 [ceil(n/16)][ceil(K/128)][4][16][16]    element (i, k): tile i/16, k/128; chunk k%128/32; row i%16; byte k%32/2, the even
+ *                                                         element in its low half.  Codes 0..7 are 0, 1/2, .. 6 in order; bit 3 is the sign.
+ *   scales  uint8 [ceil(n/16)][ceil(K/512)][4][16][4]     scale of the chunk of (i, k): i/16, k/512; k%128/32; i%16; k%512/128.  The power
+ *                                                         of two plus 127; 255 is NaN.
+ * Rows past n and elements past K are zeros in both.  A batch of matrices is one after the other.
+ *
+ * moe_mx4_quantize -- per 32 elements the scale is 2^(floor(log2 max|x|) - 2), not below 2^-127; elements are x / scale rounded to nearest even,
+ *   saturating at 6.  A chunk with an infinity or NaN gets scale 255 and codes 0.
+ *   along_rows == 0: x [batch][n][K], contraction contiguous (tokens); rows = n, cols = K
+ *   along_rows == 1: x [batch][K][n] (weights as the layer keeps them, W1[d][f], W2[f][d]); rows = K, cols = n
+ * moe_mx4_dequantize -- out [batch][n][K] of type dtype, exact.
+ * Errors: EINVAL (NULL, negative sizes, unknown dtype, pointers not 16-byte aligned), EUNSUPPORTED (K % 32 != 0; along_rows: bf16 with n % 8 != 0,
+ * fp32 with n % 4 != 0; 2^31 tiles of 16 x 512 or more).
+ */
+int moe_mx4_quantize(const void* x, int dtype, int batch, int rows, int cols, int along_rows, uint8_t* data, uint8_t* scales,
+                     moe_stream_t stream);
+int moe_mx4_dequantize(const uint8_t* data, const uint8_t* scales, int batch, int n, int K, void* out, int dtype, moe_stream_t stream);
+
+/*
+ * moe_mx4_expert_fwd -- the experts' forward for serving, with weights and activations in microscaled 4 bits:
+ *     xq = MX4(xp);  a = MX4(silu(xq W1[e]) * (xq W3[e]));  o = a W2[e]
+ *   xp [cap,d], o [cap,d] of type dtype, MOE_BF16 (MOE_F32: EUNSUPPORTED); rows as in moe_expert_fwd, rows >= R of o are left untouched
+ *   w1, w3  data of e_cnt matrices with n = f, K = d (moe_mx4_quantize of [e_cnt][d][f] along rows); s1, s3 their scales
+ *   w2      n = d, K = f; s2.  Elements past K have to be zeros, as the quantisation leaves them.
+ *   ws      moe_workspace_bytes(MOE_WS_MX4_EXPERT_FWD, dtype, 0, 0, d, f, e_cnt, cap) bytes, 256-byte aligned
+ * Products of 4-bit numbers are exact and their sums fp32; the activation is rounded to 4 bits from fp32.  d % 32 == 0 and f % 32 == 0 (EUNSUPPORTED
+ * otherwise).  A row that holds an infinity or NaN spoils its own outputs only.  Results are bit-reproducible; the order of a
+ * row's sums may follow cap and its expert's row count.
+ */
+int moe_mx4_expert_fwd(const void* xp, int dtype, int cap, int d, int f, int e_cnt, const int32_t* offsets, const uint8_t* w1,
+                       const uint8_t* s1, const uint8_t* w3, const uint8_t* s3, const uint8_t* w2, const uint8_t* s2, void* o, void* ws,
+                       size_t ws_bytes, moe_stream_t stream);
+
+/*
  * Optional per-kernel timing, for benchmarks (measurement of the grouped GEMMs against the
  * MFMA roofline and of the row movers against HBM bandwidth).  Apart from per-device caches of
  * constants (CU count, the kernels' LDS opt-in attribute, the address of the built-in plan scratch)
@@ -287,7 +368,10 @@ enum { MOE_K_ROUTE = 0,
         * dW1|dW3, each when the capacity bound gives a workgroup at most a dozen tiles of the first.
         * A shared launch is booked here and not under the single ids. */
        MOE_K_DA_WG = 16, MOE_K_DX_WGD = 17,
-       MOE_K_COUNT = 18 };
+       MOE_K_NORM_FWD = 18, MOE_K_NORM_BWD = 19, MOE_K_NORM_SUMS = 20,      /* column sums of dw_post, dw_pre */
+       MOE_K_MX4_QUANTIZE = 21, MOE_K_MX4_DEQUANTIZE = 22,
+       MOE_K_MX4_ROWS = 23, MOE_K_MX4_UP = 24, MOE_K_MX4_DOWN = 25,
+       MOE_K_COUNT = 26 };
 #define MOE_PROFILE_MAX_EVENTS 8192
 int moe_profile_enable(int on);
 int moe_profile_read(int kernel, double* total_ms /* host */, int* launches /* host */);

@@ -20,7 +20,7 @@ import warnings
 
 MOE_F32, MOE_BF16 = 0, 1
 GATE_SOFTMAX_RENORM, GATE_SIGMOID_RENORM, GATE_SOFTMAX = 0, 1, 2
-WS_DISPATCH, WS_EXPERT_FWD, WS_EXPERT_BWD, WS_ROUTER = 0, 1, 2, 3
+WS_DISPATCH, WS_EXPERT_FWD, WS_EXPERT_BWD, WS_ROUTER, WS_BLOCK_NORM, WS_MX4_EXPERT_FWD = 0, 1, 2, 3, 4, 5
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB = None
@@ -28,6 +28,7 @@ _MARSHAL = None
 
 EXPORTS = ("moe_route", "moe_dispatch", "moe_dispatch_static", "moe_expert_fwd", "moe_expert_bwd", "moe_combine",
            "moe_router_fwd", "moe_combine_bwd", "moe_gate_bwd", "moe_router_bwd",
+           "moe_block_norm_fwd", "moe_block_norm_bwd", "moe_mx4_quantize", "moe_mx4_dequantize", "moe_mx4_expert_fwd",
            "moe_profile_enable", "moe_profile_read", "moe_profile_stats", "moe_probe_mfma_bf16", "moe_probe_mfma_fed_bf16",
            "moe_probe_copy", "moe_probe_stream",
            "moe_workspace_bytes", "moe_error_string")
@@ -81,6 +82,20 @@ def load_library():
     lib.moe_router_bwd.restype = c_int
     lib.moe_router_bwd.argtypes = [c_void_p, c_void_p, c_void_p, c_int, c_int, c_int, c_int, c_void_p, c_int, c_void_p,
                                    c_int, c_void_p, c_size_t, c_void_p]
+    c_float = ctypes.c_float
+    lib.moe_block_norm_fwd.restype = c_int
+    lib.moe_block_norm_fwd.argtypes = [c_void_p, c_void_p, c_void_p, c_int, c_void_p, c_void_p, c_int, c_int, c_int, c_int, c_float,
+                                       c_float, c_float, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p]
+    lib.moe_block_norm_bwd.restype = c_int
+    lib.moe_block_norm_bwd.argtypes = [c_void_p, c_void_p, c_void_p, c_int, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
+                                       c_int, c_int, c_int, c_int, c_float, c_float, c_void_p, c_void_p, c_void_p, c_void_p, c_void_p,
+                                       c_int, c_void_p, c_size_t, c_void_p]
+    lib.moe_mx4_quantize.restype = c_int
+    lib.moe_mx4_quantize.argtypes = [c_void_p, c_int, c_int, c_int, c_int, c_int, c_void_p, c_void_p, c_void_p]
+    lib.moe_mx4_dequantize.restype = c_int
+    lib.moe_mx4_dequantize.argtypes = [c_void_p, c_void_p, c_int, c_int, c_int, c_void_p, c_int, c_void_p]
+    lib.moe_mx4_expert_fwd.restype = c_int
+    lib.moe_mx4_expert_fwd.argtypes = [c_void_p, c_int, c_int, c_int, c_int, c_int] + [c_void_p] * 9 + [c_size_t, c_void_p]
     lib.moe_workspace_bytes.restype = c_size_t
     lib.moe_workspace_bytes.argtypes = [c_int] * 8
     lib.moe_error_string.restype = ctypes.c_char_p
@@ -316,8 +331,94 @@ def moe_router_bwd(x, wr, dlogits, dwr, dwr_accumulate, dx, dx_accumulate, ws):
                                          ws.numel() * ws.element_size(), _stream()), "moe_router_bwd")
 
 
+def moe_block_norm_fwd(y, gate, w_post, post_norm, h, w_pre, alpha, beta, eps, h_out, n, r_post=None, r_pre=None):
+    """y [T,d] or None (the norm in front of a first block), h [T,d]; w_pre and n both or neither."""
+    import torch
+    T, d = h.shape
+    t = w_pre if y is None else y
+    if t is None:
+        raise MoeError("without y there must be w_pre and n")
+    dt = t.dtype
+    _need(h, name="h"); _need(y, dt, (T, d), "y"); _need(gate, torch.float32, (T,), "gate")
+    _need(w_post, dt, (d,), "w_post"); _need(w_pre, dt, (d,), "w_pre")
+    _need(h_out, h.dtype, (T, d), "h_out"); _need(n, dt, (T, d), "n")
+    _need(r_post, torch.float32, (T,), "r_post"); _need(r_pre, torch.float32, (T,), "r_pre")
+    _check(load_library().moe_block_norm_fwd(_ptr(y), _ptr(gate), _ptr(w_post), int(post_norm), _ptr(h), _ptr(w_pre), _dtype_code(t),
+                                             _dtype_code(h), T, d, alpha, beta, eps, _ptr(h_out), _ptr(n), _ptr(r_post), _ptr(r_pre),
+                                             _stream()), "moe_block_norm_fwd")
+
+
+def moe_block_norm_bwd(y, gate, w_post, post_norm, h_out, w_pre, r_post, r_pre, dh_out, dn, alpha, beta, dh, dy, dgate, dw_post,
+                       dw_pre, accumulate, ws):
+    """h_out is the saved sum of the forward (h itself where y is None); it may be None where dn is."""
+    import torch
+    res, t = (next((v for v in pair if v is not None), None) for pair in ((h_out, dh_out), (dn, y)))
+    if res is None or t is None:
+        raise MoeError("there must be h_out or dh_out, and dn or y")
+    (T, d), dt, rt = t.shape, t.dtype, res.dtype
+    _need(y, dt, (T, d), "y"); _need(gate, torch.float32, (T,), "gate")
+    _need(w_post, dt, (d,), "w_post"); _need(w_pre, dt, (d,), "w_pre")
+    _need(h_out, rt, (T, d), "h_out"); _need(dh_out, rt, (T, d), "dh_out"); _need(dn, dt, (T, d), "dn")
+    _need(r_post, torch.float32, (T,), "r_post"); _need(r_pre, torch.float32, (T,), "r_pre")
+    _need(dh, rt, (T, d), "dh"); _need(dy, dt, (T, d), "dy"); _need(dgate, torch.float32, (T,), "dgate")
+    _need(dw_post, dt, (d,), "dw_post"); _need(dw_pre, dt, (d,), "dw_pre"); _need(ws, name="ws")
+    _check(load_library().moe_block_norm_bwd(_ptr(y), _ptr(gate), _ptr(w_post), int(post_norm), _ptr(h_out), _ptr(w_pre), _ptr(r_post),
+                                             _ptr(r_pre), _ptr(dh_out), _ptr(dn), _dtype_code(t), _dtype_code(res), T, d, alpha, beta,
+                                             _ptr(dh), _ptr(dy), _ptr(dgate), _ptr(dw_post), _ptr(dw_pre), int(accumulate), _ptr(ws),
+                                             ws.numel() * ws.element_size(), _stream()), "moe_block_norm_bwd")
+
+
+def mx4_shapes(n, K):
+    """Shapes (data, scales) of n rows of K elements in microscaled 4 bits, both uint8 (layout: moe.h)."""
+    return ((n + 15) // 16, (K + 127) // 128, 4, 16, 16), ((n + 15) // 16, (K + 511) // 512, 4, 16, 4)
+
+
+def _need_mx4(data, scales, batch, n, K, name):
+    import torch
+    for t, shape, what in zip((data, scales), mx4_shapes(n, K), ("data", "scales")):
+        _need(t, torch.uint8, tuple(batch) + shape, f"{name} {what}")
+
+
+def moe_mx4_quantize(x, along_rows, data, scales):
+    """x [n,K] or [batch,n,K]; along_rows: [K,n] or [batch,K,n].  data, scales: mx4_shapes(n, K), behind the batch."""
+    if x.dim() not in (2, 3):
+        raise MoeError("x must be a matrix or a batch of matrices")
+    (rows, cols), batch = x.shape[-2:], x.shape[:-2]
+    _need(x, name="x")
+    _need_mx4(data, scales, batch, *((cols, rows) if along_rows else (rows, cols)), "x's")
+    _check(load_library().moe_mx4_quantize(_ptr(x), _dtype_code(x), batch[0] if batch else 1, rows, cols, int(along_rows), _ptr(data),
+                                           _ptr(scales), _stream()), "moe_mx4_quantize")
+
+
+def moe_mx4_dequantize(data, scales, out):
+    """out [n,K] or [batch,n,K], the values of data and scales."""
+    if out.dim() not in (2, 3):
+        raise MoeError("out must be a matrix or a batch of matrices")
+    (n, K), batch = out.shape[-2:], out.shape[:-2]
+    _need(out, name="out")
+    _need_mx4(data, scales, batch, n, K, "out's")
+    _check(load_library().moe_mx4_dequantize(_ptr(data), _ptr(scales), batch[0] if batch else 1, n, K, _ptr(out), _dtype_code(out),
+                                             _stream()), "moe_mx4_dequantize")
+
+
+def moe_mx4_expert_fwd(xp, offsets, w1, s1, w3, s3, w2, s2, o, ws):
+    """w1, s1, w3, s3: data and scales of e_cnt matrices with n = f, K = d; w2, s2: n = d, K = f (f is a multiple of 32: w1's tiles say it)."""
+    import torch
+    cap, d = xp.shape
+    if w1.dim() != 6:
+        raise MoeError("w1 must hold the tiles of e_cnt matrices")
+    e_cnt, f = w1.shape[0], 16 * w1.shape[1]
+    _need(xp, name="xp"); _need(o, xp.dtype, (cap, d), "o")
+    _need_mx4(w1, s1, (e_cnt,), f, d, "w1's"); _need_mx4(w3, s3, (e_cnt,), f, d, "w3's"); _need_mx4(w2, s2, (e_cnt,), d, f, "w2's")
+    _need(offsets, torch.int32, (e_cnt + 1,), "offsets"); _need(ws, name="ws")
+    _check(load_library().moe_mx4_expert_fwd(_ptr(xp), _dtype_code(xp), cap, d, f, e_cnt, _ptr(offsets), _ptr(w1), _ptr(s1), _ptr(w3), _ptr(s3),
+                                             _ptr(w2), _ptr(s2), _ptr(o), _ptr(ws), ws.numel() * ws.element_size(), _stream()),
+           "moe_mx4_expert_fwd")
+
+
 KERNEL_IDS = dict(route=0, plan=1, dispatch=2, combine=3, up=4, down=5, da=6, dx=7, wg=8, wgd=9, router_fwd=10,
-                  combine_bwd=11, gate_bwd=12, router_dw=13, router_dx=14, wgrad_reduce=15, da_wg=16, dx_wgd=17)
+                  combine_bwd=11, gate_bwd=12, router_dw=13, router_dx=14, wgrad_reduce=15, da_wg=16, dx_wgd=17, norm_fwd=18,
+                  norm_bwd=19, norm_sums=20, mx4_quantize=21, mx4_dequantize=22, mx4_rows=23, mx4_up=24, mx4_down=25)
 
 
 def moe_profile_enable(on: bool):

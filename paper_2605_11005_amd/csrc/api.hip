@@ -168,6 +168,10 @@ size_t moe_workspace_bytes(int which, int dtype, int T, int k, int d, int f, int
     case MOE_WS_ROUTER:       // e_cnt carries E
       if (d <= 0 || e_cnt <= 0) return 256;
       return router_ws_bytes(dtype, T, d, e_cnt);
+    case MOE_WS_BLOCK_NORM:
+      return d <= 0 ? 256 : align256(block_norm_ws_bytes(T, d)) + 256;
+    case MOE_WS_MX4_EXPERT_FWD:
+      return d <= 0 ? 256 : mx4_expert_ws_bytes(cap, d, f, e_cnt);
     default: return 256;
   }
 }
@@ -346,6 +350,85 @@ int moe_combine(const void* o, int dtype, int T, int d, int k, const int32_t* in
   if (T > 0 && (!o || !inv || !y)) return MOE_EINVAL;
   if (misaligned(o, 16) || misaligned(y, 16)) return MOE_EINVAL;
   return launch_combine_rows(o, dtype, T, d, k, inv, topk_w, y, (hipStream_t)stream);
+}
+
+namespace {
+int shape_check_norm(int dtype, int res_dtype, int T, int d) {
+  if (bad_dtype(dtype) || (res_dtype != dtype && res_dtype != MOE_F32) || T < 0 || d <= 0) return MOE_EINVAL;
+  if (d > MOE_MAX_NORM_D || (dtype == MOE_BF16 ? d % 8 : d % 4)) return MOE_EUNSUPPORTED;
+  return MOE_OK;
+}
+}  // namespace
+
+int moe_block_norm_fwd(const void* y, const float* gate, const void* w_post, int post_norm, const void* h, const void* w_pre,
+                       int dtype, int res_dtype, int T, int d, float alpha, float beta, float eps, void* h_out, void* n,
+                       float* r_post, float* r_pre, moe_stream_t stream) {
+  int rc = shape_check_norm(dtype, res_dtype, T, d);
+  if (rc) return rc;
+  if ((post_norm != 0 && post_norm != 1) || !(eps > 0.f && eps < __builtin_inff())) return MOE_EINVAL;
+  if ((w_pre == nullptr) != (n == nullptr) && T > 0) return MOE_EINVAL;
+  if (T > 0 && (!h || (!h_out && !n) || (!y && h_out))) return MOE_EINVAL;
+  if (misaligned(y, 16) || misaligned(w_post, 16) || misaligned(h, 16) || misaligned(w_pre, 16) || misaligned(h_out, 16) || misaligned(n, 16))
+    return MOE_EINVAL;
+  return launch_block_norm_fwd(y, gate, w_post, post_norm, h, w_pre, dtype, res_dtype, T, d, alpha, beta, eps, h_out, n, r_post, r_pre,
+                               (hipStream_t)stream);
+}
+
+int moe_block_norm_bwd(const void* y, const float* gate, const void* w_post, int post_norm, const void* h_out, const void* w_pre,
+                       const float* r_post, const float* r_pre, const void* dh_out, const void* dn, int dtype, int res_dtype,
+                       int T, int d, float alpha, float beta, void* dh, void* dy, float* dgate, void* dw_post, void* dw_pre,
+                       int accumulate, void* ws, size_t ws_bytes, moe_stream_t stream) {
+  int rc = shape_check_norm(dtype, res_dtype, T, d);
+  if (rc) return rc;
+  if ((post_norm != 0 && post_norm != 1) || (accumulate != 0 && accumulate != 1)) return MOE_EINVAL;
+  if (T > 0) {
+    if ((w_pre == nullptr) != (dn == nullptr) || (!dn && !dh_out) || (y == nullptr) != (dy == nullptr)) return MOE_EINVAL;
+    if (w_pre && (!h_out || !r_pre)) return MOE_EINVAL;
+    if (y && post_norm && !r_post) return MOE_EINVAL;
+    if ((!y && (dgate || dw_post)) || (!w_pre && dw_pre)) return MOE_EINVAL;
+  }
+  if (misaligned(y, 16) || misaligned(w_post, 16) || misaligned(h_out, 16) || misaligned(w_pre, 16) || misaligned(dh_out, 16) || misaligned(dn, 16) ||
+      misaligned(dh, 16) || misaligned(dy, 16))
+    return MOE_EINVAL;
+  if (!ws || misaligned(ws, 256) || ws_bytes < block_norm_ws_bytes(T, d)) return MOE_EWORKSPACE;
+  return launch_block_norm_bwd(y, gate, w_post, post_norm, h_out, w_pre, r_post, r_pre, dh_out, dn, dtype, res_dtype, T, d, alpha, beta, dh, dy, dgate,
+                               dw_post, dw_pre, accumulate, ws, (hipStream_t)stream);
+}
+
+int moe_mx4_quantize(const void* x, int dtype, int batch, int rows, int cols, int along_rows, uint8_t* data, uint8_t* scales,
+                     moe_stream_t stream) {
+  if (bad_dtype(dtype) || batch < 0 || rows < 0 || cols < 0 || (along_rows != 0 && along_rows != 1)) return MOE_EINVAL;
+  const int n = along_rows ? cols : rows, K = along_rows ? rows : cols;
+  if (K % 32 || (along_rows && n % (dtype == MOE_BF16 ? 8 : 4))) return MOE_EUNSUPPORTED;
+  if ((long long)batch * ((n + 15ll) / 16) >= (1ll << 31) / ((K + 511ll) / 512 + 1)) return MOE_EUNSUPPORTED;
+  if (batch > 0 && n > 0 && K > 0 && (!x || !data || !scales)) return MOE_EINVAL;
+  if (misaligned(x, 16) || misaligned(data, 16) || misaligned(scales, 16)) return MOE_EINVAL;
+  return launch_mx4_quantize(x, dtype, batch, n, K, along_rows, data, scales, (hipStream_t)stream);
+}
+
+int moe_mx4_dequantize(const uint8_t* data, const uint8_t* scales, int batch, int n, int K, void* out, int dtype, moe_stream_t stream) {
+  if (bad_dtype(dtype) || batch < 0 || n < 0 || K < 0) return MOE_EINVAL;
+  if (K % 32) return MOE_EUNSUPPORTED;
+  if ((long long)batch * ((n + 15ll) / 16) >= (1ll << 31) / ((K + 511ll) / 512 + 1)) return MOE_EUNSUPPORTED;
+  if (batch > 0 && n > 0 && K > 0 && (!out || !data || !scales)) return MOE_EINVAL;
+  if (misaligned(out, 16) || misaligned(data, 16) || misaligned(scales, 16)) return MOE_EINVAL;
+  return launch_mx4_dequantize(data, scales, batch, n, K, out, dtype, (hipStream_t)stream);
+}
+
+int moe_mx4_expert_fwd(const void* xp, int dtype, int cap, int d, int f, int e_cnt, const int32_t* offsets, const uint8_t* w1,
+                       const uint8_t* s1, const uint8_t* w3, const uint8_t* s3, const uint8_t* w2, const uint8_t* s2, void* o, void* ws,
+                       size_t ws_bytes, moe_stream_t stream) {
+  if (bad_dtype(dtype) || cap < 0 || d <= 0 || f <= 0 || e_cnt < 0) return MOE_EINVAL;
+  if (dtype != MOE_BF16 || e_cnt > MOE_MAX_LOCAL || d % 32 || f % 32) return MOE_EUNSUPPORTED;
+  if (d > (1 << 20) || f > (1 << 20)) return MOE_EUNSUPPORTED;
+  if (!offsets) return MOE_EINVAL;
+  if (e_cnt > 0 && (!w1 || !s1 || !w3 || !s3 || !w2 || !s2)) return MOE_EINVAL;
+  if (cap > 0 && (!xp || !o)) return MOE_EINVAL;
+  if (misaligned(xp, 16) || misaligned(o, 16) || misaligned(w1, 16) || misaligned(s1, 16) || misaligned(w3, 16) || misaligned(s3, 16) ||
+      misaligned(w2, 16) || misaligned(s2, 16))
+    return MOE_EINVAL;
+  if (!ws || misaligned(ws, 256) || ws_bytes < mx4_expert_ws_bytes(cap, d, f, e_cnt)) return MOE_EWORKSPACE;
+  return launch_mx4_expert_fwd(xp, cap, d, f, e_cnt, offsets, w1, s1, w3, s3, w2, s2, o, ws, (hipStream_t)stream);
 }
 
 }  // extern "C"

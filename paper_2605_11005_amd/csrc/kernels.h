@@ -82,6 +82,22 @@ int launch_router_dx_bf16(const void* dl_bf16, const void* wr, int T, int d, int
 size_t expert_bwd_extra_ws_bytes(int d, int f);
 size_t wgrad_split_bytes(int d, int f);
 
+// norms between blocks (block_norm.hip)
+size_t block_norm_ws_bytes(int T, int d);
+int launch_block_norm_fwd(const void* y, const float* gate, const void* w_post, int post_norm, const void* h, const void* w_pre, int dtype, int res_dtype,
+                          int T, int d, float alpha, float beta, float eps, void* h_out, void* n, float* r_post, float* r_pre, hipStream_t s);
+int launch_block_norm_bwd(const void* y, const float* gate, const void* w_post, int post_norm, const void* h_out, const void* w_pre,
+                          const float* r_post, const float* r_pre, const void* dh_out, const void* dn, int dtype, int res_dtype, int T, int d,
+                          float alpha, float beta, void* dh, void* dy, float* dgate, void* dw_post, void* dw_pre, int accumulate, void* ws,
+                          hipStream_t s);
+
+// microscaled 4 bits (mx4.hip, mx4_experts.hip)
+int launch_mx4_quantize(const void* x, int dtype, int batch, int n, int K, int along_rows, uint8_t* data, uint8_t* scales, hipStream_t s);
+int launch_mx4_dequantize(const uint8_t* data, const uint8_t* scales, int batch, int n, int K, void* out, int dtype, hipStream_t s);
+size_t mx4_expert_ws_bytes(int cap, int d, int f, int e_cnt);
+int launch_mx4_expert_fwd(const void* xp, int cap, int d, int f, int e_cnt, const int32_t* offsets, const uint8_t* w1, const uint8_t* s1,
+                          const uint8_t* w3, const uint8_t* s3, const uint8_t* w2, const uint8_t* s2, void* o, void* ws, hipStream_t s);
+
 int launch_probe_mfma(float* sink, int iters, int random_operands, hipStream_t s);
 int launch_probe_copy(const void* src, void* dst, size_t bytes, hipStream_t s);
 int launch_probe_mfma_fed(float* sink, int iters, int feed, hipStream_t s);

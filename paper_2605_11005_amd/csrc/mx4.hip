@@ -1,0 +1,163 @@
+// Quantisation to microscaled 4 bits and back (layout and rounding: mx4.h).  HBM bound: every element is read once and every byte
+// written once.
+#include "mx4.h"
+#include "kernels.h"
+
+namespace {
+
+constexpr int QUANT_BLOCK = 256;
+
+// Rows whose elements are contiguous (tokens).  A wavefront makes the tiles of 16 rows by 512 elements: a lane takes the same row and chunk
+// of four operands, 64 bytes (fp32: 128) at a time, and the four scales are the bytes of its word.
+template <typename T>
+__global__ __launch_bounds__(QUANT_BLOCK) void mx4_rows(const T* __restrict__ x, int n, int K, long long jobs, uint8_t* __restrict__ q,
+                                                         uint8_t* __restrict__ scales) {
+  const int lane = threadIdx.x & 63;
+  const long long job = (long long)blockIdx.x * (QUANT_BLOCK / WAVE) + (threadIdx.x >> 6);
+  if (job >= jobs) return;
+  const int groups = mx_groups(K), depths = mx_depths(K), tiles = (n + 15) / 16;
+  const int group = (int)(job % groups);
+  const long long rest = job / groups, batch = rest / tiles;
+  const int row = 16 * (int)(rest - batch * tiles) + (lane & 15), chunk = lane >> 4;
+  const T* src = x + ((size_t)batch * n + row) * K;
+  uint32_t word = 0;
+#pragma unroll
+  for (int p = 0; p < 4; ++p) {
+    const int depth = 4 * group + p, k = MX_DEPTH * depth + MX_CHUNK * chunk;
+    if (depth >= depths) break;
+    uint32_t byte = 0;
+    mx_u32x4 codes = {0, 0, 0, 0};
+    if (row < n && k < K) codes = mx_load_chunk(src + k, byte);
+    word |= byte << (8 * p);
+    *reinterpret_cast<mx_u32x4*>(q + ((size_t)rest * depths + depth) * MX_TILE + lane * 16) = codes;
+  }
+  *reinterpret_cast<uint32_t*>(scales + ((size_t)rest * groups + group) * MX_SCALES + lane * 4) = word;
+}
+
+// Matrices [K][n] whose contraction index is not the contiguous one (weights).  A lane takes four columns of 32 rows; the four
+// wavefronts of a block take the same chunk of four consecutive operands, whose scales meet in LDS as the bytes of a word.
+template <typename T>
+__global__ __launch_bounds__(QUANT_BLOCK) void mx4_columns(const T* __restrict__ x, int n, int K, int col_blocks, uint8_t* __restrict__ q,
+                                                            uint8_t* __restrict__ scales) {
+  __shared__ uint8_t bytes[QUANT_BLOCK * 4];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int groups = mx_groups(K), depths = mx_depths(K), tiles = (n + 15) / 16;
+  int b = blockIdx.x;
+  const int col_block = b % col_blocks; b /= col_blocks;
+  const int chunk = b % 4; b /= 4;
+  const int group = b % groups, batch = b / groups;
+  const int col = col_block * QUANT_BLOCK + 4 * lane, depth = 4 * group + wave, k = MX_DEPTH * depth + MX_CHUNK * chunk;
+  uint32_t byte[4] = {0, 0, 0, 0};
+  mx_u32x4 codes[4] = {};
+  if (col < n && k < K) {
+    const T* src = x + ((size_t)batch * K + k) * n + col;
+    if constexpr (sizeof(T) == 2) {
+      uint2 v[MX_CHUNK];
+#pragma unroll
+      for (int i = 0; i < MX_CHUNK; ++i) v[i] = *reinterpret_cast<const uint2*>(src + (size_t)i * n);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        uint32_t w[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          w[i] = __builtin_amdgcn_perm(c < 2 ? v[2 * i + 1].x : v[2 * i + 1].y, c < 2 ? v[2 * i].x : v[2 * i].y, c & 1 ? 0x07060302u : 0x05040100u);
+        codes[c] = mx_chunk(w, byte[c]);
+      }
+    } else {
+      float4 v[MX_CHUNK];
+#pragma unroll
+      for (int i = 0; i < MX_CHUNK; ++i) v[i] = *reinterpret_cast<const float4*>(src + (size_t)i * n);
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        float w[32];
+#pragma unroll
+        for (int i = 0; i < 32; ++i) w[i] = c == 0 ? v[i].x : c == 1 ? v[i].y : c == 2 ? v[i].z : v[i].w;
+        codes[c] = mx_chunk(w, byte[c]);
+      }
+    }
+  }
+#pragma unroll
+  for (int c = 0; c < 4; ++c) bytes[(4 * lane + c) * 4 + wave] = (uint8_t)byte[c];
+  if (depth < depths && col < 16 * tiles) {
+    uint8_t* dst = q + (((size_t)batch * tiles + (col >> 4)) * depths + depth) * MX_TILE + chunk * 256 + (col & 15) * 16;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) reinterpret_cast<mx_u32x4*>(dst)[c] = codes[c];
+  }
+  __syncthreads();
+  const int own = col_block * QUANT_BLOCK + threadIdx.x;
+  if (own < 16 * tiles)
+    *reinterpret_cast<uint32_t*>(scales + (((size_t)batch * tiles + (own >> 4)) * groups + group) * MX_SCALES + chunk * 64 + (own & 15) * 4) =
+        *reinterpret_cast<const uint32_t*>(bytes + 4 * threadIdx.x);
+}
+
+// Back to values [n][K]: exact in either type (an e2m1 number has two bits of mantissa).  A block takes 16 rows by 512 elements, a lane
+// eight elements of four operands: 16 lanes write 256 (fp32: 512) bytes of a row.
+template <typename T>
+__global__ __launch_bounds__(QUANT_BLOCK) void mx4_values(const uint8_t* __restrict__ q, const uint8_t* __restrict__ scales, int n, int K,
+                                                           T* __restrict__ out) {
+  const int groups = mx_groups(K), depths = mx_depths(K), tiles = (n + 15) / 16;
+  const int group = blockIdx.x % groups, rest = blockIdx.x / groups, batch = rest / tiles;
+  const int i = threadIdx.x >> 4, c = threadIdx.x & 15, chunk = c >> 2;       // row, eight elements of the 128
+  const int row = 16 * (rest - batch * tiles) + i;
+  if (row >= n) return;
+  const uint32_t word = *reinterpret_cast<const uint32_t*>(scales + ((size_t)rest * groups + group) * MX_SCALES + chunk * 64 + i * 4);
+  T* dst = out + ((size_t)batch * n + row) * K;
+#pragma unroll
+  for (int p = 0; p < 4; ++p) {
+    const int depth = 4 * group + p, k = MX_DEPTH * depth + 8 * c;
+    if (k >= K) break;
+    const uint32_t v = *reinterpret_cast<const uint32_t*>(q + ((size_t)rest * depths + depth) * MX_TILE + chunk * 256 + i * 16 + (c & 3) * 4);
+    const uint32_t byte = (word >> (8 * p)) & 255u;
+    const float s = byte == 255 ? __uint_as_float(0x7FC00000u) : mx_scale_value(byte);
+    typedef float f32x2 __attribute__((ext_vector_type(2)));
+    // codes as multiples of 1/2, times the scale: both steps are exact
+    const f32x2 e[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(v, 1.f, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(v, 1.f, 1),
+                        __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(v, 1.f, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(v, 1.f, 3)};
+    if constexpr (sizeof(T) == 2) {
+      const mx_u32x4 o = {pack_bf16x2(e[0].x * s, e[0].y * s), pack_bf16x2(e[1].x * s, e[1].y * s), pack_bf16x2(e[2].x * s, e[2].y * s),
+                          pack_bf16x2(e[3].x * s, e[3].y * s)};
+      *reinterpret_cast<mx_u32x4*>(dst + k) = o;
+    } else {
+      *reinterpret_cast<float4*>(dst + k) = {e[0].x * s, e[0].y * s, e[1].x * s, e[1].y * s};
+      *reinterpret_cast<float4*>(dst + k + 4) = {e[2].x * s, e[2].y * s, e[3].x * s, e[3].y * s};
+    }
+  }
+}
+
+}  // namespace
+
+int launch_mx4_quantize(const void* x, int dtype, int batch, int n, int K, int along_rows, uint8_t* q, uint8_t* scales, hipStream_t s) {
+  if (batch == 0 || n == 0 || K == 0) return MOE_OK;
+  ProfScope prof(MOE_K_MX4_QUANTIZE, s);
+  if (along_rows) {
+    const int col_blocks = (n + QUANT_BLOCK - 1) / QUANT_BLOCK;
+    const long long blocks = (long long)batch * mx_groups(K) * 4 * col_blocks;
+    if (blocks >= (1ll << 31)) return MOE_EUNSUPPORTED;
+    if (dtype == MOE_BF16)
+      hipLaunchKernelGGL(mx4_columns<bf16_t>, dim3((unsigned)blocks), dim3(QUANT_BLOCK), 0, s, (const bf16_t*)x, n, K, col_blocks, q, scales);
+    else
+      hipLaunchKernelGGL(mx4_columns<float>, dim3((unsigned)blocks), dim3(QUANT_BLOCK), 0, s, (const float*)x, n, K, col_blocks, q, scales);
+  } else {
+    const long long jobs = (long long)batch * ((n + 15) / 16) * mx_groups(K), blocks = (jobs + QUANT_BLOCK / WAVE - 1) / (QUANT_BLOCK / WAVE);
+    if (blocks >= (1ll << 31)) return MOE_EUNSUPPORTED;
+    if (dtype == MOE_BF16)
+      hipLaunchKernelGGL(mx4_rows<bf16_t>, dim3((unsigned)blocks), dim3(QUANT_BLOCK), 0, s, (const bf16_t*)x, n, K, jobs, q, scales);
+    else
+      hipLaunchKernelGGL(mx4_rows<float>, dim3((unsigned)blocks), dim3(QUANT_BLOCK), 0, s, (const float*)x, n, K, jobs, q, scales);
+  }
+  HIP_CHECK_LAUNCH();
+  return MOE_OK;
+}
+
+int launch_mx4_dequantize(const uint8_t* q, const uint8_t* scales, int batch, int n, int K, void* out, int dtype, hipStream_t s) {
+  if (batch == 0 || n == 0 || K == 0) return MOE_OK;
+  ProfScope prof(MOE_K_MX4_DEQUANTIZE, s);
+  const long long blocks = (long long)batch * ((n + 15) / 16) * mx_groups(K);
+  if (blocks >= (1ll << 31)) return MOE_EUNSUPPORTED;
+  if (dtype == MOE_BF16)
+    hipLaunchKernelGGL(mx4_values<bf16_t>, dim3((unsigned)blocks), dim3(QUANT_BLOCK), 0, s, q, scales, n, K, (bf16_t*)out);
+  else
+    hipLaunchKernelGGL(mx4_values<float>, dim3((unsigned)blocks), dim3(QUANT_BLOCK), 0, s, q, scales, n, K, (float*)out);
+  HIP_CHECK_LAUNCH();
+  return MOE_OK;
+}

@@ -117,3 +117,11 @@ def run_backward_router(wl, dev, buf: MoeLayerBuffers, accumulate: bool = False)
     B.moe_combine(buf.dxp, buf.inv, None, buf.dx)
     B.moe_gate_bwd(buf.logits, buf.topk_idx, buf.dgate, wl.gate_mode, buf.dlogits)
     B.moe_router_bwd(dev["x"], dev["wr"], buf.dlogits, buf.dwr, accumulate, buf.dx, True, buf.ws_router)
+
+
+def mx4_weights(w):
+    """[n_experts, K, n] weights of the layer (W1, W3 [e,d,f], W2 [e,f,d]) -> their data and scales in microscaled 4 bits."""
+    e, K, n = w.shape
+    data, scales = (torch.empty((e,) + shape, dtype=torch.uint8, device=w.device) for shape in B.mx4_shapes(n, K))
+    B.moe_mx4_quantize(w, True, data, scales)
+    return data, scales
