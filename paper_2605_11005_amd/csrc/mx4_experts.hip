@@ -178,15 +178,243 @@ __device__ __forceinline__ void few_tile(const XArgs& p, f32x4* lds, int e, int 
   }
 }
 
+// Experts in the order of RaggedTiles, but only those whose row count lies in (LO, hi]; rows in tiles of TM.
+template <int TM>
+struct SomeTiles {
+  const int32_t* off;
+  int e_cnt, lane, lo, hi;
+  int n, incl, total;
+  __device__ __forceinline__ int count(int e) const {
+    const int rows = e < e_cnt ? off[e + 1] - off[e] : 0;
+    return rows > lo && rows <= hi ? (rows + TM - 1) / TM : 0;
+  }
+  __device__ __forceinline__ SomeTiles(const int32_t* __restrict__ off_, int e_cnt_, int lane_, int lo_, int hi_)
+      : off(off_), e_cnt(e_cnt_), lane(lane_), lo(lo_), hi(hi_) {
+    n = count(lane);
+    incl = wave_scan(n);
+    total = __builtin_amdgcn_readlane(incl, WAVE - 1);
+    for (int base = WAVE; base < e_cnt; base += WAVE) total += wave_sum(count(base + lane));
+  }
+  // tile b of a walk that goes through every XCD's contiguous eighth; false: past its end
+  __device__ __forceinline__ bool tile(int n_cols, int b, int& e, int& row_tile, int& col_tile) const {
+    const int share = (total * n_cols + 7) / 8;
+    const int at = (b % 8) * share + b / 8;
+    if (b / 8 >= share || at >= total * n_cols) return false;
+    int t = at / n_cols, rows = n, up_to = incl;
+    col_tile = at - t * n_cols;
+    for (int base = 0;; base += WAVE) {          // ends: t < total
+      if (base > 0) up_to = wave_scan(rows = count(base + lane));
+      const unsigned long long past = __ballot(up_to > t);
+      if (past) {
+        const int who = __builtin_ctzll(past);
+        row_tile = t - __builtin_amdgcn_readlane(up_to - rows, who);
+        e = base + who;
+        return true;
+      }
+      t -= __builtin_amdgcn_readlane(up_to, WAVE - 1);
+    }
+  }
+};
+
 template <int MODE>
 __global__ __launch_bounds__(FEW_WAVES * WAVE) void few_rows_mx4(XArgs p) {
   __shared__ f32x4 lds[FEW_WAVES * (MODE == UP ? 4 : 2) * WAVE];
-  const RaggedTiles<FEW_ROWS> list(p.off, p.e_cnt, threadIdx.x & 63);
+  const SomeTiles<FEW_ROWS> list(p.off, p.e_cnt, threadIdx.x & 63, 0, 0x7FFFFFFF);
   int e, row_tile, col_tile;
   if (!list.tile(p.N / FEW_COLS, blockIdx.x, e, row_tile, col_tile)) return;
   const int rows = p.off[e + 1] - p.off[e] - row_tile * FEW_ROWS;
   if (rows <= 16) few_tile<MODE, 1>(p, lds, e, row_tile, col_tile * FEW_COLS, rows);
   else few_tile<MODE, 2>(p, lds, e, row_tile, col_tile * FEW_COLS, rows);
+}
+
+// ---- many rows per expert: 128 rows against 256 weight rows (UP: 128 of either matrix), four wavefronts of 64 by 128 in 32x32x64
+// instructions.  Operands go from memory to LDS directly, 128 of the contraction at a time through a ring of three stages; their layout in
+// memory is the one that the instruction wants, so every load is 1 KB of consecutive bytes and every LDS read free of conflicts.
+constexpr int GEMM_ROWS = 128, GEMM_COLS = 256, GEMM_THREADS = 256;
+constexpr int STAGE_TILES = (GEMM_ROWS + GEMM_COLS) / 16, STAGE = STAGE_TILES * MX_TILE, STAGES = 3;
+constexpr int STAGE_LOADS = STAGE_TILES / 4, SCALE_LOADS = 2;           // per wavefront
+constexpr int GEMM_LDS = STAGES * STAGE + STAGE_TILES * MX_SCALES;
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+template <int S>
+__device__ __forceinline__ f32x16 mfma32(u32x4 a, u32x4 b, f32x16 c, uint32_t sa, uint32_t sb) {
+  const i32x8 x = {(int)a[0], (int)a[1], (int)a[2], (int)a[3], 0, 0, 0, 0}, y = {(int)b[0], (int)b[1], (int)b[2], (int)b[3], 0, 0, 0, 0};
+  return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, y, c, 4, 4, S, (int)sa, S, (int)sb);
+}
+// lanes 32..63 of a and lanes 0..31 of b change places
+__device__ __forceinline__ void swap32(uint32_t& a, uint32_t& b) {
+  const auto r = __builtin_amdgcn_permlane32_swap(a, b, false, false);
+  a = r[0];
+  b = r[1];
+}
+template <int N>
+__device__ __forceinline__ void wait_and_meet() { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"(N) : "memory"); }
+
+template <int MODE>
+__device__ __forceinline__ void gemm_tile(const XArgs& p, uint8_t* lds, int e, int row_tile, int col_tile, int rows) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int depths = mx_depths(p.K), groups = mx_groups(p.K);
+  const int tile0 = p.first[e] + row_tile * (GEMM_ROWS / 16), row_tiles = (min(rows, GEMM_ROWS) + 15) / 16;
+  const int cols = MODE == UP ? GEMM_COLS / 2 : GEMM_COLS, n0 = col_tile * cols, col_tiles = min(cols, p.N - n0) / 16;
+  const uint32_t lds0 = lds_addr(lds), scales0 = lds0 + STAGES * STAGE;
+  // Operand tile i of a stage: 0..7 the rows', 8..23 the weights' (UP: 8 of W1, 8 of W3); wavefront w loads 6 w .. 6 w + 5.  Tiles past the
+  // rows or columns repeat the last one: their results are not stored.
+  const uint8_t* data[STAGE_LOADS];
+#pragma unroll
+  for (int j = 0; j < STAGE_LOADS; ++j) {
+    const int i = STAGE_LOADS * wave + j;
+    const uint8_t* base;
+    int t;
+    if (i < 8) {
+      base = p.A; t = tile0 + min(i, row_tiles - 1);
+    } else {
+      const int c = i - 8;
+      base = (MODE == UP && c >= 8 ? p.B1 : p.B0) + e * p.b_es;
+      t = n0 / 16 + min(MODE == UP ? c & 7 : c, col_tiles - 1);
+    }
+    data[j] = base + (size_t)t * depths * MX_TILE;
+  }
+  // Scales of 512: four operand tiles per load.  Of the six loads wavefront w makes the weights' w-th and the rows' w % 2-th (twice the same
+  // bytes to the same place, so that all wavefronts wait for equally many).
+  const uint8_t* scale_a;
+  const uint8_t* scale_b;
+  uint32_t voff_a, voff_b;
+  {
+    const int ta = 4 * (wave & 1) + lane / 16, tb = 4 * wave + lane / 16;
+    scale_a = p.As + (size_t)tile0 * groups * MX_SCALES;
+    voff_a = (uint32_t)(min(ta, row_tiles - 1) * groups * MX_SCALES + lane % 16 * 16);
+    scale_b = (MODE == UP && wave >= 2 ? p.Bs1 : p.Bs0) + e * p.bs_es + (size_t)(n0 / 16) * groups * MX_SCALES;
+    voff_b = (uint32_t)(min(MODE == UP ? tb & 7 : tb, col_tiles - 1) * groups * MX_SCALES + lane % 16 * 16);
+  }
+  const uint32_t voff = lane * 16;
+  auto issue = [&](int t) {
+    if (t % 4 == 0) {
+      const size_t at = (size_t)(t / 4) * MX_SCALES;
+      lds_load16((const bf16_t*)(scale_a + at), voff_a, scales0 + (wave & 1) * 1024);
+      lds_load16((const bf16_t*)(scale_b + at), voff_b, scales0 + 2048 + wave * 1024);
+    }
+    const uint32_t slot = lds0 + t % STAGES * STAGE + STAGE_LOADS * wave * MX_TILE;
+#pragma unroll
+    for (int j = 0; j < STAGE_LOADS; ++j) lds_load16((const bf16_t*)(data[j] + (size_t)t * MX_TILE), voff, slot + j * MX_TILE);
+  };
+  const int wr = wave & 1, wc = wave >> 1, h = lane >> 5;
+  const bool active = 64 * wr < rows;                 // (of a tile with up to 64 rows two wavefronts only load)
+  // weights: 32-column operand j of this wavefront begins at tile b_tile(j) of the stage
+  const auto b_tile = [&](int j) { return MODE == UP ? 8 + 8 * (j >> 1) + 4 * wc + 2 * (j & 1) : 8 + 8 * wc + 2 * j; };
+  const int at = (lane >> 4 & 1) * MX_TILE + h * 256 + (lane & 15) * 16, scale_at = (lane >> 4 & 1) * MX_SCALES + h * 64 + (lane & 15) * 4;
+  f32x16 acc[2][4];
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
+  uint32_t as[2][2], bs[4][2];
+  const uint8_t* const scales = lds + STAGES * STAGE + scale_at;
+  __syncthreads();                                    // the stages may still be read for the tile before
+  issue(0);
+  if (depths > 1) issue(1);
+  auto stage = [&](int t, auto which) {
+    constexpr int Q = decltype(which)::value;         // t % 4
+    if (t + 1 < depths) wait_and_meet<STAGE_LOADS + (Q == 3 ? SCALE_LOADS : 0)>();
+    else wait_and_meet<0>();
+    if (t + 2 < depths) issue(t + 2);
+    if (!active) return;
+    if (Q == 0) {
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) as[i][s] = *reinterpret_cast<const uint32_t*>(scales + (4 * wr + 2 * i) * MX_SCALES + 128 * s);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) bs[j][s] = *reinterpret_cast<const uint32_t*>(scales + b_tile(j) * MX_SCALES + 128 * s);
+      }
+    }
+    const uint8_t* const slot = lds + t % STAGES * STAGE + at;
+    u32x4 a[2][2], b[2][4];
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) a[s][i] = *reinterpret_cast<const u32x4*>(slot + (4 * wr + 2 * i) * MX_TILE + 512 * s);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) b[s][j] = *reinterpret_cast<const u32x4*>(slot + b_tile(j) * MX_TILE + 512 * s);
+    }
+#pragma unroll
+    for (int s = 0; s < 2; ++s)
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[i][j] = mfma32<Q>(b[s][j], a[s][i], acc[i][j], bs[j][s], as[i][s]);
+  };
+  for (int t = 0; t < depths; t += 4)
+    static_for<4>([&](auto q) {
+      if (t + decltype(q)::value < depths) stage(t + decltype(q)::value, q);
+    });
+  if (!active) return;
+  // element 4 g + r of acc[i][j]: row lane % 32, column 8 g + 4 h + r of the 32
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int row = 64 * wr + 32 * i + (lane & 31);
+    if constexpr (MODE == UP) {
+      const int tile = tile0 + row / 16;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        float v[16];
+        uint32_t top = 0;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          v[r] = silu_f(acc[i][j][r]) * acc[i][j + 2][r];
+          top = max(top, __float_as_uint(v[r]) & 0x7FFFFFFFu);
+        }
+        uint32_t other = top;
+        swap32(top, other);
+        const uint32_t byte = mx_scale_byte(max(top, other));
+        const float s = mx_scale_value(byte);
+        uint32_t lo = byte == 255 ? 0u : mx_pack8(v, s), hi = byte == 255 ? 0u : mx_pack8(v + 8, s);
+        swap32(lo, hi);                               // now bytes 8 h .. 8 h + 7 of the chunk, in halves of two lanes
+        const u32x2 codes = {__builtin_amdgcn_perm(hi, lo, 0x05040100u), __builtin_amdgcn_perm(hi, lo, 0x07060302u)};
+        const int col = n0 + 64 * wc + 32 * j;
+        if (row >= rows || col >= p.N) continue;
+        const int depth = col / MX_DEPTH, chunk = col % MX_DEPTH / MX_CHUNK;
+        *reinterpret_cast<u32x2*>(p.C + ((size_t)tile * mx_depths(p.N) + depth) * MX_TILE + chunk * 256 + row % 16 * 16 + 8 * h) = codes;
+        if (h == 0) p.Cs[((size_t)tile * mx_groups(p.N) + depth / 4) * MX_SCALES + chunk * 64 + row % 16 * 4 + depth % 4] = (uint8_t)byte;
+      }
+    } else {
+      bf16_t* const out = p.O + ((size_t)p.off[e] + row_tile * GEMM_ROWS + row) * p.N + n0 + 128 * wc + 16 * h;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        uint32_t w[8];
+#pragma unroll
+        for (int r = 0; r < 8; ++r) w[r] = pack_bf16x2(acc[i][j][2 * r], acc[i][j][2 * r + 1]);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) swap32(w[r], w[r + 4]);         // columns 16 h .. 16 h + 15
+        if (row >= rows || n0 + 128 * wc + 32 * j >= p.N) continue;
+        reinterpret_cast<u32x4*>(out + 32 * j)[0] = u32x4{w[0], w[1], w[4], w[5]};
+        reinterpret_cast<u32x4*>(out + 32 * j)[1] = u32x4{w[2], w[3], w[6], w[7]};
+      }
+    }
+  }
+}
+
+// Workgroups walk the tiles of the experts with many rows, then those of the experts with few.
+constexpr int FEW_MOST = 32;               // rows
+template <int MODE>
+__global__ __launch_bounds__(GEMM_THREADS, 2) void experts_mx4(XArgs p) {
+  extern __shared__ uint8_t gemm_lds[];
+  const int lane = threadIdx.x & 63;
+  int e, row_tile, col_tile;
+  {
+    const SomeTiles<GEMM_ROWS> list(p.off, p.e_cnt, lane, FEW_MOST, 0x7FFFFFFF);
+    const int cols = MODE == UP ? GEMM_COLS / 2 : GEMM_COLS;
+    for (int b = blockIdx.x; list.tile((p.N + cols - 1) / cols, b, e, row_tile, col_tile); b += gridDim.x)
+      gemm_tile<MODE>(p, gemm_lds, e, row_tile, col_tile, p.off[e + 1] - p.off[e] - row_tile * GEMM_ROWS);
+  }
+  const SomeTiles<FEW_ROWS> list(p.off, p.e_cnt, lane, 0, FEW_MOST);
+  for (int b = blockIdx.x; list.tile(p.N / FEW_COLS, b, e, row_tile, col_tile); b += gridDim.x) {
+    const int rows = p.off[e + 1] - p.off[e] - row_tile * FEW_ROWS;
+    __syncthreads();
+    if (rows <= 16) few_tile<MODE, 1>(p, reinterpret_cast<f32x4*>(gemm_lds), e, row_tile, col_tile * FEW_COLS, rows);
+    else few_tile<MODE, 2>(p, reinterpret_cast<f32x4*>(gemm_lds), e, row_tile, col_tile * FEW_COLS, rows);
+  }
 }
 
 inline size_t align256(size_t v) { return (v + 255) & ~(size_t)255; }
@@ -227,6 +455,19 @@ int launch_mx4_expert_fwd(const void* xp, int cap, int d, int f, int e_cnt, cons
                        e_cnt, d, f, base + at.xq, base + at.xs, base + at.aq, base + at.as, first);
     HIP_CHECK_LAUNCH();
   }
+  const bool many = cap > FEW_MOST;            // some expert may have many rows
+  if (many) {
+    static bool attr_set[64] = {};
+    int dev = 0;
+    if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return MOE_EHIP;
+    if (!attr_set[dev]) {
+      if (hipFuncSetAttribute(reinterpret_cast<const void*>(&experts_mx4<UP>), hipFuncAttributeMaxDynamicSharedMemorySize, GEMM_LDS) != hipSuccess ||
+          hipFuncSetAttribute(reinterpret_cast<const void*>(&experts_mx4<DOWN>), hipFuncAttributeMaxDynamicSharedMemorySize, GEMM_LDS) != hipSuccess)
+        return MOE_EHIP;
+      attr_set[dev] = true;
+    }
+  }
+  const dim3 walkers(8 * ((2 * device_cu_count() + 7) / 8));       // (a walk stays in its XCD's eighth)
   XArgs p{};
   p.off = offsets; p.first = first; p.e_cnt = e_cnt;
   p.A = base + at.xq; p.As = base + at.xs;
@@ -236,7 +477,8 @@ int launch_mx4_expert_fwd(const void* xp, int cap, int d, int f, int e_cnt, cons
   p.b_es = (size_t)((f + 15) / 16) * mx_depths(d) * MX_TILE; p.bs_es = (size_t)((f + 15) / 16) * mx_groups(d) * MX_SCALES;
   {
     ProfScope prof(MOE_K_MX4_UP, s);
-    hipLaunchKernelGGL(few_rows_mx4<UP>, dim3((unsigned)up), dim3(WAVE * min(FEW_WAVES, mx_groups(d))), 0, s, p);
+    if (many) hipLaunchKernelGGL(experts_mx4<UP>, walkers, dim3(GEMM_THREADS), GEMM_LDS, s, p);
+    else hipLaunchKernelGGL(few_rows_mx4<UP>, dim3((unsigned)up), dim3(WAVE * min(FEW_WAVES, mx_groups(d))), 0, s, p);
     HIP_CHECK_LAUNCH();
   }
   p.A = p.C; p.As = p.Cs;
@@ -246,7 +488,8 @@ int launch_mx4_expert_fwd(const void* xp, int cap, int d, int f, int e_cnt, cons
   p.b_es = (size_t)((d + 15) / 16) * mx_depths(f) * MX_TILE; p.bs_es = (size_t)((d + 15) / 16) * mx_groups(f) * MX_SCALES;
   {
     ProfScope prof(MOE_K_MX4_DOWN, s);
-    hipLaunchKernelGGL(few_rows_mx4<DOWN>, dim3((unsigned)down), dim3(WAVE * min(FEW_WAVES, mx_groups(f))), 0, s, p);
+    if (many) hipLaunchKernelGGL(experts_mx4<DOWN>, walkers, dim3(GEMM_THREADS), GEMM_LDS, s, p);
+    else hipLaunchKernelGGL(few_rows_mx4<DOWN>, dim3((unsigned)down), dim3(WAVE * min(FEW_WAVES, mx_groups(f))), 0, s, p);
     HIP_CHECK_LAUNCH();
   }
   return MOE_OK;
