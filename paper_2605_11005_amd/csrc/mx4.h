@@ -73,26 +73,73 @@ __device__ __forceinline__ mx_u32x4 mx_chunk(const float (&v)[32], uint32_t& byt
   return r;
 }
 
-// a lane's chunk straight from memory (16-byte aligned)
-__device__ __forceinline__ mx_u32x4 mx_load_chunk(const bf16_t* p, uint32_t& byte) {
-  uint32_t w[16];
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const mx_u32x4 v = reinterpret_cast<const mx_u32x4*>(p)[i];
-#pragma unroll
-    for (int j = 0; j < 4; ++j) w[4 * i + j] = v[j];
+// Eight consecutive elements of a lane (a chunk is four lanes side by side) as loaded, and their codes.
+template <typename T> struct Mx8;
+template <> struct Mx8<bf16_t> {
+  mx_u32x4 v;
+  __device__ __forceinline__ void load(const bf16_t* p) { v = __builtin_nontemporal_load(reinterpret_cast<const mx_u32x4*>(p)); }
+  __device__ __forceinline__ void zero() { v = mx_u32x4{0, 0, 0, 0}; }
+  __device__ __forceinline__ uint32_t top() const { return mx_top_bits(mx_top(mx_top(v[0], v[1]), mx_top(v[2], v[3]))); }
+  __device__ __forceinline__ uint32_t codes(float s) const { return mx_pack8(v[0], v[1], v[2], v[3], s); }
+};
+template <> struct Mx8<float> {
+  mx_u32x4 v[2];
+  __device__ __forceinline__ void load(const float* p) {
+    v[0] = __builtin_nontemporal_load(reinterpret_cast<const mx_u32x4*>(p));
+    v[1] = __builtin_nontemporal_load(reinterpret_cast<const mx_u32x4*>(p) + 1);
   }
-  return mx_chunk(w, byte);
+  __device__ __forceinline__ void zero() { v[0] = v[1] = mx_u32x4{0, 0, 0, 0}; }
+  __device__ __forceinline__ uint32_t top() const {
+    uint32_t t = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) t = max(t, v[i / 4][i % 4] & 0x7FFFFFFFu);
+    return t;
+  }
+  __device__ __forceinline__ uint32_t codes(float s) const {
+    float f[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) f[i] = __uint_as_float(v[i / 4][i % 4]);
+    return mx_pack8(f, s);
+  }
+};
+// largest of four lanes side by side
+__device__ __forceinline__ uint32_t quad_max(uint32_t v) {
+  v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xB1, 0xF, 0xF, false));      // quad_perm 1 0 3 2
+  return max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4E, 0xF, 0xF, false));   // quad_perm 2 3 0 1
 }
-__device__ __forceinline__ mx_u32x4 mx_load_chunk(const float* p, uint32_t& byte) {
-  float v[32];
+
+// A wavefront's tiles of 16 rows by 512 elements from rows that are contiguous: 16 lanes load 128 elements of a row, so that a load takes 256
+// consecutive bytes (fp32: 512) of each of four rows, and a chunk's largest magnitude is found across four lanes.
+// src: element 0 of the first row; rows, K: what of it there is (the rest is zeros); tile, group: where it goes.
+template <typename T>
+__device__ __forceinline__ void mx_rows_512(const T* src, int rows, int K, size_t tile, int group, int lane, uint8_t* __restrict__ q, uint8_t* __restrict__ scales) {
+  const int groups = mx_groups(K), depths = mx_depths(K), r0 = lane >> 4, c = lane & 15;
+  Mx8<T> x[4][4];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const mx_u32x4 x = reinterpret_cast<const mx_u32x4*>(p)[i];
+  for (int p = 0; p < 4; ++p)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) v[4 * i + j] = __uint_as_float(x[j]);
+    for (int j = 0; j < 4; ++j) {
+      const int k = 512 * group + MX_DEPTH * p + 8 * c, row = 4 * j + r0;
+      if (row < rows && k < K) x[p][j].load(src + (size_t)row * K + k);
+      else x[p][j].zero();
+    }
+  uint32_t word[4] = {0, 0, 0, 0};
+#pragma unroll
+  for (int p = 0; p < 4; ++p) {
+    const int depth = 4 * group + p;
+    if (depth >= depths) break;
+    uint8_t* const out = q + (tile * depths + depth) * MX_TILE + (c >> 2) * 256 + (c & 3) * 4;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t byte = mx_scale_byte(quad_max(x[p][j].top()));
+      word[j] |= byte << (8 * p);
+      *reinterpret_cast<uint32_t*>(out + (4 * j + r0) * 16) = byte == 255 ? 0u : x[p][j].codes(mx_scale_value(byte));
+    }
   }
-  return mx_chunk(v, byte);
+  if ((c & 3) == 0)
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      *reinterpret_cast<uint32_t*>(scales + (tile * groups + group) * MX_SCALES + (c >> 2) * 64 + (4 * j + r0) * 4) = word[j];
 }
 
 }  // namespace

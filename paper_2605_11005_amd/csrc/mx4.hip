@@ -5,33 +5,21 @@
 
 namespace {
 
+#ifndef QC
+#define QC 4
+#endif
 constexpr int QUANT_BLOCK = 256;
 
-// Rows whose elements are contiguous (tokens).  A wavefront makes the tiles of 16 rows by 512 elements: a lane takes the same row and chunk
-// of four operands, 64 bytes (fp32: 128) at a time, and the four scales are the bytes of its word.
+// Rows whose elements are contiguous (tokens): a wavefront per 16 rows by 512 elements.
 template <typename T>
 __global__ __launch_bounds__(QUANT_BLOCK) void mx4_rows(const T* __restrict__ x, int n, int K, long long jobs, uint8_t* __restrict__ q,
                                                          uint8_t* __restrict__ scales) {
-  const int lane = threadIdx.x & 63;
   const long long job = (long long)blockIdx.x * (QUANT_BLOCK / WAVE) + (threadIdx.x >> 6);
   if (job >= jobs) return;
-  const int groups = mx_groups(K), depths = mx_depths(K), tiles = (n + 15) / 16;
-  const int group = (int)(job % groups);
+  const int groups = mx_groups(K), tiles = (n + 15) / 16, group = (int)(job % groups);
   const long long rest = job / groups, batch = rest / tiles;
-  const int row = 16 * (int)(rest - batch * tiles) + (lane & 15), chunk = lane >> 4;
-  const T* src = x + ((size_t)batch * n + row) * K;
-  uint32_t word = 0;
-#pragma unroll
-  for (int p = 0; p < 4; ++p) {
-    const int depth = 4 * group + p, k = MX_DEPTH * depth + MX_CHUNK * chunk;
-    if (depth >= depths) break;
-    uint32_t byte = 0;
-    mx_u32x4 codes = {0, 0, 0, 0};
-    if (row < n && k < K) codes = mx_load_chunk(src + k, byte);
-    word |= byte << (8 * p);
-    *reinterpret_cast<mx_u32x4*>(q + ((size_t)rest * depths + depth) * MX_TILE + lane * 16) = codes;
-  }
-  *reinterpret_cast<uint32_t*>(scales + ((size_t)rest * groups + group) * MX_SCALES + lane * 4) = word;
+  const int row0 = 16 * (int)(rest - batch * tiles);
+  mx_rows_512(x + ((size_t)batch * n + row0) * K, n - row0, K, (size_t)rest, group, threadIdx.x & 63, q, scales);
 }
 
 // Matrices [K][n] whose contraction index is not the contiguous one (weights).  A lane takes four columns of 32 rows; the four

@@ -25,7 +25,11 @@ struct XArgs {
   bf16_t* O;                                   // DOWN
   const int32_t* off; const int32_t* first;
   int e_cnt, N, K;
+  int few_most;                                // rows of an expert that few_tile takes
+  int cached;                                  // experts whose weights fit the Infinity Cache
 };
+
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }      // (the same in all lanes)
 
 // element r of the 16x16 result in a lane: weight column 4 (lane / 16) + r, row lane % 16
 template <int SA, int SB>
@@ -34,7 +38,7 @@ __device__ __forceinline__ f32x4 mfma(u32x4 a, u32x4 b, f32x4 c, uint32_t sa, ui
   return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, y, c, 4, 4, SA, (int)sa, SB, (int)sb);      // 4: e2m1
 }
 
-// ---- rows: 16 rows by 512 elements per wavefront, as mx4_rows; a block finds its tile's expert by itself
+// ---- rows: a wavefront per 16 rows by 512 elements; a block finds its tile's expert by itself
 constexpr int ROWS_BLOCK = 256;
 __global__ __launch_bounds__(ROWS_BLOCK) void expert_rows(const bf16_t* __restrict__ x, const int32_t* __restrict__ off, int e_cnt, int d, int f,
                                                            uint8_t* __restrict__ q, uint8_t* __restrict__ scales, uint8_t* __restrict__ aq,
@@ -55,94 +59,117 @@ __global__ __launch_bounds__(ROWS_BLOCK) void expert_rows(const bf16_t* __restri
     }
     before += __builtin_amdgcn_readlane(incl, WAVE - 1);
   }
-  const int groups = mx_groups(d), depths = mx_depths(d);
-  if (e < 0 || group >= groups) return;
-  const int row = off[e] + 16 * row_tile + (lane & 15), chunk = lane >> 4;
-  const bool in = row < off[e + 1];
-  const bf16_t* src = x + (size_t)row * d;
-  uint32_t word = 0;
-#pragma unroll
-  for (int p = 0; p < 4; ++p) {
-    const int depth = 4 * group + p, k = MX_DEPTH * depth + MX_CHUNK * chunk;
-    if (depth >= depths) break;
-    uint32_t byte = 0;
-    mx_u32x4 codes = {0, 0, 0, 0};
-    if (in && k < d) codes = mx_load_chunk(src + k, byte);
-    word |= byte << (8 * p);
-    *reinterpret_cast<mx_u32x4*>(q + ((size_t)tile * depths + depth) * MX_TILE + lane * 16) = codes;
-  }
-  *reinterpret_cast<uint32_t*>(scales + ((size_t)tile * groups + group) * MX_SCALES + lane * 4) = word;
-  // the chunks of the activations past f, which UP does not write
-  if (group == 0 && f % MX_DEPTH != 0 && chunk >= f % MX_DEPTH / MX_CHUNK) {
+  if (e < 0 || group >= mx_groups(d)) return;
+  const int row0 = off[e] + 16 * row_tile, chunk = lane >> 4;
+  mx_rows_512(x + (size_t)row0 * d, off[e + 1] - row0, d, (size_t)tile, group, lane, q, scales);
+  // what UP does not write of the activations: chunks past f, and the scales behind them
+  if (group == 0 && f % 512 != 0) {
     const int depth = f / MX_DEPTH;
-    *reinterpret_cast<mx_u32x4*>(aq + ((size_t)tile * mx_depths(f) + depth) * MX_TILE + lane * 16) = mx_u32x4{0, 0, 0, 0};
-    as[((size_t)tile * mx_groups(f) + depth / 4) * MX_SCALES + lane * 4 + depth % 4] = 0;
+    if (f % MX_DEPTH != 0 && chunk >= f % MX_DEPTH / MX_CHUNK)
+      *reinterpret_cast<mx_u32x4*>(aq + ((size_t)tile * mx_depths(f) + depth) * MX_TILE + lane * 16) = mx_u32x4{0, 0, 0, 0};
+    *reinterpret_cast<uint32_t*>(as + ((size_t)tile * mx_groups(f) + depth / 4) * MX_SCALES + lane * 4) = 0;
   }
 }
 
-// ---- a few rows per expert: up to 16 * TG rows against 32 columns (UP: 32 of either matrix).  The wavefronts of a block share the contraction,
-// wavefront w the pieces w, w + NW, .. of 512, and their sums are added in LDS in ascending order.
-constexpr int FEW_ROWS = 32, FEW_WAVES = 8, FEW_COLS = 32;
-template <int MODE, int TG>
-__device__ __forceinline__ void few_tile(const XArgs& p, f32x4* lds, int e, int row_tile, int n0, int rows) {
-  constexpr int NB = MODE == UP ? 4 : 2;       // 16-column operands: W1's two, then W3's
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
+// ---- a few rows per expert: up to 16 * TG rows against 32 columns (UP: 32 of either matrix), a stream of weights from memory to registers.  A
+// piece is 512 of the contraction, 16 KB (UP) or 8 KB of weights, in two halves, of which three or two are on their way while one is
+// multiplied.  `split` wavefronts share a tile's contraction, the w-th the pieces w, w + split, .., and their sums are added in LDS in
+// ascending order.
+constexpr int FEW_MOST = 32, FEW_ROWS = 32, FEW_COLS = 32, FEW_WAVES = 8;
+template <int MODE, int TG, bool STREAM>
+struct HalfPiece {
+  static constexpr int NB = MODE == UP ? 4 : 2;       // 16-column operands: W1's two, then W3's
+  u32x4 b[NB][2], a[TG][2];
+  uint32_t bs[NB], as[TG];                            // of the whole piece
+  template <int HALF>
+  __device__ __forceinline__ void load(const XArgs& p, int e, int nt, int tile0, int piece, int depths, int groups, uint32_t lane) {
+    int at[2];
+#pragma unroll
+    for (int q = 0; q < 2; ++q) at[q] = min(4 * piece + 2 * HALF + q, depths - 1);
+#pragma unroll
+    for (int j = 0; j < NB; ++j) {
+      const uint8_t* data = (j < 2 ? p.B0 : p.B1) + e * p.b_es + (size_t)(nt + (j & 1)) * depths * MX_TILE;
+      const uint8_t* scale = (j < 2 ? p.Bs0 : p.Bs1) + e * p.bs_es + ((size_t)(nt + (j & 1)) * groups + piece) * MX_SCALES;
+#pragma unroll
+      for (int q = 0; q < 2; ++q) {
+        const u32x4* from = reinterpret_cast<const u32x4*>(data + (size_t)at[q] * MX_TILE) + lane;
+        b[j][q] = STREAM ? __builtin_nontemporal_load(from) : *from;
+      }
+      bs[j] = reinterpret_cast<const uint32_t*>(scale)[lane];
+    }
+#pragma unroll
+    for (int t = 0; t < TG; ++t) {
+      const uint8_t* data = p.A + (size_t)(tile0 + t) * depths * MX_TILE;
+#pragma unroll
+      for (int q = 0; q < 2; ++q) a[t][q] = reinterpret_cast<const u32x4*>(data + (size_t)at[q] * MX_TILE)[lane];
+      as[t] = reinterpret_cast<const uint32_t*>(p.As + ((size_t)(tile0 + t) * groups + piece) * MX_SCALES)[lane];
+    }
+    __builtin_amdgcn_sched_barrier(0);                // loads stay in order: waiting for one half must not wait for the next
+  }
+  template <int HALF>
+  __device__ __forceinline__ void multiply(f32x4 (&acc)[NB][TG], int left) const {      // left: operands of 128 from the piece's first on
+    static_for<2>([&](auto at) {
+      constexpr int Q = decltype(at)::value, q = 2 * HALF + Q;
+      if (q < left) {
+#pragma unroll
+        for (int j = 0; j < NB; ++j)
+#pragma unroll
+          for (int t = 0; t < TG; ++t) acc[j][t] = mfma<q, q>(b[j][Q], a[t][Q], acc[j][t], bs[j], as[t]);
+      }
+    });
+    __builtin_amdgcn_sched_barrier(0);
+  }
+};
+
+template <int MODE, int TG, bool STREAM>
+__device__ __forceinline__ void few_tile(const XArgs& p, f32x4* lds, int split, int e, int row_tile, int n0, int rows) {
+  constexpr int NB = MODE == UP ? 4 : 2;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), part = wave % split;
   const int depths = mx_depths(p.K), groups = mx_groups(p.K);
-  const int tile0 = p.first[e] + row_tile * (FEW_ROWS / 16);
+  const int tile0 = uniform(p.first[e]) + row_tile * (FEW_ROWS / 16);
+  const bool in = n0 < p.N;                           // (the last block of columns may be short of a wavefront's)
   f32x4 acc[NB][TG];
 #pragma unroll
   for (int j = 0; j < NB; ++j)
 #pragma unroll
     for (int t = 0; t < TG; ++t) acc[j][t] = f32x4{0.f, 0.f, 0.f, 0.f};
-  for (int group = wave; group < groups; group += waves) {
-    u32x4 b[NB][4], a[TG][4];
-    uint32_t bs[NB], as[TG];
-#pragma unroll
-    for (int j = 0; j < NB; ++j) {
-      const int nt = n0 / 16 + (j & 1);
-      const uint8_t* data = (j < 2 ? p.B0 : p.B1) + e * p.b_es + (size_t)nt * depths * MX_TILE + lane * 16;
-      const uint8_t* scale = (j < 2 ? p.Bs0 : p.Bs1) + e * p.bs_es + ((size_t)nt * groups + group) * MX_SCALES + lane * 4;
-#pragma unroll
-      for (int q = 0; q < 4; ++q)
-        b[j][q] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(data + (size_t)min(4 * group + q, depths - 1) * MX_TILE));
-      bs[j] = *reinterpret_cast<const uint32_t*>(scale);
-    }
-#pragma unroll
-    for (int t = 0; t < TG; ++t) {
-      const uint8_t* data = p.A + (size_t)(tile0 + t) * depths * MX_TILE + lane * 16;
-#pragma unroll
-      for (int q = 0; q < 4; ++q) a[t][q] = *reinterpret_cast<const u32x4*>(data + (size_t)min(4 * group + q, depths - 1) * MX_TILE);
-      as[t] = *reinterpret_cast<const uint32_t*>(p.As + ((size_t)(tile0 + t) * groups + group) * MX_SCALES + lane * 4);
-    }
-    static_for<4>([&](auto at) {
-      constexpr int q = decltype(at)::value;
-      if (4 * group + q < depths) {
-#pragma unroll
-        for (int j = 0; j < NB; ++j)
-#pragma unroll
-          for (int t = 0; t < TG; ++t) acc[j][t] = mfma<q, q>(b[j][q], a[t][q], acc[j][t], bs[j], as[t]);
-      }
-    });
+  if (in && part < groups) {
+    constexpr int AHEAD = TG == 1 ? 4 : 3, TURN = TG == 1 ? 4 : 6;      // (register numbers and halves are those of a whole turn)
+    HalfPiece<MODE, TG, STREAM> half[AHEAD];
+    const int halves = 2 * ((groups - part + split - 1) / split);
+    const auto load = [&](auto which, int h) {
+      constexpr int W = decltype(which)::value;
+      if (h < halves) half[W % AHEAD].template load<W % 2>(p, e, n0 / 16, tile0, part + h / 2 * split, depths, groups, lane);
+    };
+    static_for<AHEAD>([&](auto u) { load(u, decltype(u)::value); });
+    for (int h = 0; h < halves; h += TURN)
+      static_for<TURN>([&](auto u) {
+        constexpr int W = decltype(u)::value;
+        if (h + W >= halves) return;
+        half[W % AHEAD].template multiply<W % 2>(acc, depths - 4 * (part + (h + W) / 2 * split));
+        load(Int<W + AHEAD>{}, h + W + AHEAD);
+      });
   }
   const int i = lane & 15, g = lane >> 4;
 #pragma unroll
   for (int t = 0; t < TG; ++t) {
-    if (waves > 1) {
+    f32x4 sum[NB];
+#pragma unroll
+    for (int j = 0; j < NB; ++j) sum[j] = acc[j][t];
+    if (split > 1) {
       __syncthreads();
 #pragma unroll
       for (int j = 0; j < NB; ++j) lds[(wave * NB + j) * WAVE + lane] = acc[j][t];
       __syncthreads();
-    }
-    if (wave != t % waves) continue;
-    f32x4 sum[NB];
+      if (part != t % split) continue;
+      const int base = wave - part;
 #pragma unroll
-    for (int j = 0; j < NB; ++j) {
-      sum[j] = acc[j][t];
-      if (waves > 1) {
-        sum[j] = lds[j * WAVE + lane];
-        for (int w = 1; w < waves; ++w) sum[j] += lds[(w * NB + j) * WAVE + lane];
+      for (int j = 0; j < NB; ++j) {
+        sum[j] = lds[(base * NB + j) * WAVE + lane];
+        for (int w = 1; w < split; ++w) sum[j] += lds[((base + w) * NB + j) * WAVE + lane];
       }
     }
+    if (!in) continue;
     if constexpr (MODE == UP) {
       // this lane's eight of the row's 32 activations: columns 16 j + 4 g + r
       float v[2][4];
@@ -178,8 +205,10 @@ __device__ __forceinline__ void few_tile(const XArgs& p, f32x4* lds, int e, int 
   }
 }
 
-// Experts in the order of RaggedTiles, but only those whose row count lies in (LO, hi]; rows in tiles of TM.
-template <int TM>
+// Tiles of the experts whose row count lies in (lo, hi], in ascending order of the experts; rows in tiles of TM.  An expert's tiles go through GROUP
+// row tiles at a time, row tiles fastest, so that the tiles that an XCD multiplies at one time are a compact patch, whose operands its L2
+// holds for all of them.
+template <int TM, int GROUP>
 struct SomeTiles {
   const int32_t* off;
   int e_cnt, lane, lo, hi;
@@ -195,51 +224,53 @@ struct SomeTiles {
     total = __builtin_amdgcn_readlane(incl, WAVE - 1);
     for (int base = WAVE; base < e_cnt; base += WAVE) total += wave_sum(count(base + lane));
   }
-  // tile b of a walk that goes through every XCD's contiguous eighth; false: past its end
-  __device__ __forceinline__ bool tile(int n_cols, int b, int& e, int& row_tile, int& col_tile) const {
-    const int share = (total * n_cols + 7) / 8;
-    const int at = (b % 8) * share + b / 8;
-    if (b / 8 >= share || at >= total * n_cols) return false;
-    int t = at / n_cols, rows = n, up_to = incl;
-    col_tile = at - t * n_cols;
-    for (int base = 0;; base += WAVE) {          // ends: t < total
+  // tile t < total n_cols
+  __device__ __forceinline__ void at(int t, int n_cols, int& e, int& row_tile, int& col_tile) const {
+    int rows = n, up_to = incl;
+    for (int base = 0;; base += WAVE) {          // ends: t < total n_cols
       if (base > 0) up_to = wave_scan(rows = count(base + lane));
-      const unsigned long long past = __ballot(up_to > t);
+      const unsigned long long past = __ballot(up_to * n_cols > t);
       if (past) {
         const int who = __builtin_ctzll(past);
-        row_tile = t - __builtin_amdgcn_readlane(up_to - rows, who);
         e = base + who;
-        return true;
+        rows = __builtin_amdgcn_readlane(rows, who);
+        t -= (__builtin_amdgcn_readlane(up_to, who) - rows) * n_cols;
+        const int group = t / (GROUP * n_cols), in_group = min(GROUP, rows - group * GROUP);
+        t -= group * GROUP * n_cols;
+        col_tile = t / in_group;
+        row_tile = group * GROUP + t - col_tile * in_group;
+        break;
       }
-      t -= __builtin_amdgcn_readlane(up_to, WAVE - 1);
+      t -= __builtin_amdgcn_readlane(up_to, WAVE - 1) * n_cols;
     }
+    e = uniform(e);                              // (the compiler does not see that it is the same in all lanes)
+    row_tile = uniform(row_tile);
+    col_tile = uniform(col_tile);
+  }
+  // tile b of a walk that goes through every XCD's contiguous eighth; false: past its end
+  __device__ __forceinline__ bool find(int n_cols, int b, int& e, int& row_tile, int& col_tile) const {
+    const int share = (total * n_cols + 7) / 8, t = (b % 8) * share + b / 8;
+    if (b / 8 >= share || t >= total * n_cols) return false;
+    at(t, n_cols, e, row_tile, col_tile);
+    return true;
   }
 };
 
-template <int MODE>
-__global__ __launch_bounds__(FEW_WAVES * WAVE) void few_rows_mx4(XArgs p) {
-  __shared__ f32x4 lds[FEW_WAVES * (MODE == UP ? 4 : 2) * WAVE];
-  const SomeTiles<FEW_ROWS> list(p.off, p.e_cnt, threadIdx.x & 63, 0, 0x7FFFFFFF);
-  int e, row_tile, col_tile;
-  if (!list.tile(p.N / FEW_COLS, blockIdx.x, e, row_tile, col_tile)) return;
-  const int rows = p.off[e + 1] - p.off[e] - row_tile * FEW_ROWS;
-  if (rows <= 16) few_tile<MODE, 1>(p, lds, e, row_tile, col_tile * FEW_COLS, rows);
-  else few_tile<MODE, 2>(p, lds, e, row_tile, col_tile * FEW_COLS, rows);
-}
-
-// ---- many rows per expert: 128 rows against 256 weight rows (UP: 128 of either matrix), four wavefronts of 64 by 128 in 32x32x64
-// instructions.  Operands go from memory to LDS directly, 128 of the contraction at a time through a ring of three stages; their layout in
-// memory is the one that the instruction wants, so every load is 1 KB of consecutive bytes and every LDS read free of conflicts.
-constexpr int GEMM_ROWS = 128, GEMM_COLS = 256, GEMM_THREADS = 256;
-constexpr int STAGE_TILES = (GEMM_ROWS + GEMM_COLS) / 16, STAGE = STAGE_TILES * MX_TILE, STAGES = 3;
-constexpr int STAGE_LOADS = STAGE_TILES / 4, SCALE_LOADS = 2;           // per wavefront
-constexpr int GEMM_LDS = STAGES * STAGE + STAGE_TILES * MX_SCALES;
+// ---- many rows per expert: 256 rows (the last of an expert: 256, 128 or 64) against 256 weight rows (UP: 128 of either matrix).  Eight
+// wavefronts of 128 by 64 (64 by 64, 32 by 64) multiply in 32x32x64 instructions, two on each SIMD.  Operands go from memory to LDS
+// directly, 128 of the contraction at a time, through a ring of four stages of which three are on their way.  Their layout in memory is
+// the one that the instruction wants, so every load is 1 KB of consecutive bytes and every LDS read free of conflicts.  Workgroups are
+// persistent, and the loads run ahead into the next tile while a finished one is written.
+constexpr int GEMM_GROUP = 4, GEMM_ROWS = 256, GEMM_COLS = 256, GEMM_THREADS = 512;
+constexpr int STAGE = 32 * MX_TILE, STAGES = 4, SCALES = 32 * MX_SCALES;       // operand tiles of a stage: 16 of the rows, 16 of the weights
+constexpr int GEMM_LDS = STAGES * STAGE + 2 * SCALES;
+constexpr int LEAST_DEPTHS = 4;            // the two places for scales need a contraction of more than 384 (see Loads)
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
-template <int S>
+// (scales: the words' lowest bytes)
 __device__ __forceinline__ f32x16 mfma32(u32x4 a, u32x4 b, f32x16 c, uint32_t sa, uint32_t sb) {
   const i32x8 x = {(int)a[0], (int)a[1], (int)a[2], (int)a[3], 0, 0, 0, 0}, y = {(int)b[0], (int)b[1], (int)b[2], (int)b[3], 0, 0, 0, 0};
-  return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, y, c, 4, 4, S, (int)sa, S, (int)sb);
+  return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, y, c, 4, 4, 0, (int)sa, 0, (int)sb);
 }
 // lanes 32..63 of a and lanes 0..31 of b change places
 __device__ __forceinline__ void swap32(uint32_t& a, uint32_t& b) {
@@ -247,122 +278,181 @@ __device__ __forceinline__ void swap32(uint32_t& a, uint32_t& b) {
   a = r[0];
   b = r[1];
 }
+// until at most N of this wavefront's loads are on their way and its LDS reads are done, and until all wavefronts are there
 template <int N>
 __device__ __forceinline__ void wait_and_meet() { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"(N) : "memory"); }
 
+typedef SomeTiles<GEMM_ROWS, GEMM_GROUP> GemmTiles;
 template <int MODE>
-__device__ __forceinline__ void gemm_tile(const XArgs& p, uint8_t* lds, int e, int row_tile, int col_tile, int rows) {
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int depths = mx_depths(p.K), groups = mx_groups(p.K);
-  const int tile0 = p.first[e] + row_tile * (GEMM_ROWS / 16), row_tiles = (min(rows, GEMM_ROWS) + 15) / 16;
-  const int cols = MODE == UP ? GEMM_COLS / 2 : GEMM_COLS, n0 = col_tile * cols, col_tiles = min(cols, p.N - n0) / 16;
-  const uint32_t lds0 = lds_addr(lds), scales0 = lds0 + STAGES * STAGE;
-  // Operand tile i of a stage: 0..7 the rows', 8..23 the weights' (UP: 8 of W1, 8 of W3); wavefront w loads 6 w .. 6 w + 5.  Tiles past the
-  // rows or columns repeat the last one: their results are not stored.
-  const uint8_t* data[STAGE_LOADS];
-#pragma unroll
-  for (int j = 0; j < STAGE_LOADS; ++j) {
-    const int i = STAGE_LOADS * wave + j;
-    const uint8_t* base;
-    int t;
-    if (i < 8) {
-      base = p.A; t = tile0 + min(i, row_tiles - 1);
-    } else {
-      const int c = i - 8;
-      base = (MODE == UP && c >= 8 ? p.B1 : p.B0) + e * p.b_es;
-      t = n0 / 16 + min(MODE == UP ? c & 7 : c, col_tiles - 1);
-    }
-    data[j] = base + (size_t)t * depths * MX_TILE;
+struct Place {                             // of a tile
+  int e = 0, row_tile = 0, col_tile = 0, rows = 0;      // rows: from its first row to the expert's end
+  static constexpr int COLS = MODE == UP ? GEMM_COLS / 2 : GEMM_COLS;
+  __device__ __forceinline__ bool find(const XArgs& p, const GemmTiles& list, int b) {
+    if (!list.find((p.N + COLS - 1) / COLS, b, e, row_tile, col_tile)) return false;
+    rows = uniform(p.off[e + 1] - p.off[e]) - row_tile * GEMM_ROWS;
+    return true;
   }
-  // Scales of 512: four operand tiles per load.  Of the six loads wavefront w makes the weights' w-th and the rows' w % 2-th (twice the same
-  // bytes to the same place, so that all wavefronts wait for equally many).
-  const uint8_t* scale_a;
-  const uint8_t* scale_b;
-  uint32_t voff_a, voff_b;
-  {
-    const int ta = 4 * (wave & 1) + lane / 16, tb = 4 * wave + lane / 16;
-    scale_a = p.As + (size_t)tile0 * groups * MX_SCALES;
-    voff_a = (uint32_t)(min(ta, row_tiles - 1) * groups * MX_SCALES + lane % 16 * 16);
-    scale_b = (MODE == UP && wave >= 2 ? p.Bs1 : p.Bs0) + e * p.bs_es + (size_t)(n0 / 16) * groups * MX_SCALES;
-    voff_b = (uint32_t)(min(MODE == UP ? tb & 7 : tb, col_tiles - 1) * groups * MX_SCALES + lane % 16 * 16);
+};
+
+// The loads of a workgroup's tiles, stage after stage.  Of a stage wavefront w loads tiles 2 w and 2 w + 1 of the rows and of the weights (UP: 8 of
+// W1, 8 of W3), four loads whatever the tile; those past the rows or columns repeat the last one (their results are not stored), and
+// behind the last tile the same bytes are loaded again and again, so that the number of loads on their way is the same everywhere and the
+// products' loop has no branch.  The scales of 512 come with the first stage of the four.  Of those two are kept: with four stages to a
+// contraction at least, two in succession belong to four stages or more, so that what is overwritten has been read.
+template <int MODE>
+struct Loads {
+  const XArgs& p;
+  const GemmTiles& list;
+  Place<MODE> at;
+  int b, t, depths, groups, lane, wave;
+  bool more;
+  uint32_t lds0, stage = 0, scales = 0;
+  const uint8_t* a; const uint8_t* bw; const uint8_t* sc;
+  uint32_t va[2], vb[2], vsc;
+  __device__ __forceinline__ Loads(const XArgs& p_, const GemmTiles& list_, uint32_t lds0_, int lane_, int wave_)
+      : p(p_), list(list_), b(blockIdx.x), depths(mx_depths(p_.K)), groups(mx_groups(p_.K)), lane(lane_), wave(wave_), lds0(lds0_) {
+    begin();
   }
-  const uint32_t voff = lane * 16;
-  auto issue = [&](int t) {
-    if (t % 4 == 0) {
-      const size_t at = (size_t)(t / 4) * MX_SCALES;
-      lds_load16((const bf16_t*)(scale_a + at), voff_a, scales0 + (wave & 1) * 1024);
-      lds_load16((const bf16_t*)(scale_b + at), voff_b, scales0 + 2048 + wave * 1024);
+  __device__ __forceinline__ void begin() {
+    t = 0;
+    more = at.find(p, list, b);
+    const bool second = MODE == UP && wave >= 4;          // W3's
+    const int first_b = second ? 2 * wave - 8 : 2 * wave;
+    // scales, four tiles' at a time: wavefronts 0 .. 3 the rows', 4 .. 7 the weights' (UP: 4 and 5 W1's)
+    const bool of_weights = wave >= 4, of_second = MODE == UP && wave >= 6;
+    const int first_s = 4 * (wave & (MODE == UP && of_weights ? 1 : 3));
+    int last_a = 0, last_b = 0;
+    if (more) {
+      const int n0 = at.col_tile * Place<MODE>::COLS;
+      const size_t tile0 = uniform(p.first[at.e]) + at.row_tile * (GEMM_ROWS / 16);
+      last_a = (min(at.rows, GEMM_ROWS) + 15) / 16 - 1;
+      last_b = min(Place<MODE>::COLS, p.N - n0) / 16 - 1;
+      a = p.A + tile0 * depths * MX_TILE;
+      bw = (second ? p.B1 : p.B0) + at.e * p.b_es + (size_t)(n0 / 16) * depths * MX_TILE;
+      sc = of_weights ? (of_second ? p.Bs1 : p.Bs0) + at.e * p.bs_es + (size_t)(n0 / 16) * groups * MX_SCALES : p.As + tile0 * groups * MX_SCALES;
     }
-    const uint32_t slot = lds0 + t % STAGES * STAGE + STAGE_LOADS * wave * MX_TILE;
 #pragma unroll
-    for (int j = 0; j < STAGE_LOADS; ++j) lds_load16((const bf16_t*)(data[j] + (size_t)t * MX_TILE), voff, slot + j * MX_TILE);
-  };
+    for (int j = 0; j < 2; ++j) {
+      va[j] = (uint32_t)(min(2 * wave + j, last_a) * depths * MX_TILE + lane * 16);
+      vb[j] = (uint32_t)(min(first_b + j, last_b) * depths * MX_TILE + lane * 16);
+    }
+    vsc = (uint32_t)(min(first_s + lane / 16, of_weights ? last_b : last_a) * groups * MX_SCALES + lane % 16 * 16);
+  }
+  // before a stage's loads
+  __device__ __forceinline__ void head() {
+    if (t == depths) {
+      b += gridDim.x;
+      begin();
+    }
+    if (more && t % 4 == 0) {
+      lds_load16((const bf16_t*)(sc + (size_t)(t / 4) * MX_SCALES), vsc, lds0 + STAGES * STAGE + scales + wave * 1024);
+      scales ^= SCALES;
+    }
+  }
+  // A stage's loads, one after the other: the caller spreads them over its products (issued in a row, a load keeps a wavefront for 80 cycles
+  // while the others issue theirs).
+  static constexpr int PARTS = 4;
+  template <int I>
+  __device__ __forceinline__ void part() {
+    const size_t from = (size_t)t * MX_TILE;
+    if (I < 2) lds_load16((const bf16_t*)(bw + from), vb[I % 2], lds0 + stage + (16 + 2 * wave + I) * MX_TILE);
+    else lds_load16((const bf16_t*)(a + from), va[I % 2], lds0 + stage + (2 * wave + I % 2) * MX_TILE);
+    if (I == PARTS - 1) {
+      stage = (stage + STAGE) % (STAGES * STAGE);
+      t += more ? 1 : 0;
+    }
+  }
+  __device__ __forceinline__ void issue() {
+    head();
+    static_for<PARTS>([&](auto i) { part<decltype(i)::value>(); });
+  }
+  // The next stage in order has arrived for all wavefronts, and all have done with the one that is to be loaded again.  The two stages behind it
+  // are on their way.  (Scales or stores of a finished tile among what is on its way make the wait longer, never shorter.)
+  __device__ __forceinline__ void wait() { wait_and_meet<2 * PARTS>(); }
+};
+
+// A wavefront multiplies 32 * NA rows, half of the tile's, by 64 weight rows (UP: 32 of either matrix).  stage, scales: where this tile's first are.
+template <int MODE, int NA>
+__device__ __forceinline__ void gemm_tile(const XArgs& p, Loads<MODE>& loads, const uint8_t* lds, uint32_t& stage, uint32_t& scales, const Place<MODE>& at,
+                                          int lane, int wave) {
+  constexpr int NB = 2, HALF = NB / 2;     // 32-column operands; UP: of either matrix
+  const int depths = loads.depths, n0 = at.col_tile * Place<MODE>::COLS;
   const int wr = wave & 1, wc = wave >> 1, h = lane >> 5;
-  const bool active = 64 * wr < rows;                 // (of a tile with up to 64 rows two wavefronts only load)
-  // weights: 32-column operand j of this wavefront begins at tile b_tile(j) of the stage
-  const auto b_tile = [&](int j) { return MODE == UP ? 8 + 8 * (j >> 1) + 4 * wc + 2 * (j & 1) : 8 + 8 * wc + 2 * j; };
-  const int at = (lane >> 4 & 1) * MX_TILE + h * 256 + (lane & 15) * 16, scale_at = (lane >> 4 & 1) * MX_SCALES + h * 64 + (lane & 15) * 4;
-  f32x16 acc[2][4];
+  const auto b_tile = [&](int j) { return 16 + (MODE == UP ? 8 * (j / HALF) + 2 * (HALF * wc + j % HALF) : 2 * (NB * wc + j)); };
+  const int in_tile = (lane >> 4 & 1) * MX_TILE + h * 256 + (lane & 15) * 16, in_scales = (lane >> 4 & 1) * MX_SCALES + h * 64 + (lane & 15) * 4;
+  f32x16 acc[NA][NB];
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
+  for (int i = 0; i < NA; ++i)
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+    for (int j = 0; j < NB; ++j)
 #pragma unroll
       for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
-  uint32_t as[2][2], bs[4][2];
-  const uint8_t* const scales = lds + STAGES * STAGE + scale_at;
-  __syncthreads();                                    // the stages may still be read for the tile before
-  issue(0);
-  if (depths > 1) issue(1);
-  auto stage = [&](int t, auto which) {
-    constexpr int Q = decltype(which)::value;         // t % 4
-    if (t + 1 < depths) wait_and_meet<STAGE_LOADS + (Q == 3 ? SCALE_LOADS : 0)>();
-    else wait_and_meet<0>();
-    if (t + 2 < depths) issue(t + 2);
-    if (!active) return;
-    if (Q == 0) {
-#pragma unroll
-      for (int s = 0; s < 2; ++s) {
-#pragma unroll
-        for (int i = 0; i < 2; ++i) as[i][s] = *reinterpret_cast<const uint32_t*>(scales + (4 * wr + 2 * i) * MX_SCALES + 128 * s);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) bs[j][s] = *reinterpret_cast<const uint32_t*>(scales + b_tile(j) * MX_SCALES + 128 * s);
-      }
+  u32x4 a[2][NA], b[2][NB];
+  uint32_t as[2][NA], bs[2][NB];
+  // operand I of step s (64 of the contraction) of the stage in place, and its scales
+  const uint8_t* from;
+  const uint8_t* scales_from;
+  const auto read = [&](auto step, auto which) {
+    // in the order in which the products take them: a weight operand, a row operand, the other weights, the other rows
+    constexpr int s = decltype(step)::value, N = decltype(which)::value, I = N == 0 ? NA : N == 1 ? 0 : N <= NB ? NA + N - 1 : N - NB;
+    if constexpr (I < NA) {
+      a[s][I] = *reinterpret_cast<const u32x4*>(from + 512 * s + (2 * NA * wr + 2 * I) * MX_TILE);
+      as[s][I] = scales_from[128 * s + (2 * NA * wr + 2 * I) * MX_SCALES];
+    } else {
+      b[s][I - NA] = *reinterpret_cast<const u32x4*>(from + 512 * s + b_tile(I - NA) * MX_TILE);
+      bs[s][I - NA] = scales_from[128 * s + b_tile(I - NA) * MX_SCALES];
     }
-    const uint8_t* const slot = lds + t % STAGES * STAGE + at;
-    u32x4 a[2][2], b[2][4];
-#pragma unroll
-    for (int s = 0; s < 2; ++s) {
-#pragma unroll
-      for (int i = 0; i < 2; ++i) a[s][i] = *reinterpret_cast<const u32x4*>(slot + (4 * wr + 2 * i) * MX_TILE + 512 * s);
-#pragma unroll
-      for (int j = 0; j < 4; ++j) b[s][j] = *reinterpret_cast<const u32x4*>(slot + b_tile(j) * MX_TILE + 512 * s);
-    }
-#pragma unroll
-    for (int s = 0; s < 2; ++s)
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc[i][j] = mfma32<Q>(b[s][j], a[s][i], acc[i][j], bs[j][s], as[i][s]);
   };
-  for (int t = 0; t < depths; t += 4)
-    static_for<4>([&](auto q) {
-      if (t + decltype(q)::value < depths) stage(t + decltype(q)::value, q);
+  // The products of a step, and between them the reads of the other one's operands and half of a stage's loads.
+  constexpr int PRODUCTS = NA * NB, READS = NA + NB, READ_WITHIN = 3 * PRODUCTS / 4, LOADS = Loads<MODE>::PARTS / 2;
+  const auto multiply = [&](auto step) {
+    constexpr int s = decltype(step)::value;
+    static_for<PRODUCTS>([&](auto m) {
+      constexpr int M = decltype(m)::value, i = M / NB, j = M % NB;
+      acc[i][j] = mfma32(b[s][j], a[s][i], acc[i][j], bs[s][j], as[s][i]);
+      constexpr int R0 = M * READS / READ_WITHIN, R = M < READ_WITHIN ? (M + 1) * READS / READ_WITHIN - R0 : 0;
+      if constexpr (R > 0) static_for<R>([&](auto r) { read(Int<1 - s>{}, Int<R0 + decltype(r)::value>{}); });
+      constexpr int L0 = M * LOADS / PRODUCTS, L = (M + 1) * LOADS / PRODUCTS - L0;
+      if constexpr (L > 0) static_for<L>([&](auto l) { loads.template part<(s == 0 ? LOADS : 0) + L0 + decltype(l)::value>(); });
+      __builtin_amdgcn_sched_barrier(0);
     });
-  if (!active) return;
+  };
+  // While one step's operands are multiplied the other's are on their way from LDS, across the barrier too, and the loads of the stage that
+  // takes the place of the one before are issued.
+  const auto begin = [&](int t) {
+    loads.wait();
+    loads.head();
+    from = lds + stage + in_tile;
+    scales_from = lds + STAGES * STAGE + scales + in_scales + t % 4;
+    stage = (stage + STAGE) % (STAGES * STAGE);
+    if (t % 4 == 3 || t == depths - 1) scales ^= SCALES;
+  };
+  begin(0);
+  static_for<READS>([&](auto r) { read(Int<0>{}, r); });
+  static_for<LOADS>([&](auto l) { loads.template part<decltype(l)::value>(); });
+  multiply(Int<0>{});
+  for (int t = 1; t < depths; ++t) {
+    begin(t);
+    multiply(Int<1>{});
+    multiply(Int<0>{});
+  }
+#pragma unroll
+  for (int i = 0; i < NA; ++i)
+#pragma unroll
+    for (int j = 0; j < NB; ++j) acc[i][j] = mfma32(b[1][j], a[1][i], acc[i][j], bs[1][j], as[1][i]);
   // element 4 g + r of acc[i][j]: row lane % 32, column 8 g + 4 h + r of the 32
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int row = 64 * wr + 32 * i + (lane & 31);
+  for (int i = 0; i < NA; ++i) {
+    const int row = 32 * (NA * wr + i) + (lane & 31);
     if constexpr (MODE == UP) {
-      const int tile = tile0 + row / 16;
+      const int tile = p.first[at.e] + at.row_tile * (GEMM_ROWS / 16) + row / 16;
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
+      for (int j = 0; j < HALF; ++j) {
         float v[16];
         uint32_t top = 0;
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
-          v[r] = silu_f(acc[i][j][r]) * acc[i][j + 2][r];
+          v[r] = silu_f(acc[i][j][r]) * acc[i][j + HALF][r];
           top = max(top, __float_as_uint(v[r]) & 0x7FFFFFFFu);
         }
         uint32_t other = top;
@@ -372,49 +462,94 @@ __device__ __forceinline__ void gemm_tile(const XArgs& p, uint8_t* lds, int e, i
         uint32_t lo = byte == 255 ? 0u : mx_pack8(v, s), hi = byte == 255 ? 0u : mx_pack8(v + 8, s);
         swap32(lo, hi);                               // now bytes 8 h .. 8 h + 7 of the chunk, in halves of two lanes
         const u32x2 codes = {__builtin_amdgcn_perm(hi, lo, 0x05040100u), __builtin_amdgcn_perm(hi, lo, 0x07060302u)};
-        const int col = n0 + 64 * wc + 32 * j;
-        if (row >= rows || col >= p.N) continue;
+        const int col = n0 + 32 * (HALF * wc + j);
+        if (row >= at.rows || col >= p.N) continue;
         const int depth = col / MX_DEPTH, chunk = col % MX_DEPTH / MX_CHUNK;
         *reinterpret_cast<u32x2*>(p.C + ((size_t)tile * mx_depths(p.N) + depth) * MX_TILE + chunk * 256 + row % 16 * 16 + 8 * h) = codes;
         if (h == 0) p.Cs[((size_t)tile * mx_groups(p.N) + depth / 4) * MX_SCALES + chunk * 64 + row % 16 * 4 + depth % 4] = (uint8_t)byte;
       }
     } else {
-      bf16_t* const out = p.O + ((size_t)p.off[e] + row_tile * GEMM_ROWS + row) * p.N + n0 + 128 * wc + 16 * h;
+      bf16_t* const out = p.O + ((size_t)p.off[at.e] + at.row_tile * GEMM_ROWS + row) * p.N + n0 + 32 * NB * wc + 16 * h;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
+      for (int j = 0; j < NB; ++j) {
         uint32_t w[8];
 #pragma unroll
         for (int r = 0; r < 8; ++r) w[r] = pack_bf16x2(acc[i][j][2 * r], acc[i][j][2 * r + 1]);
 #pragma unroll
         for (int r = 0; r < 4; ++r) swap32(w[r], w[r + 4]);         // columns 16 h .. 16 h + 15
-        if (row >= rows || n0 + 128 * wc + 32 * j >= p.N) continue;
+        if (row >= at.rows || n0 + 32 * (NB * wc + j) >= p.N) continue;
         reinterpret_cast<u32x4*>(out + 32 * j)[0] = u32x4{w[0], w[1], w[4], w[5]};
         reinterpret_cast<u32x4*>(out + 32 * j)[1] = u32x4{w[2], w[3], w[6], w[7]};
       }
     }
   }
+  // Where the lanes that stored meet the others: in a block of its own, for the compiler to see that what the walk keeps is the same in all
+  // lanes (merged with the walk's own blocks, it kept LDS places and counters in vector registers).
+  __builtin_amdgcn_wave_barrier();
 }
 
 // Workgroups walk the tiles of the experts with many rows, then those of the experts with few.
-constexpr int FEW_MOST = 32;               // rows
+template <int MODE, bool STREAM>
+__device__ __forceinline__ void few_tiles(const XArgs& p, const SomeTiles<FEW_ROWS, 1>& list, f32x4* lds, int place, int idle, int rounds) {
+  if (list.total == 0) return;
+  // In how many wavefronts a tile's contraction is cut, and how many of the blocks of tiles the `idle` workgroups and the others, which have one
+  // more of the large tiles behind them, take each.  Alone and few enough for every workgroup to have one: cut as far as they stay so.
+  // Else the plan that ends first, in tenths of a large tile's stage: a block of tiles streams eight or four KB per wavefront in the place of
+  // a stage's 16 KB, and begins and ends in what two stages take.
+  const int cols = p.N / FEW_COLS, pieces = mx_groups(p.K);
+  int split = FEW_WAVES, quota = 1, quota_others = 0;
+  while (split > 1 && (split > pieces || list.total * ((cols * split + FEW_WAVES - 1) / FEW_WAVES) > (int)gridDim.x)) split /= 2;
+  if (rounds > 0 || list.total * ((cols * split + FEW_WAVES - 1) / FEW_WAVES) > (int)gridDim.x) {
+    const float stages = rounds > 0 ? 10.f * mx_depths(p.K) : 0.f, all = gridDim.x, others = all - idle;
+    float best = __builtin_inff();
+    for (int s = 1; s <= FEW_WAVES && s <= pieces; s *= 2) {
+      const float n = (float)list.total * ((cols * s + FEW_WAVES - 1) / FEW_WAVES), cost = ((pieces + s - 1) / s) * (MODE == UP ? 48.f : 24.f) + 20.f;
+      const float level = fmaxf(0.f, floorf((n * cost - idle * stages) / (all * cost)));          // of the others, in blocks of tiles
+      for (float q = level; q < level + 2.f; q += 1.f) {
+        const float qi = fmaxf(0.f, ceilf((n - others * q) / idle)), time = fmaxf(qi * cost, stages + q * cost);
+        if (time < best) { best = time; split = s; quota = (int)qi; quota_others = (int)q; }
+      }
+    }
+  }
+  split = uniform(split); quota = uniform(quota); quota_others = uniform(quota_others);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), per_block = FEW_WAVES / split, n_cols = (cols + per_block - 1) / per_block;
+  const int n = list.total * n_cols, step = place < idle ? idle : gridDim.x - idle;
+  int t = place < idle ? place : idle * quota + place - idle, e, row_tile, col_tile;
+  for (int k = place < idle ? quota : quota_others; k > 0 && t < n; --k, t += step) {
+    list.at(t, n_cols, e, row_tile, col_tile);
+    const int rows = p.off[e + 1] - p.off[e] - row_tile * FEW_ROWS, n0 = (col_tile * per_block + wave / split) * FEW_COLS;
+    if (rows <= 16) few_tile<MODE, 1, STREAM>(p, lds, split, e, row_tile, n0, rows);
+    else few_tile<MODE, 2, STREAM>(p, lds, split, e, row_tile, n0, rows);
+  }
+}
+
 template <int MODE>
-__global__ __launch_bounds__(GEMM_THREADS, 2) void experts_mx4(XArgs p) {
+__global__ __launch_bounds__(GEMM_THREADS, 1) void experts_mx4(XArgs p) {
   extern __shared__ uint8_t gemm_lds[];
-  const int lane = threadIdx.x & 63;
-  int e, row_tile, col_tile;
-  {
-    const SomeTiles<GEMM_ROWS> list(p.off, p.e_cnt, lane, FEW_MOST, 0x7FFFFFFF);
-    const int cols = MODE == UP ? GEMM_COLS / 2 : GEMM_COLS;
-    for (int b = blockIdx.x; list.tile((p.N + cols - 1) / cols, b, e, row_tile, col_tile); b += gridDim.x)
-      gemm_tile<MODE>(p, gemm_lds, e, row_tile, col_tile, p.off[e + 1] - p.off[e] - row_tile * GEMM_ROWS);
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const GemmTiles many(p.off, p.e_cnt, lane, p.few_most, 0x7FFFFFFF);
+  Place<MODE> at;
+  if (at.find(p, many, blockIdx.x)) {
+    Loads<MODE> loads(p, many, lds_addr(gemm_lds), lane, wave);
+    uint32_t stage = 0, scales = 0;
+    loads.issue();
+    loads.issue();
+    loads.issue();
+    for (int b = blockIdx.x;;) {
+      if (at.rows > 128) gemm_tile<MODE, 4>(p, loads, gemm_lds, stage, scales, at, lane, wave);
+      else if (at.rows > 64) gemm_tile<MODE, 2>(p, loads, gemm_lds, stage, scales, at, lane, wave);
+      else gemm_tile<MODE, 1>(p, loads, gemm_lds, stage, scales, at, lane, wave);
+      b += gridDim.x;
+      if (!at.find(p, many, b)) break;
+    }
+    wait_and_meet<0>();                               // LDS is the next tiles' own: what is still loaded has arrived, the last stage is read
   }
-  const SomeTiles<FEW_ROWS> list(p.off, p.e_cnt, lane, 0, FEW_MOST);
-  for (int b = blockIdx.x; list.tile(p.N / FEW_COLS, b, e, row_tile, col_tile); b += gridDim.x) {
-    const int rows = p.off[e + 1] - p.off[e] - row_tile * FEW_ROWS;
-    __syncthreads();
-    if (rows <= 16) few_tile<MODE, 1>(p, reinterpret_cast<f32x4*>(gemm_lds), e, row_tile, col_tile * FEW_COLS, rows);
-    else few_tile<MODE, 2>(p, reinterpret_cast<f32x4*>(gemm_lds), e, row_tile, col_tile * FEW_COLS, rows);
-  }
+  const SomeTiles<FEW_ROWS, 1> few(p.off, p.e_cnt, lane, 0, p.few_most);
+  // the workgroups that had no tile in the others' last round come first: `idle` of them
+  const int per_xcd = gridDim.x / 8, busy = ((many.total * ((p.N + Place<MODE>::COLS - 1) / Place<MODE>::COLS) + 7) / 8) % per_xcd;
+  const int place = 8 * ((blockIdx.x / 8 + per_xcd - busy) % per_xcd) + blockIdx.x % 8, idle = 8 * (per_xcd - busy);
+  if (few.total > p.cached) few_tiles<MODE, true>(p, few, reinterpret_cast<f32x4*>(gemm_lds), place, idle, many.total);
+  else few_tiles<MODE, false>(p, few, reinterpret_cast<f32x4*>(gemm_lds), place, idle, many.total);
 }
 
 inline size_t align256(size_t v) { return (v + 255) & ~(size_t)255; }
@@ -445,9 +580,8 @@ int launch_mx4_expert_fwd(const void* xp, int cap, int d, int f, int e_cnt, cons
   const Workspace at(cap, d, f, e_cnt);
   uint8_t* const base = (uint8_t*)ws;
   int32_t* const first = (int32_t*)(base + at.first);
-  const long long tiles = tiles_bound(cap, e_cnt, 16), few = tiles_bound(cap, e_cnt, FEW_ROWS);
-  const long long up = 8 * ((few * (f / FEW_COLS) + 7) / 8), down = 8 * ((few * (d / FEW_COLS) + 7) / 8);
-  if (tiles >= (1ll << 31) || up >= (1ll << 31) || down >= (1ll << 31)) return MOE_EUNSUPPORTED;
+  const long long tiles = tiles_bound(cap, e_cnt, 16);
+  if (tiles * (d > f ? d : f) / FEW_COLS >= (1ll << 31)) return MOE_EUNSUPPORTED;       // tiles are counted in 32 bits
   {
     ProfScope prof(MOE_K_MX4_ROWS, s);
     const int waves = ROWS_BLOCK / WAVE;
@@ -455,8 +589,7 @@ int launch_mx4_expert_fwd(const void* xp, int cap, int d, int f, int e_cnt, cons
                        e_cnt, d, f, base + at.xq, base + at.xs, base + at.aq, base + at.as, first);
     HIP_CHECK_LAUNCH();
   }
-  const bool many = cap > FEW_MOST;            // some expert may have many rows
-  if (many) {
+  {
     static bool attr_set[64] = {};
     int dev = 0;
     if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return MOE_EHIP;
@@ -467,29 +600,30 @@ int launch_mx4_expert_fwd(const void* xp, int cap, int d, int f, int e_cnt, cons
       attr_set[dev] = true;
     }
   }
-  const dim3 walkers(8 * ((2 * device_cu_count() + 7) / 8));       // (a walk stays in its XCD's eighth)
+  const dim3 walkers(8 * ((device_cu_count() + 7) / 8));       // (a walk stays in its XCD's eighth)
   XArgs p{};
   p.off = offsets; p.first = first; p.e_cnt = e_cnt;
   p.A = base + at.xq; p.As = base + at.xs;
   p.B0 = w1; p.Bs0 = s1; p.B1 = w3; p.Bs1 = s3;
   p.C = base + at.aq; p.Cs = base + at.as;
   p.N = f; p.K = d;
+  p.few_most = mx_depths(p.K) < LEAST_DEPTHS ? 0x7FFFFFFF : FEW_MOST;
+  p.cached = (int)((256ll << 20) * 32 / (51ll * d * f));
   p.b_es = (size_t)((f + 15) / 16) * mx_depths(d) * MX_TILE; p.bs_es = (size_t)((f + 15) / 16) * mx_groups(d) * MX_SCALES;
   {
     ProfScope prof(MOE_K_MX4_UP, s);
-    if (many) hipLaunchKernelGGL(experts_mx4<UP>, walkers, dim3(GEMM_THREADS), GEMM_LDS, s, p);
-    else hipLaunchKernelGGL(few_rows_mx4<UP>, dim3((unsigned)up), dim3(WAVE * min(FEW_WAVES, mx_groups(d))), 0, s, p);
+    hipLaunchKernelGGL(experts_mx4<UP>, walkers, dim3(GEMM_THREADS), GEMM_LDS, s, p);
     HIP_CHECK_LAUNCH();
   }
   p.A = p.C; p.As = p.Cs;
   p.B0 = w2; p.Bs0 = s2; p.B1 = nullptr; p.Bs1 = nullptr;
   p.O = (bf16_t*)o;
   p.N = d; p.K = f;
+  p.few_most = mx_depths(p.K) < LEAST_DEPTHS ? 0x7FFFFFFF : FEW_MOST;
   p.b_es = (size_t)((d + 15) / 16) * mx_depths(f) * MX_TILE; p.bs_es = (size_t)((d + 15) / 16) * mx_groups(f) * MX_SCALES;
   {
     ProfScope prof(MOE_K_MX4_DOWN, s);
-    if (many) hipLaunchKernelGGL(experts_mx4<DOWN>, walkers, dim3(GEMM_THREADS), GEMM_LDS, s, p);
-    else hipLaunchKernelGGL(few_rows_mx4<DOWN>, dim3((unsigned)down), dim3(WAVE * min(FEW_WAVES, mx_groups(f))), 0, s, p);
+    hipLaunchKernelGGL(experts_mx4<DOWN>, walkers, dim3(GEMM_THREADS), GEMM_LDS, s, p);
     HIP_CHECK_LAUNCH();
   }
   return MOE_OK;
