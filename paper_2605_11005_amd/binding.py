@@ -34,7 +34,8 @@ EXPORTS = ("moe_route", "moe_dispatch", "moe_dispatch_static", "moe_expert_fwd",
            "moe_workspace_bytes", "moe_error_string")
 # what csrc/marshal.cpp calls, in its order
 _MARSHALLED = ("moe_route", "moe_dispatch", "moe_dispatch_static", "moe_expert_fwd", "moe_expert_bwd", "moe_combine", "moe_router_fwd",
-               "moe_combine_bwd", "moe_gate_bwd", "moe_router_bwd")
+               "moe_combine_bwd", "moe_gate_bwd", "moe_router_bwd", "moe_block_norm_fwd", "moe_block_norm_bwd", "moe_mx4_quantize",
+               "moe_mx4_dequantize", "moe_mx4_expert_fwd")
 
 
 class MoeError(RuntimeError):
@@ -333,6 +334,9 @@ def moe_router_bwd(x, wr, dlogits, dwr, dwr_accumulate, dx, dx_accumulate, ws):
 
 def moe_block_norm_fwd(y, gate, w_post, post_norm, h, w_pre, alpha, beta, eps, h_out, n, r_post=None, r_pre=None):
     """y [T,d] or None (the norm in front of a first block), h [T,d]; w_pre and n both or neither."""
+    rc = _marshal().block_norm_fwd(y, gate, w_post, post_norm, h, w_pre, alpha, beta, eps, h_out, n, r_post, r_pre)
+    if rc >= 0:
+        return _check(rc, "moe_block_norm_fwd")
     import torch
     T, d = h.shape
     t = w_pre if y is None else y
@@ -351,6 +355,10 @@ def moe_block_norm_fwd(y, gate, w_post, post_norm, h, w_pre, alpha, beta, eps, h
 def moe_block_norm_bwd(y, gate, w_post, post_norm, h_out, w_pre, r_post, r_pre, dh_out, dn, alpha, beta, dh, dy, dgate, dw_post,
                        dw_pre, accumulate, ws):
     """h_out is the saved sum of the forward (h itself where y is None); it may be None where dn is."""
+    rc = _marshal().block_norm_bwd(y, gate, w_post, post_norm, h_out, w_pre, r_post, r_pre, dh_out, dn, alpha, beta, dh, dy, dgate, dw_post,
+                                   dw_pre, accumulate, ws)
+    if rc >= 0:
+        return _check(rc, "moe_block_norm_bwd")
     import torch
     res, t = (next((v for v in pair if v is not None), None) for pair in ((h_out, dh_out), (dn, y)))
     if res is None or t is None:
@@ -381,6 +389,9 @@ def _need_mx4(data, scales, batch, n, K, name):
 
 def moe_mx4_quantize(x, along_rows, data, scales):
     """x [n,K] or [batch,n,K]; along_rows: [K,n] or [batch,K,n].  data, scales: mx4_shapes(n, K), behind the batch."""
+    rc = _marshal().mx4_quantize(x, along_rows, data, scales)
+    if rc >= 0:
+        return _check(rc, "moe_mx4_quantize")
     if x.dim() not in (2, 3):
         raise MoeError("x must be a matrix or a batch of matrices")
     (rows, cols), batch = x.shape[-2:], x.shape[:-2]
@@ -392,6 +403,9 @@ def moe_mx4_quantize(x, along_rows, data, scales):
 
 def moe_mx4_dequantize(data, scales, out):
     """out [n,K] or [batch,n,K], the values of data and scales."""
+    rc = _marshal().mx4_dequantize(data, scales, out)
+    if rc >= 0:
+        return _check(rc, "moe_mx4_dequantize")
     if out.dim() not in (2, 3):
         raise MoeError("out must be a matrix or a batch of matrices")
     (n, K), batch = out.shape[-2:], out.shape[:-2]
@@ -403,6 +417,9 @@ def moe_mx4_dequantize(data, scales, out):
 
 def moe_mx4_expert_fwd(xp, offsets, w1, s1, w3, s3, w2, s2, o, ws):
     """w1, s1, w3, s3: data and scales of e_cnt matrices with n = f, K = d; w2, s2: n = d, K = f (f is a multiple of 32: w1's tiles say it)."""
+    rc = _marshal().mx4_expert_fwd(xp, offsets, w1, s1, w3, s3, w2, s2, o, ws)
+    if rc >= 0:
+        return _check(rc, "moe_mx4_expert_fwd")
     import torch
     cap, d = xp.shape
     if w1.dim() != 6:

@@ -33,6 +33,11 @@ struct Entry {
   decltype(&moe_combine_bwd) combine_bwd;
   decltype(&moe_gate_bwd) gate_bwd;
   decltype(&moe_router_bwd) router_bwd;
+  decltype(&moe_block_norm_fwd) block_norm_fwd;
+  decltype(&moe_block_norm_bwd) block_norm_bwd;
+  decltype(&moe_mx4_quantize) mx4_quantize;
+  decltype(&moe_mx4_dequantize) mx4_dequantize;
+  decltype(&moe_mx4_expert_fwd) mx4_expert_fwd;
 } entry;
 constexpr int N_ENTRIES = sizeof(Entry) / sizeof(void*);
 
@@ -54,6 +59,11 @@ struct Args {
     const long x = PyLong_AsLongAndOverflow(o, &over);
     if (over || x < INT32_MIN || x > INT32_MAX) refuse();
     return (int)x;
+  }
+  float real() {
+    PyObject* o = next();
+    if (!PyFloat_CheckExact(o)) refuse();
+    return (float)PyFloat_AS_DOUBLE(o);
   }
   int flag() {
     PyObject* o = next();
@@ -106,6 +116,7 @@ moe_stream_t stream() { return (moe_stream_t)c10::hip::getCurrentHIPStream().str
 
 constexpr auto F32 = at::kFloat;
 constexpr auto I32 = at::kInt;
+constexpr auto U8 = at::kByte;
 
 // f(args) marshals and returns the call to make; the interpreter's lock is not held while it enqueues.  Only marshalling may end in "not
 // taken": the call itself is made once, and what it might throw leaves as it would leave ctypes.
@@ -335,6 +346,134 @@ PyObject* router_bwd(PyObject*, PyObject* const* v, Py_ssize_t n) {
   });
 }
 
+// the norms' tensors that have T rows of d elements or are absent
+struct Rows {
+  int64_t T, d;
+  void matrix(const Buf& b, at::ScalarType type) const {
+    if (b.t && b.t->scalar_type() != type) refuse();
+    shaped(b, {T, d});
+  }
+  void vector(const Buf& b, at::ScalarType type) const {
+    if (b.t && b.t->scalar_type() != type) refuse();
+    shaped(b, {d});
+  }
+  void per_row(const Buf& b) const {
+    if (b.t && b.t->scalar_type() != F32) refuse();
+    shaped(b, {T});
+  }
+};
+
+PyObject* block_norm_fwd(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  return take(v, n, [](Args& a) {
+    const Buf y = any(a, true), gate = any(a, true), w_post = any(a, true);
+    const int post_norm = a.flag();
+    const Buf h = any(a), w_pre = any(a, true);
+    const float alpha = a.real(), beta = a.real(), eps = a.real();
+    const Buf h_out = any(a, true), out = any(a, true), r_post = any(a, true), r_pre = any(a, true);
+    dims(h, 2);
+    if (!y.t && !w_pre.t) refuse();
+    const Buf& typed_by = y.t ? y : w_pre;
+    const auto t = typed_by.t->scalar_type(), rt = h.t->scalar_type();
+    const Rows r{h.size(0), h.size(1)};
+    const int T = small(r.T), d = small(r.d), dt = dtype_code(typed_by), res = dtype_code(h);
+    r.matrix(y, t);
+    r.matrix(out, t);
+    r.matrix(h_out, rt);
+    r.vector(w_post, t);
+    r.vector(w_pre, t);
+    for (const Buf* b : {&gate, &r_post, &r_pre}) r.per_row(*b);
+    return [=, s = stream()] {
+      return entry.block_norm_fwd(y.ptr, (const float*)gate.ptr, w_post.ptr, post_norm, h.ptr, w_pre.ptr, dt, res, T, d, alpha, beta, eps, h_out.ptr,
+                                  out.ptr, (float*)r_post.ptr, (float*)r_pre.ptr, s);
+    };
+  });
+}
+
+PyObject* block_norm_bwd(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  return take(v, n, [](Args& a) {
+    const Buf y = any(a, true), gate = any(a, true), w_post = any(a, true);
+    const int post_norm = a.flag();
+    const Buf h = any(a, true), w_pre = any(a, true), r_post = any(a, true), r_pre = any(a, true), dh_out = any(a, true), dn = any(a, true);
+    const float alpha = a.real(), beta = a.real();
+    const Buf dh = any(a, true), dy = any(a, true), dgate = any(a, true), dw_post = any(a, true), dw_pre = any(a, true);
+    const int accumulate = a.flag();
+    const Buf ws = any(a);
+    const Buf &res_by = h.t ? h : dh_out, &typed_by = dn.t ? dn : y;
+    if (!res_by.t || !typed_by.t) refuse();
+    dims(typed_by, 2);
+    const auto t = typed_by.t->scalar_type(), rt = res_by.t->scalar_type();
+    const Rows r{typed_by.size(0), typed_by.size(1)};
+    const int T = small(r.T), d = small(r.d), dt = dtype_code(typed_by), res = dtype_code(res_by);
+    for (const Buf* b : {&y, &dn, &dy}) r.matrix(*b, t);
+    for (const Buf* b : {&h, &dh_out, &dh}) r.matrix(*b, rt);
+    for (const Buf* b : {&w_post, &w_pre, &dw_post, &dw_pre}) r.vector(*b, t);
+    for (const Buf* b : {&gate, &r_post, &r_pre, &dgate}) r.per_row(*b);
+    const size_t ws_bytes = (size_t)ws.bytes();
+    return [=, s = stream()] {
+      return entry.block_norm_bwd(y.ptr, (const float*)gate.ptr, w_post.ptr, post_norm, h.ptr, w_pre.ptr, (const float*)r_post.ptr,
+                                  (const float*)r_pre.ptr, dh_out.ptr, dn.ptr, dt, res, T, d, alpha, beta, dh.ptr, dy.ptr, (float*)dgate.ptr,
+                                  dw_post.ptr, dw_pre.ptr, accumulate, ws.ptr, ws_bytes, s);
+    };
+  });
+}
+
+// data and scales of `n` rows of `K` elements in 4 bits, behind a batch (-1: none)
+struct Mx4 {
+  uint8_t *data, *scales;
+  Mx4(const Buf& q, const Buf& sc, int64_t batch, int64_t n, int64_t K) : data((uint8_t*)q.ptr), scales((uint8_t*)sc.ptr) {
+    const int64_t tiles = (n + 15) / 16, depths = (K + 127) / 128, groups = (K + 511) / 512;
+    if (batch < 0) {
+      shaped(q, {tiles, depths, 4, 16, 16});
+      shaped(sc, {tiles, groups, 4, 16, 4});
+    } else {
+      shaped(q, {batch, tiles, depths, 4, 16, 16});
+      shaped(sc, {batch, tiles, groups, 4, 16, 4});
+    }
+  }
+};
+
+PyObject* mx4_quantize(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  return take(v, n, [](Args& a) {
+    const Buf x = any(a);
+    const int along_rows = a.flag();
+    const Buf q = typed(a, U8), sc = typed(a, U8);
+    const int64_t nd = x.t->dim();
+    if (nd != 2 && nd != 3) refuse();
+    const int rows = small(x.size(nd - 2)), cols = small(x.size(nd - 1)), batch = nd == 3 ? small(x.size(0)) : 1, dt = dtype_code(x);
+    const Mx4 to(q, sc, nd == 3 ? batch : -1, along_rows ? cols : rows, along_rows ? rows : cols);
+    return [=, s = stream()] { return entry.mx4_quantize(x.ptr, dt, batch, rows, cols, along_rows, to.data, to.scales, s); };
+  });
+}
+
+PyObject* mx4_dequantize(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  return take(v, n, [](Args& a) {
+    const Buf q = typed(a, U8), sc = typed(a, U8), out = any(a);
+    const int64_t nd = out.t->dim();
+    if (nd != 2 && nd != 3) refuse();
+    const int rows = small(out.size(nd - 2)), K = small(out.size(nd - 1)), batch = nd == 3 ? small(out.size(0)) : 1, dt = dtype_code(out);
+    const Mx4 from(q, sc, nd == 3 ? batch : -1, rows, K);
+    return [=, s = stream()] { return entry.mx4_dequantize(from.data, from.scales, batch, rows, K, out.ptr, dt, s); };
+  });
+}
+
+PyObject* mx4_expert_fwd(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  return take(v, n, [](Args& a) {
+    const Buf xp = any(a), off = typed(a, I32), q1 = typed(a, U8), s1 = typed(a, U8), q3 = typed(a, U8), s3 = typed(a, U8), q2 = typed(a, U8),
+              s2 = typed(a, U8), o = typed(a, xp.t->scalar_type()), ws = any(a);
+    dims(xp, 2);
+    dims(q1, 6);
+    const int cap = small(xp.size(0)), d = small(xp.size(1)), e = small(q1.size(0)), f = small(16 * q1.size(1)), dt = dtype_code(xp);
+    const Mx4 w1(q1, s1, e, f, d), w3(q3, s3, e, f, d), w2(q2, s2, e, d, f);
+    shaped(o, {cap, d});
+    shaped(off, {(int64_t)e + 1});
+    const size_t ws_bytes = (size_t)ws.bytes();
+    return [=, s = stream()] {
+      return entry.mx4_expert_fwd(xp.ptr, dt, cap, d, f, e, (const int32_t*)off.ptr, w1.data, w1.scales, w3.data, w3.scales, w2.data, w2.scales, o.ptr,
+                                  ws.ptr, ws_bytes, s);
+    };
+  });
+}
+
 // bind(addresses): the entry points in the order of Entry
 PyObject* bind(PyObject*, PyObject* const* v, Py_ssize_t n) {
   if (n != N_ENTRIES) {
@@ -353,7 +492,8 @@ PyObject* bind(PyObject*, PyObject* const* v, Py_ssize_t n) {
 
 #define METHOD(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {METHOD(route),    METHOD(dispatch),   METHOD(dispatch_static), METHOD(expert_fwd), METHOD(expert_bwd), METHOD(combine),
-                         METHOD(router_fwd), METHOD(combine_bwd), METHOD(gate_bwd),      METHOD(router_bwd), METHOD(bind),       {nullptr, nullptr, 0, nullptr}};
+                         METHOD(router_fwd), METHOD(combine_bwd), METHOD(gate_bwd),      METHOD(router_bwd), METHOD(block_norm_fwd), METHOD(block_norm_bwd),
+                         METHOD(mx4_quantize), METHOD(mx4_dequantize), METHOD(mx4_expert_fwd), METHOD(bind), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods};
 
 }  // namespace
