@@ -355,7 +355,7 @@ int moe_combine(const void* o, int dtype, int T, int d, int k, const int32_t* in
 namespace {
 int shape_check_norm(int dtype, int res_dtype, int T, int d) {
   if (bad_dtype(dtype) || (res_dtype != dtype && res_dtype != MOE_F32) || T < 0 || d <= 0) return MOE_EINVAL;
-  if (d > MOE_MAX_NORM_D || (dtype == MOE_BF16 ? d % 8 : d % 4)) return MOE_EUNSUPPORTED;
+  if (d > MOE_MAX_NORM_D || (dtype == MOE_BF16 ? d % 8 : d % 4) || T > 0x7FFF0000) return MOE_EUNSUPPORTED;   // (rows are walked in steps)
   return MOE_OK;
 }
 }  // namespace

@@ -16,24 +16,31 @@ typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 
 template <typename T> constexpr int VEC = 16 / sizeof(T);
 
-// N elements as floats
-template <int N>
-__device__ __forceinline__ void unpack(const bf16_t* p, size_t i, float (&v)[N]) {
+// N elements as they lie in memory, and as floats
+template <typename T, int N>
+struct Raw {
+  u32x4 w[N * sizeof(T) / 16];
+  __device__ __forceinline__ void load(const T* p, size_t i) {
 #pragma unroll
-  for (int j = 0; j < N / 8; ++j) {
-    const u32x4 w = *reinterpret_cast<const u32x4*>(p + i + 8 * j);
-#pragma unroll
-    for (int k = 0; k < 4; ++k) { v[8 * j + 2 * k] = bf16lo(w[k]); v[8 * j + 2 * k + 1] = bf16hi(w[k]); }
+    for (int j = 0; j < (int)(N * sizeof(T) / 16); ++j) w[j] = *reinterpret_cast<const u32x4*>(p + i + j * VEC<T>);
   }
-}
-template <int N>
-__device__ __forceinline__ void unpack(const float* p, size_t i, float (&v)[N]) {
+  __device__ __forceinline__ void clear() {
 #pragma unroll
-  for (int j = 0; j < N / 4; ++j) {
-    const u32x4 w = *reinterpret_cast<const u32x4*>(p + i + 4 * j);
-#pragma unroll
-    for (int k = 0; k < 4; ++k) v[4 * j + k] = __uint_as_float(w[k]);
+    for (int j = 0; j < (int)(N * sizeof(T) / 16); ++j) w[j] = 0;
   }
+  __device__ __forceinline__ void values(float (&v)[N]) const {
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      if constexpr (sizeof(T) == 4) v[j] = __uint_as_float(w[j / 4][j % 4]);
+      else v[j] = j % 2 ? bf16hi(w[j / 8][j % 8 / 2]) : bf16lo(w[j / 8][j % 8 / 2]);
+    }
+  }
+};
+template <int N, typename T>
+__device__ __forceinline__ void unpack(const T* p, size_t i, float (&v)[N]) {
+  Raw<T, N> raw;
+  raw.load(p, i);
+  raw.values(v);
 }
 template <int N>
 __device__ __forceinline__ void pack(bf16_t* p, size_t i, const float (&v)[N]) {
@@ -166,49 +173,84 @@ struct BwdArgs {
   float alpha, beta;
 };
 
-// Blocks walk the rows b, b + grid, .. and keep the column sums of theirs in registers.
+// What the backward reads of a row
 template <typename T, typename R, int STEPS>
-__global__ __launch_bounds__((MOST_THREADS<T, STEPS>)) void block_norm_bwd(BwdArgs<T, R> p) {
+struct BwdRow {
+  static constexpr int N = VEC<T>;
+  Raw<T, N> y[STEPS], dn[STEPS];
+  Raw<R, N> h[STEPS], dh[STEPS];
+  __device__ __forceinline__ void load(const BwdArgs<T, R>& p, int row) {
+    const size_t at = (size_t)row * p.d;
+#pragma unroll
+    for (int i = 0; i < STEPS; ++i) {
+      const int c = (i * blockDim.x + threadIdx.x) * N;
+      dn[i].clear(); h[i].clear(); dh[i].clear();
+      if (row < p.T_ && c < p.d) {
+        if (p.w_pre) { h[i].load(p.h, at + c); dn[i].load(p.dn, at + c); }
+        if (p.dh_out) dh[i].load(p.dh_out, at + c);
+      }
+    }
+  }
+  __device__ __forceinline__ void load_y(const BwdArgs<T, R>& p, int row) {
+    const size_t at = (size_t)row * p.d;
+#pragma unroll
+    for (int i = 0; i < STEPS; ++i) {
+      const int c = (i * blockDim.x + threadIdx.x) * N;
+      y[i].clear();
+      if (row < p.T_ && c < p.d && p.y) y[i].load(p.y, at + c);
+    }
+  }
+};
+
+// Blocks (or, for rows of one wavefront, wavefronts) walk the rows and keep the column sums of theirs in registers.  The next row's loads
+// are on their way while a row's sums meet; for WIDE rows the registers hold neither these nor the weights.
+constexpr int BWD_ROWS = 8, BWD_THREADS = 512, WIDE_THREADS = 1024;
+template <typename T, typename R, int STEPS, bool WIDE>
+__global__ __launch_bounds__(WIDE ? WIDE_THREADS : BWD_THREADS) void block_norm_bwd(BwdArgs<T, R> p) {
   constexpr int N = VEC<T>;
   __shared__ float red[2][MOST_WAVES];
   RowSum row_total{red, (int)blockDim.x >> 6};
   const float inv_d = 1.f / (float)p.d;
-  float w_pre[STEPS][N], w_post[STEPS][N], d_pre[STEPS][N], d_post[STEPS][N];
+  Raw<T, N> w_pre[STEPS], w_post[STEPS];
+  float d_pre[STEPS][N], d_post[STEPS][N];
 #pragma unroll
   for (int i = 0; i < STEPS; ++i) {
     const int c = (i * blockDim.x + threadIdx.x) * N;
+    w_pre[i].clear(); w_post[i].clear();
 #pragma unroll
-    for (int j = 0; j < N; ++j) { w_pre[i][j] = d_pre[i][j] = d_post[i][j] = 0.f; w_post[i][j] = 1.f; }
-    if (p.w_pre && c < p.d) unpack(p.w_pre, c, w_pre[i]);
-    if (p.w_post && c < p.d) unpack(p.w_post, c, w_post[i]);
+    for (int j = 0; j < N; ++j) d_pre[i][j] = d_post[i][j] = 0.f;
+    if (!WIDE && p.w_pre && c < p.d) w_pre[i].load(p.w_pre, c);
+    if (!WIDE && p.w_post && c < p.d) w_post[i].load(p.w_post, c);
   }
-  for (int row = blockIdx.x; row < p.T_; row += gridDim.x) {
+  BwdRow<T, R, STEPS> next;
+  int row = blockIdx.x * blockDim.y + threadIdx.y;
+  if (!WIDE) { next.load(p, row); next.load_y(p, row); }
+  for (; row < p.T_; row += gridDim.x * blockDim.y) {
     const size_t at = (size_t)row * p.d;
     float y[STEPS][N], g[STEPS][N];
     {
       float h[STEPS][N], dn[STEPS][N];
-      float sum = 0.f;
-      const float r = p.w_pre ? p.r_pre[row] : 0.f;
+      if (WIDE) next.load(p, row);
 #pragma unroll
-      for (int i = 0; i < STEPS; ++i) {
-        const int c = (i * blockDim.x + threadIdx.x) * N;
-#pragma unroll
-        for (int j = 0; j < N; ++j) y[i][j] = g[i][j] = h[i][j] = dn[i][j] = 0.f;
-        if (c < p.d) {
-          if (p.w_pre) { unpack(p.h, at + c, h[i]); unpack(p.dn, at + c, dn[i]); }
-          if (p.dh_out) unpack(p.dh_out, at + c, g[i]);
-          if (p.y) unpack(p.y, at + c, y[i]);
-        }
-      }
+      for (int i = 0; i < STEPS; ++i) { if (!WIDE) next.y[i].values(y[i]); next.dn[i].values(dn[i]); next.h[i].values(h[i]); next.dh[i].values(g[i]); }
+      const int after = row + gridDim.x * blockDim.y;
+      if (!WIDE) { next.load(p, after); next.load_y(p, after); }
       if (p.w_pre) {
+        const float r = p.r_pre[row];
+        float sum = 0.f;
 #pragma unroll
-        for (int i = 0; i < STEPS; ++i)
+        for (int i = 0; i < STEPS; ++i) {
+          const int c = (i * blockDim.x + threadIdx.x) * N;
+          float w[N];
+          if (WIDE && c < p.d) w_pre[i].load(p.w_pre, c);
+          w_pre[i].values(w);
 #pragma unroll
           for (int j = 0; j < N; ++j) {
             d_pre[i][j] += dn[i][j] * h[i][j] * r;
-            dn[i][j] *= w_pre[i][j];
+            dn[i][j] *= w[j];
             sum += dn[i][j] * h[i][j];
           }
+        }
         const float m = row_total(sum) * inv_d * r * r * r;
 #pragma unroll
         for (int i = 0; i < STEPS; ++i)
@@ -228,16 +270,26 @@ __global__ __launch_bounds__((MOST_THREADS<T, STEPS>)) void block_norm_bwd(BwdAr
       }
     }
     if (!p.y) continue;
+    if (WIDE) {
+      next.load_y(p, row);
+#pragma unroll
+      for (int i = 0; i < STEPS; ++i) next.y[i].values(y[i]);
+    }
     const float gate = p.gate ? p.gate[row] : 1.f, r = p.post_norm ? p.r_post[row] : 1.f, scale = p.beta * gate * r;
     float sum = 0.f;
 #pragma unroll
-    for (int i = 0; i < STEPS; ++i)
+    for (int i = 0; i < STEPS; ++i) {
+      const int c = (i * blockDim.x + threadIdx.x) * N;
+      float w[N];
+      if (WIDE && p.w_post && c < p.d) w_post[i].load(p.w_post, c);
+      w_post[i].values(w);
 #pragma unroll
       for (int j = 0; j < N; ++j) {
         d_post[i][j] += scale * g[i][j] * y[i][j];
-        g[i][j] *= w_post[i][j];
+        if (p.w_post) g[i][j] *= w[j];
         sum += g[i][j] * y[i][j];
       }
+    }
     float m = 0.f;
     if (p.post_norm || p.dgate) {
       const float total = row_total(sum);
@@ -252,6 +304,24 @@ __global__ __launch_bounds__((MOST_THREADS<T, STEPS>)) void block_norm_bwd(BwdAr
       if (c < p.d) pack(p.dy, at + c, g[i]);
     }
   }
+  if constexpr (!WIDE && STEPS * N <= 16)
+    if (blockDim.y > 1) {                  // a block's wavefronts' sums, in their order
+      __shared__ float part[BWD_ROWS][N][WAVE];
+#pragma unroll
+      for (int k = 0; k < 2 * STEPS; ++k) {
+        float(&v)[N] = k % 2 ? d_pre[k / 2] : d_post[k / 2];
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < N; ++j) part[threadIdx.y][j][threadIdx.x] = v[j];
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+          v[j] = 0.f;
+          for (int w = 0; w < (int)blockDim.y; ++w) v[j] += part[w][j][threadIdx.x];
+        }
+      }
+      if (threadIdx.y) return;
+    }
   float* const out = p.sums + (size_t)blockIdx.x * 2 * p.d;
 #pragma unroll
   for (int i = 0; i < STEPS; ++i) {
@@ -303,20 +373,39 @@ int forward(FwdArgs<T, R> p, hipStream_t s) {
   return MOE_OK;
 }
 
-constexpr int BWD_BLOCKS = 512;
-inline int bwd_blocks(int T) { return T < BWD_BLOCKS ? T : BWD_BLOCKS; }
+// The backward's launch.  A thread with one step of bf16 takes 124 registers, with 16 elements up to 252: one block of the latter fits on a
+// CU, of the former two.  A row of 1024 elements in one wavefront has no barrier (16384 rows of bf16: 48 us
+// against 80 us as blocks of two wavefronts); few rows go to more blocks, not to more wavefronts of a block.
+struct BwdPlan { int steps, threads, rows, most, blocks; bool wide; };
+inline BwdPlan bwd_plan(int T, int d, int vec) {
+  constexpr int CUS = 256;
+  const int vecs = d / vec, per = 16 / vec;          // steps of 16 elements
+  BwdPlan b;
+  b.wide = row_threads(vecs, per) > BWD_THREADS;
+  if (row_threads(vecs, 1) == WAVE) b.steps = 1;
+  else if (b.wide || row_threads(vecs, per) == WAVE) b.steps = per;
+  else b.steps = row_threads(vecs, 1) <= BWD_THREADS ? 1 : row_threads(vecs, 2) <= BWD_THREADS ? 2 : per;
+  b.threads = row_threads(vecs, b.steps);
+  const int per_cu = b.steps * vec == 16 ? 1 : b.threads > WAVE && b.threads <= 256 && T >= 8192 ? 4 : 2;
+  b.most = T < per_cu * CUS ? T : per_cu * CUS;
+  b.rows = b.threads > WAVE ? 1 : T >= per_cu * CUS * BWD_ROWS ? BWD_ROWS : T == 0 ? 1 : (T - 1) / (per_cu * CUS) + 1;
+  const int units = T == 0 ? 0 : (T - 1) / b.rows + 1;
+  b.blocks = units < b.most ? units : b.most;
+  return b;
+}
 
 template <typename T, typename R>
 int backward(BwdArgs<T, R> p, T* dw_post, T* dw_pre, int accumulate, hipStream_t s) {
-  const int vecs = p.d / VEC<T>, blocks = bwd_blocks(p.T_);
-  int steps = 1;
-  while (row_threads(vecs, steps) > 512 && steps < 4) steps *= 2;
-  const dim3 grid(blocks), block(row_threads(vecs, steps));
+  const BwdPlan plan = bwd_plan(p.T_, p.d, VEC<T>);
+  const int steps = plan.steps, blocks = plan.blocks;
+  const dim3 grid(blocks), block(plan.threads, plan.rows);
+  constexpr int PER = 16 / VEC<T>;
   if (p.T_ > 0) {
     ProfScope prof(MOE_K_NORM_BWD, s);
-    if (steps == 1) hipLaunchKernelGGL((block_norm_bwd<T, R, 1>), grid, block, 0, s, p);
-    else if (steps == 2) hipLaunchKernelGGL((block_norm_bwd<T, R, 2>), grid, block, 0, s, p);
-    else hipLaunchKernelGGL((block_norm_bwd<T, R, 4>), grid, block, 0, s, p);
+    if (plan.wide) hipLaunchKernelGGL((block_norm_bwd<T, R, PER, true>), grid, block, 0, s, p);
+    else if (steps == 1) hipLaunchKernelGGL((block_norm_bwd<T, R, 1, false>), grid, block, 0, s, p);
+    else if (steps == 2) hipLaunchKernelGGL((block_norm_bwd<T, R, 2, false>), grid, block, 0, s, p);
+    else hipLaunchKernelGGL((block_norm_bwd<T, R, PER, false>), grid, block, 0, s, p);
     HIP_CHECK_LAUNCH();
   }
   if (dw_post || dw_pre) {
@@ -336,7 +425,11 @@ int by_types(int dtype, int res_dtype, F f) {
 
 }  // namespace
 
-size_t block_norm_ws_bytes(int T, int d) { return (size_t)bwd_blocks(T) * 2 * d * sizeof(float); }
+// For T rows and fewer, of bf16 or fp32
+size_t block_norm_ws_bytes(int T, int d) {
+  const int a = bwd_plan(T, d, 8).most, b = bwd_plan(T, d, 4).most;
+  return (size_t)(a > b ? a : b) * 2 * d * sizeof(float);
+}
 
 int launch_block_norm_fwd(const void* y, const float* gate, const void* w_post, int post_norm, const void* h, const void* w_pre, int dtype, int res_dtype,
                           int T, int d, float alpha, float beta, float eps, void* h_out, void* n, float* r_post, float* r_pre, hipStream_t s) {
