@@ -5,9 +5,8 @@
 
 namespace {
 
-#ifndef QC
-#define QC 4
-#endif
+typedef unsigned int mx_u32x2 __attribute__((ext_vector_type(2)));
+typedef float mx_f32x4 __attribute__((ext_vector_type(4)));
 constexpr int QUANT_BLOCK = 256;
 
 // Rows whose elements are contiguous (tokens): a wavefront per 16 rows by 512 elements.
@@ -23,7 +22,8 @@ __global__ __launch_bounds__(QUANT_BLOCK) void mx4_rows(const T* __restrict__ x,
 }
 
 // Matrices [K][n] whose contraction index is not the contiguous one (weights).  A lane takes four columns of 32 rows; the four
-// wavefronts of a block take the same chunk of four consecutive operands, whose scales meet in LDS as the bytes of a word.
+// wavefronts of a block take the same chunk of four consecutive operands, whose scales meet in LDS as the bytes of a word.  16 matrices of
+// 4096 by 1536, bf16: 45 us, 5.6 TB/s (62 us without the hint that no element is read again).
 template <typename T>
 __global__ __launch_bounds__(QUANT_BLOCK) void mx4_columns(const T* __restrict__ x, int n, int K, int col_blocks, uint8_t* __restrict__ q,
                                                             uint8_t* __restrict__ scales) {
@@ -40,9 +40,9 @@ __global__ __launch_bounds__(QUANT_BLOCK) void mx4_columns(const T* __restrict__
   if (col < n && k < K) {
     const T* src = x + ((size_t)batch * K + k) * n + col;
     if constexpr (sizeof(T) == 2) {
-      uint2 v[MX_CHUNK];
+      mx_u32x2 v[MX_CHUNK];
 #pragma unroll
-      for (int i = 0; i < MX_CHUNK; ++i) v[i] = *reinterpret_cast<const uint2*>(src + (size_t)i * n);
+      for (int i = 0; i < MX_CHUNK; ++i) v[i] = __builtin_nontemporal_load(reinterpret_cast<const mx_u32x2*>(src + (size_t)i * n));
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
         uint32_t w[16];
@@ -52,9 +52,9 @@ __global__ __launch_bounds__(QUANT_BLOCK) void mx4_columns(const T* __restrict__
         codes[c] = mx_chunk(w, byte[c]);
       }
     } else {
-      float4 v[MX_CHUNK];
+      mx_f32x4 v[MX_CHUNK];
 #pragma unroll
-      for (int i = 0; i < MX_CHUNK; ++i) v[i] = *reinterpret_cast<const float4*>(src + (size_t)i * n);
+      for (int i = 0; i < MX_CHUNK; ++i) v[i] = __builtin_nontemporal_load(reinterpret_cast<const mx_f32x4*>(src + (size_t)i * n));
 #pragma unroll
       for (int c = 0; c < 4; ++c) {
         float w[32];

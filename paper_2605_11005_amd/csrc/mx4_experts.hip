@@ -507,9 +507,12 @@ __device__ __forceinline__ void few_tiles(const XArgs& p, const SomeTiles<FEW_RO
       const float level = fmaxf(0.f, floorf((n * cost - idle * stages) / (all * cost)));          // of the others, in blocks of tiles
       for (float q = level; q < level + 2.f; q += 1.f) {
         const float qi = fmaxf(0.f, ceilf((n - others * q) / idle)), time = fmaxf(qi * cost, stages + q * cost);
-        if (time < best) { best = time; split = s; quota = (int)qi; quota_others = (int)q; }
+        if (time < best) { best = time; split = s; quota_others = (int)q; }
       }
     }
+    // (in integers: no tile may be left)
+    const int rest = list.total * ((cols * split + FEW_WAVES - 1) / FEW_WAVES) - ((int)gridDim.x - idle) * quota_others;
+    quota = rest > 0 ? (rest + idle - 1) / idle : 0;
   }
   split = uniform(split); quota = uniform(quota); quota_others = uniform(quota_others);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), per_block = FEW_WAVES / split, n_cols = (cols + per_block - 1) / per_block;
@@ -581,7 +584,7 @@ int launch_mx4_expert_fwd(const void* xp, int cap, int d, int f, int e_cnt, cons
   uint8_t* const base = (uint8_t*)ws;
   int32_t* const first = (int32_t*)(base + at.first);
   const long long tiles = tiles_bound(cap, e_cnt, 16);
-  if (tiles * (d > f ? d : f) / FEW_COLS >= (1ll << 31)) return MOE_EUNSUPPORTED;       // tiles are counted in 32 bits
+  if (tiles * (d > f ? d : f) / FEW_COLS >= (1ll << 30)) return MOE_EUNSUPPORTED;       // tiles are counted in 32 bits
   {
     ProfScope prof(MOE_K_MX4_ROWS, s);
     const int waves = ROWS_BLOCK / WAVE;
