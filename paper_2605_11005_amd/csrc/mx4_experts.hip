@@ -263,8 +263,10 @@ struct SomeTiles {
 // persistent, and the loads run ahead into the next tile while a finished one is written.
 constexpr int GEMM_GROUP = 4, GEMM_ROWS = 256, GEMM_COLS = 256, GEMM_THREADS = 512;
 constexpr int STAGE = 32 * MX_TILE, STAGES = 4, SCALES = 32 * MX_SCALES;       // operand tiles of a stage: 16 of the rows, 16 of the weights
-constexpr int GEMM_LDS = STAGES * STAGE + 2 * SCALES;
-constexpr int LEAST_DEPTHS = 4;            // the two places for scales need a contraction of more than 384 (see Loads)
+constexpr int PLACES = 3;                  // for scales (see Loads)
+constexpr int GEMM_LDS = STAGES * STAGE + PLACES * SCALES;
+constexpr int LEAST_DEPTHS = 4;            // (see Loads)
+__device__ __forceinline__ uint32_t next_place(uint32_t scales) { return scales == (PLACES - 1) * SCALES ? 0 : scales + SCALES; }
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 // (scales: the words' lowest bytes)
@@ -297,8 +299,9 @@ struct Place {                             // of a tile
 // The loads of a workgroup's tiles, stage after stage.  Of a stage wavefront w loads tiles 2 w and 2 w + 1 of the rows and of the weights (UP: 8 of
 // W1, 8 of W3), four loads whatever the tile; those past the rows or columns repeat the last one (their results are not stored), and
 // behind the last tile the same bytes are loaded again and again, so that the number of loads on their way is the same everywhere and the
-// products' loop has no branch.  The scales of 512 come with the first stage of the four.  Of those two are kept: with four stages to a
-// contraction at least, two in succession belong to four stages or more, so that what is overwritten has been read.
+// products' loop has no branch.  The scales of 512 come with the first stage of the four.  Three of those have a place: the stages of a
+// contraction's last scales may be fewer than the three that the loads are ahead, and with four stages to a contraction at least (LEAST_DEPTHS),
+// two in succession belong to four stages or more, so that what is overwritten has been read.
 template <int MODE>
 struct Loads {
   const XArgs& p;
@@ -346,7 +349,7 @@ struct Loads {
     }
     if (more && t % 4 == 0) {
       lds_load16((const bf16_t*)(sc + (size_t)(t / 4) * MX_SCALES), vsc, lds0 + STAGES * STAGE + scales + wave * 1024);
-      scales ^= SCALES;
+      scales = next_place(scales);
     }
   }
   // A stage's loads, one after the other: the caller spreads them over its products (issued in a row, a load keeps a wavefront for 80 cycles
@@ -425,7 +428,7 @@ __device__ __forceinline__ void gemm_tile(const XArgs& p, Loads<MODE>& loads, co
     from = lds + stage + in_tile;
     scales_from = lds + STAGES * STAGE + scales + in_scales + t % 4;
     stage = (stage + STAGE) % (STAGES * STAGE);
-    if (t % 4 == 3 || t == depths - 1) scales ^= SCALES;
+    if (t % 4 == 3 || t == depths - 1) scales = next_place(scales);
   };
   begin(0);
   static_for<READS>([&](auto r) { read(Int<0>{}, r); });

@@ -187,3 +187,28 @@ def test_refusals():
                  (x, offsets, *a, *b, *c, o, ws[:256]), (x, offsets, *a, *b, *c, o[:3], ws), (x, offsets, a[1], a[0], *b, *c, o, ws)):
         with pytest.raises(B.MoeError):
             B.moe_mx4_expert_fwd(*args)
+
+
+@pytest.mark.parametrize("d,f", [(640, 1152), (736, 1216), (832, 1408), (512, 1536)])
+def test_workgroups_with_several_tiles(d, f):
+    """The same experts a few at a time, as many as every workgroup has one tile of: the last stages of a contraction (of 128: 5, 6, 7, 4; 9, 10,
+    11, 12) and the first of the next tile's in one ring of loads."""
+    print(f"case mx4 several tiles {d} {f}", flush=True)
+    g = torch.Generator(device="cuda").manual_seed(d)
+    E, rows, part = 32, 768, 8
+    xp = torch.randn(E * rows, d, generator=g, device="cuda").mul(torch.exp(torch.randn(E * rows, 1, generator=g, device="cuda"))).to(BF16)
+    off = rows * torch.arange(E + 1, dtype=torch.int32, device="cuda")
+    q = []
+    for shape in ((d, f), (d, f), (f, d)):
+        w = torch.randn(E, *shape, generator=g, device="cuda") * torch.exp2(torch.randint(-4, 5, (E, shape[0] // 32, shape[1]), generator=g, device="cuda")
+                                                                            ).repeat_interleave(32, 1) * shape[0] ** -0.5
+        q.append(L.mx4_weights(w.to(BF16)))
+    ws = torch.empty(B.moe_workspace_bytes(B.WS_MX4_EXPERT_FWD, B.MOE_BF16, 0, 0, d, f, E, E * rows), dtype=torch.uint8, device="cuda")
+    o, ref = torch.empty_like(xp), torch.empty_like(xp)
+    B.moe_mx4_expert_fwd(xp, off, *q[0], *q[1], *q[2], o, ws)
+    for e in range(0, E, part):
+        r = slice(e * rows, (e + part) * rows)
+        args = [t[e:e + part] for w in q for t in w]
+        B.moe_mx4_expert_fwd(xp[r], off[:part + 1], *args, ref[r], ws)
+    differ = (o != ref).any(1).sum().item()
+    assert differ == 0, f"{differ} of {E * rows} rows"
