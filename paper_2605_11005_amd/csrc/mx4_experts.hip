@@ -290,10 +290,10 @@ template <int N>
 __device__ __forceinline__ void wait_and_meet() { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" : : "n"(N) : "memory"); }
 
 typedef SomeTiles<GEMM_ROWS, GEMM_GROUP> GemmTiles;
-template <int MODE>
+template <int MODE, int NB>
 struct Place {                             // of a tile
   int e = 0, row_tile = 0, col_tile = 0, rows = 0;      // rows: from its first row to the expert's end
-  static constexpr int COLS = MODE == UP ? GEMM_COLS / 2 : GEMM_COLS;
+  static constexpr int COLS = MODE == UP ? GEMM_COLS / 2 : GEMM_COLS / 2 * NB;
   __device__ __forceinline__ bool find(const XArgs& p, const GemmTiles& list, int b) {
     if (!list.find((p.N + COLS - 1) / COLS, b, e, row_tile, col_tile)) return false;
     rows = uniform(p.off[e + 1] - p.off[e]) - row_tile * GEMM_ROWS;
@@ -307,16 +307,17 @@ struct Place {                             // of a tile
 // products' loop has no branch.  STREAM: the weights are read once.  The scales of 512 come with the first stage of the four.  Three of those have a place: the stages of a
 // contraction's last scales may be fewer than the three that the loads are ahead, and with four stages to a contraction at least (LEAST_DEPTHS),
 // two in succession belong to four stages or more, so that what is overwritten has been read.
-template <int MODE, bool STREAM>
+template <int MODE, int NB, bool STREAM>
 struct Loads {
   const XArgs& p;
   const GemmTiles& list;
-  Place<MODE> at;
+  typedef Place<MODE, NB> AtPlace;
+  AtPlace at;
   int b, t, depths, groups, lane, wave;
   bool more;
   uint32_t lds0, stage = 0, scales = 0;
   const uint8_t* a; const uint8_t* bw; const uint8_t* sc;
-  uint32_t va[2], vb[2], vsc;
+  uint32_t va[2], vb[NB], vsc;
   __device__ __forceinline__ Loads(const XArgs& p_, const GemmTiles& list_, uint32_t lds0_, int lane_, int wave_)
       : p(p_), list(list_), b(blockIdx.x), depths(mx_depths(p_.K)), groups(mx_groups(p_.K)), lane(lane_), wave(wave_), lds0(lds0_) {
     begin();
@@ -325,25 +326,24 @@ struct Loads {
     t = 0;
     more = at.find(p, list, b);
     const bool second = MODE == UP && wave >= 4;          // W3's
-    const int first_b = second ? 2 * wave - 8 : 2 * wave;
+    const int first_b = second ? 2 * wave - 8 : NB * wave;
     // scales, four tiles' at a time: wavefronts 0 .. 3 the rows', 4 .. 7 the weights' (UP: 4 and 5 W1's)
     const bool of_weights = wave >= 4, of_second = MODE == UP && wave >= 6;
     const int first_s = 4 * (wave & (MODE == UP && of_weights ? 1 : 3));
     int last_a = 0, last_b = 0;
     if (more) {
-      const int n0 = at.col_tile * Place<MODE>::COLS;
+      const int n0 = at.col_tile * AtPlace::COLS;
       const size_t tile0 = uniform(p.first[at.e]) + at.row_tile * (GEMM_ROWS / 16);
       last_a = (min(at.rows, GEMM_ROWS) + 15) / 16 - 1;
-      last_b = min(Place<MODE>::COLS, p.N - n0) / 16 - 1;
+      last_b = min(AtPlace::COLS, p.N - n0) / 16 - 1;
       a = p.A + tile0 * depths * MX_TILE;
       bw = (second ? p.B1 : p.B0) + at.e * p.b_es + (size_t)(n0 / 16) * depths * MX_TILE;
       sc = of_weights ? (of_second ? p.Bs1 : p.Bs0) + at.e * p.bs_es + (size_t)(n0 / 16) * groups * MX_SCALES : p.As + tile0 * groups * MX_SCALES;
     }
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      va[j] = (uint32_t)(min(2 * wave + j, last_a) * depths * MX_TILE + lane * 16);
-      vb[j] = (uint32_t)(min(first_b + j, last_b) * depths * MX_TILE + lane * 16);
-    }
+    for (int j = 0; j < 2; ++j) va[j] = (uint32_t)(min(2 * wave + j, last_a) * depths * MX_TILE + lane * 16);
+#pragma unroll
+    for (int j = 0; j < NB; ++j) vb[j] = (uint32_t)(min(first_b + j, last_b) * depths * MX_TILE + lane * 16);
     vsc = (uint32_t)(min(first_s + lane / 16, of_weights ? last_b : last_a) * groups * MX_SCALES + lane % 16 * 16);
   }
   // before a stage's loads
@@ -359,12 +359,12 @@ struct Loads {
   }
   // A stage's loads, one after the other: the caller spreads them over its products (issued in a row, a load keeps a wavefront for 80 cycles
   // while the others issue theirs).
-  static constexpr int PARTS = 4;
+  static constexpr int PARTS = NB + 2;
   template <int I>
   __device__ __forceinline__ void part() {
     const size_t from = (size_t)t * MX_TILE;
-    if (I < 2) lds_load16<STREAM>((const bf16_t*)(bw + from), vb[I % 2], lds0 + stage + (16 + 2 * wave + I) * MX_TILE);
-    else lds_load16((const bf16_t*)(a + from), va[I % 2], lds0 + stage + (2 * wave + I % 2) * MX_TILE);
+    if constexpr (I < NB) lds_load16<STREAM>((const bf16_t*)(bw + from), vb[I], lds0 + stage + (16 + NB * wave + I) * MX_TILE);
+    else lds_load16((const bf16_t*)(a + from), va[I - NB], lds0 + stage + (2 * wave + I - NB) * MX_TILE);
     if (I == PARTS - 1) {
       stage = (stage + STAGE) % (STAGES * STAGE);
       t += more ? 1 : 0;
@@ -380,13 +380,13 @@ struct Loads {
 };
 
 // A wavefront multiplies 32 * NA rows, half of the tile's, by 64 weight rows (UP: 32 of either matrix).  stage, scales: where this tile's first are.
-template <int MODE, int NA, bool STREAM>
-__device__ __forceinline__ void gemm_tile(const XArgs& p, Loads<MODE, STREAM>& loads, const uint8_t* lds, uint32_t& stage, uint32_t& scales, const Place<MODE>& at,
+template <int MODE, int NA, int NB, bool STREAM>
+__device__ __forceinline__ void gemm_tile(const XArgs& p, Loads<MODE, NB, STREAM>& loads, const uint8_t* lds, uint32_t& stage, uint32_t& scales, const Place<MODE, NB>& at,
                                           int lane, int wave) {
-  constexpr int NB = 2, HALF = NB / 2;     // 32-column operands; UP: of either matrix
-  const int depths = loads.depths, n0 = at.col_tile * Place<MODE>::COLS;
+  constexpr int HALF = NB / 2;             // 32-column operands; UP: HALF of either matrix
+  const int depths = loads.depths, n0 = at.col_tile * Place<MODE, NB>::COLS;
   const int wr = wave & 1, wc = wave >> 1, h = lane >> 5;
-  const auto b_tile = [&](int j) { return 16 + (MODE == UP ? 8 * (j / HALF) + 2 * (HALF * wc + j % HALF) : 2 * (NB * wc + j)); };
+  const auto b_tile = [&](int j) { return 16 + (MODE == UP ? 8 * j + 2 * wc : 2 * (NB * wc + j)); };
   const int in_tile = (lane >> 4 & 1) * MX_TILE + h * 256 + (lane & 15) * 16, in_scales = (lane >> 4 & 1) * MX_SCALES + h * 64 + (lane & 15) * 4;
   f32x16 acc[NA][NB];
 #pragma unroll
@@ -411,17 +411,17 @@ __device__ __forceinline__ void gemm_tile(const XArgs& p, Loads<MODE, STREAM>& l
       bs[s][I - NA] = scales_from[128 * s + b_tile(I - NA) * MX_SCALES];
     }
   };
-  // The products of a step, and between them the reads of the other one's operands and half of a stage's loads.
-  constexpr int PRODUCTS = NA * NB, READS = NA + NB, READ_WITHIN = 3 * PRODUCTS / 4, LOADS = Loads<MODE, STREAM>::PARTS / 2;
+  // The products of a step, and between them the reads of the other one's operands and half of a stage's loads (of three the first, then two).
+  constexpr int PRODUCTS = NA * NB, READS = NA + NB, READ_WITHIN = PRODUCTS < 4 ? PRODUCTS : 3 * PRODUCTS / 4, PARTS = Loads<MODE, NB, STREAM>::PARTS, FIRST = PARTS / 2;
   const auto multiply = [&](auto step) {
-    constexpr int s = decltype(step)::value;
+    constexpr int s = decltype(step)::value, BEHIND = s == 0 ? FIRST : 0, LOADS = s == 0 ? PARTS - FIRST : FIRST;
     static_for<PRODUCTS>([&](auto m) {
       constexpr int M = decltype(m)::value, i = M / NB, j = M % NB;
       acc[i][j] = mfma32(b[s][j], a[s][i], acc[i][j], bs[s][j], as[s][i]);
       constexpr int R0 = M * READS / READ_WITHIN, R = M < READ_WITHIN ? (M + 1) * READS / READ_WITHIN - R0 : 0;
       if constexpr (R > 0) static_for<R>([&](auto r) { read(Int<1 - s>{}, Int<R0 + decltype(r)::value>{}); });
       constexpr int L0 = M * LOADS / PRODUCTS, L = (M + 1) * LOADS / PRODUCTS - L0;
-      if constexpr (L > 0) static_for<L>([&](auto l) { loads.template part<(s == 0 ? LOADS : 0) + L0 + decltype(l)::value>(); });
+      if constexpr (L > 0) static_for<L>([&](auto l) { loads.template part<BEHIND + L0 + decltype(l)::value>(); });
       __builtin_amdgcn_sched_barrier(0);
     });
   };
@@ -437,7 +437,7 @@ __device__ __forceinline__ void gemm_tile(const XArgs& p, Loads<MODE, STREAM>& l
   };
   begin(0);
   static_for<READS>([&](auto r) { read(Int<0>{}, r); });
-  static_for<LOADS>([&](auto l) { loads.template part<decltype(l)::value>(); });
+  static_for<FIRST>([&](auto l) { loads.template part<decltype(l)::value>(); });
   multiply(Int<0>{});
   for (int t = 1; t < depths; ++t) {
     begin(t);
@@ -534,11 +534,11 @@ __device__ __forceinline__ void few_tiles(const XArgs& p, const SomeTiles<FEW_RO
   }
 }
 
-template <int MODE, bool STREAM>
+template <int MODE, int NB, bool STREAM>
 __device__ __forceinline__ void many_tiles(const XArgs& p, const GemmTiles& many, uint8_t* lds, int lane, int wave) {
-  Place<MODE> at;
+  Place<MODE, NB> at;
   if (!at.find(p, many, blockIdx.x)) return;
-  Loads<MODE, STREAM> loads(p, many, lds_addr(lds), lane, wave);
+  Loads<MODE, NB, STREAM> loads(p, many, lds_addr(lds), lane, wave);
   uint32_t stage = 0, scales = 0;
   loads.issue();
   loads.issue();
@@ -561,10 +561,16 @@ __global__ __launch_bounds__(GEMM_THREADS, 1) void experts_mx4(XArgs p) {
   const SomeTiles<FEW_ROWS, 1> few(p.off, p.e_cnt, lane, 0, p.few_most);
   // Weights that are read once and that the Infinity Cache does not keep for the next call: 21 experts (7168 to 1536) of 64 rows read 5.5 TB/s with
   // the hint, 4.7 without, of 256 rows 3.7 and 3.4.  Eight experts of 1024 rows take 3 % longer with it, and what fits the cache 6 %.
-  if (many.experts + few.experts > p.cached && many.total < 2 * many.experts) many_tiles<MODE, true>(p, many, gemm_lds, lane, wave);
-  else many_tiles<MODE, false>(p, many, gemm_lds, lane, wave);
+  const bool once = many.experts + few.experts > p.cached && many.total < 2 * many.experts;
+  // DOWN: half as many columns where that still leaves a workgroup to every tile, those of few rows with them.  Eight experts (2880 to 2880) of
+  // 200 rows: 16.5 us, 21.5 with whole ones.
+  const bool half = MODE == DOWN && 2 * many.total * ((p.N + GEMM_COLS - 1) / GEMM_COLS) + few.total * ((p.N / FEW_COLS + FEW_WAVES - 1) / FEW_WAVES) <= (int)gridDim.x;
+  if (half) many_tiles<MODE, MODE == DOWN ? 1 : 2, false>(p, many, gemm_lds, lane, wave);
+  else if (once) many_tiles<MODE, 2, true>(p, many, gemm_lds, lane, wave);
+  else many_tiles<MODE, 2, false>(p, many, gemm_lds, lane, wave);
   // the workgroups that had no tile in the others' last round come first: `idle` of them
-  const int per_xcd = gridDim.x / 8, busy = ((many.total * ((p.N + Place<MODE>::COLS - 1) / Place<MODE>::COLS) + 7) / 8) % per_xcd;
+  const int cols = half ? Place<MODE, 1>::COLS : Place<MODE, 2>::COLS;
+  const int per_xcd = gridDim.x / 8, busy = ((many.total * ((p.N + cols - 1) / cols) + 7) / 8) % per_xcd;
   const int place = 8 * ((blockIdx.x / 8 + per_xcd - busy) % per_xcd) + blockIdx.x % 8, idle = 8 * (per_xcd - busy);
   if (few.total > p.cached) few_tiles<MODE, true>(p, few, reinterpret_cast<f32x4*>(gemm_lds), place, idle, many.total);
   else few_tiles<MODE, false>(p, few, reinterpret_cast<f32x4*>(gemm_lds), place, idle, many.total);
