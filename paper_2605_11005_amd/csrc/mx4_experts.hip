@@ -1,7 +1,7 @@
 // The experts' forward in microscaled 4 bits (mx4.h): rows, weights and activations are e2m1 with a scale per 32 elements, the products run on
 // the scaled matrix instruction, sums are fp32.
 //
-//   rows    xq = MX4(xp)                                  every expert's rows begin at a tile of 16
+//   rows    xq = MX4(xp)                                  every expert's rows begin at a tile of 16; in UP itself where there are few rows in all
 //   UP      aq = MX4(silu(xq W1) * (xq W3))
 //   DOWN    o  = aq W2                                    bf16
 #include "mx4.h"
@@ -25,6 +25,7 @@ struct XArgs {
   bf16_t* O;                                   // DOWN
   const int32_t* off; const int32_t* first;
   int e_cnt, N, K;
+  const bf16_t* X; int32_t* first_out;         // UP without expert_rows
   int few_most;                                // rows of an expert that few_tile takes
   int cached;                                  // experts whose weights fit the Infinity Cache
 };
@@ -74,15 +75,17 @@ __global__ __launch_bounds__(ROWS_BLOCK) void expert_rows(const bf16_t* __restri
 // ---- a few rows per expert: up to 16 * TG rows against 32 columns (UP: 32 of either matrix), a stream of weights from memory to registers.  A
 // piece is 512 of the contraction, 16 KB (UP) or 8 KB of weights, in two halves, of which three or two are on their way while one is
 // multiplied.  `split` wavefronts share a tile's contraction, the w-th the pieces w, w + split, .., and their sums are added in LDS in
-// ascending order.
-constexpr int FEW_MOST = 32, FEW_ROWS = 32, FEW_COLS = 32, FEW_WAVES = 8;
-template <int MODE, int TG, bool STREAM>
+// ascending order.  DIRECT: rows come as bf16, a lane's 32 elements being a chunk, and become its operand in registers, 16 rows a tile.
+constexpr int FEW_MOST = 32, FEW_ROWS = 32, FEW_COLS = 32, FEW_WAVES = 8, FEW_LDS = FEW_WAVES * 4 * WAVE * 16;
+// Where a tile's rows of bf16 begin, and how many there are (the others repeat the last one: their results are not used)
+struct DirectRows { const bf16_t* x; int rows; };
+template <int MODE, int TG, bool STREAM, bool DIRECT>
 struct HalfPiece {
   static constexpr int NB = MODE == UP ? 4 : 2;       // 16-column operands: W1's two, then W3's
-  u32x4 b[NB][2], a[TG][2];
+  u32x4 b[NB][2], a[TG][2][DIRECT ? 4 : 1];
   uint32_t bs[NB], as[TG];                            // of the whole piece
   template <int HALF>
-  __device__ __forceinline__ void load(const XArgs& p, int e, int nt, int tile0, int piece, int depths, int groups, uint32_t lane) {
+  __device__ __forceinline__ void load(const XArgs& p, int e, int nt, int tile0, DirectRows direct, int piece, int depths, int groups, uint32_t lane) {
     int at[2];
 #pragma unroll
     for (int q = 0; q < 2; ++q) at[q] = min(4 * piece + 2 * HALF + q, depths - 1);
@@ -99,9 +102,20 @@ struct HalfPiece {
     }
 #pragma unroll
     for (int t = 0; t < TG; ++t) {
+      if constexpr (DIRECT) {
+        const bf16_t* row = direct.x + (size_t)min(16 * t + (int)lane % 16, direct.rows - 1) * p.K;
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          // (past the end the row's last chunk again, against weights that are zeros)
+          const u32x4* from = reinterpret_cast<const u32x4*>(row + min(MX_DEPTH * at[q] + MX_CHUNK * ((int)lane / 16), p.K - MX_CHUNK));
+#pragma unroll
+          for (int i = 0; i < 4; ++i) a[t][q][i] = from[i];
+        }
+        continue;
+      }
       const uint8_t* data = p.A + (size_t)(tile0 + t) * depths * MX_TILE;
 #pragma unroll
-      for (int q = 0; q < 2; ++q) a[t][q] = reinterpret_cast<const u32x4*>(data + (size_t)at[q] * MX_TILE)[lane];
+      for (int q = 0; q < 2; ++q) a[t][q][0] = reinterpret_cast<const u32x4*>(data + (size_t)at[q] * MX_TILE)[lane];
       as[t] = reinterpret_cast<const uint32_t*>(p.As + ((size_t)(tile0 + t) * groups + piece) * MX_SCALES)[lane];
     }
     __builtin_amdgcn_sched_barrier(0);                // loads stay in order: waiting for one half must not wait for the next
@@ -112,21 +126,37 @@ struct HalfPiece {
       constexpr int Q = decltype(at)::value, q = 2 * HALF + Q;
       if (q < left) {
 #pragma unroll
-        for (int j = 0; j < NB; ++j)
+        for (int t = 0; t < TG; ++t) {
+          u32x4 rows = a[t][Q][0];
+          uint32_t scales = as[t];
+          if constexpr (DIRECT) {
+            uint32_t w[16];
 #pragma unroll
-          for (int t = 0; t < TG; ++t) acc[j][t] = mfma<q, q>(b[j][Q], a[t][Q], acc[j][t], bs[j], as[t]);
+            for (int i = 0; i < 16; ++i) w[i] = a[t][Q][i / 4][i % 4];
+            rows = mx_chunk(w, scales);
+          }
+#pragma unroll
+          for (int j = 0; j < NB; ++j) acc[j][t] = mfma<q, DIRECT ? 0 : q>(b[j][Q], rows, acc[j][t], bs[j], scales);
+        }
       }
     });
     __builtin_amdgcn_sched_barrier(0);
   }
 };
 
-template <int MODE, int TG, bool STREAM>
+// tile in front of which the experts before e end
+__device__ __forceinline__ int first_tile(const XArgs& p, int e, int lane) {
+  int sum = 0;
+  for (int i = lane; i < e; i += WAVE) sum += (p.off[i + 1] - p.off[i] + 15) / 16;
+  return uniform(wave_sum(sum));
+}
+
+template <int MODE, int TG, bool STREAM, bool DIRECT>
 __device__ __forceinline__ void few_tile(const XArgs& p, f32x4* lds, int split, int e, int row_tile, int n0, int rows) {
-  constexpr int NB = MODE == UP ? 4 : 2;
+  constexpr int NB = MODE == UP ? 4 : 2, TILE_ROWS = DIRECT ? 16 : FEW_ROWS;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), part = wave % split;
   const int depths = mx_depths(p.K), groups = mx_groups(p.K);
-  const int tile0 = uniform(p.first[e]) + row_tile * (FEW_ROWS / 16);
+  const int tile0 = (DIRECT ? first_tile(p, e, lane) : uniform(p.first[e])) + row_tile * (TILE_ROWS / 16);
   const bool in = n0 < p.N;                           // (the last block of columns may be short of a wavefront's)
   f32x4 acc[NB][TG];
 #pragma unroll
@@ -134,12 +164,13 @@ __device__ __forceinline__ void few_tile(const XArgs& p, f32x4* lds, int split, 
 #pragma unroll
     for (int t = 0; t < TG; ++t) acc[j][t] = f32x4{0.f, 0.f, 0.f, 0.f};
   if (in && part < groups) {
-    constexpr int AHEAD = TG == 1 ? 4 : 3, TURN = TG == 1 ? 4 : 6;      // (register numbers and halves are those of a whole turn)
-    HalfPiece<MODE, TG, STREAM> half[AHEAD];
+    constexpr int AHEAD = DIRECT ? 2 : TG == 1 ? 4 : 3, TURN = AHEAD == 3 ? 6 : 4;      // (register numbers and halves are those of a whole turn)
+    HalfPiece<MODE, TG, STREAM, DIRECT> half[AHEAD];
+    const DirectRows direct = {DIRECT ? p.X + ((size_t)p.off[e] + row_tile * TILE_ROWS) * p.K : nullptr, min(rows, TILE_ROWS)};
     const int halves = 2 * ((groups - part + split - 1) / split);
     const auto load = [&](auto which, int h) {
       constexpr int W = decltype(which)::value;
-      if (h < halves) half[W % AHEAD].template load<W % 2>(p, e, n0 / 16, tile0, part + h / 2 * split, depths, groups, lane);
+      if (h < halves) half[W % AHEAD].template load<W % 2>(p, e, n0 / 16, tile0, direct, part + h / 2 * split, depths, groups, lane);
     };
     static_for<AHEAD>([&](auto u) { load(u, decltype(u)::value); });
     for (int h = 0; h < halves; h += TURN)
@@ -195,9 +226,14 @@ __device__ __forceinline__ void few_tile(const XArgs& p, f32x4* lds, int split, 
       uint16_t* out = reinterpret_cast<uint16_t*>(p.C + ((size_t)(tile0 + t) * mx_depths(p.N) + depth) * MX_TILE + chunk * 256 + i * 16);
       out[g] = (uint16_t)codes;
       out[4 + g] = (uint16_t)(codes >> 16);
-      if (g == 0) p.Cs[((size_t)(tile0 + t) * mx_groups(p.N) + depth / 4) * MX_SCALES + chunk * 64 + i * 4 + depth % 4] = (uint8_t)byte;
+      uint8_t* const scales = p.Cs + ((size_t)(tile0 + t) * mx_groups(p.N) + depth / 4) * MX_SCALES;
+      if (g == 0) scales[chunk * 64 + i * 4 + depth % 4] = (uint8_t)byte;
+      if (DIRECT && n0 + FEW_COLS == p.N && p.N % 512 != 0) {      // the last columns' wavefront writes the zeros behind them
+        if (g > chunk) *reinterpret_cast<u32x4*>(p.C + ((size_t)(tile0 + t) * mx_depths(p.N) + depth) * MX_TILE + lane * 16) = u32x4{0, 0, 0, 0};
+        for (int q = g > chunk ? depth % 4 : depth % 4 + 1; q < 4; ++q) scales[g * 64 + i * 4 + q] = 0;
+      }
     } else if (16 * t + i < rows) {
-      bf16_t* out = p.O + ((size_t)p.off[e] + row_tile * FEW_ROWS + 16 * t + i) * p.N + n0 + 4 * g;
+      bf16_t* out = p.O + ((size_t)p.off[e] + row_tile * TILE_ROWS + 16 * t + i) * p.N + n0 + 4 * g;
 #pragma unroll
       for (int j = 0; j < 2; ++j)
         *reinterpret_cast<u32x2*>(out + 16 * j) = u32x2{pack_bf16x2(sum[j][0], sum[j][1]), pack_bf16x2(sum[j][2], sum[j][3])};
@@ -497,8 +533,8 @@ __device__ __forceinline__ void gemm_tile(const XArgs& p, Loads<MODE, NB, STREAM
 }
 
 // Workgroups walk the tiles of the experts with many rows, then those of the experts with few.
-template <int MODE, bool STREAM>
-__device__ __forceinline__ void few_tiles(const XArgs& p, const SomeTiles<FEW_ROWS, 1>& list, f32x4* lds, int place, int idle, int rounds) {
+template <int MODE, bool STREAM, bool DIRECT = false>
+__device__ __forceinline__ void few_tiles(const XArgs& p, const SomeTiles<DIRECT ? 16 : FEW_ROWS, 1>& list, f32x4* lds, int place, int idle, int rounds) {
   if (list.total == 0) return;
   // In how many wavefronts a tile's contraction is cut, and how many of the blocks of tiles the `idle` workgroups and the others, which have one
   // more of the large tiles behind them, take each.  Alone and few enough for every workgroup to have one: cut as far as they stay so.
@@ -528,9 +564,9 @@ __device__ __forceinline__ void few_tiles(const XArgs& p, const SomeTiles<FEW_RO
   int t = place < idle ? place : idle * quota + place - idle, e, row_tile, col_tile;
   for (int k = place < idle ? quota : quota_others; k > 0 && t < n; --k, t += step) {
     list.at(t, n_cols, e, row_tile, col_tile);
-    const int rows = p.off[e + 1] - p.off[e] - row_tile * FEW_ROWS, n0 = (col_tile * per_block + wave / split) * FEW_COLS;
-    if (rows <= 16) few_tile<MODE, 1, STREAM>(p, lds, split, e, row_tile, n0, rows);
-    else few_tile<MODE, 2, STREAM>(p, lds, split, e, row_tile, n0, rows);
+    const int rows = p.off[e + 1] - p.off[e] - row_tile * (DIRECT ? 16 : FEW_ROWS), n0 = (col_tile * per_block + wave / split) * FEW_COLS;
+    if (DIRECT || rows <= 16) few_tile<MODE, 1, STREAM, DIRECT>(p, lds, split, e, row_tile, n0, rows);
+    else few_tile<MODE, 2, STREAM, false>(p, lds, split, e, row_tile, n0, rows);
   }
 }
 
@@ -576,6 +612,25 @@ __global__ __launch_bounds__(GEMM_THREADS, 1) void experts_mx4(XArgs p) {
   else few_tiles<MODE, false>(p, few, reinterpret_cast<f32x4*>(gemm_lds), place, idle, many.total);
 }
 
+// UP of at most FEW_MOST rows in all, from bf16: a launch less.  The whole forward (4096 to 1536) of a row of one expert takes 14.8 us, 18.7 with
+// expert_rows; of a row each of eight experts 26 and 30, of 32 experts 63 and 66.  An expert with 17 to 32 rows reads its weights twice: alone
+// (4096 to 14336) 44 us, 41 with expert_rows.
+__global__ __launch_bounds__(GEMM_THREADS, 1) void up_direct(XArgs p) {
+  extern __shared__ uint8_t gemm_lds[];
+  const int lane = threadIdx.x & 63;
+  if (blockIdx.x == 0 && threadIdx.x < WAVE) {
+    int before = 0;
+    for (int base = 0; base < p.e_cnt; base += WAVE) {
+      const int i = base + lane, n = i < p.e_cnt ? (p.off[i + 1] - p.off[i] + 15) / 16 : 0, incl = wave_scan(n);
+      if (i < p.e_cnt) p.first_out[i] = before + incl - n;
+      before += __builtin_amdgcn_readlane(incl, WAVE - 1);
+    }
+  }
+  const SomeTiles<16, 1> few(p.off, p.e_cnt, lane, 0, FEW_MOST);
+  if (few.total > p.cached) few_tiles<UP, true, true>(p, few, reinterpret_cast<f32x4*>(gemm_lds), blockIdx.x, gridDim.x, 0);
+  else few_tiles<UP, false, true>(p, few, reinterpret_cast<f32x4*>(gemm_lds), blockIdx.x, gridDim.x, 0);
+}
+
 inline size_t align256(size_t v) { return (v + 255) & ~(size_t)255; }
 // most tiles of tm rows that e_cnt experts with at most cap rows in all have
 inline long long tiles_bound(int cap, int e_cnt, int tm) { return ((long long)cap + (long long)(tm - 1) * (cap < e_cnt ? cap : e_cnt)) / tm; }
@@ -606,7 +661,8 @@ int launch_mx4_expert_fwd(const void* xp, int cap, int d, int f, int e_cnt, cons
   int32_t* const first = (int32_t*)(base + at.first);
   const long long tiles = tiles_bound(cap, e_cnt, 16);
   if (tiles * (d > f ? d : f) / FEW_COLS >= (1ll << 30)) return MOE_EUNSUPPORTED;       // tiles are counted in 32 bits
-  {
+  const bool direct = cap <= FEW_MOST;
+  if (!direct) {
     ProfScope prof(MOE_K_MX4_ROWS, s);
     const int waves = ROWS_BLOCK / WAVE;
     hipLaunchKernelGGL(expert_rows, dim3((unsigned)tiles, (mx_groups(d) + waves - 1) / waves), dim3(ROWS_BLOCK), 0, s, (const bf16_t*)xp, offsets,
@@ -627,6 +683,7 @@ int launch_mx4_expert_fwd(const void* xp, int cap, int d, int f, int e_cnt, cons
   const dim3 walkers(8 * ((device_cu_count() + 7) / 8));       // (a walk stays in its XCD's eighth)
   XArgs p{};
   p.off = offsets; p.first = first; p.e_cnt = e_cnt;
+  p.X = (const bf16_t*)xp; p.first_out = first;
   p.A = base + at.xq; p.As = base + at.xs;
   p.B0 = w1; p.Bs0 = s1; p.B1 = w3; p.Bs1 = s3;
   p.C = base + at.aq; p.Cs = base + at.as;
@@ -636,7 +693,8 @@ int launch_mx4_expert_fwd(const void* xp, int cap, int d, int f, int e_cnt, cons
   p.b_es = (size_t)((f + 15) / 16) * mx_depths(d) * MX_TILE; p.bs_es = (size_t)((f + 15) / 16) * mx_groups(d) * MX_SCALES;
   {
     ProfScope prof(MOE_K_MX4_UP, s);
-    hipLaunchKernelGGL(experts_mx4<UP>, walkers, dim3(GEMM_THREADS), GEMM_LDS, s, p);
+    if (direct) hipLaunchKernelGGL(up_direct, walkers, dim3(GEMM_THREADS), FEW_LDS, s, p);
+    else hipLaunchKernelGGL(experts_mx4<UP>, walkers, dim3(GEMM_THREADS), GEMM_LDS, s, p);
     HIP_CHECK_LAUNCH();
   }
   p.A = p.C; p.As = p.Cs;

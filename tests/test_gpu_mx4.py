@@ -212,3 +212,24 @@ def test_workgroups_with_several_tiles(d, f):
         B.moe_mx4_expert_fwd(xp[r], off[:part + 1], *args, ref[r], ws)
     differ = (o != ref).any(1).sum().item()
     assert differ == 0, f"{differ} of {E * rows} rows"
+
+
+@pytest.mark.parametrize("rows,d,f", [([1], 4096, 1536), ([1, 0, 4, 11, 16], 544, 288), ([0, 3, 0, 2], 96, 544), ([1] * 32, 1152, 96), ([17, 15], 640, 416),
+                                      ([32], 2080, 800), ([1] * 20 + [0] * 100 + [3] * 4, 160, 64)])
+def test_few_rows_in_all(rows, d, f):
+    """At most 32 rows: quantised inside the first product.  The same numbers as with a larger capacity, to the bit where no expert has more than
+    a tile of rows."""
+    print(f"case mx4 few rows {rows} {d} {f}", flush=True)
+    xp, off, w = make(rows, d, f, seed=d + f)
+    R = sum(rows)
+    o, _, _ = run(xp, off, w)
+    check(xp, off, w, o)
+    larger, _, _ = run(torch.cat([xp, torch.full((64, d), float("nan"), dtype=BF16)]), off, w)
+    check(xp, off, w, larger[:R])
+    if max(rows) <= 16:
+        assert torch.equal(o, larger[:R])
+    # a row of NaN keeps to itself; what the workspace held does not enter
+    xp[R // 2, d - 1] = float("nan")
+    bad, _, _ = run(xp, off, w, poison=False)
+    others = torch.arange(R) != R // 2
+    assert torch.isnan(bad[R // 2]).all() and torch.equal(bad[others], o[others])
