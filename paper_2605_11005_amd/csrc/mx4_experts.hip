@@ -39,7 +39,7 @@ __device__ __forceinline__ f32x4 mfma(u32x4 a, u32x4 b, f32x4 c, uint32_t sa, ui
   return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, y, c, 4, 4, SA, (int)sa, SB, (int)sb);      // 4: e2m1
 }
 
-// ---- rows: a wavefront per 16 rows by 512 elements; a block finds its tile's expert by itself
+// ---- rows: a wavefront per 16 rows by 512 elements; a block finds its tile's expert by itself.  HBM bound: 16249 rows of 7168 52 us, 5.7 TB/s.
 constexpr int ROWS_BLOCK = 256;
 __global__ __launch_bounds__(ROWS_BLOCK) void expert_rows(const bf16_t* __restrict__ x, const int32_t* __restrict__ off, int e_cnt, int d, int f,
                                                            uint8_t* __restrict__ q, uint8_t* __restrict__ scales, uint8_t* __restrict__ aq,
@@ -76,6 +76,8 @@ __global__ __launch_bounds__(ROWS_BLOCK) void expert_rows(const bf16_t* __restri
 // piece is 512 of the contraction, 16 KB (UP) or 8 KB of weights, in two halves, of which three or two are on their way while one is
 // multiplied.  `split` wavefronts share a tile's contraction, the w-th the pieces w, w + split, .., and their sums are added in LDS in
 // ascending order.  DIRECT: rows come as bf16, a lane's 32 elements being a chunk, and become its operand in registers, 16 rows a tile.
+// Bound by memory: a row or two each of 85 experts (4096 to 1536) read 6.1 TB/s of weights, 14 experts (7168 to 2048) with 208 rows 5.5.  Tiles of up to
+// 64 rows of this kind took 8 % longer at 31 experts with 63 rows on average than the larger tiles below.
 constexpr int FEW_MOST = 32, FEW_ROWS = 32, FEW_COLS = 32, FEW_WAVES = 8, FEW_LDS = FEW_WAVES * 4 * WAVE * 16;
 // Where a tile's rows of bf16 begin, and how many there are (the others repeat the last one: their results are not used)
 struct DirectRows { const bf16_t* x; int rows; };
@@ -302,6 +304,8 @@ struct SomeTiles {
 // directly, 128 of the contraction at a time, through a ring of four stages of which three are on their way.  Their layout in memory is
 // the one that the instruction wants, so every load is 1 KB of consecutive bytes and every LDS read free of conflicts.  Workgroups are
 // persistent, and the loads run ahead into the next tile while a finished one is written.
+// Eight experts (4096 to 14336) of 1024 rows: 465 us up and 220 us down, 4.2 PFLOP/s, bound by the package's power: the matrix unit is busy 47 % of
+// cycles at 1.9 GHz, and operands of zeros take 0.73 of the time.  A tile of up to 64 rows is a stream of weights, 0.7 us a stage.
 constexpr int GEMM_GROUP = 4, GEMM_ROWS = 256, GEMM_COLS = 256, GEMM_THREADS = 512;
 constexpr int STAGE = 32 * MX_TILE, STAGES = 4, SCALES = 32 * MX_SCALES;       // operand tiles of a stage: 16 of the rows, 16 of the weights
 constexpr int PLACES = 3;                  // for scales (see Loads)
