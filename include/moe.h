@@ -290,7 +290,7 @@ int moe_router_bwd(const void* x, const void* wr, const float* dlogits, int dtyp
  *   ws: moe_workspace_bytes(MOE_WS_BLOCK_NORM, dtype, T, 0, d, 0, 0, 0) bytes, 256-byte aligned.
  * The column sums are fp32, formed over rows that T alone decides and added in a fixed order: results are bit-reproducible.
  * Errors of both: EINVAL (NULL, negative sizes, unknown types, res_dtype neither dtype nor MOE_F32, eps not a positive number, outputs without their inputs),
- * EUNSUPPORTED (bf16 with d % 8 != 0, fp32 with d % 4 != 0, d > MOE_MAX_NORM_D), EWORKSPACE.
+ * EUNSUPPORTED (bf16 with d % 8 != 0, fp32 with d % 4 != 0, d > MOE_MAX_NORM_D, T > 2^31 - 2^16), EWORKSPACE.
  */
 int moe_block_norm_fwd(const void* y, const float* gate, const void* w_post, int post_norm, const void* h, const void* w_pre,
                        int dtype, int res_dtype, int T, int d, float alpha, float beta, float eps, void* h_out, void* n,
@@ -317,7 +317,7 @@ int moe_block_norm_bwd(const void* y, const float* gate, const void* w_post, int
  *   along_rows == 1: x [batch][K][n] (weights as the layer keeps them, W1[d][f], W2[f][d]); rows = K, cols = n
  * moe_mx4_dequantize -- out [batch][n][K] of type dtype, exact.
  * Errors: EINVAL (NULL, negative sizes, unknown dtype, pointers not 16-byte aligned), EUNSUPPORTED (K % 32 != 0; along_rows: bf16 with n % 8 != 0,
- * fp32 with n % 4 != 0; 2^31 tiles of 16 x 512 or more).
+ * fp32 with n % 4 != 0; 2^31 tiles of 16 x 512 or more, n or K within 511 of 2^31).
  */
 int moe_mx4_quantize(const void* x, int dtype, int batch, int rows, int cols, int along_rows, uint8_t* data, uint8_t* scales,
                      moe_stream_t stream);
@@ -331,7 +331,7 @@ int moe_mx4_dequantize(const uint8_t* data, const uint8_t* scales, int batch, in
  *   w2      n = d, K = f; s2.  Elements past K have to be zeros, as the quantisation leaves them.
  *   ws      moe_workspace_bytes(MOE_WS_MX4_EXPERT_FWD, dtype, 0, 0, d, f, e_cnt, cap) bytes, 256-byte aligned
  * Products of 4-bit numbers are exact and their sums fp32; the activation is rounded to 4 bits from fp32.  d % 32 == 0 and f % 32 == 0 (EUNSUPPORTED
- * otherwise).  A row that holds an infinity or NaN spoils its own outputs only.  Results are bit-reproducible; the order of a
+ * otherwise, and for d or f beyond 2^20 or 2^30 tiles of 16 rows by 32 columns).  A row that holds an infinity or NaN spoils its own outputs only.  Results are bit-reproducible; the order of a
  * row's sums may follow cap and its expert's row count.
  */
 int moe_mx4_expert_fwd(const void* xp, int dtype, int cap, int d, int f, int e_cnt, const int32_t* offsets, const uint8_t* w1,

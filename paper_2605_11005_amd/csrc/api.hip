@@ -395,12 +395,20 @@ int moe_block_norm_bwd(const void* y, const float* gate, const void* w_post, int
                                dw_post, dw_pre, accumulate, ws, (hipStream_t)stream);
 }
 
+namespace {
+// tiles are counted in 32 bits, and so are indices up to whole tiles past n and K
+bool mx4_too_large(int batch, int n, int K) {
+  const int most = 0x7FFFFE00;
+  return n > most || K > most || (long long)batch * ((n + 15ll) / 16) >= (1ll << 31) / ((K + 511ll) / 512 + 1);
+}
+}  // namespace
+
 int moe_mx4_quantize(const void* x, int dtype, int batch, int rows, int cols, int along_rows, uint8_t* data, uint8_t* scales,
                      moe_stream_t stream) {
   if (bad_dtype(dtype) || batch < 0 || rows < 0 || cols < 0 || (along_rows != 0 && along_rows != 1)) return MOE_EINVAL;
   const int n = along_rows ? cols : rows, K = along_rows ? rows : cols;
   if (K % 32 || (along_rows && n % (dtype == MOE_BF16 ? 8 : 4))) return MOE_EUNSUPPORTED;
-  if ((long long)batch * ((n + 15ll) / 16) >= (1ll << 31) / ((K + 511ll) / 512 + 1)) return MOE_EUNSUPPORTED;
+  if (mx4_too_large(batch, n, K)) return MOE_EUNSUPPORTED;
   if (batch > 0 && n > 0 && K > 0 && (!x || !data || !scales)) return MOE_EINVAL;
   if (misaligned(x, 16) || misaligned(data, 16) || misaligned(scales, 16)) return MOE_EINVAL;
   return launch_mx4_quantize(x, dtype, batch, n, K, along_rows, data, scales, (hipStream_t)stream);
@@ -409,7 +417,7 @@ int moe_mx4_quantize(const void* x, int dtype, int batch, int rows, int cols, in
 int moe_mx4_dequantize(const uint8_t* data, const uint8_t* scales, int batch, int n, int K, void* out, int dtype, moe_stream_t stream) {
   if (bad_dtype(dtype) || batch < 0 || n < 0 || K < 0) return MOE_EINVAL;
   if (K % 32) return MOE_EUNSUPPORTED;
-  if ((long long)batch * ((n + 15ll) / 16) >= (1ll << 31) / ((K + 511ll) / 512 + 1)) return MOE_EUNSUPPORTED;
+  if (mx4_too_large(batch, n, K)) return MOE_EUNSUPPORTED;
   if (batch > 0 && n > 0 && K > 0 && (!out || !data || !scales)) return MOE_EINVAL;
   if (misaligned(out, 16) || misaligned(data, 16) || misaligned(scales, 16)) return MOE_EINVAL;
   return launch_mx4_dequantize(data, scales, batch, n, K, out, dtype, (hipStream_t)stream);
