@@ -304,8 +304,9 @@ struct SomeTiles {
 // directly, 128 of the contraction at a time, through a ring of four stages of which three are on their way.  Their layout in memory is
 // the one that the instruction wants, so every load is 1 KB of consecutive bytes and every LDS read free of conflicts.  Workgroups are
 // persistent, and the loads run ahead into the next tile while a finished one is written.
-// Eight experts (4096 to 14336) of 1024 rows: 465 us up and 220 us down, 4.2 PFLOP/s, bound by the package's power: the matrix unit is busy 47 % of
-// cycles at 1.9 GHz, and operands of zeros take 0.73 of the time.  A tile of up to 64 rows is a stream of weights, 0.7 us a stage.
+// Eight experts (4096 to 14336) of 1024 rows: 455 us up and 215 us down, 4.3 PFLOP/s, bound by the package's power: the matrix unit is busy half of
+// the cycles at 1.9 GHz, and operands of zeros take 0.73 of the time.  Four stages are one turn of the loop, for the bytes of the scales' words to be
+// chosen by the instruction (455 us; 465 with a byte read at every stage, 503 with shifted words).  A tile of up to 64 rows is a stream of weights, 0.7 us a stage.
 constexpr int GEMM_GROUP = 4, GEMM_ROWS = 256, GEMM_COLS = 256, GEMM_THREADS = 512;
 constexpr int STAGE = 32 * MX_TILE, STAGES = 4, SCALES = 32 * MX_SCALES;       // operand tiles of a stage: 16 of the rows, 16 of the weights
 constexpr int PLACES = 3;                  // for scales (see Loads)
@@ -314,10 +315,11 @@ constexpr int LEAST_DEPTHS = 4;            // (see Loads)
 __device__ __forceinline__ uint32_t next_place(uint32_t scales) { return scales == (PLACES - 1) * SCALES ? 0 : scales + SCALES; }
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
-// (scales: the words' lowest bytes)
+// (scales: byte BYTE of the words)
+template <int BYTE>
 __device__ __forceinline__ f32x16 mfma32(u32x4 a, u32x4 b, f32x16 c, uint32_t sa, uint32_t sb) {
   const i32x8 x = {(int)a[0], (int)a[1], (int)a[2], (int)a[3], 0, 0, 0, 0}, y = {(int)b[0], (int)b[1], (int)b[2], (int)b[3], 0, 0, 0, 0};
-  return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, y, c, 4, 4, 0, (int)sa, 0, (int)sb);
+  return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, y, c, 4, 4, BYTE, (int)sa, BYTE, (int)sb);
 }
 // lanes 32..63 of a and lanes 0..31 of b change places
 __device__ __forceinline__ void swap32(uint32_t& a, uint32_t& b) {
@@ -437,29 +439,29 @@ __device__ __forceinline__ void gemm_tile(const XArgs& p, Loads<MODE, NB, STREAM
       for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
   u32x4 a[2][NA], b[2][NB];
   uint32_t as[2][NA], bs[2][NB];
-  // operand I of step s (64 of the contraction) of the stage in place, and its scales
+  // operand I of step s (64 of the contraction) of the stage in place; with the first of four stages the scales of all of them
   const uint8_t* from;
   const uint8_t* scales_from;
-  const auto read = [&](auto step, auto which) {
+  const auto read = [&](auto step, auto quarter, auto which) {
     // in the order in which the products take them: a weight operand, a row operand, the other weights, the other rows
     constexpr int s = decltype(step)::value, N = decltype(which)::value, I = N == 0 ? NA : N == 1 ? 0 : N <= NB ? NA + N - 1 : N - NB;
     if constexpr (I < NA) {
       a[s][I] = *reinterpret_cast<const u32x4*>(from + 512 * s + (2 * NA * wr + 2 * I) * MX_TILE);
-      as[s][I] = scales_from[128 * s + (2 * NA * wr + 2 * I) * MX_SCALES];
+      if constexpr (decltype(quarter)::value == 0) as[s][I] = *reinterpret_cast<const uint32_t*>(scales_from + 128 * s + (2 * NA * wr + 2 * I) * MX_SCALES);
     } else {
       b[s][I - NA] = *reinterpret_cast<const u32x4*>(from + 512 * s + b_tile(I - NA) * MX_TILE);
-      bs[s][I - NA] = scales_from[128 * s + b_tile(I - NA) * MX_SCALES];
+      if constexpr (decltype(quarter)::value == 0) bs[s][I - NA] = *reinterpret_cast<const uint32_t*>(scales_from + 128 * s + b_tile(I - NA) * MX_SCALES);
     }
   };
   // The products of a step, and between them the reads of the other one's operands and half of a stage's loads (of three the first, then two).
   constexpr int PRODUCTS = NA * NB, READS = NA + NB, READ_WITHIN = PRODUCTS < 4 ? PRODUCTS : 3 * PRODUCTS / 4, PARTS = Loads<MODE, NB, STREAM>::PARTS, FIRST = PARTS / 2;
-  const auto multiply = [&](auto step) {
-    constexpr int s = decltype(step)::value, BEHIND = s == 0 ? FIRST : 0, LOADS = s == 0 ? PARTS - FIRST : FIRST;
+  const auto multiply = [&](auto step, auto quarter) {               // quarter: of the stage whose operands are read
+    constexpr int s = decltype(step)::value, Q = decltype(quarter)::value, MINE = s == 0 ? Q : (Q + 3) % 4, BEHIND = s == 0 ? FIRST : 0, LOADS = s == 0 ? PARTS - FIRST : FIRST;
     static_for<PRODUCTS>([&](auto m) {
       constexpr int M = decltype(m)::value, i = M / NB, j = M % NB;
-      acc[i][j] = mfma32(b[s][j], a[s][i], acc[i][j], bs[s][j], as[s][i]);
+      acc[i][j] = mfma32<MINE>(b[s][j], a[s][i], acc[i][j], bs[s][j], as[s][i]);
       constexpr int R0 = M * READS / READ_WITHIN, R = M < READ_WITHIN ? (M + 1) * READS / READ_WITHIN - R0 : 0;
-      if constexpr (R > 0) static_for<R>([&](auto r) { read(Int<1 - s>{}, Int<R0 + decltype(r)::value>{}); });
+      if constexpr (R > 0) static_for<R>([&](auto r) { read(Int<1 - s>{}, quarter, Int<R0 + decltype(r)::value>{}); });
       constexpr int L0 = M * LOADS / PRODUCTS, L = (M + 1) * LOADS / PRODUCTS - L0;
       if constexpr (L > 0) static_for<L>([&](auto l) { loads.template part<BEHIND + L0 + decltype(l)::value>(); });
       __builtin_amdgcn_sched_barrier(0);
@@ -471,23 +473,28 @@ __device__ __forceinline__ void gemm_tile(const XArgs& p, Loads<MODE, NB, STREAM
     loads.wait();
     loads.head();
     from = lds + stage + in_tile;
-    scales_from = lds + STAGES * STAGE + scales + in_scales + t % 4;
+    scales_from = lds + STAGES * STAGE + scales + in_scales;
     stage = (stage + STAGE) % (STAGES * STAGE);
     if (t % 4 == 3 || t == depths - 1) scales = next_place(scales);
   };
   begin(0);
-  static_for<READS>([&](auto r) { read(Int<0>{}, r); });
+  static_for<READS>([&](auto r) { read(Int<0>{}, Int<0>{}, r); });
   static_for<FIRST>([&](auto l) { loads.template part<decltype(l)::value>(); });
-  multiply(Int<0>{});
-  for (int t = 1; t < depths; ++t) {
+  multiply(Int<0>{}, Int<0>{});
+  int t = 1;
+  const auto stage_of = [&](auto quarter) {
     begin(t);
-    multiply(Int<1>{});
-    multiply(Int<0>{});
-  }
+    multiply(Int<1>{}, quarter);
+    multiply(Int<0>{}, quarter);
+    return ++t < depths;
+  };
+  if (t < depths)
+    while (stage_of(Int<1>{}) && stage_of(Int<2>{}) && stage_of(Int<3>{}) && stage_of(Int<0>{})) {}
+  const int behind = 8 * ((depths - 1) % 4);
 #pragma unroll
   for (int i = 0; i < NA; ++i)
 #pragma unroll
-    for (int j = 0; j < NB; ++j) acc[i][j] = mfma32(b[1][j], a[1][i], acc[i][j], bs[1][j], as[1][i]);
+    for (int j = 0; j < NB; ++j) acc[i][j] = mfma32<0>(b[1][j], a[1][i], acc[i][j], bs[1][j] >> behind, as[1][i] >> behind);
   // element 4 g + r of acc[i][j]: row lane % 32, column 8 g + 4 h + r of the 32
 #pragma unroll
   for (int i = 0; i < NA; ++i) {
