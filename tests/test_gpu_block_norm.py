@@ -220,3 +220,15 @@ def test_backward_refusals():
                    dict(y=None, dy=None), dict(dh=c.dh.float()), dict(accumulate=2), dict(dw_pre=c.dw_pre[:32])):
         with pytest.raises(B.MoeError):
             B.moe_block_norm_bwd(**{**a, **change})
+
+
+@pytest.mark.parametrize("dt,rt", TYPES)
+@pytest.mark.parametrize("T,d", [(530, 8200), (300, 16384), (2100, 1024), (700, 264), (8200, 520), (600, 4104)])
+def test_blocks_that_walk_several_rows(T, d, dt, rt):
+    """Column sums over a block's rows and wavefronts, and over blocks with a row more than others: every layout of rows in blocks."""
+    print(f"case norm {T} {d} {dt} {rt}", flush=True)
+    c = Case(T, d, dt, rt, seed=T + d)
+    c.forward()
+    c.check_forward()
+    c.backward()
+    c.check_backward()
