@@ -80,35 +80,39 @@ __global__ __launch_bounds__(QUANT_BLOCK) void mx4_columns(const T* __restrict__
 }
 
 // Back to values [n][K]: exact in either type (an e2m1 number has two bits of mantissa).  A block takes 16 rows by 512 elements, a lane
-// eight elements of four operands: 16 lanes write 256 (fp32: 512) bytes of a row.  16 matrices of 4096 by 1536 to bf16: 37 us, 6.9 TB/s.
+// 16 bytes of every store, so that 16 lanes write 256 bytes of a row.  16 matrices of 4096 by 1536 to bf16: 37 us, 6.9 TB/s.
 template <typename T>
 __global__ __launch_bounds__(QUANT_BLOCK) void mx4_values(const uint8_t* __restrict__ q, const uint8_t* __restrict__ scales, int n, int K,
                                                            T* __restrict__ out) {
+  constexpr int N = 16 / sizeof(T), STORES = MX_DEPTH / (16 * N);             // elements of a lane in a store, stores of an operand's row
   const int groups = mx_groups(K), depths = mx_depths(K), tiles = (n + 15) / 16;
   const int group = blockIdx.x % groups, rest = blockIdx.x / groups, batch = rest / tiles;
-  const int i = threadIdx.x >> 4, c = threadIdx.x & 15, chunk = c >> 2;       // row, eight elements of the 128
+  const int i = threadIdx.x >> 4, c = threadIdx.x & 15;                       // row, N elements of each store's
   const int row = 16 * (rest - batch * tiles) + i;
   if (row >= n) return;
-  const uint32_t word = *reinterpret_cast<const uint32_t*>(scales + ((size_t)rest * groups + group) * MX_SCALES + chunk * 64 + i * 4);
   T* dst = out + ((size_t)batch * n + row) * K;
 #pragma unroll
-  for (int p = 0; p < 4; ++p) {
-    const int depth = 4 * group + p, k = MX_DEPTH * depth + 8 * c;
-    if (k >= K) break;
-    const uint32_t v = *reinterpret_cast<const uint32_t*>(q + ((size_t)rest * depths + depth) * MX_TILE + chunk * 256 + i * 16 + (c & 3) * 4);
-    const uint32_t byte = (word >> (8 * p)) & 255u;
-    const float s = byte == 255 ? __uint_as_float(0x7FC00000u) : mx_scale_value(byte);
-    typedef float f32x2 __attribute__((ext_vector_type(2)));
-    // codes as multiples of 1/2, times the scale: both steps are exact
-    const f32x2 e[4] = {__builtin_amdgcn_cvt_scalef32_pk_f32_fp4(v, 1.f, 0), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(v, 1.f, 1),
-                        __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(v, 1.f, 2), __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(v, 1.f, 3)};
-    if constexpr (sizeof(T) == 2) {
-      const mx_u32x4 o = {pack_bf16x2(e[0].x * s, e[0].y * s), pack_bf16x2(e[1].x * s, e[1].y * s), pack_bf16x2(e[2].x * s, e[2].y * s),
-                          pack_bf16x2(e[3].x * s, e[3].y * s)};
-      *reinterpret_cast<mx_u32x4*>(dst + k) = o;
-    } else {
-      *reinterpret_cast<float4*>(dst + k) = {e[0].x * s, e[0].y * s, e[1].x * s, e[1].y * s};
-      *reinterpret_cast<float4*>(dst + k + 4) = {e[2].x * s, e[2].y * s, e[3].x * s, e[3].y * s};
+  for (int st = 0; st < STORES; ++st) {
+    const int at = 16 * N * st + N * c, chunk = at / MX_CHUNK;                // of the 128
+    const uint32_t word = *reinterpret_cast<const uint32_t*>(scales + ((size_t)rest * groups + group) * MX_SCALES + chunk * 64 + i * 4);
+#pragma unroll
+    for (int p = 0; p < 4; ++p) {
+      const int depth = 4 * group + p, k = MX_DEPTH * depth + at;
+      if (k >= K) break;
+      const uint8_t* codes = q + ((size_t)rest * depths + depth) * MX_TILE + chunk * 256 + i * 16 + at % MX_CHUNK / 2;
+      const uint32_t v = N == 8 ? *reinterpret_cast<const uint32_t*>(codes) : *reinterpret_cast<const uint16_t*>(codes);
+      const uint32_t byte = (word >> (8 * p)) & 255u;
+      const float s = byte == 255 ? __uint_as_float(0x7FC00000u) : mx_scale_value(byte);
+      typedef float f32x2 __attribute__((ext_vector_type(2)));
+      // codes as multiples of 1/2, times the scale: both steps are exact
+      const f32x2 e0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(v, 1.f, 0), e1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(v, 1.f, 1);
+      if constexpr (N == 8) {
+        const f32x2 e2 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(v, 1.f, 2), e3 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(v, 1.f, 3);
+        *reinterpret_cast<mx_u32x4*>(dst + k) = mx_u32x4{pack_bf16x2(e0.x * s, e0.y * s), pack_bf16x2(e1.x * s, e1.y * s),
+                                                         pack_bf16x2(e2.x * s, e2.y * s), pack_bf16x2(e3.x * s, e3.y * s)};
+      } else {
+        *reinterpret_cast<mx_f32x4*>(dst + k) = mx_f32x4{e0.x * s, e0.y * s, e1.x * s, e1.y * s};
+      }
     }
   }
 }
