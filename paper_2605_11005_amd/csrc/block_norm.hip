@@ -375,7 +375,8 @@ __global__ __launch_bounds__(SUM_WAVES * WAVE) void column_sums(const float* __r
   s = 0.f;
 #pragma unroll
   for (int w = 0; w < SUM_WAVES; ++w) s += part[w][lane];
-  if constexpr (sizeof(T) == 2) out[c] = f32_to_bf16(accumulate ? bf16_to_f32(out[c]) + s : s);
+  // (the hardware's conversion: a sum may be NaN of any payload, from the residual stream or the gate)
+  if constexpr (sizeof(T) == 2) out[c] = (bf16_t)pack_bf16x2(accumulate ? bf16_to_f32(out[c]) + s : s, 0.f);
   else out[c] = accumulate ? out[c] + s : s;
 }
 
