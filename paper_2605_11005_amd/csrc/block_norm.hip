@@ -98,6 +98,7 @@ struct FwdArgs {
   R* h_out; T* n; float* r_post; float* r_pre;
   int T_, d, post_norm;
   float alpha, beta, eps;
+  int row0;                                // of this launch
 };
 
 // A block per row, or (blockDim.y rows) a wavefront per row.
@@ -105,7 +106,7 @@ template <typename T, typename R, int STEPS>
 __global__ __launch_bounds__((MOST_THREADS<T, STEPS>)) void block_norm_fwd(FwdArgs<T, R> p) {
   constexpr int N = VEC<T>;
   __shared__ float red[2][MOST_WAVES];
-  const int row = blockIdx.x * blockDim.y + threadIdx.y;
+  const int row = p.row0 + blockIdx.x * blockDim.y + threadIdx.y;
   RowSum row_total{red, (int)blockDim.x >> 6};
   if (row >= p.T_) return;
   const size_t at = (size_t)row * p.d;
@@ -392,12 +393,13 @@ int forward(FwdArgs<T, R> p, hipStream_t s) {
   // and 92.
   if (vecs > WAVE && vecs <= 3 * WAVE / 2) steps = 2;
   const int threads = row_threads(vecs, steps), rows = threads == WAVE ? 4 : 1;
-  const dim3 grid((p.T_ + rows - 1) / rows), block(threads, rows);
-  if (steps == 1) hipLaunchKernelGGL((block_norm_fwd<T, R, 1>), grid, block, 0, s, p);
-  else if (steps == 2) hipLaunchKernelGGL((block_norm_fwd<T, R, 2>), grid, block, 0, s, p);
-  else hipLaunchKernelGGL((block_norm_fwd<T, R, 4>), grid, block, 0, s, p);
-  HIP_CHECK_LAUNCH();
-  return MOE_OK;
+  const dim3 block(threads, rows);
+  return in_launches((p.T_ + rows - 1) / rows, threads * rows, [&](long long first, unsigned blocks) {
+    p.row0 = (int)first * rows;
+    if (steps == 1) hipLaunchKernelGGL((block_norm_fwd<T, R, 1>), dim3(blocks), block, 0, s, p);
+    else if (steps == 2) hipLaunchKernelGGL((block_norm_fwd<T, R, 2>), dim3(blocks), block, 0, s, p);
+    else hipLaunchKernelGGL((block_norm_fwd<T, R, 4>), dim3(blocks), block, 0, s, p);
+  });
 }
 
 // The backward's launch.  A thread with one step of bf16 takes 124 registers, with 16 elements up to 252: one block of the latter fits on a

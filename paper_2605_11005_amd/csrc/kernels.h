@@ -6,6 +6,18 @@
 #include <stdint.h>
 #include "../../include/moe.h"
 
+// `blocks` workgroups of `threads` in as many launches as they need: a launch counts its work-items in 32 bits, and HIP cuts a larger count
+// off without an error.  launch(first, n) starts the n workgroups from `first` on.
+template <typename F>
+int in_launches(long long blocks, int threads, F launch) {
+  const long long most = (1ll << 31) / threads;
+  for (long long first = 0; first < blocks; first += most) {
+    launch(first, (unsigned)(blocks - first < most ? blocks - first : most));
+    if (hipGetLastError() != hipSuccess) return MOE_EHIP;
+  }
+  return MOE_OK;
+}
+
 int launch_route(const float* logits, int T, int E, int k, int gate_mode, int e_lo, int e_cnt,
                  int32_t* topk_idx, float* topk_w, int32_t* counts, hipStream_t s);
 

@@ -1,4 +1,4 @@
-"""The block norms' gradients with NaN and infinities in the sums over rows."""
+"""The block norms with NaN and infinities in the sums over rows, and with more rows than one launch holds."""
 import numpy as np
 import pytest
 import torch
@@ -43,3 +43,22 @@ def test_sums_over_rows_keep_nan_and_infinities(bits, accumulate):
         assert np.array_equal(np.isnan(got), np.isnan(want)), (name, got, want)
         inf = np.isinf(want)
         assert np.array_equal(got[inf], want[inf]) and np.isfinite(got[np.isfinite(want)]).all(), name
+
+
+def test_more_rows_than_a_launch_holds():
+    """2^28 rows of one wavefront each are 2^32 work-items."""
+    T, d, part = (1 << 28) + 5, 8, 1 << 24
+    if torch.cuda.mem_get_info()[0] < 4 * T * d * 2:
+        pytest.skip("not enough device memory")
+    h, w = torch.empty(T, d, dtype=BF16, device="cuda"), torch.linspace(0.5, 2, d, device="cuda").to(BF16)
+    g = torch.Generator(device="cuda").manual_seed(2)
+    for lo in range(0, T, part):
+        h[lo:lo + part].normal_(generator=g)
+    n, r_pre = torch.full_like(h, float("nan")), torch.full((T,), float("nan"), device="cuda")
+    B.moe_block_norm_fwd(None, None, None, False, h, w, 1.0, 1.0, EPS, None, n, None, r_pre)
+    for lo in range(0, T, part):
+        v = h[lo:lo + part].float()
+        r = (v.square().mean(1, keepdim=True) + EPS).rsqrt()
+        ref = v * r * w.float()
+        assert ((r_pre[lo:lo + part] / r[:, 0] - 1).abs() <= 1e-5).all(), lo
+        assert ((n[lo:lo + part].float() - ref).abs() <= 2.0 ** -8 * 1.01 * ref.abs() + 1e-30).all(), lo
