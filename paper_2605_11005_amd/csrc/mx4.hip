@@ -12,9 +12,9 @@ constexpr int QUANT_BLOCK = 256;
 // Rows whose elements are contiguous (tokens): a wavefront per 16 rows by 512 elements, 64 KB of loads on their way per CU and more.  2047 rows of
 // 2880 bf16: 4 us behind an empty launch.
 template <typename T>
-__global__ __launch_bounds__(QUANT_BLOCK) void mx4_rows(const T* __restrict__ x, int n, int K, long long jobs, uint8_t* __restrict__ q,
+__global__ __launch_bounds__(QUANT_BLOCK) void mx4_rows(const T* __restrict__ x, int n, int K, long long first, long long jobs, uint8_t* __restrict__ q,
                                                          uint8_t* __restrict__ scales) {
-  const long long job = (long long)blockIdx.x * (QUANT_BLOCK / WAVE) + (threadIdx.x >> 6);
+  const long long job = (first + blockIdx.x) * (QUANT_BLOCK / WAVE) + (threadIdx.x >> 6);
   if (job >= jobs) return;
   const int groups = mx_groups(K), tiles = (n + 15) / 16, group = (int)(job % groups);
   const long long rest = job / groups, batch = rest / tiles;
@@ -26,12 +26,12 @@ __global__ __launch_bounds__(QUANT_BLOCK) void mx4_rows(const T* __restrict__ x,
 // wavefronts of a block take the same chunk of four consecutive operands, whose scales meet in LDS as the bytes of a word.  16 matrices of
 // 4096 by 1536, bf16: 45 us, 5.6 TB/s (62 us without the hint that no element is read again).
 template <typename T>
-__global__ __launch_bounds__(QUANT_BLOCK) void mx4_columns(const T* __restrict__ x, int n, int K, int col_blocks, uint8_t* __restrict__ q,
+__global__ __launch_bounds__(QUANT_BLOCK) void mx4_columns(const T* __restrict__ x, int n, int K, int first, int col_blocks, uint8_t* __restrict__ q,
                                                             uint8_t* __restrict__ scales) {
   __shared__ uint8_t bytes[QUANT_BLOCK * 4];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int groups = mx_groups(K), depths = mx_depths(K), tiles = (n + 15) / 16;
-  int b = blockIdx.x;
+  int b = first + blockIdx.x;
   const int col_block = b % col_blocks; b /= col_blocks;
   const int chunk = b % 4; b /= 4;
   const int group = b % groups, batch = b / groups;
@@ -82,11 +82,12 @@ __global__ __launch_bounds__(QUANT_BLOCK) void mx4_columns(const T* __restrict__
 // Back to values [n][K]: exact in either type (an e2m1 number has two bits of mantissa).  A block takes 16 rows by 512 elements, a lane
 // 16 bytes of every store, so that 16 lanes write 256 bytes of a row.  16 matrices of 4096 by 1536 to bf16: 37 us, 6.9 TB/s.
 template <typename T>
-__global__ __launch_bounds__(QUANT_BLOCK) void mx4_values(const uint8_t* __restrict__ q, const uint8_t* __restrict__ scales, int n, int K,
+__global__ __launch_bounds__(QUANT_BLOCK) void mx4_values(const uint8_t* __restrict__ q, const uint8_t* __restrict__ scales, int n, int K, unsigned first,
                                                            T* __restrict__ out) {
   constexpr int N = 16 / sizeof(T), STORES = MX_DEPTH / (16 * N);             // elements of a lane in a store, stores of an operand's row
   const int groups = mx_groups(K), depths = mx_depths(K), tiles = (n + 15) / 16;
-  const int group = blockIdx.x % groups, rest = blockIdx.x / groups, batch = rest / tiles;
+  const unsigned at_block = first + blockIdx.x;
+  const int group = at_block % groups, rest = at_block / groups, batch = rest / tiles;
   const int i = threadIdx.x >> 4, c = threadIdx.x & 15;                       // row, N elements of each store's
   const int row = 16 * (rest - batch * tiles) + i;
   if (row >= n) return;
@@ -126,31 +127,30 @@ int launch_mx4_quantize(const void* x, int dtype, int batch, int n, int K, int a
     const int col_blocks = (n + QUANT_BLOCK - 1) / QUANT_BLOCK;
     const long long blocks = (long long)batch * mx_groups(K) * 4 * col_blocks;
     if (blocks >= (1ll << 31)) return MOE_EUNSUPPORTED;
-    if (dtype == MOE_BF16)
-      hipLaunchKernelGGL(mx4_columns<bf16_t>, dim3((unsigned)blocks), dim3(QUANT_BLOCK), 0, s, (const bf16_t*)x, n, K, col_blocks, q, scales);
-    else
-      hipLaunchKernelGGL(mx4_columns<float>, dim3((unsigned)blocks), dim3(QUANT_BLOCK), 0, s, (const float*)x, n, K, col_blocks, q, scales);
-  } else {
-    const long long jobs = (long long)batch * ((n + 15) / 16) * mx_groups(K), blocks = (jobs + QUANT_BLOCK / WAVE - 1) / (QUANT_BLOCK / WAVE);
-    if (blocks >= (1ll << 31)) return MOE_EUNSUPPORTED;
-    if (dtype == MOE_BF16)
-      hipLaunchKernelGGL(mx4_rows<bf16_t>, dim3((unsigned)blocks), dim3(QUANT_BLOCK), 0, s, (const bf16_t*)x, n, K, jobs, q, scales);
-    else
-      hipLaunchKernelGGL(mx4_rows<float>, dim3((unsigned)blocks), dim3(QUANT_BLOCK), 0, s, (const float*)x, n, K, jobs, q, scales);
+    return in_launches(blocks, QUANT_BLOCK, [&](long long first, unsigned here) {
+      if (dtype == MOE_BF16)
+        hipLaunchKernelGGL(mx4_columns<bf16_t>, dim3(here), dim3(QUANT_BLOCK), 0, s, (const bf16_t*)x, n, K, (int)first, col_blocks, q, scales);
+      else
+        hipLaunchKernelGGL(mx4_columns<float>, dim3(here), dim3(QUANT_BLOCK), 0, s, (const float*)x, n, K, (int)first, col_blocks, q, scales);
+    });
   }
-  HIP_CHECK_LAUNCH();
-  return MOE_OK;
+  const long long jobs = (long long)batch * ((n + 15) / 16) * mx_groups(K);
+  return in_launches((jobs + QUANT_BLOCK / WAVE - 1) / (QUANT_BLOCK / WAVE), QUANT_BLOCK, [&](long long first, unsigned here) {
+    if (dtype == MOE_BF16)
+      hipLaunchKernelGGL(mx4_rows<bf16_t>, dim3(here), dim3(QUANT_BLOCK), 0, s, (const bf16_t*)x, n, K, first, jobs, q, scales);
+    else
+      hipLaunchKernelGGL(mx4_rows<float>, dim3(here), dim3(QUANT_BLOCK), 0, s, (const float*)x, n, K, first, jobs, q, scales);
+  });
 }
 
 int launch_mx4_dequantize(const uint8_t* q, const uint8_t* scales, int batch, int n, int K, void* out, int dtype, hipStream_t s) {
   if (batch == 0 || n == 0 || K == 0) return MOE_OK;
   ProfScope prof(MOE_K_MX4_DEQUANTIZE, s);
-  const long long blocks = (long long)batch * ((n + 15) / 16) * mx_groups(K);
-  if (blocks >= (1ll << 31)) return MOE_EUNSUPPORTED;
-  if (dtype == MOE_BF16)
-    hipLaunchKernelGGL(mx4_values<bf16_t>, dim3((unsigned)blocks), dim3(QUANT_BLOCK), 0, s, q, scales, n, K, (bf16_t*)out);
-  else
-    hipLaunchKernelGGL(mx4_values<float>, dim3((unsigned)blocks), dim3(QUANT_BLOCK), 0, s, q, scales, n, K, (float*)out);
-  HIP_CHECK_LAUNCH();
-  return MOE_OK;
+  // (fewer than 2^31 workgroups: the entry point refuses more tiles)
+  return in_launches((long long)batch * ((n + 15) / 16) * mx_groups(K), QUANT_BLOCK, [&](long long first, unsigned here) {
+    if (dtype == MOE_BF16)
+      hipLaunchKernelGGL(mx4_values<bf16_t>, dim3(here), dim3(QUANT_BLOCK), 0, s, q, scales, n, K, (unsigned)first, (bf16_t*)out);
+    else
+      hipLaunchKernelGGL(mx4_values<float>, dim3(here), dim3(QUANT_BLOCK), 0, s, q, scales, n, K, (unsigned)first, (float*)out);
+  });
 }
