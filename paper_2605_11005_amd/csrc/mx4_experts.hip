@@ -43,11 +43,11 @@ __device__ __forceinline__ f32x4 mfma(u32x4 a, u32x4 b, f32x4 c, uint32_t sa, ui
 constexpr int ROWS_BLOCK = 256;
 __global__ __launch_bounds__(ROWS_BLOCK) void expert_rows(const bf16_t* __restrict__ x, const int32_t* __restrict__ off, int e_cnt, int d, int f,
                                                            uint8_t* __restrict__ q, uint8_t* __restrict__ scales, uint8_t* __restrict__ aq,
-                                                           uint8_t* __restrict__ as, int32_t* __restrict__ first) {
+                                                           uint8_t* __restrict__ as, int32_t* __restrict__ first, int tile0) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int tile = blockIdx.x, group = blockIdx.y * (ROWS_BLOCK / WAVE) + wave;
+  const int tile = tile0 + blockIdx.x, group = blockIdx.y * (ROWS_BLOCK / WAVE) + wave;
   int e = -1, row_tile = 0, before = 0;
-  const bool writes = blockIdx.x == 0 && blockIdx.y == 0 && wave == 0;
+  const bool writes = tile == 0 && blockIdx.y == 0 && wave == 0;
   for (int base = 0; base < e_cnt; base += WAVE) {
     const int i = base + lane, n = i < e_cnt ? (off[i + 1] - off[i] + 15) / 16 : 0, incl = wave_scan(n);
     if (writes && i < e_cnt) first[i] = before + incl - n;
@@ -675,10 +675,12 @@ int launch_mx4_expert_fwd(const void* xp, int cap, int d, int f, int e_cnt, cons
   const bool direct = cap <= FEW_MOST;
   if (!direct) {
     ProfScope prof(MOE_K_MX4_ROWS, s);
-    const int waves = ROWS_BLOCK / WAVE;
-    hipLaunchKernelGGL(expert_rows, dim3((unsigned)tiles, (mx_groups(d) + waves - 1) / waves), dim3(ROWS_BLOCK), 0, s, (const bf16_t*)xp, offsets,
-                       e_cnt, d, f, base + at.xq, base + at.xs, base + at.aq, base + at.as, first);
-    HIP_CHECK_LAUNCH();
+    const unsigned parts = (mx_groups(d) + ROWS_BLOCK / WAVE - 1) / (ROWS_BLOCK / WAVE);
+    const int rc = in_launches(tiles, (int)parts * ROWS_BLOCK, [&](long long tile0, unsigned here) {
+      hipLaunchKernelGGL(expert_rows, dim3(here, parts), dim3(ROWS_BLOCK), 0, s, (const bf16_t*)xp, offsets, e_cnt, d, f, base + at.xq, base + at.xs,
+                         base + at.aq, base + at.as, first, (int)tile0);
+    });
+    if (rc != MOE_OK) return rc;
   }
   {
     static bool attr_set[64] = {};
