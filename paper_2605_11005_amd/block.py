@@ -64,8 +64,16 @@ class MoeServeBuffers(_Norms):
         self.counts, self.offsets, self.perm = torch.empty((wl.e_cnt,), **i32), torch.empty((wl.e_cnt + 1,), **i32), torch.empty((cap,), **i32)
         self.xp, self.o = (torch.empty((cap, wl.d), dtype=torch.bfloat16, device=device) for _ in range(2))
         self.y = torch.empty((wl.T, wl.d), dtype=torch.bfloat16, device=device)
-        ws = lambda which, n: torch.empty(B.moe_workspace_bytes(which, B.MOE_BF16, wl.T, wl.k, wl.d, wl.f, n, cap), dtype=torch.uint8, device=device)  # noqa: E731
-        self.ws_router, self.ws_dispatch, self.ws_experts = ws(B.WS_ROUTER, wl.E), ws(B.WS_DISPATCH, wl.e_cnt), ws(B.WS_MX4_EXPERT_FWD, wl.e_cnt)
+        # (what the router's logits take is not monotonic in the tokens: of all numbers of them the largest)
+        ws = lambda which, n, tokens=(wl.T,): torch.empty(  # noqa: E731
+            max(B.moe_workspace_bytes(which, B.MOE_BF16, T, wl.k, wl.d, wl.f, n, cap) for T in tokens), dtype=torch.uint8, device=device)
+        self.ws_router, self.ws_dispatch = ws(B.WS_ROUTER, wl.E, range(wl.T + 1)), ws(B.WS_DISPATCH, wl.e_cnt)
+        self.ws_experts = ws(B.WS_MX4_EXPERT_FWD, wl.e_cnt)
+
+    def of_tokens(self, T):
+        """What has a row per token, T rows of each (refused by the calls where there are fewer)."""
+        per_token = self.logits, self.topk_idx, self.topk_w, self.inv, self.y, self.h, self.x
+        return per_token if len(self.y) == T else tuple(t[:T] for t in per_token)
 
 
 def serve_weights(w):
@@ -74,10 +82,11 @@ def serve_weights(w):
 
 
 def run_block_serve(wl, w, h, x, buf: MoeServeBuffers, eps: float = 1e-6):
-    """w: serve_weights.  -> buf.h, buf.x"""
-    B.moe_router_fwd(x, w["wr"], buf.logits, buf.ws_router)
-    B.moe_route(buf.logits, wl.k, wl.gate_mode, wl.e_lo, wl.e_cnt, buf.topk_idx, buf.topk_w, buf.counts)
-    B.moe_dispatch(x, wl.k, buf.topk_idx, None, wl.e_lo, wl.e_cnt, buf.offsets, buf.perm, buf.inv, False, buf.xp, buf.ws_dispatch)
+    """w: serve_weights; h, x of as many tokens as the buffers are for, or fewer.  -> the first rows of buf.h, buf.x"""
+    logits, topk_idx, topk_w, inv, y, h_out, x_out = buf.of_tokens(x.shape[0])
+    B.moe_router_fwd(x, w["wr"], logits, buf.ws_router)
+    B.moe_route(logits, wl.k, wl.gate_mode, wl.e_lo, wl.e_cnt, topk_idx, topk_w, buf.counts)
+    B.moe_dispatch(x, wl.k, topk_idx, None, wl.e_lo, wl.e_cnt, buf.offsets, buf.perm, inv, False, buf.xp, buf.ws_dispatch)
     B.moe_mx4_expert_fwd(buf.xp, buf.offsets, *w["w1"], *w["w3"], *w["w2"], buf.o, buf.ws_experts)
-    B.moe_combine(buf.o, buf.inv, buf.topk_w, buf.y)
-    B.moe_block_norm_fwd(buf.y, None, w["w_post"], True, h, w["w_pre"], 1.0, 1.0, eps, buf.h, buf.x)
+    B.moe_combine(buf.o, inv, topk_w, y)
+    B.moe_block_norm_fwd(y, None, w["w_post"], True, h, w["w_pre"], 1.0, 1.0, eps, h_out, x_out)
