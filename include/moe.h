@@ -331,8 +331,9 @@ int moe_mx4_dequantize(const uint8_t* data, const uint8_t* scales, int batch, in
  *   w2      n = d, K = f; s2.  Elements past K have to be zeros, as the quantisation leaves them.
  *   ws      moe_workspace_bytes(MOE_WS_MX4_EXPERT_FWD, dtype, 0, 0, d, f, e_cnt, cap) bytes, 256-byte aligned
  * Products of 4-bit numbers are exact and their sums fp32; the activation is rounded to 4 bits from fp32.  d % 32 == 0 and f % 32 == 0 (EUNSUPPORTED
- * otherwise, and for d or f beyond 2^20 or 2^30 tiles of 16 rows by 32 columns).  A row that holds an infinity or NaN spoils its own outputs only.  Results are bit-reproducible; the order of a
- * row's sums may follow cap and its expert's row count.
+ * otherwise, and for d or f beyond 2^20 or 2^30 tiles of 16 rows by 32 columns).  A row that holds an infinity or NaN spoils its own outputs only.
+ * A row's results depend on that row, its expert's weights and whether its expert has up to 32 rows or more, bit for bit: not on cap, nor on the rows
+ * beside it and of other experts.
  */
 int moe_mx4_expert_fwd(const void* xp, int dtype, int cap, int d, int f, int e_cnt, const int32_t* offsets, const uint8_t* w1,
                        const uint8_t* s1, const uint8_t* w3, const uint8_t* s3, const uint8_t* w2, const uint8_t* s2, void* o, void* ws,

@@ -74,11 +74,34 @@ __global__ __launch_bounds__(ROWS_BLOCK) void expert_rows(const bf16_t* __restri
 
 // ---- a few rows per expert: up to 16 * TG rows against 32 columns (UP: 32 of either matrix), a stream of weights from memory to registers.  A
 // piece is 512 of the contraction, 16 KB (UP) or 8 KB of weights, in two halves, of which three or two are on their way while one is
-// multiplied.  `split` wavefronts share a tile's contraction, the w-th the pieces w, w + split, .., and their sums are added in LDS in
-// ascending order.  DIRECT: rows come as bf16, a lane's 32 elements being a chunk, and become its operand in registers, 16 rows a tile.
+// multiplied.  2^cut wavefronts share a tile's contraction.  That number follows the tiles of all experts; a row's results must not, so that its sum
+// is eight sums added in one order whatever the number.  DIRECT: rows come as bf16, a lane's 32 elements being a chunk, and become its operand in
+// registers, 16 rows a tile.
 // Bound by memory: a row or two each of 85 experts (4096 to 1536) read 6.1 TB/s of weights, 14 experts (7168 to 2048) with 208 rows 5.5.  Tiles of up to
 // 64 rows of this kind took 8 % longer at 31 experts with 63 rows on average than the larger tiles below.
-constexpr int FEW_MOST = 32, FEW_ROWS = 32, FEW_COLS = 32, FEW_WAVES = 8, FEW_LDS = FEW_WAVES * 4 * WAVE * 16;
+constexpr int FEW_MOST = 32, FEW_ROWS = 32, FEW_COLS = 32, FEW_WAVES = 8;
+// The pieces of a contraction belong to eight sums, piece q of `pieces` to sum 8 q / pieces.  A row's result is ((s0 + s1) + s2) + .., each sum its
+// pieces in ascending order from zero.  Of 2^cut wavefronts the w-th takes the pieces from w pieces / 2^cut on, which are whole sums: as many
+// pieces as another's, but for one.  Against one sum per wavefront the forward takes 1 to 3 % longer, at 54 experts (4096 to 1536) of a row or
+// two 4 % (108 and 112 us); a row of one expert 5 % less.
+constexpr int FEW_SUMS = 8, SUMS_LOG2 = 3;
+__device__ __forceinline__ int first_piece(int w, int cut, int pieces) { return (w * pieces + (1 << cut) - 1) >> cut; }
+struct Sums {                              // walks a wavefront's pieces
+  int sum, rest, pieces;                   // 8 q = sum pieces + rest
+  __device__ __forceinline__ Sums(int w, int cut, int pieces_) : sum(w << (SUMS_LOG2 - cut)), rest(FEW_SUMS * first_piece(w, cut, pieces_) - sum * pieces_), pieces(pieces_) {
+    settle();
+  }
+  __device__ __forceinline__ void settle() {
+    for (; rest >= pieces; rest -= pieces) ++sum;      // (a short contraction has fewer sums)
+  }
+  __device__ __forceinline__ bool last_piece() const { return rest + FEW_SUMS >= pieces; }
+  __device__ __forceinline__ void next() { rest += FEW_SUMS; settle(); }
+};
+// Places in LDS for a tile's sums: the first wavefront's, which it adds up itself, in place 0; the others keep theirs apart, sum v in place
+// 1 + v - 8 / 2^cut.
+__host__ __device__ constexpr int few_places(int cut) { return cut == 0 ? 1 : 1 + FEW_SUMS - (FEW_SUMS >> cut); }
+// (most with two wavefronts a tile: four tiles of five places)
+constexpr int few_lds(int weight_operands, int row_operands) { return FEW_WAVES / 2 * few_places(1) * weight_operands * row_operands * WAVE * 16; }
 // Where a tile's rows of bf16 begin, and how many there are (the others repeat the last one: their results are not used)
 struct DirectRows { const bf16_t* x; int rows; };
 template <int MODE, int TG, bool STREAM, bool DIRECT>
@@ -154,55 +177,94 @@ __device__ __forceinline__ int first_tile(const XArgs& p, int e, int lane) {
 }
 
 template <int MODE, int TG, bool STREAM, bool DIRECT>
-__device__ __forceinline__ void few_tile(const XArgs& p, f32x4* lds, int split, int e, int row_tile, int n0, int rows) {
+__device__ __forceinline__ void few_tile(const XArgs& p, f32x4* lds, int cut, bool first, int e, int row_tile, int n0, int rows) {
   constexpr int NB = MODE == UP ? 4 : 2, TILE_ROWS = DIRECT ? 16 : FEW_ROWS;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), part = wave % split;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), part = wave & ((1 << cut) - 1);
   const int depths = mx_depths(p.K), groups = mx_groups(p.K);
   const int tile0 = (DIRECT ? first_tile(p, e, lane) : uniform(p.first[e])) + row_tile * (TILE_ROWS / 16);
   const bool in = n0 < p.N;                           // (the last block of columns may be short of a wavefront's)
-  f32x4 acc[NB][TG];
+  constexpr bool TOTAL = MODE == DOWN || TG == 1;     // the first wavefront adds up in registers: UP has none left for 32 rows (30 spilled: 87 us
+  // for 78 at 208 rows of 14 experts)
+  f32x4 acc[NB][TG], total[NB][TG];
 #pragma unroll
   for (int j = 0; j < NB; ++j)
 #pragma unroll
-    for (int t = 0; t < TG; ++t) acc[j][t] = f32x4{0.f, 0.f, 0.f, 0.f};
-  if (in && part < groups) {
+    for (int t = 0; t < TG; ++t) acc[j][t] = total[j][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+  // (a wavefront that has a tile alone does not wait for others, which may be at a tile of another height: everyone's places are where they are)
+  constexpr int MOST_TG = DIRECT ? 1 : FEW_ROWS / 16;
+  f32x4* const places = lds + (wave >> cut) * few_places(cut) * NB * MOST_TG * WAVE + lane;
+  const auto at_place = [&](int place, int j, int t) -> f32x4& { return places[((place * NB + j) * TG + t) * WAVE]; };
+  if (in) {
     constexpr int AHEAD = DIRECT ? 2 : TG == 1 ? 4 : 3, TURN = AHEAD == 3 ? 6 : 4;      // (register numbers and halves are those of a whole turn)
     HalfPiece<MODE, TG, STREAM, DIRECT> half[AHEAD];
     const DirectRows direct = {DIRECT ? p.X + ((size_t)p.off[e] + row_tile * TILE_ROWS) * p.K : nullptr, min(rows, TILE_ROWS)};
-    const int halves = 2 * ((groups - part + split - 1) / split);
+    const int piece0 = first_piece(part, cut, groups), halves = 2 * (first_piece(part + 1, cut, groups) - piece0);
+    Sums sums(part, cut, groups);
+    bool may_write = cut == 0 || first;               // not before the tile before has been read
     const auto load = [&](auto which, int h) {
       constexpr int W = decltype(which)::value;
-      if (h < halves) half[W % AHEAD].template load<W % 2>(p, e, n0 / 16, tile0, direct, part + h / 2 * split, depths, groups, lane);
+      if (h < halves) half[W % AHEAD].template load<W % 2>(p, e, n0 / 16, tile0, direct, piece0 + h / 2, depths, groups, lane);
     };
     static_for<AHEAD>([&](auto u) { load(u, decltype(u)::value); });
     for (int h = 0; h < halves; h += TURN)
       static_for<TURN>([&](auto u) {
         constexpr int W = decltype(u)::value;
         if (h + W >= halves) return;
-        half[W % AHEAD].template multiply<W % 2>(acc, depths - 4 * (part + (h + W) / 2 * split));
+        half[W % AHEAD].template multiply<W % 2>(acc, depths - 4 * (piece0 + (h + W) / 2));
         load(Int<W + AHEAD>{}, h + W + AHEAD);
+        if (W % 2 == 0) return;
+        if (sums.last_piece()) {
+          if (!may_write) __syncthreads();
+          may_write = true;
+          const int place = part == 0 ? 0 : 1 + sums.sum - (FEW_SUMS >> cut);
+          const bool add = part == 0 && sums.sum > 0;         // (s0 is never without pieces)
+#pragma unroll
+          for (int j = 0; j < NB; ++j)
+#pragma unroll
+            for (int t = 0; t < TG; ++t) {
+              if constexpr (TOTAL) {
+                if (part > 0) at_place(place, j, t) = acc[j][t];
+                total[j][t] += acc[j][t];
+              } else {
+                if (add) acc[j][t] += at_place(place, j, t);
+                at_place(place, j, t) = acc[j][t];
+              }
+              acc[j][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+            }
+        }
+        sums.next();
       });
+  } else if (cut > 0 && !first) {
+    __syncthreads();
+  }
+  if (cut > 0) {
+    if (TOTAL && TG > 1 && in && part == 0)
+#pragma unroll
+      for (int j = 0; j < NB; ++j)
+#pragma unroll
+        for (int t = 1; t < TG; ++t) at_place(0, j, t) = total[j][t];
+    __syncthreads();
   }
   const int i = lane & 15, g = lane >> 4;
 #pragma unroll
   for (int t = 0; t < TG; ++t) {
+    if (!in || part != (t & ((1 << cut) - 1))) continue;
     f32x4 sum[NB];
 #pragma unroll
-    for (int j = 0; j < NB; ++j) sum[j] = acc[j][t];
-    if (split > 1) {
-      __syncthreads();
+    for (int j = 0; j < NB; ++j) sum[j] = TOTAL && (t == 0 || cut == 0) ? total[j][t] : at_place(0, j, t);
+    if (cut > 0) {
+      const int own = FEW_SUMS >> cut;
+      f32x4 other[FEW_SUMS][NB];
 #pragma unroll
-      for (int j = 0; j < NB; ++j) lds[(wave * NB + j) * WAVE + lane] = acc[j][t];
-      __syncthreads();
-      if (part != t % split) continue;
-      const int base = wave - part;
+      for (int v = 1; v < FEW_SUMS; ++v)
 #pragma unroll
-      for (int j = 0; j < NB; ++j) {
-        sum[j] = lds[(base * NB + j) * WAVE + lane];
-        for (int w = 1; w < split; ++w) sum[j] += lds[((base + w) * NB + j) * WAVE + lane];
-      }
+        for (int j = 0; j < NB; ++j) other[v][j] = at_place(max(1 + v - own, 0), j, t);
+#pragma unroll
+      for (int v = 1; v < FEW_SUMS; ++v)
+        if (v >= own && first_piece(v, SUMS_LOG2, groups) < first_piece(v + 1, SUMS_LOG2, groups))
+#pragma unroll
+          for (int j = 0; j < NB; ++j) sum[j] += other[v][j];
     }
-    if (!in) continue;
     if constexpr (MODE == UP) {
       // this lane's eight of the row's 32 activations: columns 16 j + 4 g + r
       float v[2][4];
@@ -311,6 +373,8 @@ constexpr int GEMM_GROUP = 4, GEMM_ROWS = 256, GEMM_COLS = 256, GEMM_THREADS = 5
 constexpr int STAGE = 32 * MX_TILE, STAGES = 4, SCALES = 32 * MX_SCALES;       // operand tiles of a stage: 16 of the rows, 16 of the weights
 constexpr int PLACES = 3;                  // for scales (see Loads)
 constexpr int GEMM_LDS = STAGES * STAGE + PLACES * SCALES;
+constexpr int UP_LDS = GEMM_LDS > few_lds(4, 2) ? GEMM_LDS : few_lds(4, 2), DOWN_LDS = GEMM_LDS > few_lds(2, 2) ? GEMM_LDS : few_lds(2, 2), DIRECT_LDS = few_lds(4, 1);
+static_assert(UP_LDS <= 160 * 1024 && DOWN_LDS <= 160 * 1024);
 constexpr int LEAST_DEPTHS = 4;            // (see Loads)
 __device__ __forceinline__ uint32_t next_place(uint32_t scales) { return scales == (PLACES - 1) * SCALES ? 0 : scales + SCALES; }
 typedef float f32x16 __attribute__((ext_vector_type(16)));
@@ -569,15 +633,17 @@ __device__ __forceinline__ void few_tiles(const XArgs& p, const SomeTiles<DIRECT
     const int rest = list.total * ((cols * split + FEW_WAVES - 1) / FEW_WAVES) - ((int)gridDim.x - idle) * quota_others;
     quota = rest > 0 ? (rest + idle - 1) / idle : 0;
   }
-  split = uniform(split); quota = uniform(quota); quota_others = uniform(quota_others);
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), per_block = FEW_WAVES / split, n_cols = (cols + per_block - 1) / per_block;
+  const int cut = __builtin_ctz(uniform(split));
+  quota = uniform(quota); quota_others = uniform(quota_others);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), per_block = FEW_WAVES >> cut, n_cols = (cols + per_block - 1) / per_block;
   const int n = list.total * n_cols, step = place < idle ? idle : gridDim.x - idle;
   int t = place < idle ? place : idle * quota + place - idle, e, row_tile, col_tile;
-  for (int k = place < idle ? quota : quota_others; k > 0 && t < n; --k, t += step) {
+  bool first = true;
+  for (int k = place < idle ? quota : quota_others; k > 0 && t < n; --k, t += step, first = false) {
     list.at(t, n_cols, e, row_tile, col_tile);
-    const int rows = p.off[e + 1] - p.off[e] - row_tile * (DIRECT ? 16 : FEW_ROWS), n0 = (col_tile * per_block + wave / split) * FEW_COLS;
-    if (DIRECT || rows <= 16) few_tile<MODE, 1, STREAM, DIRECT>(p, lds, split, e, row_tile, n0, rows);
-    else few_tile<MODE, 2, STREAM, false>(p, lds, split, e, row_tile, n0, rows);
+    const int rows = p.off[e + 1] - p.off[e] - row_tile * (DIRECT ? 16 : FEW_ROWS), n0 = (col_tile * per_block + (wave >> cut)) * FEW_COLS;
+    if (DIRECT || rows <= 16) few_tile<MODE, 1, STREAM, DIRECT>(p, lds, cut, first, e, row_tile, n0, rows);
+    else few_tile<MODE, 2, STREAM, false>(p, lds, cut, first, e, row_tile, n0, rows);
   }
 }
 
@@ -687,8 +753,9 @@ int launch_mx4_expert_fwd(const void* xp, int cap, int d, int f, int e_cnt, cons
     int dev = 0;
     if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return MOE_EHIP;
     if (!attr_set[dev]) {
-      if (hipFuncSetAttribute(reinterpret_cast<const void*>(&experts_mx4<UP>), hipFuncAttributeMaxDynamicSharedMemorySize, GEMM_LDS) != hipSuccess ||
-          hipFuncSetAttribute(reinterpret_cast<const void*>(&experts_mx4<DOWN>), hipFuncAttributeMaxDynamicSharedMemorySize, GEMM_LDS) != hipSuccess)
+      if (hipFuncSetAttribute(reinterpret_cast<const void*>(&experts_mx4<UP>), hipFuncAttributeMaxDynamicSharedMemorySize, UP_LDS) != hipSuccess ||
+          hipFuncSetAttribute(reinterpret_cast<const void*>(&experts_mx4<DOWN>), hipFuncAttributeMaxDynamicSharedMemorySize, DOWN_LDS) != hipSuccess ||
+          hipFuncSetAttribute(reinterpret_cast<const void*>(&up_direct), hipFuncAttributeMaxDynamicSharedMemorySize, DIRECT_LDS) != hipSuccess)
         return MOE_EHIP;
       attr_set[dev] = true;
     }
@@ -706,8 +773,8 @@ int launch_mx4_expert_fwd(const void* xp, int cap, int d, int f, int e_cnt, cons
   p.b_es = (size_t)((f + 15) / 16) * mx_depths(d) * MX_TILE; p.bs_es = (size_t)((f + 15) / 16) * mx_groups(d) * MX_SCALES;
   {
     ProfScope prof(MOE_K_MX4_UP, s);
-    if (direct) hipLaunchKernelGGL(up_direct, walkers, dim3(GEMM_THREADS), FEW_LDS, s, p);
-    else hipLaunchKernelGGL(experts_mx4<UP>, walkers, dim3(GEMM_THREADS), GEMM_LDS, s, p);
+    if (direct) hipLaunchKernelGGL(up_direct, walkers, dim3(GEMM_THREADS), DIRECT_LDS, s, p);
+    else hipLaunchKernelGGL(experts_mx4<UP>, walkers, dim3(GEMM_THREADS), UP_LDS, s, p);
     HIP_CHECK_LAUNCH();
   }
   p.A = p.C; p.As = p.Cs;
@@ -718,7 +785,7 @@ int launch_mx4_expert_fwd(const void* xp, int cap, int d, int f, int e_cnt, cons
   p.b_es = (size_t)((d + 15) / 16) * mx_depths(f) * MX_TILE; p.bs_es = (size_t)((d + 15) / 16) * mx_groups(f) * MX_SCALES;
   {
     ProfScope prof(MOE_K_MX4_DOWN, s);
-    hipLaunchKernelGGL(experts_mx4<DOWN>, walkers, dim3(GEMM_THREADS), GEMM_LDS, s, p);
+    hipLaunchKernelGGL(experts_mx4<DOWN>, walkers, dim3(GEMM_THREADS), DOWN_LDS, s, p);
     HIP_CHECK_LAUNCH();
   }
   return MOE_OK;

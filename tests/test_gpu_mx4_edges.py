@@ -1,4 +1,5 @@
-"""Microscaled 4-bit calls of more workgroups than one launch holds."""
+"""Microscaled 4-bit calls at the edges of their sizes, and experts beside other experts: whatever those get, a row's results are the same bits."""
+import numpy as np
 import pytest
 import torch
 
@@ -84,3 +85,66 @@ def test_experts_of_more_tiles_than_one_launch():
     last = torch.empty_like(o[:57])
     B.moe_mx4_expert_fwd(x[cap - 60:cap - 3], offsets(0, 57), *w, last, ws)
     assert torch.equal(o[cap - 60:cap - 3], last)
+
+
+# ---- experts beside other experts
+def weights(E, d, f, seed, order_shows=False):
+    """order_shows: what the first third of a contraction adds the second takes back, and the last adds 2^-16 of it: the order of the sums, and
+    where they are rounded, decides the results."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    raw = [torch.randn(E, *shape, generator=g, device="cuda").mul(shape[0] ** -0.5).to(BF16) for shape in ((d, f), (d, f), (f, d))]
+    if order_shows:
+        for w in raw:
+            third = 32 * (w.shape[1] // 96)
+            w[:, third:2 * third] = -w[:, :third]
+            w[:, 2 * third:] *= 2.0 ** -16
+        for w in raw[:2]:
+            third = 32 * (f // 96)
+            w[:, :, third:2 * third] = w[:, :, :third]
+    return raw, [L.mx4_weights(w) for w in raw]
+
+
+def forward(x, rows, q, cap=None):
+    """o of the rows (expert after expert) with the experts' weights q, out of buffers of `cap` rows."""
+    R, (cap, d), e = sum(rows), (cap or max(sum(rows), 1), x.shape[1]), len(rows)
+    f = 16 * q[0][0].shape[1]
+    xp = torch.full((cap, d), float("nan"), dtype=BF16, device="cuda")
+    xp[:R] = x
+    off = torch.tensor([0] + list(np.cumsum(rows)), dtype=torch.int32, device="cuda")
+    o = torch.full_like(xp, float("nan"))
+    ws = torch.full((B.moe_workspace_bytes(B.WS_MX4_EXPERT_FWD, B.MOE_BF16, 0, 0, d, f, e, cap),), 0xFF, dtype=torch.uint8, device="cuda")
+    B.moe_mx4_expert_fwd(xp, off, *q[0], *q[1], *q[2], o, ws)
+    assert torch.isnan(o[R:]).all()
+    return o[:R]
+
+
+def tokens(n, d, seed, order_shows=False):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    x = torch.randn(n, d, generator=g, device="cuda").mul(torch.exp(0.5 * torch.randn(d, generator=g, device="cuda"))).to(BF16)
+    if order_shows:
+        third = 32 * (d // 96)
+        x[:, third:2 * third] = x[:, :third]
+    return x
+
+
+OTHERS = {"alone": [0] * 31, "one": [1] + [0] * 30, "three": [0, 5, 0, 2, 0, 1] + [0] * 25, "seven": [3] * 7 + [0] * 24, "fifteen": [2, 0] * 15 + [1],
+          "all": [4] * 31, "more": [30] * 31, "large": [0] * 30 + [600], "mixed": [33, 1, 0] * 10 + [300], "larger": [700] * 4 + [20] * 27}
+
+
+@pytest.mark.parametrize("d,f", [(4096, 1536), (7168, 2048), (2880, 1440), (768, 3328)])
+@pytest.mark.parametrize("mine", [1, 16, 20, 45, 300])
+def test_rows_of_other_experts_do_not_enter(mine, d, f):
+    print(f"case mx4 beside others {mine} {d} {f}", flush=True)
+    _, q = weights(32, d, f, d + f, order_shows=True)
+    x = tokens(mine, d, mine, order_shows=True)
+    want = {}
+    for name, others in OTHERS.items():
+        rest = tokens(sum(others), d, 9)
+        # among the first, and among the last
+        o = forward(torch.cat([x, rest]), [mine] + others, q)[:mine]
+        assert torch.isfinite(o).all()
+        last = forward(torch.cat([rest, x]), others + [mine], [tuple(t.roll(-1, 0) for t in w) for w in q])[sum(others):]
+        wide = forward(torch.cat([x, rest]), [mine] + others, q, cap=mine + sum(others) + 900)[:mine]
+        want[name] = o, last, wide
+    differ = {(name, i): (o != want["alone"][0]).sum().item() for name, all_ in want.items() for i, o in enumerate(all_)}
+    assert not any(differ.values()), {k: v for k, v in differ.items() if v}
