@@ -288,7 +288,7 @@ int moe_router_bwd(const void* x, const void* wr, const float* dlogits, int dtyp
  *   out; dw_post, dw_pre [d] dtype out, added to their contents with accumulate == 1.  dh, dgate, dw_post and dw_pre: NULL: not formed.
  *   r_post is read where post_norm is set, r_pre where w_pre is given.
  *   ws: moe_workspace_bytes(MOE_WS_BLOCK_NORM, dtype, T, 0, d, 0, 0, 0) bytes, 256-byte aligned.
- * The column sums are fp32, formed over rows that T alone decides and added in a fixed order: results are bit-reproducible.
+ * The column sums are fp32, formed over rows that T, d and dtype decide and added in a fixed order: results are bit-reproducible.
  * Errors of both: EINVAL (NULL, negative sizes, unknown types, res_dtype neither dtype nor MOE_F32, eps not a positive number, outputs without their inputs),
  * EUNSUPPORTED (bf16 with d % 8 != 0, fp32 with d % 4 != 0, d > MOE_MAX_NORM_D, T > 2^31 - 2^16), EWORKSPACE.
  */
