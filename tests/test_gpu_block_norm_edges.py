@@ -1,4 +1,7 @@
-"""The block norms with NaN and infinities in the sums over rows, and with more rows than one launch holds."""
+"""The block norms where sizes and values are at their edges: NaN in the sums over rows, rows beyond one launch's, blocks four to a CU.
+
+Bounds, set before the first run.  Column sums: a block adds at most T/256 + 1 rows one after the other, and at most 1024/16 + 16 blocks' sums follow;
+each product is a chain of some twenty fp32 operations with 1/rms factors of trees over d: (T/256 + 200) * 2^-24 * sum |terms|."""
 import numpy as np
 import pytest
 import torch
@@ -62,3 +65,21 @@ def test_more_rows_than_a_launch_holds():
         ref = v * r * w.float()
         assert ((r_pre[lo:lo + part] / r[:, 0] - 1).abs() <= 1e-5).all(), lo
         assert ((n[lo:lo + part].float() - ref).abs() <= 2.0 ** -8 * 1.01 * ref.abs() + 1e-30).all(), lo
+
+
+@pytest.mark.parametrize("T,d,dt,rt", [(8200, 1408, BF16, BF16), (8193, 2048, BF16, F32), (8300, 520, F32, F32), (8192, 1032, BF16, F32)])
+def test_four_blocks_on_a_cu(T, d, dt, rt):
+    print(f"case norm {T} {d} {dt} {rt}", flush=True)
+    g = torch.Generator().manual_seed(d)
+    r = lambda *s, dtype=dt: torch.randn(s, generator=g).to(dtype).cuda()  # noqa: E731
+    y, h, w_post, w_pre, dn, dh_out = r(T, d), r(T, d, dtype=rt), r(d), r(d), r(T, d), r(T, d, dtype=rt)
+    h_out, n, dh, dy = torch.empty_like(h), torch.empty_like(y), torch.empty_like(h), torch.empty_like(y)
+    r_post, r_pre, dgate, gate = (torch.rand(T, generator=g).cuda() for _ in range(4))
+    dw_post, dw_pre = torch.empty_like(w_post), torch.empty_like(w_pre)
+    B.moe_block_norm_fwd(y, gate, w_post, True, h, w_pre, 0.5, 1.5, EPS, h_out, n, r_post, r_pre)
+    B.moe_block_norm_bwd(y, gate, w_post, True, h_out, w_pre, r_post, r_pre, dh_out, dn, 0.5, 1.5, dh, dy, dgate, dw_post, dw_pre, False, workspace(T, d))
+    ref, mag = N.bwd(host(y), host(gate), host(w_post), True, host(h_out), host(w_pre), host(r_post), host(r_pre), host(dh_out), host(dn), 0.5, 1.5)
+    half = {BF16: 2.0 ** -8, F32: 2.0 ** -24}
+    for name, got, steps in (("dh", dh, 100), ("dy", dy, 100), ("dgate", dgate, 100), ("dw_post", dw_post, T / 256 + 200), ("dw_pre", dw_pre, T / 256 + 200)):
+        over = np.abs(host(got) - ref[name]) - (half[got.dtype] * np.abs(ref[name]) * (1 + 2.0 ** -7) + steps * 2.0 ** -24 * mag[name])
+        assert (over <= 0).all(), (name, float(over.max()))

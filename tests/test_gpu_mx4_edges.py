@@ -148,3 +148,70 @@ def test_rows_of_other_experts_do_not_enter(mine, d, f):
         want[name] = o, last, wide
     differ = {(name, i): (o != want["alone"][0]).sum().item() for name, all_ in want.items() for i, o in enumerate(all_)}
     assert not any(differ.values()), {k: v for k, v in differ.items() if v}
+
+
+def exact(x, raw, e):
+    """Oracle of one expert, and what it may be off by."""
+    host = lambda t: t.double().cpu().numpy()  # noqa: E731
+    v = [M.values(*M.quantize(host(w[e]).T))[None] for w in raw]
+    d = x.shape[1]
+    return M.expert_fwd(host(x), np.array([0, len(x)]), *v, h_err=(d / 128 + 16) * 2.0 ** -23)
+
+
+def check(o, x, rows, raw, experts):
+    """Bound as for a few experts at a time: half a unit of bf16, the fp32 sums, activations near a halfway value."""
+    off = np.concatenate([[0], np.cumsum(rows)])
+    for e in experts:
+        ref, slack = exact(x[off[e]:off[e + 1]], raw, e)
+        got = o[off[e]:off[e + 1]].double().cpu().numpy()
+        assert (np.abs(got - ref) <= 2.0 ** -8 * np.abs(ref) + slack + 1e-5 * np.abs(ref).max()).all(), e
+        assert np.linalg.norm(got - ref) <= 6e-3 * np.linalg.norm(ref), e
+
+
+def fits_the_cache(d, f):
+    """Experts whose weights in 4 bits fit 256 MB: with more, weights are loaded with the hint that they are used once."""
+    return (256 << 20) * 32 // (51 * d * f)
+
+
+MANY = {
+    # every expert a stream of few rows
+    "few": ([1, 2, 3] * 24, [0, 41, 71]),
+    "up to 32": ([32, 17, 5, 1] * 18, [0, 1, 70]),
+    # large experts among the first 64 and behind them, few of them
+    "large behind 64": ([3] * 66 + [300, 40, 257, 33, 128, 1], [5, 66, 69, 71]),
+    # so many streams that the workgroups with a large tile take some too
+    "both": ([31] * 64 + [300] * 4 + [20] * 4, [0, 64, 67, 70]),
+    # every large tile's weights are read once
+    "one tile each": ([33, 64, 65, 128, 129, 256] * 12, [0, 33, 68, 71]),
+    # and several times
+    "several tiles each": ([300, 513] * 36, [0, 71]),
+}
+
+
+@pytest.mark.parametrize("name", MANY)
+def test_more_experts_than_the_cache_holds(name):
+    d, f = 2048, 1408
+    rows, looked_at = MANY[name]
+    E = len(rows)
+    assert E > fits_the_cache(d, f)
+    print(f"case mx4 many experts {name}", flush=True)
+    raw, q = weights(E, d, f, 7)
+    x = tokens(sum(rows), d, 8)
+    o = forward(x, rows, q, cap=sum(rows) + 5)
+    off = np.concatenate([[0], np.cumsum(rows)])
+    for e in range(0, E, 6):                    # six at a time, as the cache holds them
+        part = forward(x[off[e]:off[e + 6]], rows[e:e + 6], [tuple(t[e:e + 6] for t in w) for w in q])
+        assert torch.equal(part, o[off[e]:off[e + 6]]), e
+    check(o, x, rows, raw, looked_at)
+
+
+@pytest.mark.parametrize("rows", [[1] * 32, [1] * 28 + [4]])
+def test_few_rows_in_all_of_more_experts_than_the_cache_holds(rows):
+    d, f = 4096, 1536
+    E = len(rows)
+    assert E > fits_the_cache(d, f) and sum(rows) <= 32
+    raw, q = weights(E, d, f, 9)
+    x = tokens(sum(rows), d, 10)
+    o = forward(x, rows, q)
+    assert torch.equal(forward(x, rows, q, cap=200), o)
+    check(o, x, rows, raw, [0, E - 1])
