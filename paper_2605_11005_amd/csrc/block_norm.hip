@@ -7,7 +7,7 @@
 //     dw_pre = sum_t dn h' r_pre                                       dw_post = sum_t du y r_post
 // HBM bound.  A row stays in the registers of its threads from the load to the store, 16 bytes of y (bf16: eight elements, fp32:
 // four) per thread and step, so that every tensor crosses memory once; sums are fp32.  Measured, of 6.5 TB/s that a copy reaches: forward of
-// 32768 rows of 7168 (y, n bf16, h fp32) 490 us, 5.8 TB/s; backward of 16384 rows of 4096 (h fp32) 220 us, 5.5 TB/s, of 32768 rows of 7168 bf16 517 us,
+// 32768 rows of 7168 (y, n bf16, h fp32) 495 us, 5.7 TB/s; backward of 16384 rows of 4096 (h fp32) 229 us, 5.3 TB/s, of 32768 rows of 7168 bf16 523 us,
 // 5.4 TB/s; the forward of four rows takes 1 us over an empty launch.  Hints that data are not used again cost the forward a tenth.
 #include "common.h"
 #include "kernels.h"
@@ -208,7 +208,8 @@ struct BwdRow {
 
 // Blocks (or, for rows of one wavefront, wavefronts) walk the rows and keep the column sums of theirs in registers.  The next row's loads
 // are on their way while a row's sums meet; for WIDE rows the registers hold neither these nor the weights, and the column sums are in LDS:
-// 4096 rows of 16384 bf16 take 168 us (4.8 TB/s), fp32 342 (4.7 TB/s); with the sums in registers, of which 30 to 100 spilled, 240 and 514.
+// 4096 rows of 16384 bf16 take 168 to 177 us (4.6 TB/s), fp32, which spills 20 registers, 342 to 352 (4.6 TB/s); with the sums in registers, of which
+// 30 to 100 spilled, 240 and 514.
 constexpr int BWD_ROWS = 8, BWD_THREADS = 512, WIDE_THREADS = 1024;
 template <typename T, typename R, int STEPS, bool WIDE>
 __global__ __launch_bounds__(WIDE ? WIDE_THREADS : BWD_THREADS) void block_norm_bwd(BwdArgs<T, R> p) {
@@ -404,7 +405,8 @@ int forward(FwdArgs<T, R> p, hipStream_t s) {
 
 // The backward's launch.  A thread with one step of bf16 takes 124 registers, with 16 elements up to 252: one block of the latter fits on a
 // CU, of the former two.  A row of 1024 elements in one wavefront has no barrier (16384 rows of bf16: 48 us
-// against 80 us as blocks of two wavefronts); few rows go to more blocks, not to more wavefronts of a block.
+// against 80 us as blocks of two wavefronts); few rows go to more blocks, not to more wavefronts of a block.  Of blocks of up to 256 threads four fit,
+// and from 8192 rows on they are worth twice the column sums: 8192 rows of 1408 bf16 37.5 us, 46.8 with two, 65536 of 2048 320 and 358.
 struct BwdPlan { int steps, threads, rows, most, blocks; bool wide; };
 inline BwdPlan bwd_plan(int T, int d, int vec) {
   constexpr int CUS = 256;

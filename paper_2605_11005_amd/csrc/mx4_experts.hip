@@ -39,7 +39,8 @@ __device__ __forceinline__ f32x4 mfma(u32x4 a, u32x4 b, f32x4 c, uint32_t sa, ui
   return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, y, c, 4, 4, SA, (int)sa, SB, (int)sb);      // 4: e2m1
 }
 
-// ---- rows: a wavefront per 16 rows by 512 elements; a block finds its tile's expert by itself.  HBM bound: 16249 rows of 7168 52 us, 5.7 TB/s.
+// ---- rows: a wavefront per 16 rows by 512 elements; a block finds its tile's expert by itself.  HBM bound: 16249 rows of 7168 56 us, 5.2 TB/s;
+// a capacity of 131072 rows for them costs 8 us more, in blocks that find no tile.
 constexpr int ROWS_BLOCK = 256;
 __global__ __launch_bounds__(ROWS_BLOCK) void expert_rows(const bf16_t* __restrict__ x, const int32_t* __restrict__ off, int e_cnt, int d, int f,
                                                            uint8_t* __restrict__ q, uint8_t* __restrict__ scales, uint8_t* __restrict__ aq,
@@ -77,8 +78,8 @@ __global__ __launch_bounds__(ROWS_BLOCK) void expert_rows(const bf16_t* __restri
 // multiplied.  2^cut wavefronts share a tile's contraction.  That number follows the tiles of all experts; a row's results must not, so that its sum
 // is eight sums added in one order whatever the number.  DIRECT: rows come as bf16, a lane's 32 elements being a chunk, and become its operand in
 // registers, 16 rows a tile.
-// Bound by memory: a row or two each of 85 experts (4096 to 1536) read 6.1 TB/s of weights, 14 experts (7168 to 2048) with 208 rows 5.5.  Tiles of up to
-// 64 rows of this kind took 8 % longer at 31 experts with 63 rows on average than the larger tiles below.
+// Bound by memory: the forward of a row each of 85 experts (4096 to 1536) reads 5.4 TB/s of weights, UP of 14 experts (7168 to 2048) with 208 rows 5.3.
+// Tiles of up to 64 rows of this kind took 8 % longer at 31 experts with 63 rows on average than the larger tiles below.
 constexpr int FEW_MOST = 32, FEW_ROWS = 32, FEW_COLS = 32, FEW_WAVES = 8;
 // The pieces of a contraction belong to eight sums, piece q of `pieces` to sum 8 q / pieces.  A row's result is ((s0 + s1) + s2) + .., each sum its
 // pieces in ascending order from zero.  Of 2^cut wavefronts the w-th takes the pieces from w pieces / 2^cut on, which are whole sums: as many
@@ -366,16 +367,18 @@ struct SomeTiles {
 // directly, 128 of the contraction at a time, through a ring of four stages of which three are on their way.  Their layout in memory is
 // the one that the instruction wants, so every load is 1 KB of consecutive bytes and every LDS read free of conflicts.  Workgroups are
 // persistent, and the loads run ahead into the next tile while a finished one is written.
-// Eight experts (4096 to 14336) of 1024 rows: 455 us up and 215 us down, 4.3 PFLOP/s, bound by the package's power: the matrix unit is busy half of
-// the cycles at 1.9 GHz, and operands of zeros take 0.73 of the time.  Four stages are one turn of the loop, for the bytes of the scales' words to be
-// chosen by the instruction (455 us; 465 with a byte read at every stage, 503 with shifted words).  A tile of up to 64 rows is a stream of weights, 0.7 us a stage.
+// Eight experts (4096 to 14336) of 1024 rows: 455 us up and 215 us down, a call 680 us, 4.2 PFLOP/s (a loop of these products on operands from LDS
+// reaches 5.7, from registers 6.5), bound by the package's power: the matrix unit is busy half of the cycles at 1.9 GHz, and operands of zeros take
+// 0.73 of the time.  Four stages are one turn of the loop, for the bytes of the scales' words to be chosen by the instruction (455 us; 465 with a
+// byte read at every stage, 503 with shifted words).  A tile of up to 64 rows is a stream of weights, 0.7 us a stage.
 constexpr int GEMM_GROUP = 4, GEMM_ROWS = 256, GEMM_COLS = 256, GEMM_THREADS = 512;
 constexpr int STAGE = 32 * MX_TILE, STAGES = 4, SCALES = 32 * MX_SCALES;       // operand tiles of a stage: 16 of the rows, 16 of the weights
 constexpr int PLACES = 3;                  // for scales (see Loads)
 constexpr int GEMM_LDS = STAGES * STAGE + PLACES * SCALES;
 constexpr int UP_LDS = GEMM_LDS > few_lds(4, 2) ? GEMM_LDS : few_lds(4, 2), DOWN_LDS = GEMM_LDS > few_lds(2, 2) ? GEMM_LDS : few_lds(2, 2), DIRECT_LDS = few_lds(4, 1);
 static_assert(UP_LDS <= 160 * 1024 && DOWN_LDS <= 160 * 1024);
-constexpr int LEAST_DEPTHS = 4;            // (see Loads)
+// (see Loads)  A contraction of up to 384 has fewer, and is a stream whatever the rows: 32 experts (384 to 384) of 2048 rows 162 us, of 416 to 416 77 us.
+constexpr int LEAST_DEPTHS = 4;
 __device__ __forceinline__ uint32_t next_place(uint32_t scales) { return scales == (PLACES - 1) * SCALES ? 0 : scales + SCALES; }
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
@@ -481,7 +484,8 @@ struct Loads {
     static_for<PARTS>([&](auto i) { part<decltype(i)::value>(); });
   }
   // The next stage in order has arrived for all wavefronts, and all have done with the one that is to be loaded again.  The two stages behind it
-  // are on their way.  (Scales or stores of a finished tile among what is on its way make the wait longer, never shorter.)
+  // are on their way.  (Scales, and at a tile's first stages the stores of the one before, are among what is on its way: they make the wait longer,
+  // never shorter.)
   __device__ __forceinline__ void wait() { wait_and_meet<2 * PARTS>(); }
 };
 
@@ -675,7 +679,8 @@ __global__ __launch_bounds__(GEMM_THREADS, 1) void experts_mx4(XArgs p) {
   // Weights that are read once and that the Infinity Cache does not keep for the next call: 21 experts (7168 to 1536) of 64 rows read 5.5 TB/s with
   // the hint, 4.7 without, of 256 rows 3.7 and 3.4.  Eight experts of 1024 rows take 3 % longer with it, and what fits the cache 6 %.
   const bool once = many.experts + few.experts > p.cached && many.total < 2 * many.experts;
-  // DOWN: half as many columns where that still leaves a workgroup to every tile, those of few rows with them.  Eight experts (2880 to 2880) of
+  // DOWN: half as many columns where that still leaves a workgroup to every tile, those of few rows with them (two halves are counted for a whole
+  // one, also where the last columns have but one).  Eight experts (2880 to 2880) of
   // 200 rows: 16.5 us, 21.5 with whole ones.
   const bool half = MODE == DOWN && 2 * many.total * ((p.N + GEMM_COLS - 1) / GEMM_COLS) + few.total * ((p.N / FEW_COLS + FEW_WAVES - 1) / FEW_WAVES) <= (int)gridDim.x;
   if (half) many_tiles<MODE, MODE == DOWN ? 1 : 2, false>(p, many, gemm_lds, lane, wave);
@@ -689,9 +694,9 @@ __global__ __launch_bounds__(GEMM_THREADS, 1) void experts_mx4(XArgs p) {
   else few_tiles<MODE, false>(p, few, reinterpret_cast<f32x4*>(gemm_lds), place, idle, many.total);
 }
 
-// UP of at most FEW_MOST rows in all, from bf16: a launch less.  The whole forward (4096 to 1536) of a row of one expert takes 14.8 us, 18.7 with
-// expert_rows; of a row each of eight experts 26 and 30, of 32 experts 63 and 66.  An expert with 17 to 32 rows reads its weights twice: alone
-// (4096 to 14336) 44 us, 41 with expert_rows.
+// UP of at most FEW_MOST rows in all, from bf16: a launch less.  The whole forward (4096 to 1536) of a row of one expert takes 13.3 us, 17.1 with
+// expert_rows; of a row each of eight experts 22.6 and 26.4, of 32 experts 61 and 66.  An expert with 17 to 32 rows reads its weights twice: 20 rows
+// of one alone (4096 to 14336) 37 us, 32 with expert_rows.
 __global__ __launch_bounds__(GEMM_THREADS, 1) void up_direct(XArgs p) {
   extern __shared__ uint8_t gemm_lds[];
   const int lane = threadIdx.x & 63;

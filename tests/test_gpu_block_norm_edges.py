@@ -1,4 +1,4 @@
-"""The block norms where sizes and values are at their edges: NaN in the sums over rows, rows beyond one launch's, blocks four to a CU.
+"""The block norms where sizes and values are at their edges: NaN in the sums over rows, rows beyond one launch's, four blocks on a CU.
 
 Bounds, set before the first run.  Column sums: a block adds at most T/256 + 1 rows one after the other, and at most 1024/16 + 16 blocks' sums follow;
 each product is a chain of some twenty fp32 operations with 1/rms factors of trees over d: (T/256 + 200) * 2^-24 * sum |terms|."""
@@ -67,7 +67,7 @@ def test_more_rows_than_a_launch_holds():
         assert ((n[lo:lo + part].float() - ref).abs() <= 2.0 ** -8 * 1.01 * ref.abs() + 1e-30).all(), lo
 
 
-@pytest.mark.parametrize("T,d,dt,rt", [(8200, 1408, BF16, BF16), (8193, 2048, BF16, F32), (8300, 520, F32, F32), (8192, 1032, BF16, F32)])
+@pytest.mark.parametrize("T,d,dt,rt", [(8200, 1408, BF16, BF16), (8193, 2048, BF16, F32), (8200, 1544, BF16, F32), (8192, 1032, BF16, F32)])
 def test_four_blocks_on_a_cu(T, d, dt, rt):
     print(f"case norm {T} {d} {dt} {rt}", flush=True)
     g = torch.Generator().manual_seed(d)
