@@ -316,7 +316,7 @@ __global__ __launch_bounds__(WIDE ? WIDE_THREADS : BWD_THREADS) void block_norm_
     if (p.post_norm || p.dgate) {
       const float total = row_total(sum);
       if (p.dgate && threadIdx.x == 0) p.dgate[row] = p.beta * r * total;
-      if (p.post_norm) m = scale * r * r * total * inv_d;
+      if (p.post_norm) m = total * inv_d * r * r * scale;          // (from the sum on: r^3 of a row of zeros may pass fp32)
     }
 #pragma unroll
     for (int i = 0; i < STEPS; ++i) {

@@ -48,6 +48,28 @@ def test_sums_over_rows_keep_nan_and_infinities(bits, accumulate):
         assert np.array_equal(got[inf], want[inf]) and np.isfinite(got[np.isfinite(want)]).all(), name
 
 
+@pytest.mark.parametrize("dt,rt", [(BF16, BF16), (BF16, F32), (F32, F32)])
+def test_rows_of_zeros_with_a_small_eps(dt, rt):
+    """1/rms is 1e15 there, and its cube no number of fp32: what it multiplies is zero."""
+    T, d, eps = 5, 136, 1e-30
+    g = torch.Generator().manual_seed(4)
+    r = lambda *s, dtype=dt: torch.randn(s, generator=g).to(dtype).cuda()  # noqa: E731
+    y, h, w_post, w_pre, dn, dh_out = r(T, d), r(T, d, dtype=rt), r(d), r(d), r(T, d), r(T, d, dtype=rt)
+    y[1] = 0
+    y[3], h[3] = 0, 0
+    h_out, n, dh, dy = torch.empty_like(h), torch.empty_like(y), torch.empty_like(h), torch.empty_like(y)
+    r_post, r_pre, dgate = (torch.empty(T, device="cuda") for _ in range(3))
+    dw_post, dw_pre = torch.empty_like(w_post), torch.empty_like(w_pre)
+    B.moe_block_norm_fwd(y, None, w_post, True, h, w_pre, 0.5, 1.5, eps, h_out, n, r_post, r_pre)
+    B.moe_block_norm_bwd(y, None, w_post, True, h_out, w_pre, r_post, r_pre, dh_out, dn, 0.5, 1.5, dh, dy, dgate, dw_post, dw_pre, False, workspace(T, d))
+    ref, mag = N.bwd(host(y), None, host(w_post), True, host(h_out), host(w_pre), host(r_post), host(r_pre), host(dh_out), host(dn), 0.5, 1.5)
+    half = {BF16: 2.0 ** -8, F32: 2.0 ** -24}
+    for name, got in (("dh", dh), ("dy", dy), ("dgate", dgate), ("dw_post", dw_post), ("dw_pre", dw_pre)):
+        assert torch.isfinite(got).all(), name
+        over = np.abs(host(got) - ref[name]) - (half[got.dtype] * np.abs(ref[name]) * (1 + 2.0 ** -7) + 200 * 2.0 ** -24 * mag[name])
+        assert (over <= 0).all(), (name, float(over.max()))
+
+
 def test_more_rows_than_a_launch_holds():
     """2^28 rows of one wavefront each are 2^32 work-items."""
     T, d, part = (1 << 28) + 5, 8, 1 << 24
