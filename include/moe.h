@@ -41,13 +41,15 @@ enum { MOE_OK = 0, MOE_EINVAL = 1, MOE_EUNSUPPORTED = 2, MOE_EWORKSPACE = 3, MOE
 enum { MOE_F32 = 0, MOE_BF16 = 1 };
 enum { MOE_GATE_SOFTMAX_RENORM = 0, MOE_GATE_SIGMOID_RENORM = 1, MOE_GATE_SOFTMAX = 2 };
 enum { MOE_WS_DISPATCH = 0, MOE_WS_EXPERT_FWD = 1, MOE_WS_EXPERT_BWD = 2, MOE_WS_ROUTER = 3,
-       MOE_WS_BLOCK_NORM = 4, MOE_WS_MX4_EXPERT_FWD = 5 };
+       MOE_WS_BLOCK_NORM = 4, MOE_WS_MX4_EXPERT_FWD = 5, MOE_WS_LAYER_NORM = 6, MOE_WS_LINEAR_FWD = 7, MOE_WS_LINEAR_BWD = 8 };
+enum { MOE_ACT_NONE = 0, MOE_ACT_RELU = 1, MOE_ACT_GELU = 2, MOE_ACT_GELU_TANH = 3, MOE_ACT_SILU = 4 };
 
 /* Limits checked by the entry points (MOE_EUNSUPPORTED beyond them). */
 #define MOE_MAX_EXPERTS 1024 /* E */
 #define MOE_MAX_LOCAL 1024   /* e_cnt */
 #define MOE_MAX_TOPK 64      /* k */
-#define MOE_MAX_NORM_D 16384 /* d of moe_block_norm_fwd and _bwd */
+#define MOE_MAX_NORM_D 16384 /* d of moe_block_norm_fwd and _bwd and of moe_layer_norm_fwd and _bwd */
+#define MOE_MAX_LINEAR (1 << 20) /* K and N of moe_linear_fwd and _bwd */
 
 /*
  * moe_route -- top-k gating (MoE background section: a gate network selects the top-k
@@ -301,6 +303,66 @@ int moe_block_norm_bwd(const void* y, const float* gate, const void* w_post, int
                        int accumulate, void* ws, size_t ws_bytes, moe_stream_t stream);
 
 /*
+ * Layer norm between two blocks, for models whose norms take the mean off and have a bias:
+ *     h' = h + y        n = (h' - mean) * rstd * w + b        mean[t] = mean_c h'[t,c]        rstd[t] = (mean_c (h'[t,c] - mean[t])^2 + eps)^-1/2
+ *
+ * moe_layer_norm_fwd
+ *   y      [T,d] dtype      the block's output; NULL: there is none yet, h' = h
+ *   h      [T,d] res_dtype  the residual stream; res_dtype is dtype or MOE_F32
+ *   w, b   [d] dtype        NULL: 1 and 0
+ *   h_out  [T,d] res_dtype  out: h', may be h itself; NULL: not stored.  NULL where y is.
+ *   n      [T,d] dtype      out, may be y itself
+ *   mean, rstd [T] float    out, what the backward needs; NULL: not stored
+ * Sums are fp32, the squares are taken after the mean.  n is formed from h' before its rounding to res_dtype: it is rounded once.
+ *
+ * moe_layer_norm_bwd -- the gradient, at the saved h' (h_out; h where y is NULL), mean and rstd, with t = w dn and xh = (h' - mean) rstd:
+ *     dh = dh_out + rstd (t - mean_c(t) - xh mean_c(t xh))        dy = dh        dw (+)= sum_t dn xh        db (+)= sum_t dn
+ *   dh_out [T,d] res_dtype  gradient of h' from further on; NULL: none.  dn [T,d] dtype
+ *   dh [T,d] res_dtype out, may be dh_out itself; dy [T,d] dtype out, the same in the type of y, may be dn itself; dw, db [d] dtype out, added to
+ *   their contents with accumulate == 1.  Each may be NULL: not formed.
+ *   ws: moe_workspace_bytes(MOE_WS_LAYER_NORM, dtype, T, 0, d, 0, 0, 0) bytes, 256-byte aligned.
+ * The column sums are fp32, formed over rows that T, d and dtype decide and added in a fixed order: results are bit-reproducible.
+ * Errors of both: EINVAL (NULL, negative sizes, unknown types, res_dtype neither dtype nor MOE_F32, eps not a positive number, h_out without y),
+ * EUNSUPPORTED (bf16 with d % 8 != 0, fp32 with d % 4 != 0, d > MOE_MAX_NORM_D, T > 2^31 - 2^16), EWORKSPACE.
+ */
+int moe_layer_norm_fwd(const void* y, const void* h, const void* w, const void* b, int dtype, int res_dtype, int T, int d, float eps, void* h_out,
+                       void* n, float* mean, float* rstd, moe_stream_t stream);
+int moe_layer_norm_bwd(const void* h_out, const void* w, const float* mean, const float* rstd, const void* dh_out, const void* dn, int dtype,
+                       int res_dtype, int T, int d, void* dh, void* dy, void* dw, void* db, int accumulate, void* ws, size_t ws_bytes,
+                       moe_stream_t stream);
+
+/*
+ * A linear layer with everything around its product: matrices of experts over expert-contiguous rows, or one matrix over all rows.
+ * For each expert e and its rows [offsets[e], offsets[e+1]):
+ *     z = x W[e] + bias[e]        y = act(z) + residual
+ * act is MOE_ACT_NONE, RELU (max(z, 0)), GELU (z times the normal distribution's integral at z), GELU_TANH (z (1 + tanh(sqrt(2/pi) (z + 0.044715
+ * z^3))) / 2) or SILU (z / (1 + exp(-z))).
+ *
+ * moe_linear_fwd
+ *   x [cap,K]; w [e_cnt,K,N]; bias [e_cnt,N], NULL: none; residual [cap,N], NULL: none
+ *   offsets [e_cnt+1] int32 as moe_dispatch writes them.  NULL, with e_cnt == 1: one matrix, all cap rows.
+ *   z [cap,N] out, what the backward needs where act is not MOE_ACT_NONE; NULL: not stored
+ *   y [cap,N] out, may be residual itself.  Rows past the last expert's of y and z are left untouched.
+ *   ws: moe_workspace_bytes(MOE_WS_LINEAR_FWD, dtype, 0, 0, K, N, e_cnt, cap) bytes, 256-byte aligned
+ * Sums, bias, activation and residual are fp32; z and y are rounded once each (y from the unrounded z).
+ *
+ * moe_linear_bwd -- the gradient, at the saved x and z:
+ *     dz = dy act'(z)        dx = dz W[e]^T        dw[e] (+)= sum_rows x^T dz        db[e] (+)= sum_rows dz        (residual's is dy)
+ *   z NULL where act is MOE_ACT_NONE.  dx [cap,K] out (rows past the last expert's left untouched), dw [e_cnt,K,N], db [e_cnt,N] out; each may be
+ *   NULL: not formed.  accumulate == 1 adds to dw and db; with 0 an expert without rows gets zeros.
+ *   ws: moe_workspace_bytes(MOE_WS_LINEAR_BWD, dtype, 0, 0, K, N, e_cnt, cap) bytes, 256-byte aligned
+ * All sums are fp32.  In bf16 the products take dz rounded to bf16; db sums it unrounded.  relu's slope at 0 is 0.
+ * Results are bit-reproducible from run to run.  fp32 products are those of moe_expert_fwd and _bwd.
+ * Errors of both: EINVAL (NULL, negative sizes, unknown dtype or act, offsets NULL with e_cnt != 1, pointers not 16-byte aligned), EUNSUPPORTED (bf16
+ * with K % 8 != 0 or N % 8 != 0, fp32 with % 4, K or N > MOE_MAX_LINEAR, e_cnt > MOE_MAX_LOCAL, 2^23 tiles of 64 x 64 or more in y, x or the
+ * matrices), EWORKSPACE.
+ */
+int moe_linear_fwd(const void* x, int dtype, int cap, int K, int N, int e_cnt, const int32_t* offsets, const void* w, const void* bias, int act,
+                   const void* residual, void* z, void* y, void* ws, size_t ws_bytes, moe_stream_t stream);
+int moe_linear_bwd(const void* x, const void* z, const void* dy, int dtype, int cap, int K, int N, int e_cnt, const int32_t* offsets, const void* w,
+                   int act, void* dx, void* dw, void* db, int accumulate, void* ws, size_t ws_bytes, moe_stream_t stream);
+
+/*
  * Microscaled 4-bit numbers (the OCP MX format of e2m1 elements with one e8m0 scale per 32): an element is 0, 1/2, 1, 3/2, 2, 3, 4, 6 or the
  * negative of one, times a power of two that 32 elements along the contraction share.
  *
@@ -372,7 +434,11 @@ enum { MOE_K_ROUTE = 0,
        MOE_K_NORM_FWD = 18, MOE_K_NORM_BWD = 19, MOE_K_NORM_SUMS = 20,      /* column sums of dw_post, dw_pre */
        MOE_K_MX4_QUANTIZE = 21, MOE_K_MX4_DEQUANTIZE = 22,
        MOE_K_MX4_ROWS = 23, MOE_K_MX4_UP = 24, MOE_K_MX4_DOWN = 25,
-       MOE_K_COUNT = 26 };
+       MOE_K_LAYER_NORM_FWD = 26, MOE_K_LAYER_NORM_BWD = 27, MOE_K_LAYER_NORM_SUMS = 28,
+       MOE_K_LINEAR = 29, MOE_K_LINEAR_ACT = 30,      /* dz and the column sums of its row tiles */
+       MOE_K_LINEAR_BIAS = 31, MOE_K_LINEAR_DX = 32, MOE_K_LINEAR_DW = 33,
+       MOE_K_LINEAR_DX_DW = 34,                       /* both in one launch */
+       MOE_K_COUNT = 35 };
 #define MOE_PROFILE_MAX_EVENTS 8192
 int moe_profile_enable(int on);
 int moe_profile_read(int kernel, double* total_ms /* host */, int* launches /* host */);

@@ -21,6 +21,9 @@ import warnings
 MOE_F32, MOE_BF16 = 0, 1
 GATE_SOFTMAX_RENORM, GATE_SIGMOID_RENORM, GATE_SOFTMAX = 0, 1, 2
 WS_DISPATCH, WS_EXPERT_FWD, WS_EXPERT_BWD, WS_ROUTER, WS_BLOCK_NORM, WS_MX4_EXPERT_FWD = 0, 1, 2, 3, 4, 5
+WS_LAYER_NORM, WS_LINEAR_FWD, WS_LINEAR_BWD = 6, 7, 8
+ACT_NONE, ACT_RELU, ACT_GELU, ACT_GELU_TANH, ACT_SILU = 0, 1, 2, 3, 4
+ACTIVATIONS = dict(none=ACT_NONE, relu=ACT_RELU, gelu=ACT_GELU, gelu_tanh=ACT_GELU_TANH, silu=ACT_SILU)
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB = None
@@ -28,14 +31,15 @@ _MARSHAL = None
 
 EXPORTS = ("moe_route", "moe_dispatch", "moe_dispatch_static", "moe_expert_fwd", "moe_expert_bwd", "moe_combine",
            "moe_router_fwd", "moe_combine_bwd", "moe_gate_bwd", "moe_router_bwd",
-           "moe_block_norm_fwd", "moe_block_norm_bwd", "moe_mx4_quantize", "moe_mx4_dequantize", "moe_mx4_expert_fwd",
+           "moe_block_norm_fwd", "moe_block_norm_bwd", "moe_layer_norm_fwd", "moe_layer_norm_bwd", "moe_linear_fwd", "moe_linear_bwd",
+           "moe_mx4_quantize", "moe_mx4_dequantize", "moe_mx4_expert_fwd",
            "moe_profile_enable", "moe_profile_read", "moe_profile_stats", "moe_probe_mfma_bf16", "moe_probe_mfma_fed_bf16",
            "moe_probe_copy", "moe_probe_stream",
            "moe_workspace_bytes", "moe_error_string")
 # what csrc/marshal.cpp calls, in its order
 _MARSHALLED = ("moe_route", "moe_dispatch", "moe_dispatch_static", "moe_expert_fwd", "moe_expert_bwd", "moe_combine", "moe_router_fwd",
                "moe_combine_bwd", "moe_gate_bwd", "moe_router_bwd", "moe_block_norm_fwd", "moe_block_norm_bwd", "moe_mx4_quantize",
-               "moe_mx4_dequantize", "moe_mx4_expert_fwd")
+               "moe_mx4_dequantize", "moe_mx4_expert_fwd", "moe_layer_norm_fwd", "moe_layer_norm_bwd", "moe_linear_fwd", "moe_linear_bwd")
 
 
 class MoeError(RuntimeError):
@@ -97,6 +101,14 @@ def load_library():
     lib.moe_mx4_dequantize.argtypes = [c_void_p, c_void_p, c_int, c_int, c_int, c_void_p, c_int, c_void_p]
     lib.moe_mx4_expert_fwd.restype = c_int
     lib.moe_mx4_expert_fwd.argtypes = [c_void_p, c_int, c_int, c_int, c_int, c_int] + [c_void_p] * 9 + [c_size_t, c_void_p]
+    lib.moe_layer_norm_fwd.restype = c_int
+    lib.moe_layer_norm_fwd.argtypes = [c_void_p] * 4 + [c_int] * 4 + [c_float] + [c_void_p] * 5
+    lib.moe_layer_norm_bwd.restype = c_int
+    lib.moe_layer_norm_bwd.argtypes = [c_void_p] * 6 + [c_int] * 4 + [c_void_p] * 4 + [c_int, c_void_p, c_size_t, c_void_p]
+    lib.moe_linear_fwd.restype = c_int
+    lib.moe_linear_fwd.argtypes = [c_void_p] + [c_int] * 5 + [c_void_p] * 3 + [c_int] + [c_void_p] * 4 + [c_size_t, c_void_p]
+    lib.moe_linear_bwd.restype = c_int
+    lib.moe_linear_bwd.argtypes = [c_void_p] * 3 + [c_int] * 5 + [c_void_p] * 2 + [c_int] + [c_void_p] * 3 + [c_int, c_void_p, c_size_t, c_void_p]
     lib.moe_workspace_bytes.restype = c_size_t
     lib.moe_workspace_bytes.argtypes = [c_int] * 8
     lib.moe_error_string.restype = ctypes.c_char_p
@@ -376,6 +388,71 @@ def moe_block_norm_bwd(y, gate, w_post, post_norm, h_out, w_pre, r_post, r_pre, 
                                              ws.numel() * ws.element_size(), _stream()), "moe_block_norm_bwd")
 
 
+def moe_layer_norm_fwd(y, h, w, b, eps, h_out, n, mean=None, rstd=None):
+    """h [T,d], n [T,d]; y [T,d] or None (nothing is added), and then h_out None."""
+    rc = _marshal().layer_norm_fwd(y, h, w, b, eps, h_out, n, mean, rstd)
+    if rc >= 0:
+        return _check(rc, "moe_layer_norm_fwd")
+    import torch
+    (T, d), dt = h.shape, n.dtype
+    _need(h, name="h"); _need(y, dt, (T, d), "y"); _need(w, dt, (d,), "w"); _need(b, dt, (d,), "b")
+    _need(h_out, h.dtype, (T, d), "h_out"); _need(n, dt, (T, d), "n")
+    _need(mean, torch.float32, (T,), "mean"); _need(rstd, torch.float32, (T,), "rstd")
+    _check(load_library().moe_layer_norm_fwd(_ptr(y), _ptr(h), _ptr(w), _ptr(b), _dtype_code(n), _dtype_code(h), T, d, eps, _ptr(h_out), _ptr(n),
+                                             _ptr(mean), _ptr(rstd), _stream()), "moe_layer_norm_fwd")
+
+
+def moe_layer_norm_bwd(h_out, w, mean, rstd, dh_out, dn, dh, dy, dw, db, accumulate, ws):
+    """h_out is the saved sum of the forward (h itself where y was None); dh_out None: no gradient from further on.  Outputs may be None."""
+    rc = _marshal().layer_norm_bwd(h_out, w, mean, rstd, dh_out, dn, dh, dy, dw, db, accumulate, ws)
+    if rc >= 0:
+        return _check(rc, "moe_layer_norm_bwd")
+    import torch
+    (T, d), dt, rt = h_out.shape, dn.dtype, h_out.dtype
+    _need(h_out, name="h_out"); _need(w, dt, (d,), "w"); _need(mean, torch.float32, (T,), "mean"); _need(rstd, torch.float32, (T,), "rstd")
+    _need(dh_out, rt, (T, d), "dh_out"); _need(dn, dt, (T, d), "dn"); _need(dh, rt, (T, d), "dh"); _need(dy, dt, (T, d), "dy")
+    _need(dw, dt, (d,), "dw"); _need(db, dt, (d,), "db"); _need(ws, name="ws")
+    _check(load_library().moe_layer_norm_bwd(_ptr(h_out), _ptr(w), _ptr(mean), _ptr(rstd), _ptr(dh_out), _ptr(dn), _dtype_code(dn), _dtype_code(h_out),
+                                             T, d, _ptr(dh), _ptr(dy), _ptr(dw), _ptr(db), int(accumulate), _ptr(ws),
+                                             ws.numel() * ws.element_size(), _stream()), "moe_layer_norm_bwd")
+
+
+def _linear_shapes(rows, weights, offsets):
+    """(cap, K, N, e_cnt, batch of a weight) of rows [cap,K] and weights [K,N] without offsets, [e_cnt,K,N] with them."""
+    if rows.dim() != 2 or weights.dim() != (2 if offsets is None else 3):
+        raise MoeError("rows must be a matrix, and weights a matrix without offsets, matrices with them")
+    return rows.shape[0], *weights.shape[-2:], 1 if offsets is None else weights.shape[0], tuple(weights.shape[:-2])
+
+
+def moe_linear_fwd(x, offsets, w, bias, act, residual, z, y, ws):
+    """x [cap,K]; offsets None: w [K,N], bias [N]; else w [e_cnt,K,N], bias [e_cnt,N].  act: ACT_*; bias, residual and z may be None."""
+    rc = _marshal().linear_fwd(x, offsets, w, bias, act, residual, z, y, ws)
+    if rc >= 0:
+        return _check(rc, "moe_linear_fwd")
+    import torch
+    cap, K, N, e_cnt, batch = _linear_shapes(x, w, offsets)
+    dt = x.dtype
+    _need(x, dt, (cap, K), "x"); _need(w, dt, name="w"); _need(bias, dt, batch + (N,), "bias"); _need(offsets, torch.int32, (e_cnt + 1,), "offsets")
+    _need(residual, dt, (cap, N), "residual"); _need(z, dt, (cap, N), "z"); _need(y, dt, (cap, N), "y"); _need(ws, name="ws")
+    _check(load_library().moe_linear_fwd(_ptr(x), _dtype_code(x), cap, K, N, e_cnt, _ptr(offsets), _ptr(w), _ptr(bias), int(act), _ptr(residual),
+                                         _ptr(z), _ptr(y), _ptr(ws), ws.numel() * ws.element_size(), _stream()), "moe_linear_fwd")
+
+
+def moe_linear_bwd(x, z, dy, offsets, w, act, dx, dw, db, accumulate, ws):
+    """Shapes as in moe_linear_fwd; z None where act is ACT_NONE; outputs may be None.  The gradient of a residual is dy."""
+    rc = _marshal().linear_bwd(x, z, dy, offsets, w, act, dx, dw, db, accumulate, ws)
+    if rc >= 0:
+        return _check(rc, "moe_linear_bwd")
+    import torch
+    cap, K, N, e_cnt, batch = _linear_shapes(x, w, offsets)
+    dt = x.dtype
+    _need(x, dt, (cap, K), "x"); _need(w, dt, name="w"); _need(offsets, torch.int32, (e_cnt + 1,), "offsets")
+    _need(z, dt, (cap, N), "z"); _need(dy, dt, (cap, N), "dy"); _need(dx, dt, (cap, K), "dx"); _need(dw, dt, batch + (K, N), "dw")
+    _need(db, dt, batch + (N,), "db"); _need(ws, name="ws")
+    _check(load_library().moe_linear_bwd(_ptr(x), _ptr(z), _ptr(dy), _dtype_code(x), cap, K, N, e_cnt, _ptr(offsets), _ptr(w), int(act), _ptr(dx),
+                                         _ptr(dw), _ptr(db), int(accumulate), _ptr(ws), ws.numel() * ws.element_size(), _stream()), "moe_linear_bwd")
+
+
 def mx4_shapes(n, K):
     """Shapes (data, scales) of n rows of K elements in microscaled 4 bits, both uint8 (layout: moe.h)."""
     return ((n + 15) // 16, (K + 127) // 128, 4, 16, 16), ((n + 15) // 16, (K + 511) // 512, 4, 16, 4)
@@ -435,7 +512,9 @@ def moe_mx4_expert_fwd(xp, offsets, w1, s1, w3, s3, w2, s2, o, ws):
 
 KERNEL_IDS = dict(route=0, plan=1, dispatch=2, combine=3, up=4, down=5, da=6, dx=7, wg=8, wgd=9, router_fwd=10,
                   combine_bwd=11, gate_bwd=12, router_dw=13, router_dx=14, wgrad_reduce=15, da_wg=16, dx_wgd=17, norm_fwd=18,
-                  norm_bwd=19, norm_sums=20, mx4_quantize=21, mx4_dequantize=22, mx4_rows=23, mx4_up=24, mx4_down=25)
+                  norm_bwd=19, norm_sums=20, mx4_quantize=21, mx4_dequantize=22, mx4_rows=23, mx4_up=24, mx4_down=25,
+                  layer_norm_fwd=26, layer_norm_bwd=27, layer_norm_sums=28, linear=29, linear_act=30, linear_bias=31, linear_dx=32,
+                  linear_dw=33, linear_dx_dw=34)
 
 
 def moe_profile_enable(on: bool):

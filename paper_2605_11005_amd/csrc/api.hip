@@ -172,6 +172,12 @@ size_t moe_workspace_bytes(int which, int dtype, int T, int k, int d, int f, int
       return d <= 0 ? 256 : align256(block_norm_ws_bytes(T, d)) + 256;
     case MOE_WS_MX4_EXPERT_FWD:
       return d <= 0 ? 256 : mx4_expert_ws_bytes(cap, d, f, e_cnt);
+    case MOE_WS_LAYER_NORM:
+      return d <= 0 ? 256 : align256(layer_norm_ws_bytes(T, d)) + 256;
+    case MOE_WS_LINEAR_FWD:   // d inputs, f outputs
+      return d <= 0 || f <= 0 ? 256 : align256(linear_fwd_ws_bytes(dtype, cap, d, f, e_cnt));
+    case MOE_WS_LINEAR_BWD:
+      return d <= 0 || f <= 0 ? 256 : align256(linear_bwd_ws_bytes(dtype, cap, d, f, e_cnt));
     default: return 256;
   }
 }
@@ -393,6 +399,69 @@ int moe_block_norm_bwd(const void* y, const float* gate, const void* w_post, int
   if (!ws || misaligned(ws, 256) || ws_bytes < block_norm_ws_bytes(T, d)) return MOE_EWORKSPACE;
   return launch_block_norm_bwd(y, gate, w_post, post_norm, h_out, w_pre, r_post, r_pre, dh_out, dn, dtype, res_dtype, T, d, alpha, beta, dh, dy, dgate,
                                dw_post, dw_pre, accumulate, ws, (hipStream_t)stream);
+}
+
+int moe_layer_norm_fwd(const void* y, const void* h, const void* w, const void* b, int dtype, int res_dtype, int T, int d, float eps, void* h_out,
+                       void* n, float* mean, float* rstd, moe_stream_t stream) {
+  int rc = shape_check_norm(dtype, res_dtype, T, d);
+  if (rc) return rc;
+  if (!(eps > 0.f && eps < __builtin_inff())) return MOE_EINVAL;
+  if (T > 0 && (!h || !n || (!y && h_out))) return MOE_EINVAL;
+  if (misaligned(y, 16) || misaligned(h, 16) || misaligned(w, 16) || misaligned(b, 16) || misaligned(h_out, 16) || misaligned(n, 16))
+    return MOE_EINVAL;
+  return launch_layer_norm_fwd(y, h, w, b, dtype, res_dtype, T, d, eps, h_out, n, mean, rstd, (hipStream_t)stream);
+}
+
+int moe_layer_norm_bwd(const void* h_out, const void* w, const float* mean, const float* rstd, const void* dh_out, const void* dn, int dtype,
+                       int res_dtype, int T, int d, void* dh, void* dy, void* dw, void* db, int accumulate, void* ws, size_t ws_bytes,
+                       moe_stream_t stream) {
+  int rc = shape_check_norm(dtype, res_dtype, T, d);
+  if (rc) return rc;
+  if (accumulate != 0 && accumulate != 1) return MOE_EINVAL;
+  if (T > 0 && (!h_out || !mean || !rstd || !dn)) return MOE_EINVAL;
+  if (misaligned(h_out, 16) || misaligned(w, 16) || misaligned(dh_out, 16) || misaligned(dn, 16) || misaligned(dh, 16) || misaligned(dy, 16))
+    return MOE_EINVAL;
+  if (!ws || misaligned(ws, 256) || ws_bytes < layer_norm_ws_bytes(T, d)) return MOE_EWORKSPACE;
+  return launch_layer_norm_bwd(h_out, w, mean, rstd, dh_out, dn, dtype, res_dtype, T, d, dh, dy, dw, db, accumulate, ws, (hipStream_t)stream);
+}
+
+namespace {
+int shape_check_linear(int dtype, int cap, int K, int N, int e_cnt, const int32_t* offsets, int act) {
+  if (bad_dtype(dtype) || cap < 0 || K <= 0 || N <= 0 || e_cnt < 0 || act < MOE_ACT_NONE || act > MOE_ACT_SILU) return MOE_EINVAL;
+  if (!offsets && e_cnt != 1) return MOE_EINVAL;
+  const int step = dtype == MOE_BF16 ? 8 : 4, widest = K > N ? K : N;
+  if (e_cnt > MOE_MAX_LOCAL || K % step || N % step || widest > MOE_MAX_LINEAR) return MOE_EUNSUPPORTED;
+  // workgroups of 256 are counted in 32 bits of work-items, over 64 rows by 64 columns at the finest
+  if ((((long long)cap + 63) / 64 + e_cnt) * ((widest + 63) / 64) >= (1ll << 23)) return MOE_EUNSUPPORTED;
+  if (e_cnt * ((K + 63ll) / 64) * ((N + 63) / 64) >= (1ll << 23)) return MOE_EUNSUPPORTED;
+  return MOE_OK;
+}
+}  // namespace
+
+int moe_linear_fwd(const void* x, int dtype, int cap, int K, int N, int e_cnt, const int32_t* offsets, const void* w, const void* bias, int act,
+                   const void* residual, void* z, void* y, void* ws, size_t ws_bytes, moe_stream_t stream) {
+  int rc = shape_check_linear(dtype, cap, K, N, e_cnt, offsets, act);
+  if (rc) return rc;
+  if (e_cnt > 0 && !w) return MOE_EINVAL;
+  if (cap > 0 && (!x || !y)) return MOE_EINVAL;
+  if (misaligned(x, 16) || misaligned(w, 16) || misaligned(bias, 16) || misaligned(residual, 16) || misaligned(z, 16) || misaligned(y, 16))
+    return MOE_EINVAL;
+  if (!ws || misaligned(ws, 256) || ws_bytes < linear_fwd_ws_bytes(dtype, cap, K, N, e_cnt)) return MOE_EWORKSPACE;
+  return launch_linear_fwd(LinearArgs{x, w, bias, residual, z, y, dtype, cap, K, N, e_cnt, act, offsets}, ws, (hipStream_t)stream);
+}
+
+int moe_linear_bwd(const void* x, const void* z, const void* dy, int dtype, int cap, int K, int N, int e_cnt, const int32_t* offsets, const void* w,
+                   int act, void* dx, void* dw, void* db, int accumulate, void* ws, size_t ws_bytes, moe_stream_t stream) {
+  int rc = shape_check_linear(dtype, cap, K, N, e_cnt, offsets, act);
+  if (rc) return rc;
+  if (accumulate != 0 && accumulate != 1) return MOE_EINVAL;
+  if (cap > 0 && (!dy || (dw && !x) || (act != MOE_ACT_NONE && !z))) return MOE_EINVAL;
+  if (cap > 0 && e_cnt > 0 && dx && !w) return MOE_EINVAL;
+  if (misaligned(x, 16) || misaligned(z, 16) || misaligned(dy, 16) || misaligned(w, 16) || misaligned(dx, 16) || misaligned(dw, 16) || misaligned(db, 16))
+    return MOE_EINVAL;
+  if (!ws || misaligned(ws, 256) || ws_bytes < linear_bwd_ws_bytes(dtype, cap, K, N, e_cnt)) return MOE_EWORKSPACE;
+  return launch_linear_bwd(LinearArgs{x, w, nullptr, nullptr, (void*)z, nullptr, dtype, cap, K, N, e_cnt, act, offsets}, dy, dx, dw, db, accumulate, ws,
+                           (hipStream_t)stream);
 }
 
 namespace {

@@ -7,6 +7,9 @@
 //   DX     dxp   = dH1 W1^T + dH3 W3^T   ragged M, K = 2f in two segments
 //   WG     dW2   = a^T d_o           ragged K (the expert's rows), both operands read transposed
 //   WGD    dW1|dW3 = xp^T [dH1|dH3]  ragged K, two outputs sharing the A operand
+// and those of a linear layer, grouped by expert or dense (WG is its weight gradient):
+//   LIN    y = act(x W + b) + residual   ragged M, B read transposed, the whole epilogue fused
+//   LDX    dx = dz W^T               ragged M, B K-contiguous
 //
 // Tiling: 256x256 block tile, 32-deep k-tiles, 256 threads = 4 wavefronts in a 2x2 grid,
 // 128x128 per wavefront = 4x4 MFMA blocks (256 accumulator registers), one wavefront per SIMD.
@@ -32,6 +35,7 @@
 // Workgroups are persistent and walk a device-built tile list (row counts never visit the
 // host); the list is ordered so that the tiles resident on one XCD share operand panels.  In the
 // ragged-M shapes a second list of 128x128 tiles (quarter tiles) follows where that ends sooner.
+#include "activation.h"
 #include "few_rows.h"
 #include "kernels.h"
 
@@ -77,7 +81,8 @@ enum { UP = 0, DOWN = 1, DA = 2, DX = 3, WG = 4, WGD = 5,
        // the trainable router reuses the same machinery on one full-height "expert":
        RL = 6,    // logits = x Wr            ragged-M shape, B read transposed, fp32 output
        RW = 7,    // dWr partials = x^T dl    ragged-K shape over fixed chunks of the tokens, fp32 output
-       RX = 8 };  // dx (+)= dl Wr^T          ragged-M shape, B K-contiguous, optional bf16 accumulate
+       RX = 8,    // dx (+)= dl Wr^T          ragged-M shape, B K-contiguous, optional bf16 accumulate
+       LIN = 9, LDX = 10 };
 
 struct GArgs {
   const bf16_t* A0; const bf16_t* A1;     // A sources (A1: second K segment of DX)
@@ -110,15 +115,21 @@ struct GArgs {
   int accumulate;
   int save_h;
   int pair_first;                         // another GEMM follows in this launch and fills the last round
-  int cached;                             // UP, DOWN: cached_experts
+  int cached;                             // UP, DOWN, LIN: experts whose weights fit the Infinity Cache
+  const bf16_t* bias;                     // LIN: [e_cnt][N] or NULL
+  const bf16_t* R0;                       // LIN: residual, laid out as C0, or NULL.  C0 is y, C1 is z or NULL
+  int act;
 };
 
 template <int MODE> struct Traits {
   static constexpr bool A_TRANS = MODE == WG || MODE == WGD || MODE == RW;
-  static constexpr bool B_TRANS = MODE == UP || MODE == DOWN || MODE == WG || MODE == WGD || MODE == RL || MODE == RW;
+  static constexpr bool B_TRANS = MODE == UP || MODE == DOWN || MODE == WG || MODE == WGD || MODE == RL || MODE == RW || MODE == LIN;
   static constexpr bool DUAL = MODE == UP || MODE == WGD;
   static constexpr bool RAGGED_K = MODE == WG || MODE == WGD || MODE == RW;
   static constexpr int BN_EFF = DUAL ? BN / 2 : BN;   // output columns covered per tile
+  // The contraction may end inside a pair of k-tiles (at a multiple of 8, a chunk).  Loads of chunks and rows past its end are sent to
+  // valid ones, and what they bring is zeroed in the fragments of both operands.
+  static constexpr bool TAIL = MODE == LIN || MODE == LDX;
 };
 
 // ---- K-contiguous operand B (source rows are tile rows; a k-tile is 64 contiguous bytes) -
@@ -140,9 +151,10 @@ struct KcIssue {
     }
   }
   template <bool STREAM>
-  __device__ __forceinline__ void issue1(int j, uint32_t oper_lds, int wave, long kofs) const {
-    lds_load16<STREAM>(base + kofs, voff[j], oper_lds + (4 * wave + j) * 1024);
+  __device__ __forceinline__ void issue1(int j, uint32_t oper_lds, int wave, long kofs, uint32_t back = 0) const {
+    lds_load16<STREAM>(base + kofs, voff[j] - back, oper_lds + (4 * wave + j) * 1024);
   }
+  static __device__ __forceinline__ int chunk(int lane) { return (lane & 3) ^ ((lane >> 4) & 3); }
 };
 
 // ---- K-contiguous operand A of the ragged-M shapes, fetched two k-tiles at a time ----------
@@ -165,10 +177,13 @@ struct KcPairIssue {
       voff[q] = (uint32_t)(r * ld * 2 + c * 16);
     }
   }
-  __device__ __forceinline__ void issue1(int q, uint32_t dstage_lds, int wave, long kofs) const {
-    lds_load16(base + kofs, voff[q], dstage_lds + (8 * wave + q) * 1024);
+  __device__ __forceinline__ void issue1(int q, uint32_t dstage_lds, int wave, long kofs, uint32_t back = 0) const {
+    lds_load16(base + kofs, voff[q] - back, dstage_lds + (8 * wave + q) * 1024);
   }
+  static __device__ __forceinline__ int chunk(int q, int lane) { return (lane & 7) ^ (4 * (q & 1) + (lane >> 4)); }
 };
+// Bytes that a load of the chunk of 8 k at k goes back by so as not to read past the contraction's K
+__device__ __forceinline__ uint32_t past_end(int k, int K) { return 2u * (uint32_t)max(0, k - (K - 8)); }
 
 // ---- transposed operand (source is [k][n], n contiguous) --------------------------------
 // Kept in LDS as two sub-tiles [32 k][128 n] of 8 KB (for a dual tile they come from two
@@ -308,7 +323,7 @@ __device__ __forceinline__ float plan_price(const GArgs& p, int n_big, int n_qua
   const float quarter = MODE == DA ? (0.008f + 0.0025f * alone) * k + 6.f : (0.0073f + 0.0025f * alone) * k + 4.5f;
   // the weights at the rate that either kind streams them, MB per us (UP's quarters read 128 bytes of a row, DA's and DX's
   // 256x256 tiles 64)
-  constexpr float RATE_BIG = MODE == UP || MODE == DOWN ? 5.6f : 5.1f, RATE_QUARTER = MODE == UP ? 4.8f : 5.8f;
+  constexpr float RATE_BIG = MODE == UP || MODE == DOWN || MODE == LIN ? 5.6f : 5.1f, RATE_QUARTER = MODE == UP ? 4.8f : 5.8f;
   const float weights = k * (float)p.N * (MODE == UP ? 4e-6f : 2e-6f) * ((float)active_big / RATE_BIG + (float)active_quarter / RATE_QUARTER);
   const int grid = gridDim.x, full = n_big / grid, rest = n_big - full * grid;
   const float per_cu = 1.f / (float)grid;
@@ -401,6 +416,15 @@ __device__ __forceinline__ void finish_da(const GArgs& p, size_t idx, const floa
 }
 
 
+// LIN: z = x + bias, y = act(z) + residual
+__device__ __forceinline__ void finish_lin(const GArgs& p, size_t idx, float* x, uint4 bias, uint4 residual) {
+  add8(x, bias);
+  if (p.C1) store16(p.C1 + idx, pack8(x));
+  activate(p.act, x);
+  add8(x, residual);
+  store16(p.C0 + idx, pack8(x));
+}
+
 // ---- quarter tiles: 128x128 (a dual tile: 64 columns of either output) --------------------------------------------------
 // What is left of a GEMM when the 256x256 tiles no longer fill a round of the chip, and the row tiles of which half is empty, is
 // multiplied in quarters.  The four wavefronts hold 64x64 each; a k-tile is 64 deep, so that every load fetches whole cache
@@ -423,9 +447,10 @@ struct QuarterKc {         // load j of a wavefront: rows 8*(4w+j) + lane/8, who
       voff[j] = (uint32_t)(min(rl, rows_valid - 1) * ld * 2 + c * 16);
     }
   }
-  __device__ __forceinline__ void issue1(int j, uint32_t oper_lds, int wave, long kofs) const {
-    lds_load16(base + kofs, voff[j], oper_lds + (4 * wave + j) * 1024);
+  __device__ __forceinline__ void issue1(int j, uint32_t oper_lds, int wave, long kofs, uint32_t back = 0) const {
+    lds_load16(base + kofs, voff[j] - back, oper_lds + (4 * wave + j) * 1024);
   }
+  static __device__ __forceinline__ int chunk(int j, int lane) { return (lane & 7) ^ (4 * (j & 1) + (lane >> 4)); }
 };
 struct QuarterTr {         // sub-tile wave/2, load j: k rows 8*(4*(w%2)+j) + lane/8, 64 columns each
   const bf16_t* src;
@@ -492,7 +517,7 @@ __device__ __forceinline__ void quarter_tiles(const GArgs& p, const Quarters& li
                                            : TR::DUAL ? quarter_tr_off(i, wn * 32, lane) : quarter_tr_off(wn, i * 32, lane));
   }
 
-  int row0 = 0, row_end = 0, n0 = 0, nk0 = 0, nk = 0;
+  int row0 = 0, row_end = 0, n0 = 0, nk0 = 0, nk = 0, tile_e = 0;
   QuarterKc ia, ib_kc;
   QuarterTr ib_tr;
   // q = 0..3: operand A of k-tile kt, 4..7: operand B.  kt is clamped to the last one as in the 256x256 tiles.
@@ -501,9 +526,10 @@ __device__ __forceinline__ void quarter_tiles(const GArgs& p, const Quarters& li
     const uint32_t st = smem_base + (kt & (NSTAGE - 1)) * (2 * QOPER_BYTES);
     const bool seg1 = MODE == DX && kt >= nk0;
     const long k0 = (long)(seg1 ? kt - nk0 : kt) * QK;
-    if (q < 4) ia.issue1(q, st, wave, k0 + (seg1 ? p.A1 - p.A0 : 0));
-    else if (TR::B_TRANS) ib_tr.template issue1<false>(q - 4, st + QOPER_BYTES, wave, lane, k0, 0);
-    else ib_kc.issue1(q - 4, st + QOPER_BYTES, wave, k0 + (seg1 ? p.B1 - p.B0 : 0));
+    const uint32_t back = TR::TAIL && kt == nk - 1 ? past_end((int)k0 + 8 * QuarterKc::chunk(q, lane), p.K) : 0;
+    if (q < 4) ia.issue1(q, st, wave, k0 + (seg1 ? p.A1 - p.A0 : 0), back);
+    else if (TR::B_TRANS) ib_tr.template issue1<TR::TAIL>(q - 4, st + QOPER_BYTES, wave, lane, k0, p.K - 1 - (int)k0);
+    else ib_kc.issue1(q - 4, st + QOPER_BYTES, wave, k0 + (seg1 ? p.B1 - p.B0 : 0), back);
   };
   auto next_tile = [&]() -> bool {
     const int L = take_ticket<true>(counters, n_queues, queue, list.total, list.next_q, wave, lane, 0);
@@ -521,8 +547,9 @@ __device__ __forceinline__ void quarter_tiles(const GArgs& p, const Quarters& li
     row0 = lo + (band * 8 + in_band - nt * band_rows) * QT;
     row_end = hi;
     n0 = nt * QN;
-    nk0 = p.K / QK;
+    nk0 = TR::TAIL ? (p.K + QK - 1) / QK : p.K / QK;
     nk = MODE == DX ? 2 * nk0 : nk0;
+    tile_e = e;
     ia.setup(p.A0 + (size_t)row0 * p.lda, p.lda, hi - row0, wave, lane);
     if (TR::B_TRANS) ib_tr.setup(p.B0 + (size_t)e * p.b_es, p.B1 + (size_t)e * p.b_es, TR::DUAL, p.ldb, n0, p.N, wave, lane);
     else ib_kc.setup(p.B0 + (size_t)e * p.b_es + (size_t)n0 * p.ldb, p.ldb, p.N - n0, wave, lane);
@@ -556,6 +583,19 @@ __device__ __forceinline__ void quarter_tiles(const GArgs& p, const Quarters& li
           pre3[sl][pass] = load16_once(p.H3 + idx);
         }
     }
+    // LIN: so are its residual (pre1) and its bias
+    uint4 bias = make_uint4(0, 0, 0, 0);
+    if (MODE == LIN) {
+      const int gcol = min(n0 + wn * 64 + c8 * 8, p.N - 8);
+      if (p.bias) bias = *reinterpret_cast<const uint4*>(p.bias + (size_t)tile_e * p.N + gcol);
+#pragma unroll
+      for (int sl = 0; sl < 4; ++sl)
+#pragma unroll
+        for (int pass = 0; pass < 2; ++pass) {
+          const int grow = min(row0 + wm * 64 + 16 * sl + pass * 8 + (lane >> 3), row_end - 1);
+          pre1[sl][pass] = p.R0 ? load16_once(p.R0 + (size_t)grow * p.ldc + gcol) : make_uint4(0, 0, 0, 0);
+        }
+    }
     f32x16 acc[2][2];
 #pragma unroll
     for (int i = 0; i < 2; ++i)
@@ -587,6 +627,13 @@ __device__ __forceinline__ void quarter_tiles(const GArgs& p, const Quarters& li
       auto live = [](int o) { return MV == 2 || (MV == 1 && (o & 3) != 3); };
       auto half = [&](int kt, auto h_tag) {
         constexpr int H = decltype(h_tag)::value;
+        if (TR::TAIL && (kt + 1) * QK > p.K) {
+#pragma unroll
+          for (int t = 0; t < 2; ++t)
+            if (kt * QK + 16 * (2 * H + t) + 8 * (lane >> 5) >= p.K)
+#pragma unroll
+              for (int i = 0; i < 2; ++i) fa[H][t][i] = fb[H][t][i] = bf16x8{};
+        }
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int m = 0; m < 8; m += 2) {
@@ -622,15 +669,22 @@ __device__ __forceinline__ void quarter_tiles(const GArgs& p, const Quarters& li
     else if (rows_left > 0) k_loop(IntC<1>{});
     else k_loop(IntC<0>{});
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-    if (MODE == DA) {      // these have arrived: the compiler is to wait for them here, not behind the next tile's first loads
+    if (MODE == DA || MODE == LIN) {      // these have arrived: the compiler is to wait for them here, not behind the next tile's first loads
+      u32x4_t ub = __builtin_bit_cast(u32x4_t, bias);
+      asm volatile("" : "+v"(ub));
+      bias = __builtin_bit_cast(uint4, ub);
 #pragma unroll
       for (int sl = 0; sl < 4; ++sl)
 #pragma unroll
         for (int pass = 0; pass < 2; ++pass) {
-          u32x4_t u1 = __builtin_bit_cast(u32x4_t, pre1[sl][pass]), u3 = __builtin_bit_cast(u32x4_t, pre3[sl][pass]);
-          asm volatile("" : "+v"(u1), "+v"(u3));
+          u32x4_t u1 = __builtin_bit_cast(u32x4_t, pre1[sl][pass]);
+          asm volatile("" : "+v"(u1));
           pre1[sl][pass] = __builtin_bit_cast(uint4, u1);
-          pre3[sl][pass] = __builtin_bit_cast(uint4, u3);
+          if (MODE == DA) {
+            u32x4_t u3 = __builtin_bit_cast(u32x4_t, pre3[sl][pass]);
+            asm volatile("" : "+v"(u3));
+            pre3[sl][pass] = __builtin_bit_cast(uint4, u3);
+          }
         }
     }
     if (tid == 0) list.next_q[0] = my_ticket;
@@ -641,6 +695,39 @@ __device__ __forceinline__ void quarter_tiles(const GArgs& p, const Quarters& li
     // epilogue: slabs of 16 rows x 64 columns (a dual tile: 32 of either output) through the wavefront's own staging area
     float* stage = reinterpret_cast<float*>(smem + STAGING_OFF) + wave * (STAGING_WAVE_BYTES / 4);
     const int acc_col = lane & 31, acc_rg = lane >> 5;
+    if constexpr (MODE == LIN) {           // (a loop, for the code of the activations to be there once)
+#pragma unroll 1
+      for (int sl = 0; sl < 4; ++sl) {
+        uint4 res[2];
+        static_for<4>([&](auto which) {
+          constexpr int S = decltype(which)::value, mi = S >> 1, h = S & 1;
+          if (sl != S) return;
+          res[0] = pre1[S][0];
+          res[1] = pre1[S][1];
+#pragma unroll
+          for (int gg = 0; gg < 2; ++gg)
+#pragma unroll
+            for (int nn = 0; nn < 2; ++nn)
+#pragma unroll
+              for (int i = 0; i < 4; ++i)
+                stage[(8 * gg + 4 * acc_rg + i) * SPITCH + nn * 32 + acc_col] = acc[mi][nn][4 * (2 * h + gg) + i];
+          asm volatile("; accumulators %0" : : "n"(S));         // (the cases are not to become one with an address among the accumulators)
+        });
+        __builtin_amdgcn_wave_barrier();
+        float xs[2][8];
+#pragma unroll
+        for (int pass = 0; pass < 2; ++pass)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) xs[pass][i] = stage[(pass * 8 + (lane >> 3)) * SPITCH + c8 * 8 + i];
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int pass = 0; pass < 2; ++pass) {
+          const int grow = ep_row0 + 16 * sl + pass * 8 + (lane >> 3), gcol = ep_n0 + wn * 64 + c8 * 8;
+          if (grow < ep_row_end && gcol < p.N) finish_lin(p, (size_t)grow * p.ldc + gcol, xs[pass], bias, res[pass]);
+        }
+      }
+      continue;
+    }
 #pragma unroll
     for (int sl = 0; sl < 4; ++sl) {
       const int mi = sl >> 1, h = sl & 1;
@@ -688,7 +775,7 @@ __device__ __forceinline__ void gg_body(const GArgs& p) {
   int32_t* offs = tile_start + (MOE_MAX_LOCAL + 1);      // LDS copy of the row offsets
   int32_t* split = offs + (MOE_MAX_LOCAL + 1);           // ragged-K modes: (first piece << 8) | pieces, by expert
   int32_t* q_start = split;                              // ragged-M modes: quarter tiles before a position
-  constexpr bool SPLIT = MODE <= DX;                     // the rest of a GEMM may be multiplied in quarter tiles
+  constexpr bool SPLIT = MODE <= DX || MODE == LIN || MODE == LDX;      // the rest of a GEMM may be multiplied in quarter tiles
   uint16_t* order = reinterpret_cast<uint16_t*>(split + MOE_MAX_LOCAL + 1);   // experts by descending row count
   int32_t* next_q = reinterpret_cast<int32_t*>(order + MOE_MAX_LOCAL);    // hand-over slot of the tile scheduler
 
@@ -957,7 +1044,7 @@ __device__ __forceinline__ void gg_body(const GArgs& p) {
   // 1936 tokens at the former 1616 -> 1586.  (Of layers that fit, the backward finds them: Qwen-like share 821 against 829.  In every
   // tile, which drops panels that tiles share, steps take 1 to 3 % longer; in dA and dX, whose weights are read 64 bytes of a row at a
   // time, up to 7 % even in tiles that share nothing.)  A loop of its own: a branch at every load costs 2 %.
-  constexpr bool ONCE = MODE == UP || MODE == DOWN;
+  constexpr bool ONCE = MODE == UP || MODE == DOWN || MODE == LIN;
   bool once = false;      // no other tile reads this one's weights
   int active = 0;         // experts that have rows, of a layer that does not fit as a whole
   if (ONCE && e_cnt > p.cached)
@@ -968,6 +1055,7 @@ __device__ __forceinline__ void gg_body(const GArgs& p) {
   KcPairIssue ia_kp;
   KcIssue ib_kc;
   TrIssue ia_tr, ib_tr;
+  uint4 bias[2] = {};     // LIN: of this lane's columns in either half of its wavefront's 128
 
   // One of the 8 loads (q = 0..3: operand A, 4..7: operand B) of k-tile kt.  kt is clamped to
   // the last tile, so every iteration issues the same number of loads and the vmcnt
@@ -989,16 +1077,19 @@ __device__ __forceinline__ void gg_body(const GArgs& p) {
     const int kt0 = 2 * pj;
     const bool seg1 = MODE == DX && kt0 >= nk0;
     const long kofs = (long)(seg1 ? kt0 - nk0 : kt0) * BK + (seg1 ? p.A1 - p.A0 : 0);
-    ia_kp.issue1(q, smem_base + (pj & 1) * (2 * OPER_BYTES), wave, kofs);
+    const uint32_t back = TR::TAIL && kt0 == nk - 2 ? past_end(kt0 * BK + 8 * KcPairIssue::chunk(q, lane), p.K) : 0;
+    ia_kp.issue1(q, smem_base + (pj & 1) * (2 * OPER_BYTES), wave, kofs, back);
   };
   auto issue_b = [&](int kt, int j, auto once_tag) {
     constexpr bool STREAM = decltype(once_tag)::value != 0;
     if (kt > nk - 1) kt = nk - 1;
     const uint32_t st = smem_base + B_REGION + (kt & (NSTAGE - 1)) * OPER_BYTES;
     const bool seg1 = MODE == DX && kt >= nk0;
+    if (TR::TAIL) kt = min(kt, (p.K - 1) / BK);          // (the last pair's second k-tile may lie past the end)
     const int k0 = (seg1 ? kt - nk0 : kt) * BK;
-    if (TR::B_TRANS) ib_tr.template issue1<false, STREAM>(j, st, wave, lane, k0, 0);
-    else ib_kc.template issue1<STREAM>(j, st, wave, k0 + (seg1 ? p.B1 - p.B0 : 0));
+    const uint32_t back = TR::TAIL && k0 + BK > p.K ? past_end(k0 + 8 * KcIssue::chunk(lane), p.K) : 0;
+    if (TR::B_TRANS) ib_tr.template issue1<TR::TAIL, STREAM>(j, st, wave, lane, k0, p.K - 1 - k0);
+    else ib_kc.template issue1<STREAM>(j, st, wave, k0 + (seg1 ? p.B1 - p.B0 : 0), back);
   };
   auto issue_tile = [&](int kt) {
 #pragma unroll
@@ -1066,11 +1157,16 @@ __device__ __forceinline__ void gg_body(const GArgs& p) {
       row0 = lo + mt * BM;
       row_end = hi;
       const size_t kfirst = MODE == RL ? (size_t)krange * p.K : 0;      // first column of this tile's range
-      nk0 = (MODE == RL && p.ksplit > 1 ? min(p.K, p.k_total - krange * p.K) : p.K) / BK;
+      nk0 = TR::TAIL ? 2 * ((p.K + 2 * BK - 1) / (2 * BK)) : (MODE == RL && p.ksplit > 1 ? min(p.K, p.k_total - krange * p.K) : p.K) / BK;
       nk = MODE == DX ? 2 * nk0 : nk0;
       ia_kp.setup(p.A0 + (size_t)row0 * p.lda + kfirst, p.lda, hi - row0, wave, lane);
       if (TR::B_TRANS) ib_tr.setup(p.B0 + (size_t)e * p.b_es + kfirst * p.ldb, p.B1 + (size_t)e * p.b_es, TR::DUAL, p.ldb, n0, p.N, wave, lane);
       else ib_kc.setup(p.B0 + (size_t)e * p.b_es + (size_t)n0 * p.ldb, p.ldb, p.N - n0, wave, lane);
+    }
+    if (MODE == LIN && p.bias) {           // (ahead of the loads that the compiler does not know of)
+#pragma unroll
+      for (int np = 0; np < 2; ++np)
+        bias[np] = *reinterpret_cast<const uint4*>(p.bias + (size_t)e * p.N + min(n0 + wn * 128 + np * 64 + (lane & 7) * 8, p.N - 8));
     }
     if (nk > 0) {
       if (PAIR) {       // what the k loop's iterations -2 and -1 would have issued, in its order
@@ -1175,6 +1271,12 @@ __device__ __forceinline__ void gg_body(const GArgs& p) {
     // 0 and half of pair 1, B's k-tiles 0..2) were issued by next_tile; the stores of the previous
     // tile's epilogue were issued after them and share the counter, so the first wait is for
     // everything.
+    // TAIL: zeros for what lies past the contraction's end
+    auto mask_end = [&](int h, int kt, int s) {
+      if (kt * BK + 16 * s + 8 * (lane >> 5) >= p.K)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) fa[h][i] = fb[h][i] = bf16x8{};
+    };
     if (nk > 0) {
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
       __syncthreads();
@@ -1230,6 +1332,8 @@ __device__ __forceinline__ void gg_body(const GArgs& p) {
       auto live = [](int o) { return MV == 4 || (MV == 2 && o <= 5); };
       auto iteration = [&](int kt, auto odd_tag) {
         constexpr bool ODD = decltype(odd_tag)::value != 0;
+        const bool tail = TR::TAIL && (kt + 1) * BK > p.K;
+        if (tail) mask_end(0, kt, 0);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int m = 0; m < 16; m += 2) {
@@ -1249,6 +1353,7 @@ __device__ __forceinline__ void gg_body(const GArgs& p) {
         else asm volatile("s_waitcnt vmcnt(12) lgkmcnt(0)" ::: "memory");
         __builtin_amdgcn_s_barrier();
         __builtin_amdgcn_sched_barrier(0);
+        if (tail) mask_end(1, kt, 1);
 #pragma unroll
         for (int m = 0; m < 16; m += 2) {
           if (m < 4 * MV) mfma_one(1, m);
@@ -1286,6 +1391,7 @@ __device__ __forceinline__ void gg_body(const GArgs& p) {
 
     // the ring is free: decode the next tile and start its first loads, then store this one
     const int ep_e = e, ep_row0 = row0, ep_row_end = row_end, ep_n0 = n0, ep_piece = piece, ep_krange = krange;
+    const uint4 ep_bias[2] = {bias[0], bias[1]};
     have = next_tile();
 
     // ---------------------------------------------------------------- epilogue
@@ -1401,6 +1507,56 @@ __device__ __forceinline__ void gg_body(const GArgs& p) {
           pre1[sl % (DA_AHEAD + 1)][pass] = load16_once(p.C0 + idx);
         }
       };
+      if constexpr (MODE == LIN) {
+        // a loop over the accumulators' blocks, for the code of the activations to be there four times and not sixteen
+        auto res_fetch = [&](int block, int part) {
+          const int mi = block + (part >> 2), h = (part >> 1) & 1, np = part & 1;
+#pragma unroll
+          for (int pass = 0; pass < 2; ++pass) {
+            const int grow = min(ep_row0 + wm * 128 + mi * 32 + 16 * h + pass * 8 + (lane >> 3), ep_row_end - 1);
+            const int gcol = min(ep_n0 + wn * 128 + np * 64 + c8 * 8, p.N - 8);
+            pre1[part & 3][pass] = load16_once(p.R0 + (size_t)grow * p.ldc + gcol);
+          }
+        };
+        static_assert(DA_AHEAD == 3, "a block's four slabs take turns");
+        if (RMW_TAG)
+#pragma unroll
+          for (int part = 0; part < DA_AHEAD; ++part) res_fetch(0, part);
+#pragma unroll 1
+        for (int block = 0; block < 4; ++block)
+#pragma unroll
+          for (int part = 0; part < 4; ++part) {
+            const int h = part >> 1, np = part & 1;
+            if (RMW_TAG && (block < 3 || part == 0)) res_fetch(block, part + DA_AHEAD);
+            static_for<4>([&](auto which) {
+              constexpr int mi = decltype(which)::value;
+              if (block != mi) return;
+#pragma unroll
+              for (int gg = 0; gg < 2; ++gg)
+#pragma unroll
+                for (int nn = 0; nn < 2; ++nn)
+#pragma unroll
+                  for (int i = 0; i < 4; ++i)
+                    stage[(8 * gg + 4 * acc_rg + i) * SPITCH + nn * 32 + acc_col] = acc[mi][2 * np + nn][4 * (2 * h + gg) + i];
+              asm volatile("; accumulators %0" : : "n"(mi));      // (the cases are not to become one with an address among the accumulators)
+            });
+            __builtin_amdgcn_wave_barrier();
+            float xs[2][8];
+#pragma unroll
+            for (int pass = 0; pass < 2; ++pass)
+#pragma unroll
+              for (int i = 0; i < 8; ++i) xs[pass][i] = stage[(pass * 8 + (lane >> 3)) * SPITCH + c8 * 8 + i];
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll
+            for (int pass = 0; pass < 2; ++pass) {
+              const int grow = ep_row0 + wm * 128 + block * 32 + 16 * h + pass * 8 + (lane >> 3);
+              const int gcol = ep_n0 + wn * 128 + np * 64 + c8 * 8;
+              if (grow < ep_row_end && gcol < p.N)
+                finish_lin(p, (size_t)grow * p.ldc + gcol, xs[pass], ep_bias[np], RMW_TAG ? pre1[part][pass] : make_uint4(0, 0, 0, 0));
+            }
+          }
+        return;
+      }
       if (MODE == DA) {
 #pragma unroll
         for (int sl = 0; sl < DA_AHEAD; ++sl) da_fetch(sl);
@@ -1459,7 +1615,7 @@ __device__ __forceinline__ void gg_body(const GArgs& p) {
     }
     };
     if ((MODE == WG || MODE == WGD) && ep_piece >= 0) epilogue(IntC<1>{}, IntC<0>{});
-    else if ((MODE == WG || MODE == WGD || MODE == RX) && p.accumulate) epilogue(IntC<0>{}, IntC<1>{});
+    else if (((MODE == WG || MODE == WGD || MODE == RX) && p.accumulate) || (MODE == LIN && p.R0)) epilogue(IntC<0>{}, IntC<1>{});
     else epilogue(IntC<0>{}, IntC<0>{});
   }
   if constexpr (SPLIT) {
@@ -1647,7 +1803,7 @@ int launch_gg_or_few(const GArgs& a, int d, int f, hipStream_t s) {
 }
 
 template <int MODE>
-int launch_gg(const GArgs& a, hipStream_t s) {
+int launch_gg(const GArgs& a, hipStream_t s, int prof_id = -1) {
   // the LDS opt-in is a per-device attribute of the kernel
   static bool attr_set[64] = {};
   int dev = 0;
@@ -1659,7 +1815,9 @@ int launch_gg(const GArgs& a, hipStream_t s) {
     attr_set[dev] = true;
   }
   int grid = device_cu_count();
-  ProfScope prof(MODE == RL ? MOE_K_ROUTER_FWD : MODE == RW ? MOE_K_ROUTER_DW : MODE == RX ? MOE_K_ROUTER_DX : MOE_K_UP + MODE, s);
+  constexpr int id = MODE == RL ? MOE_K_ROUTER_FWD : MODE == RW ? MOE_K_ROUTER_DW : MODE == RX ? MOE_K_ROUTER_DX : MODE == LIN ? MOE_K_LINEAR
+                     : MODE == LDX ? MOE_K_LINEAR_DX : MOE_K_UP + MODE;
+  ProfScope prof(prof_id < 0 ? id : prof_id, s);
   hipLaunchKernelGGL(gg_kernel<MODE>, dim3(grid), dim3(NT), SMEM_BYTES, s, a);
   HIP_CHECK_LAUNCH();
   return MOE_OK;
@@ -1893,3 +2051,57 @@ size_t wgrad_split_bytes(int d, int f) {
   return b;
 }
 size_t expert_bwd_extra_ws_bytes(int d, int f) { return 256 + WGRAD_PLAN_BYTES + wgrad_split_bytes(d, f); }
+
+// ---- linear layer, grouped by expert or dense --------------------------------------------------------------------------
+// The rows of expert e are [offsets[e], offsets[e+1]); offsets NULL: one matrix, all rows.
+int launch_linear_fwd_tiles(const LinearArgs& l, int32_t* sched, hipStream_t s) {
+  GArgs g = {};
+  g.A0 = g.A1 = (const bf16_t*)l.x; g.lda = l.K;
+  g.B0 = g.B1 = (const bf16_t*)l.w; g.ldb = l.N; g.b_es = (long)l.K * l.N;
+  g.C0 = (bf16_t*)l.y; g.C1 = (bf16_t*)l.z; g.ldc = l.N;
+  g.bias = (const bf16_t*)l.bias; g.R0 = (const bf16_t*)l.residual; g.act = l.act;
+  g.off = l.offsets; g.rows = g.chunk = l.rows; g.sched = sched; g.e_cnt = l.e_cnt; g.N = l.N; g.K = l.K;
+  g.cached = (int)((256ll << 20) / (2ll * l.K * l.N));
+  return launch_gg<LIN>(g, s);
+}
+
+// Room for the fp32 partial tiles of experts whose rows are cut: 32 pieces, at most 256 MB
+size_t linear_split_bytes(int K, int N) {
+  const size_t piece = (size_t)K * N * 4, most = (size_t)256 << 20;
+  return 32 * piece <= most ? 32 * piece : most / piece * piece;
+}
+
+// dx = dz W^T and dW (+)= x^T dz; either may be left out.  ws: plan of MOE_MAX_LOCAL words, then linear_split_bytes
+int launch_linear_bwd_tiles(const LinearArgs& l, const void* dz, void* dx, void* dw, int accumulate, int32_t* sched, void* ws, hipStream_t s) {
+  const long mn = (long)l.K * l.N;
+  GArgs x = {};
+  x.A0 = x.A1 = (const bf16_t*)dz; x.lda = l.N;
+  x.B0 = x.B1 = (const bf16_t*)l.w; x.ldb = l.N; x.b_es = mn;
+  x.C0 = (bf16_t*)dx; x.ldc = l.K;
+  x.off = l.offsets; x.rows = x.chunk = l.rows; x.sched = sched; x.e_cnt = l.e_cnt; x.N = l.K; x.K = l.N;
+  GArgs w = {};
+  w.A0 = w.A1 = (const bf16_t*)l.x; w.lda = l.K;
+  w.B0 = w.B1 = (const bf16_t*)dz; w.ldb = l.N;
+  w.C0 = (bf16_t*)dw; w.ldc = l.N; w.c_es = mn;
+  w.off = l.offsets; w.rows = w.chunk = l.rows; w.sched = sched + 16; w.e_cnt = l.e_cnt; w.M = l.K; w.N = l.N; w.accumulate = accumulate;
+  w.plan = (int32_t*)ws;
+  w.P0 = (float*)((char*)ws + MOE_MAX_LOCAL * 4); w.p_stride = mn;
+  w.split_budget = (int)(linear_split_bytes(l.K, l.N) / ((size_t)mn * 4));
+  // as for the experts' backward: the weight gradient fills dx's last round while that is a visible part of it
+  const long long m_tiles = (l.rows + BM - 1) / BM + l.e_cnt / 2, rounds = m_tiles * ((l.K + BN - 1) / BN) / device_cu_count();
+  const bool have_dx = dx && l.rows > 0;
+  int rc;
+  if (have_dx && dw && rounds <= 12) {
+    if ((rc = launch_pair<LDX, WG>(x, w, MOE_K_LINEAR_DX_DW, s))) return rc;
+  } else {
+    if (have_dx && (rc = launch_gg<LDX>(x, s))) return rc;
+    if (dw && (rc = launch_gg<WG>(w, s, MOE_K_LINEAR_DW))) return rc;
+  }
+  if (dw && w.split_budget >= 2) {
+    ProfScope prof(MOE_K_WGRAD_REDUCE, s);
+    hipLaunchKernelGGL(wgrad_reduce, dim3(4 * device_cu_count()), dim3(256), 0, s, w.plan, l.e_cnt, w.P0, mn, mn, 1, (bf16_t*)dw, (bf16_t*)dw, mn,
+                       accumulate);
+    HIP_CHECK_LAUNCH();
+  }
+  return MOE_OK;
+}

@@ -8,6 +8,7 @@
 //   DX     dxp   = dH1 W1^T + dH3 W3^T   ragged M, K in two segments
 //   WG     dW2   = a^T d_o      ragged K (the expert's rows)
 //   WGD    dW1|dW3 = xp^T [dH1|dH3]      ragged K, two outputs of one tile
+// and those of a linear layer (WG is its weight gradient): LIN, y = act(x W + b) + residual, and LDX, dx = dz W^T.
 //
 // The fp32 matrix instruction does 256 FLOP per cycle and CU, the bf16 one sixteen times that, so six bf16 products take 3/8 of
 // the time.  Three terms hold all 24 bits of a number.  The three products of terms that are left out are up to 2^-24.0 of a product of
@@ -25,6 +26,7 @@
 // two LDS buffers and two blocks per CU 87 + 176; splitting between the matrix instructions of one wavefront, which takes more
 // registers, 104 + 181; tiles of 128x64 95 + 199 (better only for a thousand rows and more per expert: 145 for 176 at 3000, d = f =
 // 1024).
+#include "activation.h"
 #include "common.h"
 #include "kernels.h"
 
@@ -33,7 +35,7 @@ namespace {
 constexpr int TM = 64, TN = 64, TK = 32, NT = 256;
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
-enum { UP, DOWN, DA, DX, WG, WGD };
+enum { UP, DOWN, DA, DX, WG, WGD, LIN, LDX };
 
 // An fp32 matrix instruction contracts two values of k, one per half of the wavefront.  Which two is free as long as both
 // operands agree: in groups of eight steps the lower half takes k = 0..7 and the upper one k = 8..15 of a group of 16, so
@@ -238,6 +240,9 @@ struct Args {
   int M, N, K;              // M: WG / WGD, K: ragged-M shapes (per segment)
   const int32_t* off;
   int e_cnt, beta;
+  const float* bias;        // LIN: [e_cnt][N] or NULL
+  const float* R;           // LIN: residual, laid out as y (C[0]), or NULL.  C[1]: z or NULL
+  int act;
 };
 
 // LDS of one k-tile: the three bf16 terms of each operand, or the operands themselves
@@ -246,7 +251,7 @@ template <int MODE> struct Traits {
   static constexpr bool DUAL = MODE == UP || MODE == WGD;
   static constexpr int NB = DUAL ? 2 : 1;
   typedef typename Pick<RAGGED_K, OperMN, OperKC>::type OperA;
-  typedef typename Pick<MODE == DA || MODE == DX, OperKC, OperMN>::type OperB;
+  typedef typename Pick<MODE == DA || MODE == DX || MODE == LDX, OperKC, OperMN>::type OperB;
   static constexpr int SPLIT_BYTES = (1 + NB) * 3 * PLANE_BYTES, PLAIN_BYTES = (OperA::WORDS + NB * OperB::WORDS) * 4;
   static constexpr int BUFFER = SPLIT_BYTES > PLAIN_BYTES ? SPLIT_BYTES : PLAIN_BYTES;
   static constexpr int BLOCKS = DUAL ? 3 : 4;      // per CU, with one LDS buffer
@@ -298,7 +303,7 @@ __device__ __forceinline__ void gemm_tile(const Args& p, int block, char* lds) {
 #pragma unroll
       for (int i = 0; i < NB; ++i) {
         const float* w = p.B[DUAL ? i : seg] + (size_t)e * p.b_es;
-        if constexpr (MODE == DA || MODE == DX) b[i].setup(w + (size_t)col0 * p.ldb, p.ldb, p.N - col0, K, tid);
+        if constexpr (MODE == DA || MODE == DX || MODE == LDX) b[i].setup(w + (size_t)col0 * p.ldb, p.ldb, p.N - col0, K, tid);
         else b[i].setup(w + col0, p.ldb, p.N - col0, K, tid);
       }
     }
@@ -432,6 +437,22 @@ __device__ __forceinline__ void gemm_tile(const Args& p, int block, char* lds) {
   auto finish = [&](uint32_t todo, float scale) {
     const int col = col0 + wn * 32 + (lane & 31);
     if (col >= p.N) return;
+    if constexpr (MODE == LIN) {
+      const float bias = p.bias ? p.bias[(size_t)e * p.N + col] : 0.f;
+      with_activation(p.act, [&](auto a) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int row = row0 + wm * 32 + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3);
+          if (row >= row_end || !(todo >> r & 1)) continue;
+          const size_t idx = (size_t)row * p.ldc + col;
+          const float z = (acc[0][0][r] + acc[0][1][r]) * scale + bias;
+          const float v = act_value<decltype(a)::value, false>(z);
+          if (p.C[1]) p.C[1][idx] = z;
+          p.C[0][idx] = p.R ? v + p.R[idx] : v;
+        }
+      });
+      return;
+    }
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
       float h1[4], h3[4];
@@ -602,4 +623,29 @@ int launch_expert_bwd_f32(const float* xp, const float* h1, const float* h3, con
     if ((rc = launch<WG>(w, wt, s))) return rc;
   }
   return launch_pair<DX, WGD>(x, mtb, v, vt, gradients_first(f), s);
+}
+
+// linear layer, grouped by expert or dense (offsets of one expert)
+int launch_linear_fwd_f32(const LinearArgs& l, hipStream_t s) {
+  Args u = {};
+  u.A[0] = (const float*)l.x; u.lda = l.K; u.B[0] = (const float*)l.w; u.ldb = l.N; u.b_es = (long)l.K * l.N;
+  u.C[0] = (float*)l.y; u.C[1] = (float*)l.z; u.ldc = l.N; u.N = l.N; u.K = l.K; u.off = l.offsets; u.e_cnt = l.e_cnt;
+  u.bias = (const float*)l.bias; u.R = (const float*)l.residual; u.act = l.act;
+  ProfScope prof(MOE_K_LINEAR, s);
+  return launch<LIN>(u, ((long long)l.rows + TM - 1) / TM + l.e_cnt, s);
+}
+
+int launch_linear_bwd_f32(const LinearArgs& l, const void* dz, void* dx, void* dw, int accumulate, hipStream_t s) {
+  Args x = {};
+  x.A[0] = (const float*)dz; x.lda = l.N; x.B[0] = (const float*)l.w; x.ldb = l.N; x.b_es = (long)l.K * l.N;
+  x.C[0] = (float*)dx; x.ldc = l.K; x.N = l.K; x.K = l.N; x.off = l.offsets; x.e_cnt = l.e_cnt;
+  Args w = {};
+  w.A[0] = (const float*)l.x; w.lda = l.K; w.B[0] = (const float*)dz; w.ldb = l.N;
+  w.C[0] = (float*)dw; w.ldc = l.N; w.c_es = (long)l.K * l.N; w.M = l.K; w.N = l.N; w.off = l.offsets; w.e_cnt = l.e_cnt; w.beta = accumulate;
+  const long long mtb = ((long long)l.rows + TM - 1) / TM + l.e_cnt, wt = (long long)l.e_cnt * ((l.K + TM - 1) / TM);
+  const bool have_dx = dx && l.rows > 0;
+  ProfScope prof(have_dx && dw ? MOE_K_LINEAR_DX_DW : dw ? MOE_K_LINEAR_DW : MOE_K_LINEAR_DX, s);
+  if (have_dx && dw) return launch_pair<LDX, WG>(x, mtb, w, wt, 5ll * l.rows > 6ll * l.e_cnt * l.N, s);
+  if (dw) return launch<WG>(w, wt, s);
+  return have_dx ? launch<LDX>(x, mtb, s) : MOE_OK;
 }

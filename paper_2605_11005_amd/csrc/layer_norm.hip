@@ -1,0 +1,353 @@
+// Layer norm between two blocks in one pass: a block's output is added to the residual stream, and the sum is normalised for the next one.
+//     h' = h + y        n = (h' - mean) rstd w + b        rstd = (mean (h' - mean)^2 + eps)^-1/2
+// and its gradient, with t = w dn and xh = (h' - mean) rstd,
+//     dh = dh' + rstd (t - mean t - xh mean(t xh))        dw = sum_t dn xh        db = sum_t dn
+// HBM bound.  A row stays in the registers of its threads, 16 bytes of y or n per thread and step, so that every tensor crosses memory once.
+// The squares are of what is left of a value after its mean: a row whose mean is large beside its deviation keeps its digits.  Each wavefront
+// takes its own mean first, and the wavefronts' sums and squares join behind one barrier: with counts c_w, means m_w and squares q_w,
+//     sum (x - mean)^2 = sum_w q_w + c_w (m_w - mean)^2.
+#include "common.h"
+#include "kernels.h"
+#include "norm_rows.h"
+
+namespace {
+
+// Threads of a row's elements (d up to 16384): fp32 with four steps of four elements takes 1024.
+template <typename T, int STEPS> constexpr int MOST_THREADS = sizeof(T) == 4 && STEPS == 4 ? 1024 : 512;
+
+template <typename T, typename R>
+struct FwdArgs {
+  const T* y; const R* h; const T* w; const T* b;
+  R* h_out; T* n; float* mean; float* rstd;
+  int T_, d;
+  float eps;
+  int row0;                                // of this launch
+};
+
+// A block per row, or (blockDim.y rows) a wavefront per row.
+template <typename T, typename R, int STEPS>
+__global__ __launch_bounds__((MOST_THREADS<T, STEPS>)) void layer_norm_fwd(FwdArgs<T, R> p) {
+  constexpr int N = VEC<T>;
+  __shared__ float2 red[MOST_WAVES];
+  const int row = p.row0 + blockIdx.x * blockDim.y + threadIdx.y;
+  if (row >= p.T_) return;                 // (a block of several rows has no barrier)
+  const int waves = blockDim.x >> 6, wave = threadIdx.x >> 6;
+  const size_t at = (size_t)row * p.d;
+  float h[STEPS][N];
+#pragma unroll
+  for (int i = 0; i < STEPS; ++i) {
+    const int c = (i * blockDim.x + threadIdx.x) * N;
+    float y[N];
+#pragma unroll
+    for (int j = 0; j < N; ++j) y[j] = h[i][j] = 0.f;
+    if (c < p.d) {
+      unpack(p.h, at + c, h[i]);
+      if (p.y) unpack(p.y, at + c, y);
+    }
+#pragma unroll
+    for (int j = 0; j < N; ++j) h[i][j] += y[j];
+    if (p.y && p.h_out && c < p.d) pack(p.h_out, at + c, h[i]);
+  }
+  // of wavefront w: its elements, in all steps
+  const auto count = [&](int w) {
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < STEPS; ++i) n += max(0, min(WAVE * N, p.d - (int)(i * blockDim.x + w * WAVE) * N));
+    return (float)n;
+  };
+  float sum = 0.f;
+#pragma unroll
+  for (int i = 0; i < STEPS; ++i)
+#pragma unroll
+    for (int j = 0; j < N; ++j) sum += h[i][j];
+  sum = wave_total(sum);
+  float mean = sum / fmaxf(count(wave), 1.f), squares = 0.f;
+#pragma unroll
+  for (int i = 0; i < STEPS; ++i) {
+    const bool in = (int)(i * blockDim.x + threadIdx.x) * N < p.d;
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      const float v = h[i][j] - mean;
+      squares += in ? v * v : 0.f;
+    }
+  }
+  squares = wave_total(squares);
+  const float inv_d = 1.f / (float)p.d;
+  if (waves > 1) {
+    if ((threadIdx.x & 63) == 0) red[wave] = make_float2(sum, squares);
+    __syncthreads();
+    sum = squares = 0.f;
+    for (int w = 0; w < waves; ++w) sum += red[w].x;
+    mean = sum * inv_d;
+    for (int w = 0; w < waves; ++w) {
+      const float n = count(w), off = red[w].x / fmaxf(n, 1.f) - mean;
+      squares += red[w].y + n * off * off;
+    }
+  }
+  const float rstd = 1.f / sqrtf(squares * inv_d + p.eps);
+  if (threadIdx.x == 0) {
+    if (p.mean) p.mean[row] = mean;
+    if (p.rstd) p.rstd[row] = rstd;
+  }
+#pragma unroll
+  for (int i = 0; i < STEPS; ++i) {
+    const int c = (i * blockDim.x + threadIdx.x) * N;
+    if (c >= p.d) continue;
+    float w[N], b[N];
+#pragma unroll
+    for (int j = 0; j < N; ++j) { w[j] = 1.f; b[j] = 0.f; }
+    if (p.w) unpack(p.w, c, w);
+    if (p.b) unpack(p.b, c, b);
+#pragma unroll
+    for (int j = 0; j < N; ++j) h[i][j] = (h[i][j] - mean) * rstd * w[j] + b[j];
+    pack(p.n, at + c, h[i]);
+  }
+}
+
+template <typename T, typename R>
+struct BwdArgs {
+  const R* h; const T* w; const float* mean; const float* rstd;
+  const R* dh_out; const T* dn;
+  R* dh; T* dy;
+  float* sums;                             // [blocks][2][d]: dw, db
+  int T_, d;
+};
+
+// What the backward reads of a row
+template <typename T, typename R, int STEPS>
+struct BwdRow {
+  static constexpr int N = VEC<T>;
+  Raw<T, N> dn[STEPS];
+  Raw<R, N> h[STEPS], dh[STEPS];
+  float mean, rstd;
+  __device__ __forceinline__ void load(const BwdArgs<T, R>& p, int row) {
+    const size_t at = (size_t)row * p.d;
+    mean = rstd = 0.f;
+    if (row < p.T_) { mean = p.mean[row]; rstd = p.rstd[row]; }
+#pragma unroll
+    for (int i = 0; i < STEPS; ++i) {
+      const int c = (i * blockDim.x + threadIdx.x) * N;
+      dn[i].clear(); h[i].clear(); dh[i].clear();
+      if (row < p.T_ && c < p.d) {
+        h[i].load(p.h, at + c);
+        dn[i].load(p.dn, at + c);
+        if (p.dh_out) dh[i].load(p.dh_out, at + c);
+      }
+    }
+  }
+};
+
+// Blocks (or, for rows of one wavefront, wavefronts) walk the rows and keep the column sums of theirs in registers; the next row's loads are on
+// their way while a row's sums meet.  For WIDE rows the registers hold neither these nor the weights, and the column sums are in LDS.
+constexpr int BWD_ROWS = 8, BWD_THREADS = 512, WIDE_THREADS = 1024;
+template <typename T, typename R, int STEPS, bool WIDE>
+__global__ __launch_bounds__(WIDE ? WIDE_THREADS : BWD_THREADS) void layer_norm_bwd(BwdArgs<T, R> p) {
+  constexpr int N = VEC<T>;
+  __shared__ float2 red[2][MOST_WAVES];
+  const int waves = blockDim.x >> 6;
+  int turn = 0;
+  const float inv_d = 1.f / (float)p.d;
+  Raw<T, N> w_raw[STEPS];
+  float dw[STEPS][N], db[STEPS][N];
+  extern __shared__ f32x4 column_lds[];               // WIDE: [dw, db][step][four columns][thread]
+  const auto column = [&](int which, int i, int q) -> f32x4& { return column_lds[((which * STEPS + i) * (N / 4) + q) * blockDim.x + threadIdx.x]; };
+  const auto add = [&](int which, int i, float(&sums)[N], const float(&v)[N]) {
+    if constexpr (WIDE) {
+#pragma unroll
+      for (int q = 0; q < N / 4; ++q) column(which, i, q) += f32x4{v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
+    } else {
+#pragma unroll
+      for (int j = 0; j < N; ++j) sums[j] += v[j];
+    }
+  };
+#pragma unroll
+  for (int i = 0; i < STEPS; ++i) {
+    const int c = (i * blockDim.x + threadIdx.x) * N;
+    w_raw[i].clear();
+#pragma unroll
+    for (int j = 0; j < N; ++j) dw[i][j] = db[i][j] = 0.f;
+    if constexpr (WIDE)
+#pragma unroll
+      for (int q = 0; q < N / 4; ++q) column(0, i, q) = column(1, i, q) = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (!WIDE && p.w && c < p.d) w_raw[i].load(p.w, c);
+  }
+  BwdRow<T, R, STEPS> next;
+  int row = blockIdx.x * blockDim.y + threadIdx.y;
+  if (!WIDE) next.load(p, row);
+  for (; row < p.T_; row += gridDim.x * blockDim.y) {
+    const size_t at = (size_t)row * p.d;
+    float xh[STEPS][N], t[STEPS][N], g[STEPS][N];
+    if (WIDE) next.load(p, row);
+    const float mean = next.mean, rstd = next.rstd;
+#pragma unroll
+    for (int i = 0; i < STEPS; ++i) { next.dn[i].values(t[i]); next.h[i].values(xh[i]); next.dh[i].values(g[i]); }
+    if (!WIDE) next.load(p, row + gridDim.x * blockDim.y);
+    float s1 = 0.f, s2 = 0.f;
+#pragma unroll
+    for (int i = 0; i < STEPS; ++i) {
+      const int c = (i * blockDim.x + threadIdx.x) * N;
+      float w[N], v[N];
+      if (WIDE && p.w && c < p.d) w_raw[i].load(p.w, c);
+      w_raw[i].values(w);
+      add(1, i, db[i], t[i]);
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        xh[i][j] = (xh[i][j] - mean) * rstd;
+        v[j] = t[i][j] * xh[i][j];
+        if (p.w) t[i][j] *= w[j];
+        s1 += t[i][j];
+        s2 += t[i][j] * xh[i][j];
+      }
+      add(0, i, dw[i], v);
+    }
+    s1 = wave_total(s1);
+    s2 = wave_total(s2);
+    if (waves > 1) {                       // (two places in turn: one is written again only behind the barrier of the row in between)
+      float2* const place = red[turn];
+      turn ^= 1;
+      if ((threadIdx.x & 63) == 0) place[threadIdx.x >> 6] = make_float2(s1, s2);
+      __syncthreads();
+      s1 = s2 = 0.f;
+      for (int k = 0; k < waves; ++k) { s1 += place[k].x; s2 += place[k].y; }
+    }
+    s1 *= inv_d;
+    s2 *= inv_d;
+#pragma unroll
+    for (int i = 0; i < STEPS; ++i) {
+      const int c = (i * blockDim.x + threadIdx.x) * N;
+#pragma unroll
+      for (int j = 0; j < N; ++j) g[i][j] += rstd * (t[i][j] - s1 - xh[i][j] * s2);
+      if (c < p.d) {
+        if (p.dh) pack(p.dh, at + c, g[i]);
+        if (p.dy) pack(p.dy, at + c, g[i]);
+      }
+    }
+  }
+  if constexpr (!WIDE && STEPS * N <= 16)
+    if (blockDim.y > 1) {                  // a block's wavefronts' sums, in their order
+      __shared__ float part[BWD_ROWS][N][WAVE];
+#pragma unroll
+      for (int k = 0; k < 2 * STEPS; ++k) {
+        float(&v)[N] = k % 2 ? db[k / 2] : dw[k / 2];
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < N; ++j) part[threadIdx.y][j][threadIdx.x] = v[j];
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+          v[j] = 0.f;
+          for (int q = 0; q < (int)blockDim.y; ++q) v[j] += part[q][j][threadIdx.x];
+        }
+      }
+      if (threadIdx.y) return;
+    }
+  float* const out = p.sums + (size_t)blockIdx.x * 2 * p.d;
+#pragma unroll
+  for (int i = 0; i < STEPS; ++i) {
+    const int c = (i * blockDim.x + threadIdx.x) * N;
+    if (c >= p.d) continue;
+    if constexpr (WIDE)
+#pragma unroll
+      for (int j = 0; j < N; ++j) { dw[i][j] = column(0, i, j / 4)[j % 4]; db[i][j] = column(1, i, j / 4)[j % 4]; }
+    pack(out, c, dw[i]);
+    pack(out + p.d, c, db[i]);
+  }
+}
+
+template <typename T, typename R>
+int forward(FwdArgs<T, R> p, hipStream_t s) {
+  const int vecs = p.d / VEC<T>;
+  int steps = 1;
+  while (row_threads(vecs, steps) > 512 && steps < 4) steps *= 2;
+  if (vecs > WAVE && vecs <= 3 * WAVE / 2) steps = 2;
+  const int threads = row_threads(vecs, steps), rows = threads == WAVE ? 4 : 1;
+  const dim3 block(threads, rows);
+  return in_launches(((long long)p.T_ + rows - 1) / rows, threads * rows, [&](long long first, unsigned blocks) {
+    p.row0 = (int)first * rows;
+    if (steps == 1) hipLaunchKernelGGL((layer_norm_fwd<T, R, 1>), dim3(blocks), block, 0, s, p);
+    else if (steps == 2) hipLaunchKernelGGL((layer_norm_fwd<T, R, 2>), dim3(blocks), block, 0, s, p);
+    else hipLaunchKernelGGL((layer_norm_fwd<T, R, 4>), dim3(blocks), block, 0, s, p);
+  });
+}
+
+// The backward's launch: rows of up to 16 elements a lane in one wavefront, several of them in a block; longer rows in a block each.
+struct BwdPlan { int steps, threads, rows, most, blocks; bool wide; };
+inline BwdPlan bwd_plan(int T, int d, int vec) {
+  constexpr int CUS = 256;
+  const int vecs = d / vec, per = 16 / vec;          // steps of 16 elements
+  BwdPlan b;
+  b.wide = row_threads(vecs, per) > BWD_THREADS;
+  if (row_threads(vecs, 1) == WAVE) b.steps = 1;
+  else if (b.wide || row_threads(vecs, per) == WAVE) b.steps = per;
+  else b.steps = row_threads(vecs, 1) <= BWD_THREADS ? 1 : row_threads(vecs, 2) <= BWD_THREADS ? 2 : per;
+  b.threads = row_threads(vecs, b.steps);
+  const int per_cu = b.steps * vec == 16 ? 1 : b.threads > WAVE && b.threads <= 256 && T >= 8192 ? 4 : 2;
+  b.most = T < per_cu * CUS ? T : per_cu * CUS;
+  b.rows = b.threads > WAVE ? 1 : T >= per_cu * CUS * BWD_ROWS ? BWD_ROWS : T == 0 ? 1 : (T - 1) / (per_cu * CUS) + 1;
+  const int units = T == 0 ? 0 : (T - 1) / b.rows + 1;
+  b.blocks = units < b.most ? units : b.most;
+  return b;
+}
+
+template <typename T, typename R>
+int backward(BwdArgs<T, R> p, T* dw, T* db, int accumulate, hipStream_t s) {
+  const BwdPlan plan = bwd_plan(p.T_, p.d, VEC<T>);
+  const int steps = plan.steps, blocks = plan.blocks;
+  const dim3 grid(blocks), block(plan.threads, plan.rows);
+  constexpr int PER = 16 / VEC<T>;
+  if (p.T_ > 0) {
+    ProfScope prof(MOE_K_LAYER_NORM_BWD, s);
+    if (plan.wide) {
+      const size_t lds = 2 * sizeof(float) * 16 * plan.threads;
+      static bool attr_set[64] = {};
+      int dev = 0;
+      if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return MOE_EHIP;
+      if (!attr_set[dev]) {
+        if (hipFuncSetAttribute(reinterpret_cast<const void*>(&layer_norm_bwd<T, R, PER, true>), hipFuncAttributeMaxDynamicSharedMemorySize,
+                                2 * sizeof(float) * 16 * WIDE_THREADS) != hipSuccess)
+          return MOE_EHIP;
+        attr_set[dev] = true;
+      }
+      hipLaunchKernelGGL((layer_norm_bwd<T, R, PER, true>), grid, block, lds, s, p);
+    }
+    else if (steps == 1) hipLaunchKernelGGL((layer_norm_bwd<T, R, 1, false>), grid, block, 0, s, p);
+    else if (steps == 2) hipLaunchKernelGGL((layer_norm_bwd<T, R, 2, false>), grid, block, 0, s, p);
+    else hipLaunchKernelGGL((layer_norm_bwd<T, R, PER, false>), grid, block, 0, s, p);
+    HIP_CHECK_LAUNCH();
+  }
+  if (dw || db) {
+    ProfScope prof(MOE_K_LAYER_NORM_SUMS, s);
+    hipLaunchKernelGGL(column_sums<T>, dim3((p.d + WAVE - 1) / WAVE, 2), dim3(SUM_WAVES * WAVE), 0, s, p.sums, blocks, p.d, accumulate, dw, db);
+    HIP_CHECK_LAUNCH();
+  }
+  return MOE_OK;
+}
+
+}  // namespace
+
+// For T rows and fewer, of bf16 or fp32
+size_t layer_norm_ws_bytes(int T, int d) {
+  const int a = bwd_plan(T, d, 8).most, b = bwd_plan(T, d, 4).most;
+  return (size_t)(a > b ? a : b) * 2 * d * sizeof(float);
+}
+
+int launch_layer_norm_fwd(const void* y, const void* h, const void* w, const void* b, int dtype, int res_dtype, int T, int d, float eps, void* h_out,
+                          void* n, float* mean, float* rstd, hipStream_t s) {
+  if (T == 0) return MOE_OK;
+  ProfScope prof(MOE_K_LAYER_NORM_FWD, s);
+  return by_types(dtype, res_dtype, [&](auto* t, auto* r) {
+    typedef std::remove_pointer_t<decltype(t)> X;
+    typedef std::remove_pointer_t<decltype(r)> R;
+    return forward(FwdArgs<X, R>{(const X*)y, (const R*)h, (const X*)w, (const X*)b, (R*)h_out, (X*)n, mean, rstd, T, d, eps}, s);
+  });
+}
+
+int launch_layer_norm_bwd(const void* h_out, const void* w, const float* mean, const float* rstd, const void* dh_out, const void* dn, int dtype,
+                          int res_dtype, int T, int d, void* dh, void* dy, void* dw, void* db, int accumulate, void* ws, hipStream_t s) {
+  return by_types(dtype, res_dtype, [&](auto* t, auto* r) {
+    typedef std::remove_pointer_t<decltype(t)> X;
+    typedef std::remove_pointer_t<decltype(r)> R;
+    return backward(BwdArgs<X, R>{(const R*)h_out, (const X*)w, mean, rstd, (const R*)dh_out, (const X*)dn, (R*)dh, (X*)dy, (float*)ws, T, d},
+                    (X*)dw, (X*)db, accumulate, s);
+  });
+}

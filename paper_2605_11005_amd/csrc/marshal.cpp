@@ -38,6 +38,10 @@ struct Entry {
   decltype(&moe_mx4_quantize) mx4_quantize;
   decltype(&moe_mx4_dequantize) mx4_dequantize;
   decltype(&moe_mx4_expert_fwd) mx4_expert_fwd;
+  decltype(&moe_layer_norm_fwd) layer_norm_fwd;
+  decltype(&moe_layer_norm_bwd) layer_norm_bwd;
+  decltype(&moe_linear_fwd) linear_fwd;
+  decltype(&moe_linear_bwd) linear_bwd;
 } entry;
 constexpr int N_ENTRIES = sizeof(Entry) / sizeof(void*);
 
@@ -474,6 +478,120 @@ PyObject* mx4_expert_fwd(PyObject*, PyObject* const* v, Py_ssize_t n) {
   });
 }
 
+PyObject* layer_norm_fwd(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  return take(v, n, [](Args& a) {
+    const Buf y = any(a, true), h = any(a), w = any(a, true), b = any(a, true);
+    const float eps = a.real();
+    const Buf h_out = any(a, true), out = any(a), mean = any(a, true), rstd = any(a, true);
+    dims(h, 2);
+    const auto t = out.t->scalar_type(), rt = h.t->scalar_type();
+    const Rows r{h.size(0), h.size(1)};
+    const int T = small(r.T), d = small(r.d), dt = dtype_code(out), res = dtype_code(h);
+    for (const Buf* m : {&y, &out}) r.matrix(*m, t);
+    r.matrix(h_out, rt);
+    for (const Buf* m : {&w, &b}) r.vector(*m, t);
+    for (const Buf* m : {&mean, &rstd}) r.per_row(*m);
+    return [=, s = stream()] {
+      return entry.layer_norm_fwd(y.ptr, h.ptr, w.ptr, b.ptr, dt, res, T, d, eps, h_out.ptr, out.ptr, (float*)mean.ptr, (float*)rstd.ptr, s);
+    };
+  });
+}
+
+PyObject* layer_norm_bwd(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  return take(v, n, [](Args& a) {
+    const Buf h = any(a), w = any(a, true), mean = any(a), rstd = any(a), dh_out = any(a, true), dn = any(a), dh = any(a, true), dy = any(a, true),
+              dw = any(a, true), db = any(a, true);
+    const int accumulate = a.flag();
+    const Buf ws = any(a);
+    dims(h, 2);
+    const auto t = dn.t->scalar_type(), rt = h.t->scalar_type();
+    const Rows r{h.size(0), h.size(1)};
+    const int T = small(r.T), d = small(r.d), dt = dtype_code(dn), res = dtype_code(h);
+    for (const Buf* m : {&dn, &dy}) r.matrix(*m, t);
+    for (const Buf* m : {&dh_out, &dh}) r.matrix(*m, rt);
+    for (const Buf* m : {&w, &dw, &db}) r.vector(*m, t);
+    for (const Buf* m : {&mean, &rstd}) r.per_row(*m);
+    const size_t ws_bytes = (size_t)ws.bytes();
+    return [=, s = stream()] {
+      return entry.layer_norm_bwd(h.ptr, w.ptr, (const float*)mean.ptr, (const float*)rstd.ptr, dh_out.ptr, dn.ptr, dt, res, T, d, dh.ptr, dy.ptr,
+                                  dw.ptr, db.ptr, accumulate, ws.ptr, ws_bytes, s);
+    };
+  });
+}
+
+// the sizes of a linear layer, from rows [cap,K] and weights [K,N] without offsets, [e_cnt,K,N] with them
+struct Linear {
+  int cap, K, N, e_cnt;
+  bool grouped;
+  at::ScalarType t;
+  Linear(const Buf& x, const Buf& off, const Buf& w) : grouped(off.t != nullptr), t(x.t->scalar_type()) {
+    dims(x, 2);
+    dims(w, grouped ? 3 : 2);
+    cap = small(x.size(0));
+    e_cnt = grouped ? small(w.size(0)) : 1;
+    K = small(w.size(grouped ? 1 : 0));
+    N = small(w.size(grouped ? 2 : 1));
+    rows(x, K);
+    if (w.t->scalar_type() != t) refuse();
+    shaped(off, {(int64_t)e_cnt + 1});
+  }
+  void typed_as(const Buf& b) const {
+    if (b.t && b.t->scalar_type() != t) refuse();
+  }
+  void rows(const Buf& b, int width) const {
+    typed_as(b);
+    shaped(b, {cap, width});
+  }
+  void matrix(const Buf& b) const {
+    typed_as(b);
+    if (grouped) shaped(b, {e_cnt, K, N});
+    else shaped(b, {K, N});
+  }
+  void bias(const Buf& b) const {
+    typed_as(b);
+    if (grouped) shaped(b, {e_cnt, N});
+    else shaped(b, {N});
+  }
+};
+
+PyObject* linear_fwd(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  return take(v, n, [](Args& a) {
+    const Buf x = any(a), off = typed(a, I32, true), w = any(a), bias = any(a, true);
+    const int act = a.integer();
+    const Buf residual = any(a, true), z = any(a, true), y = any(a), ws = any(a);
+    const Linear l(x, off, w);
+    l.bias(bias);
+    for (const Buf* m : {&residual, &z, &y}) l.rows(*m, l.N);
+    const int dt = dtype_code(x);
+    const size_t ws_bytes = (size_t)ws.bytes();
+    return [=, s = stream()] {
+      return entry.linear_fwd(x.ptr, dt, l.cap, l.K, l.N, l.e_cnt, (const int32_t*)off.ptr, w.ptr, bias.ptr, act, residual.ptr, z.ptr, y.ptr, ws.ptr,
+                              ws_bytes, s);
+    };
+  });
+}
+
+PyObject* linear_bwd(PyObject*, PyObject* const* v, Py_ssize_t n) {
+  return take(v, n, [](Args& a) {
+    const Buf x = any(a), z = any(a, true), dy = any(a), off = typed(a, I32, true), w = any(a);
+    const int act = a.integer();
+    const Buf dx = any(a, true), dw = any(a, true), db = any(a, true);
+    const int accumulate = a.flag();
+    const Buf ws = any(a);
+    const Linear l(x, off, w);
+    for (const Buf* m : {&z, &dy}) l.rows(*m, l.N);
+    l.rows(dx, l.K);
+    l.matrix(dw);
+    l.bias(db);
+    const int dt = dtype_code(x);
+    const size_t ws_bytes = (size_t)ws.bytes();
+    return [=, s = stream()] {
+      return entry.linear_bwd(x.ptr, z.ptr, dy.ptr, dt, l.cap, l.K, l.N, l.e_cnt, (const int32_t*)off.ptr, w.ptr, act, dx.ptr, dw.ptr, db.ptr,
+                              accumulate, ws.ptr, ws_bytes, s);
+    };
+  });
+}
+
 // bind(addresses): the entry points in the order of Entry
 PyObject* bind(PyObject*, PyObject* const* v, Py_ssize_t n) {
   if (n != N_ENTRIES) {
@@ -493,7 +611,8 @@ PyObject* bind(PyObject*, PyObject* const* v, Py_ssize_t n) {
 #define METHOD(name) {#name, (PyCFunction)(void (*)(void))name, METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {METHOD(route),    METHOD(dispatch),   METHOD(dispatch_static), METHOD(expert_fwd), METHOD(expert_bwd), METHOD(combine),
                          METHOD(router_fwd), METHOD(combine_bwd), METHOD(gate_bwd),      METHOD(router_bwd), METHOD(block_norm_fwd), METHOD(block_norm_bwd),
-                         METHOD(mx4_quantize), METHOD(mx4_dequantize), METHOD(mx4_expert_fwd), METHOD(bind), {nullptr, nullptr, 0, nullptr}};
+                         METHOD(mx4_quantize), METHOD(mx4_dequantize), METHOD(mx4_expert_fwd), METHOD(layer_norm_fwd),
+                         METHOD(layer_norm_bwd), METHOD(linear_fwd), METHOD(linear_bwd), METHOD(bind), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods};
 
 }  // namespace
