@@ -1,5 +1,6 @@
 // The C ABI (include/moe.h): argument validation on the host, then kernel launches.
 #include "kernels.h"
+#include "linear.h"
 
 #include <algorithm>
 #include <mutex>

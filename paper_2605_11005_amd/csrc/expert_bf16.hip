@@ -37,7 +37,9 @@
 // ragged-M shapes a second list of 128x128 tiles (quarter tiles) follows where that ends sooner.
 #include "activation.h"
 #include "few_rows.h"
+#include "tile128.h"
 #include "kernels.h"
+#include "linear.h"
 
 namespace {
 
@@ -55,12 +57,7 @@ __device__ __forceinline__ uint4 load16_once(const void* ptr) {
   return __builtin_bit_cast(uint4, __builtin_nontemporal_load(reinterpret_cast<const u32x4_t*>(ptr)));
 }
 
-typedef short s16x4 __attribute__((ext_vector_type(4)));
-typedef short s16x8 __attribute__((ext_vector_type(8)));
-typedef float f32x16 __attribute__((ext_vector_type(16)));
-
 constexpr int BM = 256, BN = 256, BK = 32;
-constexpr int QT = 128, QK = 64;        // quarter tiles
 constexpr int NT = 256;                 // threads
 constexpr int NSTAGE = 4;
 constexpr int OPER_BYTES = 256 * BK * 2;           // 16384: one operand tile
@@ -182,8 +179,6 @@ struct KcPairIssue {
   }
   static __device__ __forceinline__ int chunk(int q, int lane) { return (lane & 7) ^ (4 * (q & 1) + (lane >> 4)); }
 };
-// Bytes that a load of the chunk of 8 k at k goes back by so as not to read past the contraction's K
-__device__ __forceinline__ uint32_t past_end(int k, int K) { return 2u * (uint32_t)max(0, k - (K - 8)); }
 
 // ---- transposed operand (source is [k][n], n contiguous) --------------------------------
 // Kept in LDS as two sub-tiles [32 k][128 n] of 8 KB (for a dual tile they come from two
@@ -240,7 +235,6 @@ __device__ __forceinline__ int tr_frag_off(int nb, int lane) {
   return sub * 8192 + k * 256 + (((nl >> 3) ^ (4 * (k & 3))) << 4) + ((n & 4) << 1);
 }
 
-__device__ __forceinline__ bf16x8 lds_frag_kc(const char* p) { return *reinterpret_cast<const bf16x8*>(p); }
 __device__ __forceinline__ bf16x8 lds_frag_tr(const char* p) {
   s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(p));
   s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(p + 1024));
@@ -430,57 +424,8 @@ __device__ __forceinline__ void finish_lin(const GArgs& p, size_t idx, float* x,
 // multiplied in quarters.  The four wavefronts hold 64x64 each; a k-tile is 64 deep, so that every load fetches whole cache
 // lines of either operand, and four of them (128 KB) make the ring.  Every output is the same chain of sums as in a 256x256
 // tile, bit for bit.
-//   K-contiguous operand   [128 rows][8 chunks of 8 k]       chunk' = chunk ^ ((row>>1)&7)
-//   transposed operand     2 x [64 k][8 chunks of 8 n]       chunk' = chunk ^ (4*((k>>1)&1))
-constexpr int QOPER_BYTES = QT * QK * 2;
+//   (layouts: tile128.h)
 static_assert(NSTAGE * 2 * QOPER_BYTES == TILE_LDS, "the ring holds four k-tiles of quarter tiles");
-
-struct QuarterKc {         // load j of a wavefront: rows 8*(4w+j) + lane/8, whole 128-byte lines
-  const bf16_t* base;
-  uint32_t voff[4];
-  __device__ __forceinline__ void setup(const bf16_t* base_, long ld, int rows_valid, int wave, int lane) {
-    base = base_;
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int rl = 8 * (4 * wave + j) + (lane >> 3);
-      const int c = (lane & 7) ^ ((rl >> 1) & 7);
-      voff[j] = (uint32_t)(min(rl, rows_valid - 1) * ld * 2 + c * 16);
-    }
-  }
-  __device__ __forceinline__ void issue1(int j, uint32_t oper_lds, int wave, long kofs, uint32_t back = 0) const {
-    lds_load16(base + kofs, voff[j] - back, oper_lds + (4 * wave + j) * 1024);
-  }
-  static __device__ __forceinline__ int chunk(int j, int lane) { return (lane & 7) ^ (4 * (j & 1) + (lane >> 4)); }
-};
-struct QuarterTr {         // sub-tile wave/2, load j: k rows 8*(4*(w%2)+j) + lane/8, 64 columns each
-  const bf16_t* src;
-  long ld;
-  uint32_t coff;
-  __device__ __forceinline__ void setup(const bf16_t* b0, const bf16_t* b1, bool dual, long ld_, int n0, int n_lim, int wave, int lane) {
-    ld = ld_;
-    const int sub = wave >> 1, c = (lane & 7) ^ (4 * ((lane >> 4) & 1));
-    src = (dual && sub) ? b1 : b0;
-    coff = (uint32_t)(2 * min(n0 + (dual ? 0 : sub * 64) + c * 8, n_lim - 8));
-  }
-  template <bool CLAMP>    // source rows above k_last_rel are clamped (the caller zeroes the matching A fragments)
-  __device__ __forceinline__ void issue1(int j, uint32_t oper_lds, int wave, int lane, long k0, int k_last_rel) const {
-    int kr = 8 * (4 * (wave & 1) + j) + (lane >> 3);
-    if (CLAMP && kr > k_last_rel) kr = k_last_rel;
-    lds_load16(src + k0 * ld, (uint32_t)(kr * ld * 2) + coff, oper_lds + (4 * wave + j) * 1024);
-  }
-};
-// transposed sub-tile: byte offset of the first transposing read of 32 columns at nl (0 or 32), k-step 0; add s*2048 + t*512
-__device__ __forceinline__ int quarter_tr_off(int sub, int nl, int lane) {
-  const int i = lane & 15, g = lane >> 4;
-  const int k = 8 * (g >> 1) + (i >> 2);
-  const int n = nl + 16 * (g & 1) + 4 * (i & 3);
-  return sub * 8192 + k * 128 + (((n >> 3) ^ (4 * ((k >> 1) & 1))) << 4) + ((n & 4) << 1);
-}
-__device__ __forceinline__ bf16x8 quarter_frag_tr(const char* p) {
-  s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(p));
-  s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(p + 512));
-  return __builtin_bit_cast(bf16x8, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
-}
 
 // The list of quarter tiles: positions in order[], each with the rows that its 256-row tiles leave.
 struct Quarters {
@@ -2054,7 +1999,7 @@ size_t expert_bwd_extra_ws_bytes(int d, int f) { return 256 + WGRAD_PLAN_BYTES +
 
 // ---- linear layer, grouped by expert or dense --------------------------------------------------------------------------
 // The rows of expert e are [offsets[e], offsets[e+1]); offsets NULL: one matrix, all rows.
-int launch_linear_fwd_tiles(const LinearArgs& l, int32_t* sched, hipStream_t s) {
+int launch_linear_fwd_large(const LinearArgs& l, int32_t* sched, hipStream_t s) {
   GArgs g = {};
   g.A0 = g.A1 = (const bf16_t*)l.x; g.lda = l.K;
   g.B0 = g.B1 = (const bf16_t*)l.w; g.ldb = l.N; g.b_es = (long)l.K * l.N;
@@ -2072,7 +2017,7 @@ size_t linear_split_bytes(int K, int N) {
 }
 
 // dx = dz W^T and dW (+)= x^T dz; either may be left out.  ws: plan of MOE_MAX_LOCAL words, then linear_split_bytes
-int launch_linear_bwd_tiles(const LinearArgs& l, const void* dz, void* dx, void* dw, int accumulate, int32_t* sched, void* ws, hipStream_t s) {
+int launch_linear_bwd_large(const LinearArgs& l, const void* dz, void* dx, void* dw, int accumulate, int32_t* sched, void* ws, hipStream_t s) {
   const long mn = (long)l.K * l.N;
   GArgs x = {};
   x.A0 = x.A1 = (const bf16_t*)dz; x.lda = l.N;

@@ -29,6 +29,7 @@
 #include "activation.h"
 #include "common.h"
 #include "kernels.h"
+#include "linear.h"
 
 namespace {
 

@@ -110,23 +110,6 @@ int launch_layer_norm_fwd(const void* y, const void* h, const void* w, const voi
 int launch_layer_norm_bwd(const void* h_out, const void* w, const float* mean, const float* rstd, const void* dh_out, const void* dn, int dtype,
                           int res_dtype, int T, int d, void* dh, void* dy, void* dw, void* db, int accumulate, void* ws, hipStream_t s);
 
-// linear layer, grouped by expert or dense (linear.hip; its products in expert_bf16.hip and expert_f32.hip)
-struct LinearArgs {
-  const void *x, *w, *bias, *residual;
-  void *z, *y;
-  int dtype, rows, K, N, e_cnt, act;
-  const int32_t* offsets;                 // NULL: one matrix, all rows
-};
-size_t linear_fwd_ws_bytes(int dtype, int rows, int K, int N, int e_cnt);
-size_t linear_bwd_ws_bytes(int dtype, int rows, int K, int N, int e_cnt);
-int launch_linear_fwd(const LinearArgs& l, void* ws, hipStream_t s);
-int launch_linear_bwd(const LinearArgs& l, const void* dy, void* dx, void* dw, void* db, int accumulate, void* ws, hipStream_t s);
-int launch_linear_fwd_tiles(const LinearArgs& l, int32_t* sched, hipStream_t s);
-size_t linear_split_bytes(int K, int N);
-int launch_linear_bwd_tiles(const LinearArgs& l, const void* dz, void* dx, void* dw, int accumulate, int32_t* sched, void* ws, hipStream_t s);
-int launch_linear_fwd_f32(const LinearArgs& l, hipStream_t s);
-int launch_linear_bwd_f32(const LinearArgs& l, const void* dz, void* dx, void* dw, int accumulate, hipStream_t s);
-
 // microscaled 4 bits (mx4.hip, mx4_experts.hip)
 int launch_mx4_quantize(const void* x, int dtype, int batch, int n, int K, int along_rows, uint8_t* data, uint8_t* scales, hipStream_t s);
 int launch_mx4_dequantize(const uint8_t* data, const uint8_t* scales, int batch, int n, int K, void* out, int dtype, hipStream_t s);

@@ -4,18 +4,21 @@
 // The products are those of expert_bf16.hip and expert_f32.hip; here are what surrounds them, dz with the sums of its columns, and which
 // kernel a call takes.
 #include "activation.h"
+#include "bias_grad.h"
 #include "common.h"
 #include "kernels.h"
+#include "linear.h"
 
 namespace {
 
 typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int SETUP_WORDS = 64;            // ticket counters, then the row offsets of a dense call
-__global__ void linear_setup(int32_t* words, int rows) {
+__device__ __forceinline__ void write_setup(int32_t* words, int rows) {
   const int i = threadIdx.x;
   if (i < SETUP_WORDS + 2) words[i] = i == SETUP_WORDS + 1 ? rows : 0;
 }
+__global__ void linear_setup(int32_t* words, int rows) { write_setup(words, rows); }
 
 template <typename T> constexpr int VEC = 16 / sizeof(T);
 __device__ __forceinline__ void values(u32x4 w, float (&v)[8]) {
@@ -34,20 +37,28 @@ __device__ __forceinline__ u32x4 words(const float (&v)[4]) {
 }
 
 // dz = dy act'(z), rounded to the type that the products take, and the column sums of what it was before, over 64 rows of an expert by
-// 64 lanes' 16 bytes.  Four wavefronts take every fourth row each; their sums meet in ascending order.  HBM bound: dy and z in, dz out.
+// 64 lanes' 16 bytes.  Eight wavefronts take every eighth row each; their sums meet in ascending order.  HBM bound: dy and z in, dz out.
 // The sums of row tile i of expert e go to line offsets[e] / 64 + e + i: lines of different tiles differ, as floor((o + n) / 64) + 1 >=
 // floor(o / 64) + ceil(n / 64).
-constexpr int SUM_ROWS = 64, GRAD_WAVES = 4;
+constexpr int SUM_ROWS = LINEAR_SUM_ROWS, GRAD_WAVES = 8;
 inline long long sum_lines(int rows, int e_cnt) { return rows / SUM_ROWS + (long long)e_cnt; }
 template <typename T>
-__global__ __launch_bounds__(GRAD_WAVES * WAVE) void act_grad(const int32_t* __restrict__ off, int e_cnt, int N, int act, const T* __restrict__ dy,
-                                                              const T* __restrict__ z, T* __restrict__ dz, float* __restrict__ sums) {
+__global__ __launch_bounds__(GRAD_WAVES * WAVE) void act_grad(const int32_t* __restrict__ off, int rows, int e_cnt, int N, int act,
+                                                              const T* __restrict__ dy, const T* __restrict__ z, T* __restrict__ dz,
+                                                              float* __restrict__ sums, int32_t* __restrict__ setup) {
+  if (setup && blockIdx.x == 0) write_setup(setup, rows);
   constexpr int V = VEC<T>, WIDTH = WAVE * V;
   __shared__ float part[GRAD_WAVES][V][WAVE];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  int e, row_tile, col_tile;
-  if (!RaggedTiles<SUM_ROWS>(off, e_cnt, lane).tile((N + WIDTH - 1) / WIDTH, blockIdx.x, e, row_tile, col_tile)) return;
-  const int first = off[e], row0 = first + row_tile * SUM_ROWS, end = min(off[e + 1], row0 + SUM_ROWS);
+  const int cols = (N + WIDTH - 1) / WIDTH;
+  int e = 0, row_tile = blockIdx.x / cols, col_tile = blockIdx.x % cols, first = 0;
+  if (off) {
+    if (!RaggedTiles<SUM_ROWS>(off, e_cnt, lane).tile(cols, blockIdx.x, e, row_tile, col_tile)) return;
+    first = off[e];
+    rows = off[e + 1];
+  }
+  const int row0 = first + row_tile * SUM_ROWS, end = min(rows, row0 + SUM_ROWS);
+  if (row0 >= end) return;
   const int c = col_tile * WIDTH + lane * V;
   float sum[V];
 #pragma unroll
@@ -55,7 +66,7 @@ __global__ __launch_bounds__(GRAD_WAVES * WAVE) void act_grad(const int32_t* __r
   if (c < N)
     with_activation(act, [&](auto a) {
       constexpr int ACT = decltype(a)::value;
-#pragma unroll 4
+#pragma unroll 8
       for (int row = row0 + wave; row < end; row += GRAD_WAVES) {
         const size_t at = (size_t)row * N + c;
         float g[V];
@@ -86,47 +97,75 @@ __global__ __launch_bounds__(GRAD_WAVES * WAVE) void act_grad(const int32_t* __r
   }
 }
 
-// db of expert blockIdx.y from the sums of its row tiles, in ascending order: wavefront w of 16 adds the w-th part of them, 64 columns a block.
-constexpr int BIAS_WAVES = 16;
+// db, where no launch of the products takes it along
 template <typename T>
-__global__ __launch_bounds__(BIAS_WAVES * WAVE) void bias_grad(const int32_t* __restrict__ off, int N, const float* __restrict__ sums, int accumulate,
-                                                               T* __restrict__ db) {
-  __shared__ float part[BIAS_WAVES][WAVE];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = blockIdx.x * WAVE + lane, e = blockIdx.y;
-  const int first = off[e], tiles = (off[e + 1] - first + SUM_ROWS - 1) / SUM_ROWS;
-  const int share = (tiles + BIAS_WAVES - 1) / BIAS_WAVES, end = min(tiles, (wave + 1) * share);
-  const float* const line = sums + ((size_t)(first / SUM_ROWS) + e) * N;
-  float s = 0.f;
-  if (c < N)
-#pragma unroll 8
-    for (int i = wave * share; i < end; ++i) s += line[(size_t)i * N + c];
-  part[wave][lane] = s;
-  __syncthreads();
-  if (wave || c >= N) return;
-  s = 0.f;
-#pragma unroll
-  for (int w = 0; w < BIAS_WAVES; ++w) s += part[w][lane];
-  T* const to = db + (size_t)e * N + c;
-  if constexpr (sizeof(T) == 2) *to = (bf16_t)pack_bf16x2(accumulate ? bf16_to_f32(*to) + s : s, 0.f);      // (the hardware's conversion keeps every NaN)
-  else *to = accumulate ? *to + s : s;
+__global__ __launch_bounds__(BIAS_THREADS) void bias_grad(BiasGrad p) {
+  __shared__ float part[BIAS_THREADS];
+  bias_columns<T>(p, blockIdx.x, part);
 }
 
 template <typename T>
-int gradients(const LinearArgs& l, const int32_t* off, const void* dy, void* dz, void* db, float* sums, int accumulate, hipStream_t s) {
+int gradients(const LinearArgs& l, const void* dy, void* dz, float* sums, int32_t* setup, hipStream_t s) {
   constexpr int WIDTH = WAVE * VEC<T>;
-  if (l.rows > 0) {
+  {
     ProfScope prof(MOE_K_LINEAR_ACT, s);
     const long long tiles = ((long long)(l.rows + SUM_ROWS - 1) / SUM_ROWS + l.e_cnt) * ((l.N + WIDTH - 1) / WIDTH);
-    hipLaunchKernelGGL(act_grad<T>, dim3((unsigned)((tiles + 7) / 8 * 8)), dim3(GRAD_WAVES * WAVE), 0, s, off, l.e_cnt, l.N, l.act, (const T*)dy,
-                       (const T*)l.z, (T*)dz, db ? sums : nullptr);
-    HIP_CHECK_LAUNCH();
-  }
-  if (db) {
-    ProfScope prof(MOE_K_LINEAR_BIAS, s);
-    hipLaunchKernelGGL(bias_grad<T>, dim3((l.N + WAVE - 1) / WAVE, l.e_cnt), dim3(BIAS_WAVES * WAVE), 0, s, off, l.N, sums, accumulate, (T*)db);
+    hipLaunchKernelGGL(act_grad<T>, dim3((unsigned)((tiles + 7) / 8 * 8)), dim3(GRAD_WAVES * WAVE), 0, s, l.offsets, l.rows, l.e_cnt, l.N, l.act, (const T*)dy,
+                       (const T*)l.z, (T*)dz, sums, setup);
     HIP_CHECK_LAUNCH();
   }
   return MOE_OK;
+}
+
+enum Route { FEW_ROWS, TILES, LARGE };
+#ifndef FWD_ROUTE
+#define FWD_ROUTE -1
+#define BWD_ROUTE -1
+#endif
+// Time in us of the 256x256 tiles, with all experts alike: whole rounds of the chip, each tile by the length of its contraction
+struct Large {
+  long long n;             // tiles
+  float each;
+};
+inline long long tiles256(int n) { return (n + 255) / 256; }
+inline Large large_rows(const LinearArgs& l, int N, int K) {
+  const long long per = (l.rows + l.e_cnt - 1) / l.e_cnt;
+  return {l.e_cnt * tiles256((int)per) * tiles256(N), 0.026f * (float)K + 3.f};
+}
+inline float large_fwd_time(const LinearArgs& l) {
+  const Large f = large_rows(l, l.N, l.K);
+  return 10.f + (float)((f.n + 255) / 256) * f.each;
+}
+// dx's tiles first, dW's after them by whoever is free: CUs that ran a last tile of dx, and the others
+inline float large_bwd_time(const LinearArgs& l, bool dx, bool dw) {
+  const Large x = dx ? large_rows(l, l.K, l.N) : Large{0, 0.f};
+  const long long per = (l.rows + l.e_cnt - 1) / l.e_cnt;
+  const float each = 0.027f * (float)per + 6.f;
+  long long left = dw ? l.e_cnt * tiles256(l.K) * tiles256(l.N) : 0;
+  const long long late = x.n % 256, early = 256 - late;
+  float at_early = (float)(x.n / 256) * x.each, at_late = at_early + (late ? x.each : 0.f);
+  if (left > 16384) {                                // (many rounds: everybody ends together)
+    const float mean = ((float)early * at_early + (float)late * at_late) / 256.f;
+    at_early = at_late = mean + (float)(left / 256) * each;
+    left %= 256;
+  }
+  while (left > 0) {
+    const bool e = at_early <= at_late || !late;
+    left -= e ? early : late;
+    (e ? at_early : at_late) += each;
+  }
+  return 15.f + (at_early > at_late ? at_early : at_late);
+}
+Route forward_route(const LinearArgs& l) {
+  if (l.dtype != MOE_BF16) return LARGE;
+  if (FWD_ROUTE >= 0) return (Route)FWD_ROUTE;
+  if (l.rows <= 32ll * l.e_cnt) return FEW_ROWS;
+  return linear_tiles_fwd_time(l) <= large_fwd_time(l) ? TILES : LARGE;
+}
+Route backward_route(const LinearArgs& l, bool dx, bool dw) {
+  if (l.dtype != MOE_BF16) return LARGE;
+  if (BWD_ROUTE >= 0) return (Route)BWD_ROUTE;
+  return linear_tiles_bwd_time(l, dx, dw) <= large_bwd_time(l, dx, dw) ? TILES : LARGE;
 }
 
 inline size_t align256(size_t v) { return (v + 255) & ~(size_t)255; }
@@ -134,28 +173,41 @@ constexpr size_t SETUP_BYTES = 512;
 static_assert((SETUP_WORDS + 2) * 4 <= SETUP_BYTES, "");
 // The backward's workspace: what linear_setup writes, dz, the column sums, then what the products of bf16 take
 struct BwdSpace {
-  size_t dz, sums, products, end;
+  size_t dz, sums, products, dw_parts, end;
   BwdSpace(int dtype, int rows, int K, int N, int e_cnt) {
     dz = SETUP_BYTES;
     sums = dz + align256((size_t)rows * N * (dtype == MOE_BF16 ? 2 : 4));
     products = sums + align256((size_t)sum_lines(rows, e_cnt) * N * 4);
-    end = products + (dtype == MOE_BF16 ? MOE_MAX_LOCAL * 4 + linear_split_bytes(K, N) : 0);
+    dw_parts = products + linear_parts_bytes(rows, K);
+    end = products;
+    if (dtype == MOE_BF16) {
+      const size_t parts = dw_parts + linear_parts_bytes((long long)e_cnt * K, N), pieces = products + MOE_MAX_LOCAL * 4 + linear_split_bytes(K, N);
+      end = parts > pieces ? parts : pieces;
+    }
   }
 };
 
 }  // namespace
 
-size_t linear_fwd_ws_bytes(int dtype, int rows, int K, int N, int e_cnt) { return SETUP_BYTES; }
+size_t linear_fwd_ws_bytes(int dtype, int rows, int K, int N, int e_cnt) {
+  if (dtype != MOE_BF16) return SETUP_BYTES;
+  const size_t few = linear_few_ws_bytes(rows, N), parts = linear_parts_bytes(rows, N);
+  return SETUP_BYTES + (few > parts ? few : parts);
+}
 size_t linear_bwd_ws_bytes(int dtype, int rows, int K, int N, int e_cnt) { return BwdSpace(dtype, rows, K, N, e_cnt).end; }
 
 int launch_linear_fwd(const LinearArgs& l, void* ws, hipStream_t s) {
   if (l.rows == 0 || l.e_cnt == 0) return MOE_OK;
+  void* const parts = (char*)ws + SETUP_BYTES;
+  const Route route = forward_route(l);
+  if (route == FEW_ROWS) return launch_linear_few(l, parts, s);
+  if (route == TILES) return launch_linear_tiles_fwd(l, parts, s);
   int32_t* const setup = (int32_t*)ws;
   if (l.dtype == MOE_BF16 || !l.offsets) {
     hipLaunchKernelGGL(linear_setup, dim3(1), dim3(128), 0, s, setup, l.rows);
     HIP_CHECK_LAUNCH();
   }
-  if (l.dtype == MOE_BF16) return launch_linear_fwd_tiles(l, setup, s);
+  if (l.dtype == MOE_BF16) return launch_linear_fwd_large(l, setup, s);
   LinearArgs with_offsets = l;
   if (!l.offsets) with_offsets.offsets = setup + SETUP_WORDS;
   return launch_linear_fwd_f32(with_offsets, s);
@@ -165,21 +217,30 @@ int launch_linear_bwd(const LinearArgs& l, const void* dy, void* dx, void* dw, v
   if (l.e_cnt == 0) return MOE_OK;
   const BwdSpace space(l.dtype, l.rows, l.K, l.N, l.e_cnt);
   char* const base = (char*)ws;
-  int32_t* const setup = (int32_t*)ws;
-  hipLaunchKernelGGL(linear_setup, dim3(1), dim3(128), 0, s, setup, l.rows);
-  HIP_CHECK_LAUNCH();
-  const int32_t* const off = l.offsets ? l.offsets : setup + SETUP_WORDS;
-  const bool through = l.act != MOE_ACT_NONE;
+  const bool through = l.act != MOE_ACT_NONE, tiles = backward_route(l, dx, dw) == TILES, setup_needed = !tiles && (l.dtype == MOE_BF16 || !l.offsets);
   void* const dz = through ? base + space.dz : nullptr;
+  float* const sums = (float*)(base + space.sums);
+  int32_t* const setup = (int32_t*)ws;
   int rc;
-  if (db || (through && (dx || dw))) {
-    float* const sums = (float*)(base + space.sums);
-    rc = l.dtype == MOE_BF16 ? gradients<bf16_t>(l, off, dy, dz, db, sums, accumulate, s) : gradients<float>(l, off, dy, dz, db, sums, accumulate, s);
+  if (l.rows > 0 && (db || (through && (dx || dw)))) {
+    rc = l.dtype == MOE_BF16 ? gradients<bf16_t>(l, dy, dz, db ? sums : nullptr, setup_needed ? setup : nullptr, s)
+                             : gradients<float>(l, dy, dz, db ? sums : nullptr, setup_needed ? setup : nullptr, s);
     if (rc) return rc;
+  } else if (setup_needed) {
+    hipLaunchKernelGGL(linear_setup, dim3(1), dim3(128), 0, s, setup, l.rows);
+    HIP_CHECK_LAUNCH();
   }
   const void* const g = through ? dz : dy;
-  if (l.dtype == MOE_BF16) return launch_linear_bwd_tiles(l, g, dx, dw, accumulate, setup, base + space.products, s);
+  const BiasGrad bias = {l.offsets, l.rows, l.N, accumulate, sums, db};
+  if (tiles) return launch_linear_tiles_bwd(l, g, dx, dw, accumulate, bias, base + space.products, base + space.dw_parts, s);
+  if (db) {
+    ProfScope prof(MOE_K_LINEAR_BIAS, s);
+    if (l.dtype == MOE_BF16) hipLaunchKernelGGL(bias_grad<bf16_t>, dim3(bias_blocks(l.N, l.e_cnt)), dim3(BIAS_THREADS), 0, s, bias);
+    else hipLaunchKernelGGL(bias_grad<float>, dim3(bias_blocks(l.N, l.e_cnt)), dim3(BIAS_THREADS), 0, s, bias);
+    HIP_CHECK_LAUNCH();
+  }
+  if (l.dtype == MOE_BF16) return launch_linear_bwd_large(l, g, dx, dw, accumulate, setup, base + space.products, s);
   LinearArgs with_offsets = l;
-  with_offsets.offsets = off;
+  if (!l.offsets) with_offsets.offsets = setup + SETUP_WORDS;
   return launch_linear_bwd_f32(with_offsets, g, dx, dw, accumulate, s);
 }

@@ -1,0 +1,444 @@
+// The linear layer's products in bf16 where the large tiles of expert_bf16.hip would leave most of the chip idle: 128x128 tiles, as many workgroups as
+// it takes, contractions in parts.
+//     FWD  y  = act(x W + b) + residual    ragged rows, W read transposed
+//     DX   dx = dz W^T                     ragged rows, both operands contiguous along the contraction
+//     DW   dW (+)= x^T dz                  contraction over an expert's rows, both operands read transposed
+// Four wavefronts of 64x64 each, k-tiles 64 deep in two stages of 32 KB, two workgroups per CU: while one waits for its barrier or its operands
+// or finishes its outputs, the other multiplies.  A k-tile's fragments are read as a whole, so that its stage is free for the k-tile after the
+// next half-way through its multiplication.  Where the tiles alone would not fill the chip the contraction is cut; a part's sums are stored
+// in fp32 and added in order by a launch behind (linear_join_*).
+// Every output is one chain of sums over ascending k per part.
+#include "activation.h"
+#include "bias_grad.h"
+#include "kernels.h"
+#include "linear.h"
+#include "tile128.h"
+
+namespace {
+
+typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+enum { FWD, DX, DW };
+constexpr int NT = 256, TILE_PITCH = 68;
+constexpr int STAGE = 2 * QOPER_BYTES, SLAB = 64 * TILE_PITCH * 4;
+constexpr int TILE_LDS = 4 * SLAB > 2 * STAGE ? 4 * SLAB : 2 * STAGE;
+static_assert(TILE_LDS <= 80 * 1024, "two workgroups per CU");
+
+// one product: rows [rows of an expert] x N columns (DW: M x N per expert), contraction K (DW: the expert's rows)
+struct Product {
+  const bf16_t *A, *B;
+  long lda, ldb, b_es;
+  bf16_t* C;
+  int M, N, K;
+  float* sums;             // [parts] of the whole output
+  size_t sums_stride;
+  int parts, accumulate;
+  long long tiles;         // at most, of one part (dense: exactly)
+};
+struct TileArgs {
+  LinearArgs l;
+  Product p;
+};
+
+struct Tile { int e, mt, nt, first, end; };      // rows [first, end) of expert e
+
+// tile b of a part's list: an expert's tiles in bands of 8 row tiles, column tile next, row tile inside the band fastest, so that what an XCD
+// multiplies at a time shares panels
+template <int OP>
+__device__ __forceinline__ bool tile_of(const LinearArgs& l, const Product& p, int b, int lane, Tile& t) {
+  const int n_tiles = (p.N + QT - 1) / QT;
+  int e = 0, at, m;
+  t.first = 0;
+  t.end = l.rows;
+  if (OP == DW) {
+    m = (p.M + QT - 1) / QT;
+    // an XCD takes an eighth of the list; where experts differ in rows, every eighth chunk of 32 tiles
+    const int total = l.e_cnt * m * n_tiles, share = (total + 7) / 8;
+    at = l.offsets ? (b / 256 * 8 + b % 8) * 32 + b / 8 % 32 : b / 8 < share ? b % 8 * share + b / 8 : total;
+    if (at >= total) return false;
+    e = at / (m * n_tiles);
+    at -= e * m * n_tiles;
+    if (l.offsets) { t.first = l.offsets[e]; t.end = l.offsets[e + 1]; }
+  } else if (l.offsets) {
+    int row_tile, col_tile;
+    if (!RaggedTiles<QT>(l.offsets, l.e_cnt, lane).tile(n_tiles, b, e, row_tile, col_tile)) return false;
+    t.first = l.offsets[e];
+    t.end = l.offsets[e + 1];
+    m = (t.end - t.first + QT - 1) / QT;
+    at = row_tile * n_tiles + col_tile;
+  } else {
+    m = (l.rows + QT - 1) / QT;
+    const int total = m * n_tiles, share = (total + 7) / 8;
+    at = (b % 8) * share + b / 8;
+    if (b / 8 >= share || at >= total) return false;
+  }
+  const int band = at / (8 * n_tiles), in_band = at - band * 8 * n_tiles, high = min(8, m - 8 * band);
+  t.nt = __builtin_amdgcn_readfirstlane(in_band / high);
+  t.mt = __builtin_amdgcn_readfirstlane(8 * band + in_band % high);
+  t.e = __builtin_amdgcn_readfirstlane(e);
+  t.first = __builtin_amdgcn_readfirstlane(t.first);
+  t.end = __builtin_amdgcn_readfirstlane(t.end);
+  return true;
+}
+
+__device__ __forceinline__ void add8(float (&y)[8], u32x4 u) {
+#pragma unroll
+  for (int q = 0; q < 4; ++q) { y[2 * q] += bf16lo(u[q]); y[2 * q + 1] += bf16hi(u[q]); }
+}
+__device__ __forceinline__ u32x4 pack8(const float (&y)[8]) {
+  return u32x4{pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]), pack_bf16x2(y[4], y[5]), pack_bf16x2(y[6], y[7])};
+}
+__device__ __forceinline__ u32x4 load8(const void* p, size_t at) { return *reinterpret_cast<const u32x4*>((const bf16_t*)p + at); }
+__device__ __forceinline__ void store8(void* p, size_t at, const float (&y)[8]) { *reinterpret_cast<u32x4*>((bf16_t*)p + at) = pack8(y); }
+
+// eight finished columns of a row
+template <int OP>
+__device__ __forceinline__ void finish(const LinearArgs& l, const Product& p, int e, size_t at, int col, float (&y)[8]) {
+  if (OP == FWD) {
+    if (l.bias) add8(y, load8(l.bias, (size_t)e * l.N + col));
+    if (l.z) store8(l.z, at, y);
+    activate(l.act, y);
+    if (l.residual) add8(y, load8(l.residual, at));
+  }
+  if (OP == DW && p.accumulate) add8(y, load8(p.C, at));
+  store8(p.C, at, y);
+}
+
+// STREAM (FWD): weights that one tile reads are loaded as such
+template <int OP, bool STREAM = false>
+__device__ __forceinline__ void multiply_tile(const LinearArgs& l, const Product& p, int b, int part, char* lds) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = wave >> 1, wn = wave & 1;
+  Tile t;
+  if (!tile_of<OP>(l, p, b, lane, t)) return;
+  const int n0 = t.nt * QT;
+  const int row0 = OP == DW ? t.mt * QT : t.first + t.mt * QT, row_end = OP == DW ? p.M : t.end;      // of the output
+  // k-tiles [kt, kt1) of 64, of the whole contraction [0, depth)
+  const int depth = OP == DW ? t.end - t.first : p.K, all = (depth + QK - 1) / QK, per = (all + p.parts - 1) / p.parts;
+  const int kt0 = min(all, part * per), kt1 = min(all, kt0 + per);
+
+  const uint32_t base = lds_addr(lds);
+  QuarterKc a_kc, b_kc;
+  QuarterTr a_tr, b_tr;
+  if (OP == DW) {
+    a_tr.setup(p.A + (size_t)t.first * p.lda, nullptr, false, p.lda, row0, p.M, wave, lane);
+    b_tr.setup(p.B + (size_t)t.first * p.ldb, nullptr, false, p.ldb, n0, p.N, wave, lane);
+  } else {
+    a_kc.setup(p.A + (size_t)row0 * p.lda, p.lda, row_end - row0, wave, lane);
+    if (OP == FWD) b_tr.setup(p.B + (size_t)t.e * p.b_es, nullptr, false, p.ldb, n0, p.N, wave, lane);
+    else b_kc.setup(p.B + (size_t)t.e * p.b_es + (size_t)n0 * p.ldb, p.ldb, p.N - n0, wave, lane);
+  }
+  auto issue = [&](int kt) {
+    const uint32_t st = base + (kt & 1) * STAGE;
+    const long k0 = (long)kt * QK;
+    const int last = depth - 1 - (int)k0;          // >= 0
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t back = OP != DW && last < QK - 1 ? past_end((int)k0 + 8 * QuarterKc::chunk(j, lane), depth) : 0;
+      if (OP == DW) a_tr.template issue1<true>(j, st, wave, lane, k0, last);
+      else a_kc.issue1(j, st, wave, k0, back);
+      if (OP == DX) b_kc.issue1(j, st + QOPER_BYTES, wave, k0, back);
+      else b_tr.template issue1<true, STREAM>(j, st + QOPER_BYTES, wave, lane, k0, last);
+    }
+  };
+  int a_off[2], b_off[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int row = wm * 64 + i * 32 + (lane & 31), col = wn * 64 + i * 32 + (lane & 31);
+    a_off[i] = OP == DW ? quarter_tr_off(wm, i * 32, lane) : row * 128 + (((lane >> 5) ^ ((row >> 1) & 7)) << 4);
+    b_off[i] = QOPER_BYTES + (OP == DX ? col * 128 + (((lane >> 5) ^ ((col >> 1) & 7)) << 4) : quarter_tr_off(wn, i * 32, lane));
+  }
+  f32x16 acc[2][2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[i][j][r] = 0.f;
+  if (kt0 < kt1) issue(kt0);
+  if (kt0 + 1 < kt1) issue(kt0 + 1);
+  for (int kt = kt0; kt < kt1; ++kt) {
+    if (kt + 1 < kt1) asm volatile("s_waitcnt vmcnt(8)" ::: "memory");
+    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    const char* st = lds + (kt & 1) * STAGE;
+    bf16x8 fa[4][2], fb[4][2];
+#pragma unroll
+    for (int s = 0; s < 4; ++s)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        fa[s][i] = OP == DW ? quarter_frag_tr(st + a_off[i] + s * 2048) : lds_frag_kc(st + (a_off[i] ^ (s * 32)));
+        fb[s][i] = OP == DX ? lds_frag_kc(st + (b_off[i] ^ (s * 32))) : quarter_frag_tr(st + b_off[i] + s * 2048);
+      }
+    if ((kt + 1) * QK > depth) {                   // zeros past the contraction's end, in both operands: either may be no number there
+#pragma unroll
+      for (int s = 0; s < 4; ++s) {
+        const int k = kt * QK + 16 * s + 8 * (lane >> 5);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          if (OP == DW) {                          // (the rows of an expert end anywhere)
+            s16x8 u = __builtin_bit_cast(s16x8, fa[s][i]), v = __builtin_bit_cast(s16x8, fb[s][i]);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) { u[j] = k + j < depth ? u[j] : (short)0; v[j] = k + j < depth ? v[j] : (short)0; }
+            fa[s][i] = __builtin_bit_cast(bf16x8, u);
+            fb[s][i] = __builtin_bit_cast(bf16x8, v);
+          } else if (k >= depth) {
+            fa[s][i] = fb[s][i] = bf16x8{};
+          }
+        }
+      }
+    }
+    const auto step = [&](int s) {                 // blocks (0,0), (0,1), (1,1), (1,0)
+#pragma unroll
+      for (int m = 0; m < 4; ++m) {
+        const int i = m >> 1, j = i ^ (m & 1);
+        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[s][i], fb[s][j], acc[i][j], 0, 0, 0);
+      }
+    };
+    step(0);
+    step(1);
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();                  // every wavefront has its fragments: the stage is free
+    if (kt + 2 < kt1) issue(kt + 2);
+    step(2);
+    step(3);
+  }
+  // Element 4 g + q of a lane's block is row 8 g + 4 (lane / 32) + q, column lane % 32: through the wavefront's own slab to eight columns a lane.
+  float* const slab = reinterpret_cast<float*>(lds) + wave * (SLAB / 4);
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        slab[(32 * i + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3)) * TILE_PITCH + 32 * j + (lane & 31)] = acc[i][j][r];
+  __builtin_amdgcn_wave_barrier();
+  const int col = n0 + wn * 64 + (lane & 7) * 8;
+  if (col >= p.N) return;
+#pragma unroll 2
+  for (int q = 0; q < 8; ++q) {
+    const int in = 8 * q + (lane >> 3), row = row0 + wm * 64 + in;
+    if (row >= row_end) break;
+    const float* from = slab + in * TILE_PITCH + (lane & 7) * 8;
+    const f32x4 lo = *reinterpret_cast<const f32x4*>(from), hi = *reinterpret_cast<const f32x4*>(from + 4);
+    const size_t at = ((size_t)(OP == DW ? t.e : 0) * p.M + row) * p.N + col;
+    if (p.parts > 1) {
+      float* const to = p.sums + (size_t)part * p.sums_stride + at;
+      *reinterpret_cast<f32x4*>(to) = lo;
+      *reinterpret_cast<f32x4*>(to + 4) = hi;
+    } else {
+      float y[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+      finish<OP>(l, p, t.e, at, col, y);
+    }
+  }
+}
+
+template <int OP, bool STREAM = false>
+__global__ __launch_bounds__(NT, 2) void linear_tiles(TileArgs a) {
+  __shared__ __align__(1024) char lds[TILE_LDS];
+  multiply_tile<OP, STREAM>(a.l, a.p, blockIdx.x, blockIdx.y, lds);
+}
+
+// The gradients in one launch: dW's blocks, dx's, db's.  (dx_blocks, dw_blocks: of one part; multiples of 8)
+struct Gradients {
+  LinearArgs l;
+  Product dx, dw;
+  BiasGrad db;
+  int dx_blocks, dw_blocks, dx_total, dw_total;
+};
+__global__ __launch_bounds__(NT, 2) void linear_gradients(Gradients g) {
+  __shared__ __align__(1024) char lds[TILE_LDS];
+  int b = blockIdx.x;
+  if (b < g.dw_total) return multiply_tile<DW>(g.l, g.dw, b % g.dw_blocks, b / g.dw_blocks, lds);
+  b -= g.dw_total;
+  if (b < g.dx_total) return multiply_tile<DX>(g.l, g.dx, b % g.dx_blocks, b / g.dx_blocks, lds);
+  bias_columns<bf16_t>(g.db, b - g.dx_total, reinterpret_cast<float*>(lds));
+}
+static_assert(NT == BIAS_THREADS, "");
+
+__device__ __forceinline__ void total_of(const Product& p, size_t at, float (&y)[8]) {
+  const float* s = p.sums + at;
+  f32x4 lo = f32x4{0.f, 0.f, 0.f, 0.f}, hi = lo;
+#pragma unroll 8
+  for (int q = 0; q < p.parts; ++q, s += p.sums_stride) {
+    lo += *reinterpret_cast<const f32x4*>(s);
+    hi += *reinterpret_cast<const f32x4*>(s + 4);
+  }
+#pragma unroll
+  for (int j = 0; j < 4; ++j) { y[j] = lo[j]; y[4 + j] = hi[j]; }
+}
+// The parts' sums of the forward: 16 rows of a tile a block
+__global__ __launch_bounds__(NT) void linear_join_fwd(TileArgs a) {
+  Tile t;
+  if (!tile_of<FWD>(a.l, a.p, blockIdx.x, threadIdx.x & 63, t)) return;
+  const int row = t.first + t.mt * QT + 16 * blockIdx.y + threadIdx.x / 16, col = t.nt * QT + 8 * (threadIdx.x % 16);
+  if (row >= t.end || col >= a.p.N) return;
+  const size_t at = (size_t)row * a.p.N + col;
+  float y[8];
+  total_of(a.p, at, y);
+  finish<FWD>(a.l, a.p, t.e, at, col, y);
+}
+// and of the gradients: of all rows of all experts, and of all matrices; a product that was not cut has no part in it
+__global__ __launch_bounds__(NT) void linear_join_bwd(LinearArgs l, Product dx, Product dw) {
+  const size_t rows = l.offsets ? (size_t)l.offsets[l.e_cnt] : (size_t)l.rows;
+  const size_t n_dx = dx.parts > 1 ? rows * dx.N / 8 : 0, n_dw = dw.parts > 1 ? (size_t)l.e_cnt * dw.M * dw.N / 8 : 0;
+  for (size_t v = (size_t)blockIdx.x * NT + threadIdx.x; v < n_dx + n_dw; v += (size_t)gridDim.x * NT) {
+    float y[8];
+    if (v < n_dx) {
+      total_of(dx, 8 * v, y);
+      finish<DX>(l, dx, 0, 8 * v, 0, y);
+    } else {
+      const size_t at = 8 * (v - n_dx);
+      total_of(dw, at, y);
+      finish<DW>(l, dw, 0, at, 0, y);
+    }
+  }
+}
+
+constexpr int MOST_PARTS = 16, WORKGROUPS = 512;
+#ifndef TILE_PARTS
+#define TILE_PARTS 0
+#endif
+// Time in us of a k-tile on a CU: one workgroup alone, two beside each other (both of them), and of each of many when the whole chip multiplies.
+// Operands that come from memory and not from the caches take longer.
+struct KTile { float alone, two, many; };
+constexpr KTile CACHED = {0.58f, 0.82f, 0.56f}, STREAMED = {0.72f, 1.3f, 0.65f};
+inline float k_tile(const KTile& k, float per_cu) {
+  const float least = per_cu <= 1.f ? k.alone : k.two;
+  return per_cu * k.many > least ? per_cu * k.many : least;
+}
+// What adding up the parts of n outputs takes
+inline float join_time(int parts, double n) { return parts > 1 ? 3.f + (float)(parts * n * (8.0 / 9e6)) : 0.f; }
+inline long long most_parts(long long tiles, long long k_tiles) {
+  const long long parts = tiles > 0 ? WORKGROUPS / tiles : 1, deep = k_tiles / 2;
+  return parts < 1 || deep < 1 ? 1 : parts > MOST_PARTS ? (deep < MOST_PARTS ? deep : MOST_PARTS) : parts < deep ? parts : deep;
+}
+// The forward's parts, and its time
+inline float forward_time(long long tiles, long long k_tiles, double outputs, const KTile& k, int* parts) {
+  float best = 0.f;
+  for (int p = 1; p <= most_parts(tiles, k_tiles); ++p) {
+    const float t = 6.f + (float)((k_tiles + p - 1) / p) * k_tile(k, (float)(tiles * p) / 256.f) + join_time(p, outputs);
+    if (p == 1 || t < best) { best = t; *parts = p; }
+  }
+  if (TILE_PARTS) *parts = TILE_PARTS;
+  return best;
+}
+// Parts of both gradients' products in one launch: as many as bring either's longest tile down to what the chip takes for all of them
+inline int chain_parts(long long tiles, long long k_tiles, float all) {
+  if (TILE_PARTS) return TILE_PARTS;
+  const long long most = most_parts(tiles, k_tiles);
+  const float goal = all > 5.f ? all : 5.f;
+  long long p = 1;
+  while (p < most && (float)((k_tiles + p - 1) / p) * CACHED.alone > goal) ++p;
+  return (int)p;
+}
+inline long long row_tiles(const LinearArgs& l) {
+  return ((long long)l.rows + QT - 1) / QT + (l.offsets ? (l.e_cnt < l.rows ? l.e_cnt : l.rows) - 1 : 0);
+}
+inline long long column_tiles(int n) { return (n + QT - 1) / QT; }
+inline unsigned blocks_of(long long tiles) { return (unsigned)((tiles + 7) / 8 * 8); }
+
+// No empty part: as many as parts of the rounded-up length need
+inline int whole_parts(int parts, long long k_tiles) {
+  const long long per = (k_tiles + parts - 1) / parts;
+  return per > 0 ? (int)((k_tiles + per - 1) / per) : 1;
+}
+// whether the forward's weights come from memory: those of one layer, beyond what the Infinity Cache may keep of them
+inline bool streamed(const LinearArgs& l) { return 2ll * l.K * l.N * l.e_cnt > (100ll << 20); }
+Product forward_of(const LinearArgs& l, void* ws, float* time) {
+  Product p = {(const bf16_t*)l.x, (const bf16_t*)l.w, l.K, l.N, (long)l.K * l.N, (bf16_t*)l.y, 0, l.N, l.K, (float*)ws, (size_t)l.rows * l.N, 1, 0};
+  p.tiles = row_tiles(l) * column_tiles(l.N);
+  const long long k_tiles = (l.K + QK - 1) / QK;
+  *time = forward_time(p.tiles, k_tiles, (double)l.rows * l.N, streamed(l) ? STREAMED : CACHED, &p.parts);
+  p.parts = whole_parts(p.parts, k_tiles);
+  return p;
+}
+Product dx_of(const LinearArgs& l, const void* dz, void* dx, void* ws) {
+  Product p = {(const bf16_t*)dz, (const bf16_t*)l.w, l.N, l.N, (long)l.K * l.N, (bf16_t*)dx, 0, l.K, l.N, (float*)ws, (size_t)l.rows * l.K, 1, 0};
+  p.tiles = row_tiles(l) * column_tiles(l.K);
+  return p;
+}
+Product dw_of(const LinearArgs& l, const void* dz, void* dw, int accumulate, void* ws) {
+  Product p = {(const bf16_t*)l.x, (const bf16_t*)dz, l.K, l.N, 0, (bf16_t*)dw, l.K, l.N, 0, (float*)ws, (size_t)l.e_cnt * l.K * l.N, 1, accumulate};
+  p.tiles = l.e_cnt * column_tiles(l.K) * column_tiles(l.N);
+  return p;
+}
+// parts of both; returns the time of their launch and of the one that adds the parts up
+float plan_gradients(const LinearArgs& l, Product& x, Product& w) {
+  const long long kx = (l.N + QK - 1) / QK, kw = ((long long)l.rows / l.e_cnt + QK - 1) / QK;
+  const float all = CACHED.many / 256.f * (float)((x.C ? x.tiles * kx : 0) + (w.C ? w.tiles * kw : 0));
+  float chain = 0.f, join = 0.f;
+  double parts = 0;
+  if (x.C) {
+    x.parts = whole_parts(chain_parts(x.tiles, kx, all), kx);
+    chain = (float)((kx + x.parts - 1) / x.parts) * CACHED.alone;
+    if (x.parts > 1) { join = 3.f; parts += (double)x.parts * l.rows * l.K; }
+  }
+  if (w.C) {
+    w.parts = chain_parts(w.tiles, kw, all);             // (experts' rows differ: parts of some may be empty)
+    const float c = (float)((kw + w.parts - 1) / w.parts) * CACHED.alone;
+    chain = c > chain ? c : chain;
+    if (w.parts > 1) { join = 3.f; parts += (double)w.parts * l.e_cnt * l.K * l.N; }
+  }
+  return 6.f + (all > chain ? all : chain) + join + (float)(parts * (8.0 / 9e6));
+}
+
+}  // namespace
+
+// Sums of parts of an output of `rows` x `columns`, for any number of rows up to this one: at most MOST_PARTS times the output, and WORKGROUPS tiles
+size_t linear_parts_bytes(long long rows, int columns) {
+  const size_t all = (size_t)MOST_PARTS * rows * columns * 4, most = (size_t)WORKGROUPS * QT * QT * 4;
+  return all < most ? all : most;
+}
+
+float linear_tiles_fwd_time(const LinearArgs& l) {
+  float t;
+  forward_of(l, nullptr, &t);
+  return t;
+}
+float linear_tiles_bwd_time(const LinearArgs& l, bool dx, bool dw) {
+  void* const some = (void*)1;
+  Product x = dx_of(l, nullptr, dx && l.rows > 0 ? some : nullptr, nullptr), w = dw_of(l, nullptr, dw ? some : nullptr, 0, nullptr);
+  return plan_gradients(l, x, w);
+}
+
+int launch_linear_tiles_fwd(const LinearArgs& l, void* ws, hipStream_t s) {
+  float time;
+  const TileArgs a = {l, forward_of(l, ws, &time)};
+  const unsigned blocks = blocks_of(a.p.tiles);
+  ProfScope prof(MOE_K_LINEAR, s);
+  // (stream_rule.h: weights that one tile reads and that the Infinity Cache does not keep)
+  if (l.rows <= (long long)QT * l.e_cnt && 2ll * l.K * l.N * l.e_cnt > (256ll << 20)) hipLaunchKernelGGL((linear_tiles<FWD, true>), dim3(blocks, a.p.parts), dim3(NT), 0, s, a);
+  else hipLaunchKernelGGL(linear_tiles<FWD>, dim3(blocks, a.p.parts), dim3(NT), 0, s, a);
+  HIP_CHECK_LAUNCH();
+  if (a.p.parts > 1) {
+    hipLaunchKernelGGL(linear_join_fwd, dim3(blocks, ((l.rows < QT ? l.rows : QT) + 15) / 16), dim3(NT), 0, s, a);
+    HIP_CHECK_LAUNCH();
+  }
+  return MOE_OK;
+}
+
+// ws_dx: linear_parts_bytes(rows, K), ws_dw: linear_parts_bytes(e_cnt * K, N)
+int launch_linear_tiles_bwd(const LinearArgs& l, const void* dz, void* dx, void* dw, int accumulate, const BiasGrad& db, void* ws_dx, void* ws_dw,
+                            hipStream_t s) {
+  Product x = dx_of(l, dz, l.rows > 0 ? dx : nullptr, ws_dx), w = dw_of(l, dz, dw, accumulate, ws_dw);
+  plan_gradients(l, x, w);
+  Gradients g = {l, x, w, db, (int)blocks_of(x.tiles), l.offsets ? (int)((w.tiles + 255) / 256 * 256) : (int)blocks_of(w.tiles), 0, 0};
+  if (x.C) g.dx_total = g.dx_blocks * x.parts;
+  if (w.C) g.dw_total = g.dw_blocks * w.parts;
+  const unsigned blocks = g.dx_total + g.dw_total + (db.db ? bias_blocks(l.N, l.e_cnt) : 0);
+  if (blocks > 0) {
+    ProfScope prof(x.C && w.C ? MOE_K_LINEAR_DX_DW : w.C ? MOE_K_LINEAR_DW : x.C ? MOE_K_LINEAR_DX : MOE_K_LINEAR_BIAS, s);
+    hipLaunchKernelGGL(linear_gradients, dim3(blocks), dim3(NT), 0, s, g);
+    HIP_CHECK_LAUNCH();
+  }
+  if (x.parts > 1 || w.parts > 1) {
+    const long long n = ((x.parts > 1 ? (long long)l.rows * l.K : 0) + (w.parts > 1 ? (long long)l.e_cnt * l.K * l.N : 0)) / 8;
+    const long long blocks = (n + NT - 1) / NT, most = 8ll * device_cu_count();
+    ProfScope prof(MOE_K_WGRAD_REDUCE, s);
+    hipLaunchKernelGGL(linear_join_bwd, dim3((unsigned)(blocks < most ? blocks : most)), dim3(NT), 0, s, l, x, w);
+    HIP_CHECK_LAUNCH();
+  }
+  return MOE_OK;
+}
