@@ -354,7 +354,7 @@ int moe_layer_norm_bwd(const void* h_out, const void* w, const float* mean, cons
  * All sums are fp32.  In bf16 the products take dz rounded to bf16; db sums it unrounded.  relu's slope at 0 is 0.
  * Results are bit-reproducible from run to run.  fp32 products are those of moe_expert_fwd and _bwd.
  * Errors of both: EINVAL (NULL, negative sizes, unknown dtype or act, offsets NULL with e_cnt != 1, pointers not 16-byte aligned), EUNSUPPORTED (bf16
- * with K % 8 != 0 or N % 8 != 0, fp32 with % 4, K or N > MOE_MAX_LINEAR, e_cnt > MOE_MAX_LOCAL, 2^23 tiles of 64 x 64 or more in y, x or the
+ * with K % 8 != 0 or N % 8 != 0, fp32 with % 4, K or N > MOE_MAX_LINEAR, e_cnt > MOE_MAX_LOCAL, 2^22 tiles of 64 x 64 or more in y, x or the
  * matrices), EWORKSPACE.
  */
 int moe_linear_fwd(const void* x, int dtype, int cap, int K, int N, int e_cnt, const int32_t* offsets, const void* w, const void* bias, int act,

@@ -432,9 +432,9 @@ int shape_check_linear(int dtype, int cap, int K, int N, int e_cnt, const int32_
   if (!offsets && e_cnt != 1) return MOE_EINVAL;
   const int step = dtype == MOE_BF16 ? 8 : 4, widest = K > N ? K : N;
   if (e_cnt > MOE_MAX_LOCAL || K % step || N % step || widest > MOE_MAX_LINEAR) return MOE_EUNSUPPORTED;
-  // workgroups of 256 are counted in 32 bits of work-items, over 64 rows by 64 columns at the finest
-  if ((((long long)cap + 63) / 64 + e_cnt) * ((widest + 63) / 64) >= (1ll << 23)) return MOE_EUNSUPPORTED;
-  if (e_cnt * ((K + 63ll) / 64) * ((N + 63) / 64) >= (1ll << 23)) return MOE_EUNSUPPORTED;
+  // workgroups of 256 are counted in 32 bits of work-items, over 64 rows by 64 columns at the finest, for both gradients in one launch
+  if ((((long long)cap + 63) / 64 + e_cnt) * ((widest + 63) / 64) >= (1ll << 22)) return MOE_EUNSUPPORTED;
+  if (e_cnt * ((K + 63ll) / 64) * ((N + 63) / 64) >= (1ll << 22)) return MOE_EUNSUPPORTED;
   return MOE_OK;
 }
 }  // namespace

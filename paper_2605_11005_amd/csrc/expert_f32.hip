@@ -8,7 +8,7 @@
 //   DX     dxp   = dH1 W1^T + dH3 W3^T   ragged M, K in two segments
 //   WG     dW2   = a^T d_o      ragged K (the expert's rows)
 //   WGD    dW1|dW3 = xp^T [dH1|dH3]      ragged K, two outputs of one tile
-// and those of a linear layer (WG is its weight gradient): LIN, y = act(x W + b) + residual, and LDX, dx = dz W^T.
+// and those of a linear layer, whose contractions may be cut in parts: LIN, y = act(x W + b) + residual, LDX, dx = dz W^T, and LWG, dW = x^T dz.
 //
 // The fp32 matrix instruction does 256 FLOP per cycle and CU, the bf16 one sixteen times that, so six bf16 products take 3/8 of
 // the time.  Three terms hold all 24 bits of a number.  The three products of terms that are left out are up to 2^-24.0 of a product of
@@ -26,17 +26,17 @@
 // two LDS buffers and two blocks per CU 87 + 176; splitting between the matrix instructions of one wavefront, which takes more
 // registers, 104 + 181; tiles of 128x64 95 + 199 (better only for a thousand rows and more per expert: 145 for 176 at 3000, d = f =
 // 1024).
-#include "activation.h"
+#include "bias_grad.h"
 #include "common.h"
 #include "kernels.h"
-#include "linear.h"
+#include "linear_finish.h"
 
 namespace {
 
 constexpr int TM = 64, TN = 64, TK = 32, NT = 256;
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
-enum { UP, DOWN, DA, DX, WG, WGD, LIN, LDX };
+enum { UP, DOWN, DA, DX, WG, WGD, LIN, LDX, LWG };
 
 // An fp32 matrix instruction contracts two values of k, one per half of the wavefront.  Which two is free as long as both
 // operands agree: in groups of eight steps the lower half takes k = 0..7 and the upper one k = 8..15 of a group of 16, so
@@ -241,14 +241,17 @@ struct Args {
   int M, N, K;              // M: WG / WGD, K: ragged-M shapes (per segment)
   const int32_t* off;
   int e_cnt, beta;
+  // LIN, LDX, LWG
+  int rows;                 // off == NULL: of the only expert
   const float* bias;        // LIN: [e_cnt][N] or NULL
   const float* R;           // LIN: residual, laid out as y (C[0]), or NULL.  C[1]: z or NULL
   int act;
+  Parts parts;
 };
 
 // LDS of one k-tile: the three bf16 terms of each operand, or the operands themselves
 template <int MODE> struct Traits {
-  static constexpr bool RAGGED_K = MODE == WG || MODE == WGD;
+  static constexpr bool RAGGED_K = MODE == WG || MODE == WGD || MODE == LWG, LINEAR = MODE >= LIN;
   static constexpr bool DUAL = MODE == UP || MODE == WGD;
   static constexpr int NB = DUAL ? 2 : 1;
   typedef typename Pick<RAGGED_K, OperMN, OperKC>::type OperA;
@@ -261,8 +264,9 @@ template <int MODE> struct Traits {
 // Block `block` of one GEMM, a 1-D list of tiles: RaggedTiles' for the ragged-M shapes, the same with a fixed number of row tiles
 // per expert for the ragged-K ones.
 // BUFS: LDS buffers, two in launches of few blocks (use_two()).
+// part (LINEAR): of the contraction, whose sums go to p.parts.
 template <int MODE, int BUFS>
-__device__ __forceinline__ void gemm_tile(const Args& p, int block, char* lds) {
+__device__ __forceinline__ void gemm_tile(const Args& p, int block, char* lds, int part = 0) {
   using TR = Traits<MODE>;
   constexpr bool RAGGED_K = TR::RAGGED_K, DUAL = TR::DUAL;
   constexpr int NB = TR::NB, BUFFER = TR::BUFFER;
@@ -273,7 +277,18 @@ __device__ __forceinline__ void gemm_tile(const Args& p, int block, char* lds) {
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int n_tiles = (p.N + TN - 1) / TN, m_tiles = (p.M + TM - 1) / TM;
   int e, mt, nt, row0, row_end, K;                       // output rows [row0, row_end)
-  if (RAGGED_K) {
+  int k_from = 0;
+  if (TR::LINEAR && !p.off) {                            // one expert: the tiles are known
+    const int total = (RAGGED_K ? m_tiles : (p.rows + TM - 1) / TM) * n_tiles, share = (total + 7) / 8;
+    const int tile = (block % 8) * share + block / 8;
+    if (block / 8 >= share || tile >= total) return;
+    e = 0;
+    mt = tile / n_tiles;
+    nt = tile - mt * n_tiles;
+    row0 = mt * TM;
+    row_end = RAGGED_K ? p.M : p.rows;
+    K = RAGGED_K ? p.rows : p.K;
+  } else if (RAGGED_K) {
     const int total = p.e_cnt * m_tiles * n_tiles, share = (total + 7) / 8;
     const int tile = (block % 8) * share + block / 8;
     if (block / 8 >= share || tile >= total) return;
@@ -290,22 +305,27 @@ __device__ __forceinline__ void gemm_tile(const Args& p, int block, char* lds) {
     K = p.K;
   }
   const int col0 = nt * TN;
+  if (TR::LINEAR && p.parts.n > 1) {                     // whole k-tiles
+    const int per = ((K + TK - 1) / TK + p.parts.n - 1) / p.parts.n * TK;
+    k_from = min(K, part * per);
+    K = min(K - k_from, per);
+  }
 
   OperA a;
   OperB b[NB];
   auto setup = [&](int seg) {
     if constexpr (RAGGED_K) {
-      const size_t first = p.off[e];
+      const size_t first = (TR::LINEAR && !p.off ? 0 : p.off[e]) + k_from;
       a.setup(p.A[0] + first * p.lda + row0, p.lda, p.M - row0, K, tid);
 #pragma unroll
       for (int i = 0; i < NB; ++i) b[i].setup(p.B[i] + first * p.ldb + col0, p.ldb, p.N - col0, K, tid);
     } else {
-      a.setup(p.A[seg] + (size_t)row0 * p.lda, p.lda, row_end - row0, K, tid);
+      a.setup(p.A[seg] + (size_t)row0 * p.lda + k_from, p.lda, row_end - row0, K, tid);
 #pragma unroll
       for (int i = 0; i < NB; ++i) {
         const float* w = p.B[DUAL ? i : seg] + (size_t)e * p.b_es;
-        if constexpr (MODE == DA || MODE == DX || MODE == LDX) b[i].setup(w + (size_t)col0 * p.ldb, p.ldb, p.N - col0, K, tid);
-        else b[i].setup(w + col0, p.ldb, p.N - col0, K, tid);
+        if constexpr (MODE == DA || MODE == DX || MODE == LDX) b[i].setup(w + (size_t)col0 * p.ldb + k_from, p.ldb, p.N - col0, K, tid);
+        else b[i].setup(w + (size_t)k_from * p.ldb + col0, p.ldb, p.N - col0, K, tid);
       }
     }
   };
@@ -438,6 +458,15 @@ __device__ __forceinline__ void gemm_tile(const Args& p, int block, char* lds) {
   auto finish = [&](uint32_t todo, float scale) {
     const int col = col0 + wn * 32 + (lane & 31);
     if (col >= p.N) return;
+    if (TR::LINEAR && p.parts.n > 1) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int row = row0 + wm * 32 + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3);
+        if (row < row_end && (todo >> r & 1))
+          p.parts.sums[part * p.parts.stride + (size_t)e * p.c_es + (size_t)row * p.ldc + col] = (acc[0][0][r] + acc[0][1][r]) * scale;
+      }
+      return;
+    }
     if constexpr (MODE == LIN) {
       const float bias = p.bias ? p.bias[(size_t)e * p.N + col] : 0.f;
       with_activation(p.act, [&](auto a) {
@@ -626,27 +655,101 @@ int launch_expert_bwd_f32(const float* xp, const float* h1, const float* h3, con
   return launch_pair<DX, WGD>(x, mtb, v, vt, gradients_first(f), s);
 }
 
-// linear layer, grouped by expert or dense (offsets of one expert)
-int launch_linear_fwd_f32(const LinearArgs& l, hipStream_t s) {
-  Args u = {};
-  u.A[0] = (const float*)l.x; u.lda = l.K; u.B[0] = (const float*)l.w; u.ldb = l.N; u.b_es = (long)l.K * l.N;
-  u.C[0] = (float*)l.y; u.C[1] = (float*)l.z; u.ldc = l.N; u.N = l.N; u.K = l.K; u.off = l.offsets; u.e_cnt = l.e_cnt;
-  u.bias = (const float*)l.bias; u.R = (const float*)l.residual; u.act = l.act;
-  ProfScope prof(MOE_K_LINEAR, s);
-  return launch<LIN>(u, ((long long)l.rows + TM - 1) / TM + l.e_cnt, s);
+// ---- linear layer, grouped by expert or dense ------------------------------------------------------------------------
+namespace {
+
+// (tile, part) of one product, and of both gradients
+template <int MODE, int BUFS>
+__global__ __launch_bounds__(NT, BUFS == 2 ? 2 : Traits<MODE>::BLOCKS) void linear_f32(Args p) {
+  __shared__ __align__(16) char lds[BUFS * Traits<MODE>::BUFFER];
+  gemm_tile<MODE, BUFS>(p, blockIdx.x, lds, blockIdx.y);
+}
+struct Gradients {
+  Args x, w;
+  BiasGrad db;
+  int x_blocks, w_blocks, x_total, w_total;      // of one part (multiples of 8); of all
+  int w_first;
+};
+template <int BUFS>
+__global__ __launch_bounds__(NT, BUFS == 2 ? 2 : Traits<LDX>::BLOCKS) void gradients_f32(Gradients g) {
+  __shared__ __align__(16) char lds[BUFS * (Traits<LDX>::BUFFER > Traits<LWG>::BUFFER ? Traits<LDX>::BUFFER : Traits<LWG>::BUFFER)];
+  int b = blockIdx.x;
+  if (b >= g.x_total + g.w_total) return bias_columns<float>(g.db, b - g.x_total - g.w_total, reinterpret_cast<float*>(lds));
+  const int first = g.w_first ? g.w_total : g.x_total;
+  const bool in_first = b < first;
+  if (!in_first) b -= first;
+  if (in_first == (g.w_first != 0)) gemm_tile<LWG, BUFS>(g.w, b % g.w_blocks, lds, b / g.w_blocks);
+  else gemm_tile<LDX, BUFS>(g.x, b % g.x_blocks, lds, b / g.x_blocks);
+}
+static_assert(NT == BIAS_THREADS, "");
+
+// A k-tile takes 0.65 us while its workgroup has a CU for itself, and the chip multiplies 140 TFLOP/s: a contraction is cut until its tiles end
+// with everything, or in 6 us, while there are workgroups to take the parts.  1, 64 and 1000 rows of 2048 to 2048 fp32 forward 45, 50, 77 us uncut.
+constexpr float K_TILE = 0.65f;
+int f32_parts(long long tiles, long long k_tiles, float all) {
+  const float goal = all > 6.f ? all : 6.f;
+  int p = 1;
+  while (p < MOST_PARTS && (p + 1) * tiles <= 4 * CUT_WORKGROUPS && 4 * (p + 1) <= k_tiles && (float)((k_tiles + p - 1) / p) * K_TILE > goal) ++p;
+  return p;
+}
+long long f32_row_tiles(const LinearArgs& l) {
+  return ((long long)l.rows + TM - 1) / TM + (l.offsets ? (l.e_cnt < l.rows ? l.e_cnt : l.rows) - 1 : 0);
+}
+float f32_time(double products) { return (float)(2 * products / 140e6); }
+inline long long blocks8(long long tiles) { return (tiles + 7) / 8 * 8; }
+
+}  // namespace
+
+// rows * columns floats times the parts of at most 4 CUT_WORKGROUPS tiles of 64x64
+size_t linear_f32_parts_bytes(long long rows, int columns) {
+  const size_t all = (size_t)MOST_PARTS * rows * columns * 4, most = (size_t)4 * CUT_WORKGROUPS * TM * TN * 4;
+  return all < most ? all : most;
 }
 
-int launch_linear_bwd_f32(const LinearArgs& l, const void* dz, void* dx, void* dw, int accumulate, hipStream_t s) {
-  Args x = {};
+int launch_linear_fwd_f32(const LinearArgs& l, void* ws, hipStream_t s) {
+  Args u = {};
+  u.A[0] = (const float*)l.x; u.lda = l.K; u.B[0] = (const float*)l.w; u.ldb = l.N; u.b_es = (long)l.K * l.N;
+  u.C[0] = (float*)l.y; u.C[1] = (float*)l.z; u.ldc = l.N; u.N = l.N; u.K = l.K; u.off = l.offsets; u.e_cnt = l.e_cnt; u.rows = l.rows;
+  u.bias = (const float*)l.bias; u.R = (const float*)l.residual; u.act = l.act;
+  const long long tiles = f32_row_tiles(l) * ((l.N + TN - 1) / TN), blocks = blocks8(tiles);
+  u.parts = {(float*)ws, (size_t)l.rows * l.N, f32_parts(tiles, (l.K + TK - 1) / TK, f32_time((double)l.rows * l.K * l.N))};
+  {
+    ProfScope prof(MOE_K_LINEAR, s);
+    const auto kernel = use_two(blocks * u.parts.n) ? linear_f32<LIN, 2> : linear_f32<LIN, 1>;
+    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks, u.parts.n), dim3(NT), 0, s, u);
+    HIP_CHECK_LAUNCH();
+  }
+  return launch_join_forward<float>(l, u.parts, s);
+}
+
+// ws_dx: linear_f32_parts_bytes(rows, K), ws_dw: linear_f32_parts_bytes(e_cnt * K, N)
+int launch_linear_bwd_f32(const LinearArgs& l, const void* dz, void* dx, void* dw, int accumulate, const BiasGrad& db, void* ws_dx, void* ws_dw,
+                          hipStream_t s) {
+  const bool have_dx = dx && l.rows > 0;
+  Gradients g = {};
+  g.db = db;
+  Args& x = g.x;
   x.A[0] = (const float*)dz; x.lda = l.N; x.B[0] = (const float*)l.w; x.ldb = l.N; x.b_es = (long)l.K * l.N;
-  x.C[0] = (float*)dx; x.ldc = l.K; x.N = l.K; x.K = l.N; x.off = l.offsets; x.e_cnt = l.e_cnt;
-  Args w = {};
+  x.C[0] = (float*)dx; x.ldc = l.K; x.N = l.K; x.K = l.N; x.off = l.offsets; x.e_cnt = l.e_cnt; x.rows = l.rows;
+  Args& w = g.w;
   w.A[0] = (const float*)l.x; w.lda = l.K; w.B[0] = (const float*)dz; w.ldb = l.N;
   w.C[0] = (float*)dw; w.ldc = l.N; w.c_es = (long)l.K * l.N; w.M = l.K; w.N = l.N; w.off = l.offsets; w.e_cnt = l.e_cnt; w.beta = accumulate;
-  const long long mtb = ((long long)l.rows + TM - 1) / TM + l.e_cnt, wt = (long long)l.e_cnt * ((l.K + TM - 1) / TM);
-  const bool have_dx = dx && l.rows > 0;
-  ProfScope prof(have_dx && dw ? MOE_K_LINEAR_DX_DW : dw ? MOE_K_LINEAR_DW : MOE_K_LINEAR_DX, s);
-  if (have_dx && dw) return launch_pair<LDX, WG>(x, mtb, w, wt, 5ll * l.rows > 6ll * l.e_cnt * l.N, s);
-  if (dw) return launch<WG>(w, wt, s);
-  return have_dx ? launch<LDX>(x, mtb, s) : MOE_OK;
+  w.rows = l.rows;
+  const long long x_tiles = f32_row_tiles(l) * ((l.K + TN - 1) / TN), w_tiles = (long long)l.e_cnt * ((l.K + TM - 1) / TM) * ((l.N + TN - 1) / TN);
+  const float all = f32_time((double)l.rows * l.K * l.N * ((have_dx ? 1 : 0) + (dw ? 1 : 0)));
+  x.parts = {(float*)ws_dx, (size_t)l.rows * l.K, have_dx ? f32_parts(x_tiles, (l.N + TK - 1) / TK, all) : 1};
+  w.parts = {(float*)ws_dw, (size_t)l.e_cnt * l.K * l.N, dw ? f32_parts(w_tiles, (l.rows / l.e_cnt + TK - 1) / TK, all) : 1};
+  g.x_blocks = (int)blocks8(x_tiles);
+  g.w_blocks = (int)blocks8(w_tiles);
+  g.x_total = have_dx ? g.x_blocks * x.parts.n : 0;
+  g.w_total = dw ? g.w_blocks * w.parts.n : 0;
+  g.w_first = 5ll * l.rows / w.parts.n > 6ll * l.e_cnt * l.N / x.parts.n;      // the longer tiles (see the experts' backward)
+  const unsigned blocks = g.x_total + g.w_total + (db.db ? bias_blocks(l.N, l.e_cnt) : 0);
+  if (blocks > 0) {
+    ProfScope prof(have_dx && dw ? MOE_K_LINEAR_DX_DW : dw ? MOE_K_LINEAR_DW : have_dx ? MOE_K_LINEAR_DX : MOE_K_LINEAR_BIAS, s);
+    const auto kernel = use_two(blocks) ? gradients_f32<2> : gradients_f32<1>;
+    hipLaunchKernelGGL(kernel, dim3(blocks), dim3(NT), 0, s, g);
+    HIP_CHECK_LAUNCH();
+  }
+  return launch_join_gradients<float>(l, x.parts, dx, w.parts, dw, accumulate, s);
 }

@@ -32,5 +32,7 @@ size_t linear_parts_bytes(long long rows, int columns);
 int launch_linear_fwd_large(const LinearArgs& l, int32_t* sched, hipStream_t s);
 size_t linear_split_bytes(int K, int N);
 int launch_linear_bwd_large(const LinearArgs& l, const void* dz, void* dx, void* dw, int accumulate, int32_t* sched, void* ws, hipStream_t s);
-int launch_linear_fwd_f32(const LinearArgs& l, hipStream_t s);
-int launch_linear_bwd_f32(const LinearArgs& l, const void* dz, void* dx, void* dw, int accumulate, hipStream_t s);
+size_t linear_f32_parts_bytes(long long rows, int columns);
+int launch_linear_fwd_f32(const LinearArgs& l, void* ws, hipStream_t s);
+int launch_linear_bwd_f32(const LinearArgs& l, const void* dz, void* dx, void* dw, int accumulate, const BiasGrad& db, void* ws_dx, void* ws_dw,
+                          hipStream_t s);

@@ -6,35 +6,15 @@
 #include "activation.h"
 #include "bias_grad.h"
 #include "common.h"
-#include "kernels.h"
-#include "linear.h"
+#include "linear_finish.h"
 
 namespace {
 
-typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
-
-constexpr int SETUP_WORDS = 64;            // ticket counters, then the row offsets of a dense call
-__device__ __forceinline__ void write_setup(int32_t* words, int rows) {
-  const int i = threadIdx.x;
-  if (i < SETUP_WORDS + 2) words[i] = i == SETUP_WORDS + 1 ? rows : 0;
+constexpr int SETUP_WORDS = 64;            // ticket counters of the large tiles
+__device__ __forceinline__ void clear(int32_t* words) {
+  if (threadIdx.x < SETUP_WORDS) words[threadIdx.x] = 0;
 }
-__global__ void linear_setup(int32_t* words, int rows) { write_setup(words, rows); }
-
-template <typename T> constexpr int VEC = 16 / sizeof(T);
-__device__ __forceinline__ void values(u32x4 w, float (&v)[8]) {
-#pragma unroll
-  for (int j = 0; j < 4; ++j) { v[2 * j] = bf16lo(w[j]); v[2 * j + 1] = bf16hi(w[j]); }
-}
-__device__ __forceinline__ void values(u32x4 w, float (&v)[4]) {
-#pragma unroll
-  for (int j = 0; j < 4; ++j) v[j] = __uint_as_float(w[j]);
-}
-__device__ __forceinline__ u32x4 words(const float (&v)[8]) {
-  return u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
-}
-__device__ __forceinline__ u32x4 words(const float (&v)[4]) {
-  return u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])};
-}
+__global__ void linear_setup(int32_t* words) { clear(words); }
 
 // dz = dy act'(z), rounded to the type that the products take, and the column sums of what it was before, over 64 rows of an expert by
 // 64 lanes' 16 bytes.  Eight wavefronts take every eighth row each; their sums meet in ascending order.  HBM bound: dy and z in, dz out.
@@ -46,7 +26,7 @@ template <typename T>
 __global__ __launch_bounds__(GRAD_WAVES * WAVE) void act_grad(const int32_t* __restrict__ off, int rows, int e_cnt, int N, int act,
                                                               const T* __restrict__ dy, const T* __restrict__ z, T* __restrict__ dz,
                                                               float* __restrict__ sums, int32_t* __restrict__ setup) {
-  if (setup && blockIdx.x == 0) write_setup(setup, rows);
+  if (setup && blockIdx.x == 0) clear(setup);
   constexpr int V = VEC<T>, WIDTH = WAVE * V;
   __shared__ float part[GRAD_WAVES][V][WAVE];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -98,10 +78,9 @@ __global__ __launch_bounds__(GRAD_WAVES * WAVE) void act_grad(const int32_t* __r
 }
 
 // db, where no launch of the products takes it along
-template <typename T>
 __global__ __launch_bounds__(BIAS_THREADS) void bias_grad(BiasGrad p) {
   __shared__ float part[BIAS_THREADS];
-  bias_columns<T>(p, blockIdx.x, part);
+  bias_columns<bf16_t>(p, blockIdx.x, part);
 }
 
 template <typename T>
@@ -157,40 +136,36 @@ inline float large_bwd_time(const LinearArgs& l, bool dx, bool dw) {
   return 15.f + (at_early > at_late ? at_early : at_late);
 }
 Route forward_route(const LinearArgs& l) {
-  if (l.dtype != MOE_BF16) return LARGE;
   if (FWD_ROUTE >= 0) return (Route)FWD_ROUTE;
   if (l.rows <= 32ll * l.e_cnt) return FEW_ROWS;
   return linear_tiles_fwd_time(l) <= large_fwd_time(l) ? TILES : LARGE;
 }
 Route backward_route(const LinearArgs& l, bool dx, bool dw) {
-  if (l.dtype != MOE_BF16) return LARGE;
   if (BWD_ROUTE >= 0) return (Route)BWD_ROUTE;
   return linear_tiles_bwd_time(l, dx, dw) <= large_bwd_time(l, dx, dw) ? TILES : LARGE;
 }
 
 inline size_t align256(size_t v) { return (v + 255) & ~(size_t)255; }
-constexpr size_t SETUP_BYTES = 512;
-static_assert((SETUP_WORDS + 2) * 4 <= SETUP_BYTES, "");
-// The backward's workspace: what linear_setup writes, dz, the column sums, then what the products of bf16 take
+constexpr size_t SETUP_BYTES = SETUP_WORDS * 4;
+// The backward's workspace: the ticket counters, dz, the column sums, then what the products take
 struct BwdSpace {
   size_t dz, sums, products, dw_parts, end;
   BwdSpace(int dtype, int rows, int K, int N, int e_cnt) {
     dz = SETUP_BYTES;
     sums = dz + align256((size_t)rows * N * (dtype == MOE_BF16 ? 2 : 4));
     products = sums + align256((size_t)sum_lines(rows, e_cnt) * N * 4);
-    dw_parts = products + linear_parts_bytes(rows, K);
-    end = products;
-    if (dtype == MOE_BF16) {
-      const size_t parts = dw_parts + linear_parts_bytes((long long)e_cnt * K, N), pieces = products + MOE_MAX_LOCAL * 4 + linear_split_bytes(K, N);
-      end = parts > pieces ? parts : pieces;
-    }
+    const auto parts = dtype == MOE_BF16 ? linear_parts_bytes : linear_f32_parts_bytes;
+    dw_parts = products + align256(parts(rows, K));
+    end = dw_parts + parts((long long)e_cnt * K, N);
+    const size_t pieces = products + (dtype == MOE_BF16 ? MOE_MAX_LOCAL * 4 + linear_split_bytes(K, N) : 0);
+    if (end < pieces) end = pieces;
   }
 };
 
 }  // namespace
 
 size_t linear_fwd_ws_bytes(int dtype, int rows, int K, int N, int e_cnt) {
-  if (dtype != MOE_BF16) return SETUP_BYTES;
+  if (dtype != MOE_BF16) return SETUP_BYTES + linear_f32_parts_bytes(rows, N);
   const size_t few = linear_few_ws_bytes(rows, N), parts = linear_parts_bytes(rows, N);
   return SETUP_BYTES + (few > parts ? few : parts);
 }
@@ -199,48 +174,39 @@ size_t linear_bwd_ws_bytes(int dtype, int rows, int K, int N, int e_cnt) { retur
 int launch_linear_fwd(const LinearArgs& l, void* ws, hipStream_t s) {
   if (l.rows == 0 || l.e_cnt == 0) return MOE_OK;
   void* const parts = (char*)ws + SETUP_BYTES;
+  if (l.dtype == MOE_F32) return launch_linear_fwd_f32(l, parts, s);
   const Route route = forward_route(l);
   if (route == FEW_ROWS) return launch_linear_few(l, parts, s);
   if (route == TILES) return launch_linear_tiles_fwd(l, parts, s);
-  int32_t* const setup = (int32_t*)ws;
-  if (l.dtype == MOE_BF16 || !l.offsets) {
-    hipLaunchKernelGGL(linear_setup, dim3(1), dim3(128), 0, s, setup, l.rows);
-    HIP_CHECK_LAUNCH();
-  }
-  if (l.dtype == MOE_BF16) return launch_linear_fwd_large(l, setup, s);
-  LinearArgs with_offsets = l;
-  if (!l.offsets) with_offsets.offsets = setup + SETUP_WORDS;
-  return launch_linear_fwd_f32(with_offsets, s);
+  hipLaunchKernelGGL(linear_setup, dim3(1), dim3(SETUP_WORDS), 0, s, (int32_t*)ws);
+  HIP_CHECK_LAUNCH();
+  return launch_linear_fwd_large(l, (int32_t*)ws, s);
 }
 
 int launch_linear_bwd(const LinearArgs& l, const void* dy, void* dx, void* dw, void* db, int accumulate, void* ws, hipStream_t s) {
   if (l.e_cnt == 0) return MOE_OK;
   const BwdSpace space(l.dtype, l.rows, l.K, l.N, l.e_cnt);
   char* const base = (char*)ws;
-  const bool through = l.act != MOE_ACT_NONE, tiles = backward_route(l, dx, dw) == TILES, setup_needed = !tiles && (l.dtype == MOE_BF16 || !l.offsets);
+  const bool through = l.act != MOE_ACT_NONE, bf16 = l.dtype == MOE_BF16, large = bf16 && backward_route(l, dx, dw) == LARGE;
   void* const dz = through ? base + space.dz : nullptr;
   float* const sums = (float*)(base + space.sums);
-  int32_t* const setup = (int32_t*)ws;
+  int32_t* const setup = large ? (int32_t*)ws : nullptr;
   int rc;
   if (l.rows > 0 && (db || (through && (dx || dw)))) {
-    rc = l.dtype == MOE_BF16 ? gradients<bf16_t>(l, dy, dz, db ? sums : nullptr, setup_needed ? setup : nullptr, s)
-                             : gradients<float>(l, dy, dz, db ? sums : nullptr, setup_needed ? setup : nullptr, s);
+    rc = bf16 ? gradients<bf16_t>(l, dy, dz, db ? sums : nullptr, setup, s) : gradients<float>(l, dy, dz, db ? sums : nullptr, setup, s);
     if (rc) return rc;
-  } else if (setup_needed) {
-    hipLaunchKernelGGL(linear_setup, dim3(1), dim3(128), 0, s, setup, l.rows);
+  } else if (large) {
+    hipLaunchKernelGGL(linear_setup, dim3(1), dim3(SETUP_WORDS), 0, s, setup);
     HIP_CHECK_LAUNCH();
   }
   const void* const g = through ? dz : dy;
   const BiasGrad bias = {l.offsets, l.rows, l.N, accumulate, sums, db};
-  if (tiles) return launch_linear_tiles_bwd(l, g, dx, dw, accumulate, bias, base + space.products, base + space.dw_parts, s);
+  if (!bf16) return launch_linear_bwd_f32(l, g, dx, dw, accumulate, bias, base + space.products, base + space.dw_parts, s);
+  if (!large) return launch_linear_tiles_bwd(l, g, dx, dw, accumulate, bias, base + space.products, base + space.dw_parts, s);
   if (db) {
     ProfScope prof(MOE_K_LINEAR_BIAS, s);
-    if (l.dtype == MOE_BF16) hipLaunchKernelGGL(bias_grad<bf16_t>, dim3(bias_blocks(l.N, l.e_cnt)), dim3(BIAS_THREADS), 0, s, bias);
-    else hipLaunchKernelGGL(bias_grad<float>, dim3(bias_blocks(l.N, l.e_cnt)), dim3(BIAS_THREADS), 0, s, bias);
+    hipLaunchKernelGGL(bias_grad, dim3(bias_blocks(l.N, l.e_cnt)), dim3(BIAS_THREADS), 0, s, bias);
     HIP_CHECK_LAUNCH();
   }
-  if (l.dtype == MOE_BF16) return launch_linear_bwd_large(l, g, dx, dw, accumulate, setup, base + space.products, s);
-  LinearArgs with_offsets = l;
-  if (!l.offsets) with_offsets.offsets = setup + SETUP_WORDS;
-  return launch_linear_bwd_f32(with_offsets, g, dx, dw, accumulate, s);
+  return launch_linear_bwd_large(l, g, dx, dw, accumulate, setup, base + space.products, s);
 }

@@ -7,9 +7,8 @@
 // of a lane's eight instructions are then eight consecutive columns of one row of x.
 // A CU takes in about 33 GB/s of weights however many of its wavefronts ask for them, so what counts is how many CUs ask: few strips
 // are cut along the contraction (plan()), each part stores fp32 sums, and a second launch adds them in order and finishes them.
-#include "activation.h"
 #include "few_rows.h"
-#include "linear.h"
+#include "linear_finish.h"
 
 namespace {
 
@@ -17,8 +16,8 @@ constexpr int STRIP = 128, DEPTH = 2, PITCH = STRIP + 4, W = 4, TM = 64;
 
 struct FewArgs {
   LinearArgs l;
-  float* sums;             // [parts][rows][N]; parts == 1: none
-  int parts, part_steps;   // steps of 32 k of a part
+  Parts parts;
+  int part_steps;          // steps of 32 k of a part
 };
 
 // The expert (e), rows [row0, row0 + rows) and strip of a launch's tile `b`; false: the list is shorter.  An expert's tiles are listed by strip, row
@@ -46,24 +45,6 @@ __device__ __forceinline__ bool place_of(const LinearArgs& l, int b, int lane, P
   at.rows = __builtin_amdgcn_readfirstlane(min(TM, end - first - row_tile * TM));
   at.n0 = __builtin_amdgcn_readfirstlane(strip * STRIP);
   return true;
-}
-
-// z, activation and residual of eight columns of a row
-__device__ __forceinline__ void finish(const LinearArgs& l, int e, int row, int col, float (&y)[8]) {
-  const auto add = [&](const void* from, size_t at) {
-    const u32x4 u = *reinterpret_cast<const u32x4*>((const bf16_t*)from + at);
-#pragma unroll
-    for (int q = 0; q < 4; ++q) { y[2 * q] += bf16lo(u[q]); y[2 * q + 1] += bf16hi(u[q]); }
-  };
-  const auto store = [&](void* to, size_t at) {
-    *reinterpret_cast<u32x4*>((bf16_t*)to + at) = u32x4{pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]), pack_bf16x2(y[4], y[5]), pack_bf16x2(y[6], y[7])};
-  };
-  const size_t at = (size_t)row * l.N + col;
-  if (l.bias) add(l.bias, (size_t)e * l.N + col);
-  if (l.z) store(l.z, at);
-  activate(l.act, y);
-  if (l.residual) add(l.residual, at);
-  store(l.y, at);
 }
 
 template <int TG, bool STREAM>
@@ -140,13 +121,14 @@ __device__ __forceinline__ void few_tile(const FewArgs& p, const Place& at, int 
         hi += *reinterpret_cast<const f32x4*>(&sums[q][row][c + 4]);
       }
       const int to = at.row0 + 16 * t + row;
-      if (p.parts > 1) {
-        float* const s = p.sums + ((size_t)part * l.rows + to) * N + col;
+      const size_t out = (size_t)to * N + col;
+      if (p.parts.n > 1) {
+        float* const s = p.parts.sums + part * p.parts.stride + out;
         *reinterpret_cast<f32x4*>(s) = lo;
         *reinterpret_cast<f32x4*>(s + 4) = hi;
       } else {
         float y[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-        finish(l, at.e, to, col, y);
+        finish_forward<bf16_t>(l, at.e, out, col, y);
       }
     }
   }
@@ -163,28 +145,9 @@ __global__ __launch_bounds__(W * WAVE, 2) void linear_few(FewArgs p) {
   else few_tile<4, STREAM>(p, at, blockIdx.y, sums);
 }
 
-// The parts' sums, in ascending order: a thread takes eight columns of a row, a block 16 rows of a tile.
-__global__ __launch_bounds__(W * WAVE) void linear_join(FewArgs p) {
-  Place at;
-  if (!place_of(p.l, blockIdx.x, threadIdx.x & 63, at)) return;
-  const int row = 16 * blockIdx.y + threadIdx.x / (STRIP / 8), col = at.n0 + 8 * (threadIdx.x % (STRIP / 8));
-  if (row >= at.rows || col >= p.l.N) return;
-  const float* s = p.sums + (size_t)(at.row0 + row) * p.l.N + col;
-  f32x4 lo = f32x4{0.f, 0.f, 0.f, 0.f}, hi = lo;
-#pragma unroll 8
-  for (int q = 0; q < p.parts; ++q) {
-    lo += *reinterpret_cast<const f32x4*>(s);
-    hi += *reinterpret_cast<const f32x4*>(s + 4);
-    s += (size_t)p.l.rows * p.l.N;
-  }
-  float y[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-  finish(p.l, at.e, at.row0 + row, col, y);
-}
-
 #ifndef FEW_PARTS
 #define FEW_PARTS 0
 #endif
-constexpr int MOST_PARTS = 16, WORKGROUPS = 512;
 // tiles of 64 rows by a strip, at most
 inline long long tiles_of(int rows, int N, int e_cnt) {
   return (((long long)rows + TM - 1) / TM + (e_cnt < rows ? e_cnt : rows) - 1) * ((N + STRIP - 1) / STRIP);
@@ -197,9 +160,9 @@ inline int parts_of(int rows, int K, int N, int e_cnt) {
   const double memory = (double)(e_cnt < rows ? e_cnt : rows) * K * N * (2 / 6.5e6);
   double best = 0;
   int parts = 1;
-  for (int p = 1; p <= MOST_PARTS && p <= steps / (2 * W) && (p == 1 || p * tiles <= WORKGROUPS); ++p) {
+  for (int p = 1; p <= MOST_PARTS && p <= steps / (2 * W) && (p == 1 || p * tiles <= CUT_WORKGROUPS); ++p) {
     const double cu = (double)((p * tiles + 255) / 256) * ((steps + p - 1) / p) * (KP * 2 * STRIP / 40e3);
-    const double t = (cu > memory ? cu : memory) + (p > 1 ? 3 + p * (double)rows * N * (8 / 9e6) : 0);
+    const double t = (cu > memory ? cu : memory) + join_time(p, (double)rows * N);
     if (p == 1 || t < best) { best = t; parts = p; }
   }
   return parts;
@@ -207,27 +170,20 @@ inline int parts_of(int rows, int K, int N, int e_cnt) {
 
 }  // namespace
 
-// parts * rows * N floats for any number of rows up to this one: parts is at most MOST_PARTS, and WORKGROUPS strips of 64 rows
+// parts * rows * N floats for any number of rows up to this one: parts is at most MOST_PARTS, and CUT_WORKGROUPS strips of 64 rows
 size_t linear_few_ws_bytes(int rows, int N) {
-  const size_t all = (size_t)MOST_PARTS * rows * N * 4, most = (size_t)WORKGROUPS * TM * STRIP * 4;
+  const size_t all = (size_t)MOST_PARTS * rows * N * 4, most = (size_t)CUT_WORKGROUPS * TM * STRIP * 4;
   return all < most ? all : most;
 }
 
 int launch_linear_few(const LinearArgs& l, void* ws, hipStream_t s) {
-  FewArgs p = {l, (float*)ws, parts_of(l.rows, l.K, l.N, l.e_cnt), 0};
-  const int steps = (l.K + KP - 1) / KP;
-  p.part_steps = (steps + p.parts - 1) / p.parts;
-  p.parts = (steps + p.part_steps - 1) / p.part_steps;
-  const unsigned blocks = (unsigned)((tiles_of(l.rows, l.N, l.e_cnt) + 7) / 8 * 8);
-  const bool stream = 2ll * l.K * l.N * l.e_cnt > (256ll << 20);
+  const int steps = (l.K + KP - 1) / KP, parts = parts_of(l.rows, l.K, l.N, l.e_cnt), per = (steps + parts - 1) / parts;
+  const FewArgs p = {l, {(float*)ws, (size_t)l.rows * l.N, (steps + per - 1) / per}, per};
+  const dim3 grid((unsigned)((tiles_of(l.rows, l.N, l.e_cnt) + 7) / 8 * 8), p.parts.n);
   ProfScope prof(MOE_K_LINEAR, s);
-  if (stream) hipLaunchKernelGGL(linear_few<true>, dim3(blocks, p.parts), dim3(W * WAVE), 0, s, p);
-  else hipLaunchKernelGGL(linear_few<false>, dim3(blocks, p.parts), dim3(W * WAVE), 0, s, p);
+  // (stream_rule.h: weights that the Infinity Cache does not keep)
+  if (2ll * l.K * l.N * l.e_cnt > (256ll << 20)) hipLaunchKernelGGL(linear_few<true>, grid, dim3(W * WAVE), 0, s, p);
+  else hipLaunchKernelGGL(linear_few<false>, grid, dim3(W * WAVE), 0, s, p);
   HIP_CHECK_LAUNCH();
-  if (p.parts > 1) {
-    const int most = l.rows < TM ? l.rows : TM;
-    hipLaunchKernelGGL(linear_join, dim3(blocks, (most + 15) / 16), dim3(W * WAVE), 0, s, p);
-    HIP_CHECK_LAUNCH();
-  }
-  return MOE_OK;
+  return launch_join_forward<bf16_t>(l, p.parts, s);
 }

@@ -8,16 +8,11 @@
 // next half-way through its multiplication.  Where the tiles alone would not fill the chip the contraction is cut; a part's sums are stored
 // in fp32 and added in order by a launch behind (linear_join_*).
 // Every output is one chain of sums over ascending k per part.
-#include "activation.h"
 #include "bias_grad.h"
-#include "kernels.h"
-#include "linear.h"
+#include "linear_finish.h"
 #include "tile128.h"
 
 namespace {
-
-typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 enum { FWD, DX, DW };
 constexpr int NT = 256, TILE_PITCH = 68;
@@ -31,9 +26,8 @@ struct Product {
   long lda, ldb, b_es;
   bf16_t* C;
   int M, N, K;
-  float* sums;             // [parts] of the whole output
-  size_t sums_stride;
-  int parts, accumulate;
+  Parts parts;
+  int accumulate;
   long long tiles;         // at most, of one part (dense: exactly)
 };
 struct TileArgs {
@@ -82,27 +76,12 @@ __device__ __forceinline__ bool tile_of(const LinearArgs& l, const Product& p, i
   return true;
 }
 
-__device__ __forceinline__ void add8(float (&y)[8], u32x4 u) {
-#pragma unroll
-  for (int q = 0; q < 4; ++q) { y[2 * q] += bf16lo(u[q]); y[2 * q + 1] += bf16hi(u[q]); }
-}
-__device__ __forceinline__ u32x4 pack8(const float (&y)[8]) {
-  return u32x4{pack_bf16x2(y[0], y[1]), pack_bf16x2(y[2], y[3]), pack_bf16x2(y[4], y[5]), pack_bf16x2(y[6], y[7])};
-}
-__device__ __forceinline__ u32x4 load8(const void* p, size_t at) { return *reinterpret_cast<const u32x4*>((const bf16_t*)p + at); }
-__device__ __forceinline__ void store8(void* p, size_t at, const float (&y)[8]) { *reinterpret_cast<u32x4*>((bf16_t*)p + at) = pack8(y); }
-
 // eight finished columns of a row
 template <int OP>
 __device__ __forceinline__ void finish(const LinearArgs& l, const Product& p, int e, size_t at, int col, float (&y)[8]) {
-  if (OP == FWD) {
-    if (l.bias) add8(y, load8(l.bias, (size_t)e * l.N + col));
-    if (l.z) store8(l.z, at, y);
-    activate(l.act, y);
-    if (l.residual) add8(y, load8(l.residual, at));
-  }
-  if (OP == DW && p.accumulate) add8(y, load8(p.C, at));
-  store8(p.C, at, y);
+  if (OP == FWD) return finish_forward<bf16_t>(l, e, at, col, y);
+  if (OP == DW && p.accumulate) add_from<bf16_t>(p.C, at, y);
+  store_to<bf16_t>(p.C, at, y);
 }
 
 // STREAM (FWD): weights that one tile reads are loaded as such
@@ -115,7 +94,7 @@ __device__ __forceinline__ void multiply_tile(const LinearArgs& l, const Product
   const int n0 = t.nt * QT;
   const int row0 = OP == DW ? t.mt * QT : t.first + t.mt * QT, row_end = OP == DW ? p.M : t.end;      // of the output
   // k-tiles [kt, kt1) of 64, of the whole contraction [0, depth)
-  const int depth = OP == DW ? t.end - t.first : p.K, all = (depth + QK - 1) / QK, per = (all + p.parts - 1) / p.parts;
+  const int depth = OP == DW ? t.end - t.first : p.K, all = (depth + QK - 1) / QK, per = (all + p.parts.n - 1) / p.parts.n;
   const int kt0 = min(all, part * per), kt1 = min(all, kt0 + per);
 
   const uint32_t base = lds_addr(lds);
@@ -223,8 +202,8 @@ __device__ __forceinline__ void multiply_tile(const LinearArgs& l, const Product
     const float* from = slab + in * TILE_PITCH + (lane & 7) * 8;
     const f32x4 lo = *reinterpret_cast<const f32x4*>(from), hi = *reinterpret_cast<const f32x4*>(from + 4);
     const size_t at = ((size_t)(OP == DW ? t.e : 0) * p.M + row) * p.N + col;
-    if (p.parts > 1) {
-      float* const to = p.sums + (size_t)part * p.sums_stride + at;
+    if (p.parts.n > 1) {
+      float* const to = p.parts.sums + part * p.parts.stride + at;
       *reinterpret_cast<f32x4*>(to) = lo;
       *reinterpret_cast<f32x4*>(to + 4) = hi;
     } else {
@@ -257,46 +236,6 @@ __global__ __launch_bounds__(NT, 2) void linear_gradients(Gradients g) {
 }
 static_assert(NT == BIAS_THREADS, "");
 
-__device__ __forceinline__ void total_of(const Product& p, size_t at, float (&y)[8]) {
-  const float* s = p.sums + at;
-  f32x4 lo = f32x4{0.f, 0.f, 0.f, 0.f}, hi = lo;
-#pragma unroll 8
-  for (int q = 0; q < p.parts; ++q, s += p.sums_stride) {
-    lo += *reinterpret_cast<const f32x4*>(s);
-    hi += *reinterpret_cast<const f32x4*>(s + 4);
-  }
-#pragma unroll
-  for (int j = 0; j < 4; ++j) { y[j] = lo[j]; y[4 + j] = hi[j]; }
-}
-// The parts' sums of the forward: 16 rows of a tile a block
-__global__ __launch_bounds__(NT) void linear_join_fwd(TileArgs a) {
-  Tile t;
-  if (!tile_of<FWD>(a.l, a.p, blockIdx.x, threadIdx.x & 63, t)) return;
-  const int row = t.first + t.mt * QT + 16 * blockIdx.y + threadIdx.x / 16, col = t.nt * QT + 8 * (threadIdx.x % 16);
-  if (row >= t.end || col >= a.p.N) return;
-  const size_t at = (size_t)row * a.p.N + col;
-  float y[8];
-  total_of(a.p, at, y);
-  finish<FWD>(a.l, a.p, t.e, at, col, y);
-}
-// and of the gradients: of all rows of all experts, and of all matrices; a product that was not cut has no part in it
-__global__ __launch_bounds__(NT) void linear_join_bwd(LinearArgs l, Product dx, Product dw) {
-  const size_t rows = l.offsets ? (size_t)l.offsets[l.e_cnt] : (size_t)l.rows;
-  const size_t n_dx = dx.parts > 1 ? rows * dx.N / 8 : 0, n_dw = dw.parts > 1 ? (size_t)l.e_cnt * dw.M * dw.N / 8 : 0;
-  for (size_t v = (size_t)blockIdx.x * NT + threadIdx.x; v < n_dx + n_dw; v += (size_t)gridDim.x * NT) {
-    float y[8];
-    if (v < n_dx) {
-      total_of(dx, 8 * v, y);
-      finish<DX>(l, dx, 0, 8 * v, 0, y);
-    } else {
-      const size_t at = 8 * (v - n_dx);
-      total_of(dw, at, y);
-      finish<DW>(l, dw, 0, at, 0, y);
-    }
-  }
-}
-
-constexpr int MOST_PARTS = 16, WORKGROUPS = 512;
 #ifndef TILE_PARTS
 #define TILE_PARTS 0
 #endif
@@ -308,10 +247,8 @@ inline float k_tile(const KTile& k, float per_cu) {
   const float least = per_cu <= 1.f ? k.alone : k.two;
   return per_cu * k.many > least ? per_cu * k.many : least;
 }
-// What adding up the parts of n outputs takes
-inline float join_time(int parts, double n) { return parts > 1 ? 3.f + (float)(parts * n * (8.0 / 9e6)) : 0.f; }
 inline long long most_parts(long long tiles, long long k_tiles) {
-  const long long parts = tiles > 0 ? WORKGROUPS / tiles : 1, deep = k_tiles / 2;
+  const long long parts = tiles > 0 ? CUT_WORKGROUPS / tiles : 1, deep = k_tiles / 2;
   return parts < 1 || deep < 1 ? 1 : parts > MOST_PARTS ? (deep < MOST_PARTS ? deep : MOST_PARTS) : parts < deep ? parts : deep;
 }
 // The forward's parts, and its time
@@ -347,20 +284,20 @@ inline int whole_parts(int parts, long long k_tiles) {
 // whether the forward's weights come from memory: those of one layer, beyond what the Infinity Cache may keep of them
 inline bool streamed(const LinearArgs& l) { return 2ll * l.K * l.N * l.e_cnt > (100ll << 20); }
 Product forward_of(const LinearArgs& l, void* ws, float* time) {
-  Product p = {(const bf16_t*)l.x, (const bf16_t*)l.w, l.K, l.N, (long)l.K * l.N, (bf16_t*)l.y, 0, l.N, l.K, (float*)ws, (size_t)l.rows * l.N, 1, 0};
+  Product p = {(const bf16_t*)l.x, (const bf16_t*)l.w, l.K, l.N, (long)l.K * l.N, (bf16_t*)l.y, 0, l.N, l.K, {(float*)ws, (size_t)l.rows * l.N, 1}, 0};
   p.tiles = row_tiles(l) * column_tiles(l.N);
   const long long k_tiles = (l.K + QK - 1) / QK;
-  *time = forward_time(p.tiles, k_tiles, (double)l.rows * l.N, streamed(l) ? STREAMED : CACHED, &p.parts);
-  p.parts = whole_parts(p.parts, k_tiles);
+  *time = forward_time(p.tiles, k_tiles, (double)l.rows * l.N, streamed(l) ? STREAMED : CACHED, &p.parts.n);
+  p.parts.n = whole_parts(p.parts.n, k_tiles);
   return p;
 }
 Product dx_of(const LinearArgs& l, const void* dz, void* dx, void* ws) {
-  Product p = {(const bf16_t*)dz, (const bf16_t*)l.w, l.N, l.N, (long)l.K * l.N, (bf16_t*)dx, 0, l.K, l.N, (float*)ws, (size_t)l.rows * l.K, 1, 0};
+  Product p = {(const bf16_t*)dz, (const bf16_t*)l.w, l.N, l.N, (long)l.K * l.N, (bf16_t*)dx, 0, l.K, l.N, {(float*)ws, (size_t)l.rows * l.K, 1}, 0};
   p.tiles = row_tiles(l) * column_tiles(l.K);
   return p;
 }
 Product dw_of(const LinearArgs& l, const void* dz, void* dw, int accumulate, void* ws) {
-  Product p = {(const bf16_t*)l.x, (const bf16_t*)dz, l.K, l.N, 0, (bf16_t*)dw, l.K, l.N, 0, (float*)ws, (size_t)l.e_cnt * l.K * l.N, 1, accumulate};
+  Product p = {(const bf16_t*)l.x, (const bf16_t*)dz, l.K, l.N, 0, (bf16_t*)dw, l.K, l.N, 0, {(float*)ws, (size_t)l.e_cnt * l.K * l.N, 1}, accumulate};
   p.tiles = l.e_cnt * column_tiles(l.K) * column_tiles(l.N);
   return p;
 }
@@ -371,24 +308,24 @@ float plan_gradients(const LinearArgs& l, Product& x, Product& w) {
   float chain = 0.f, join = 0.f;
   double parts = 0;
   if (x.C) {
-    x.parts = whole_parts(chain_parts(x.tiles, kx, all), kx);
-    chain = (float)((kx + x.parts - 1) / x.parts) * CACHED.alone;
-    if (x.parts > 1) { join = 3.f; parts += (double)x.parts * l.rows * l.K; }
+    x.parts.n = whole_parts(chain_parts(x.tiles, kx, all), kx);
+    chain = (float)((kx + x.parts.n - 1) / x.parts.n) * CACHED.alone;
+    if (x.parts.n > 1) { join = 3.f; parts += (double)x.parts.n * l.rows * l.K; }
   }
   if (w.C) {
-    w.parts = chain_parts(w.tiles, kw, all);             // (experts' rows differ: parts of some may be empty)
-    const float c = (float)((kw + w.parts - 1) / w.parts) * CACHED.alone;
+    w.parts.n = chain_parts(w.tiles, kw, all);             // (experts' rows differ: parts of some may be empty)
+    const float c = (float)((kw + w.parts.n - 1) / w.parts.n) * CACHED.alone;
     chain = c > chain ? c : chain;
-    if (w.parts > 1) { join = 3.f; parts += (double)w.parts * l.e_cnt * l.K * l.N; }
+    if (w.parts.n > 1) { join = 3.f; parts += (double)w.parts.n * l.e_cnt * l.K * l.N; }
   }
   return 6.f + (all > chain ? all : chain) + join + (float)(parts * (8.0 / 9e6));
 }
 
 }  // namespace
 
-// Sums of parts of an output of `rows` x `columns`, for any number of rows up to this one: at most MOST_PARTS times the output, and WORKGROUPS tiles
+// Sums of parts of an output of `rows` x `columns`, for any number of rows up to this one: at most MOST_PARTS times the output, and CUT_WORKGROUPS tiles
 size_t linear_parts_bytes(long long rows, int columns) {
-  const size_t all = (size_t)MOST_PARTS * rows * columns * 4, most = (size_t)WORKGROUPS * QT * QT * 4;
+  const size_t all = (size_t)MOST_PARTS * rows * columns * 4, most = (size_t)CUT_WORKGROUPS * QT * QT * 4;
   return all < most ? all : most;
 }
 
@@ -409,14 +346,10 @@ int launch_linear_tiles_fwd(const LinearArgs& l, void* ws, hipStream_t s) {
   const unsigned blocks = blocks_of(a.p.tiles);
   ProfScope prof(MOE_K_LINEAR, s);
   // (stream_rule.h: weights that one tile reads and that the Infinity Cache does not keep)
-  if (l.rows <= (long long)QT * l.e_cnt && 2ll * l.K * l.N * l.e_cnt > (256ll << 20)) hipLaunchKernelGGL((linear_tiles<FWD, true>), dim3(blocks, a.p.parts), dim3(NT), 0, s, a);
-  else hipLaunchKernelGGL(linear_tiles<FWD>, dim3(blocks, a.p.parts), dim3(NT), 0, s, a);
+  if (l.rows <= (long long)QT * l.e_cnt && 2ll * l.K * l.N * l.e_cnt > (256ll << 20)) hipLaunchKernelGGL((linear_tiles<FWD, true>), dim3(blocks, a.p.parts.n), dim3(NT), 0, s, a);
+  else hipLaunchKernelGGL(linear_tiles<FWD>, dim3(blocks, a.p.parts.n), dim3(NT), 0, s, a);
   HIP_CHECK_LAUNCH();
-  if (a.p.parts > 1) {
-    hipLaunchKernelGGL(linear_join_fwd, dim3(blocks, ((l.rows < QT ? l.rows : QT) + 15) / 16), dim3(NT), 0, s, a);
-    HIP_CHECK_LAUNCH();
-  }
-  return MOE_OK;
+  return launch_join_forward<bf16_t>(l, a.p.parts, s);
 }
 
 // ws_dx: linear_parts_bytes(rows, K), ws_dw: linear_parts_bytes(e_cnt * K, N)
@@ -425,20 +358,13 @@ int launch_linear_tiles_bwd(const LinearArgs& l, const void* dz, void* dx, void*
   Product x = dx_of(l, dz, l.rows > 0 ? dx : nullptr, ws_dx), w = dw_of(l, dz, dw, accumulate, ws_dw);
   plan_gradients(l, x, w);
   Gradients g = {l, x, w, db, (int)blocks_of(x.tiles), l.offsets ? (int)((w.tiles + 255) / 256 * 256) : (int)blocks_of(w.tiles), 0, 0};
-  if (x.C) g.dx_total = g.dx_blocks * x.parts;
-  if (w.C) g.dw_total = g.dw_blocks * w.parts;
+  if (x.C) g.dx_total = g.dx_blocks * x.parts.n;
+  if (w.C) g.dw_total = g.dw_blocks * w.parts.n;
   const unsigned blocks = g.dx_total + g.dw_total + (db.db ? bias_blocks(l.N, l.e_cnt) : 0);
   if (blocks > 0) {
     ProfScope prof(x.C && w.C ? MOE_K_LINEAR_DX_DW : w.C ? MOE_K_LINEAR_DW : x.C ? MOE_K_LINEAR_DX : MOE_K_LINEAR_BIAS, s);
     hipLaunchKernelGGL(linear_gradients, dim3(blocks), dim3(NT), 0, s, g);
     HIP_CHECK_LAUNCH();
   }
-  if (x.parts > 1 || w.parts > 1) {
-    const long long n = ((x.parts > 1 ? (long long)l.rows * l.K : 0) + (w.parts > 1 ? (long long)l.e_cnt * l.K * l.N : 0)) / 8;
-    const long long blocks = (n + NT - 1) / NT, most = 8ll * device_cu_count();
-    ProfScope prof(MOE_K_WGRAD_REDUCE, s);
-    hipLaunchKernelGGL(linear_join_bwd, dim3((unsigned)(blocks < most ? blocks : most)), dim3(NT), 0, s, l, x, w);
-    HIP_CHECK_LAUNCH();
-  }
-  return MOE_OK;
+  return launch_join_gradients<bf16_t>(l, x.parts, dx, w.parts, dw, accumulate, s);
 }

@@ -150,6 +150,21 @@ def test_many_tiles(rows, K, N):
     Case(rows, K, N, "gelu_tanh", seed=N).check_both()
 
 
+@pytest.mark.parametrize("rows", [4096, [1030, 1000, 0, 1026, 1040]], ids=str)
+def test_a_whole_round_of_the_largest_tiles(rows):
+    """About 256 tiles of 256x256 in each product, one per CU, with a contraction that ends inside a k-tile."""
+    print(f"case linear {rows} 4088 4088", flush=True)
+    Case(rows, 4088, 4088, "silu", residual=isinstance(rows, int), seed=9).check_both()
+
+
+@pytest.mark.parametrize("dt,K,N", [(BF16, 4104, 136), (BF16, 136, 4104), (BF16, 7176, 2056), (F32, 2052, 68), (F32, 68, 2052)])
+@pytest.mark.parametrize("rows", [1, 33, 200, [3, 0, 40, 1], [130, 0, 70, 1, 5]], ids=str)
+def test_long_contractions(rows, dt, K, N):
+    """Few tiles, whose contractions are cut in parts."""
+    print(f"case linear {rows} {K} {N} {dt}", flush=True)
+    Case(rows, K, N, "gelu", dt, seed=K).check_both()
+
+
 @pytest.mark.parametrize("dt", (BF16, F32))
 @pytest.mark.parametrize("rows", [20000, [18000, 12, 0, 300]], ids=str)
 def test_weight_gradient_of_many_rows(rows, dt):
