@@ -6,6 +6,8 @@
 // The squares are of what is left of a value after its mean: a row whose mean is large beside its deviation keeps its digits.  Each wavefront
 // takes its own mean first, and the wavefronts' sums and squares join behind one barrier: with counts c_w, means m_w and squares q_w,
 //     sum (x - mean)^2 = sum_w q_w + c_w (m_w - mean)^2.
+#include <algorithm>
+
 #include "common.h"
 #include "kernels.h"
 #include "norm_rows.h"
@@ -24,8 +26,8 @@ struct FwdArgs {
   int row0;                                // of this launch
 };
 
-// A block per row, or (blockDim.y rows) a wavefront per row.
-template <typename T, typename R, int STEPS>
+// A block per row, or (blockDim.y rows) a wavefront per row.  STREAM: y is loaded and n stored as not used again soon.
+template <typename T, typename R, int STEPS, bool STREAM>
 __global__ __launch_bounds__((MOST_THREADS<T, STEPS>)) void layer_norm_fwd(FwdArgs<T, R> p) {
   constexpr int N = VEC<T>;
   __shared__ float2 red[MOST_WAVES];
@@ -42,7 +44,7 @@ __global__ __launch_bounds__((MOST_THREADS<T, STEPS>)) void layer_norm_fwd(FwdAr
     for (int j = 0; j < N; ++j) y[j] = h[i][j] = 0.f;
     if (c < p.d) {
       unpack(p.h, at + c, h[i]);
-      if (p.y) unpack(p.y, at + c, y);
+      if (p.y) unpack<N, STREAM>(p.y, at + c, y);
     }
 #pragma unroll
     for (int j = 0; j < N; ++j) h[i][j] += y[j];
@@ -100,7 +102,7 @@ __global__ __launch_bounds__((MOST_THREADS<T, STEPS>)) void layer_norm_fwd(FwdAr
     if (p.b) unpack(p.b, c, b);
 #pragma unroll
     for (int j = 0; j < N; ++j) h[i][j] = (h[i][j] - mean) * rstd * w[j] + b[j];
-    pack(p.n, at + c, h[i]);
+    pack<N, STREAM>(p.n, at + c, h[i]);
   }
 }
 
@@ -114,7 +116,7 @@ struct BwdArgs {
 };
 
 // What the backward reads of a row
-template <typename T, typename R, int STEPS>
+template <typename T, typename R, int STEPS, bool STREAM>
 struct BwdRow {
   static constexpr int N = VEC<T>;
   Raw<T, N> dn[STEPS];
@@ -129,9 +131,9 @@ struct BwdRow {
       const int c = (i * blockDim.x + threadIdx.x) * N;
       dn[i].clear(); h[i].clear(); dh[i].clear();
       if (row < p.T_ && c < p.d) {
-        h[i].load(p.h, at + c);
-        dn[i].load(p.dn, at + c);
-        if (p.dh_out) dh[i].load(p.dh_out, at + c);
+        h[i].template load<STREAM>(p.h, at + c);
+        dn[i].template load<STREAM>(p.dn, at + c);
+        if (p.dh_out) dh[i].template load<STREAM>(p.dh_out, at + c);
       }
     }
   }
@@ -139,8 +141,9 @@ struct BwdRow {
 
 // Blocks (or, for rows of one wavefront, wavefronts) walk the rows and keep the column sums of theirs in registers; the next row's loads are on
 // their way while a row's sums meet.  For WIDE rows the registers hold neither these nor the weights, and the column sums are in LDS.
+// STREAM: inputs beyond what the Infinity Cache holds are loaded as used once (streams()).
 constexpr int BWD_ROWS = 8, BWD_THREADS = 512, WIDE_THREADS = 1024;
-template <typename T, typename R, int STEPS, bool WIDE>
+template <typename T, typename R, int STEPS, bool WIDE, bool STREAM>
 __global__ __launch_bounds__(WIDE ? WIDE_THREADS : BWD_THREADS) void layer_norm_bwd(BwdArgs<T, R> p) {
   constexpr int N = VEC<T>;
   __shared__ float2 red[2][MOST_WAVES];
@@ -171,7 +174,7 @@ __global__ __launch_bounds__(WIDE ? WIDE_THREADS : BWD_THREADS) void layer_norm_
       for (int q = 0; q < N / 4; ++q) column(0, i, q) = column(1, i, q) = f32x4{0.f, 0.f, 0.f, 0.f};
     if (!WIDE && p.w && c < p.d) w_raw[i].load(p.w, c);
   }
-  BwdRow<T, R, STEPS> next;
+  BwdRow<T, R, STEPS, STREAM> next;
   int row = blockIdx.x * blockDim.y + threadIdx.y;
   if (!WIDE) next.load(p, row);
   for (; row < p.T_; row += gridDim.x * blockDim.y) {
@@ -262,17 +265,30 @@ int forward(FwdArgs<T, R> p, hipStream_t s) {
   if (vecs > WAVE && vecs <= 3 * WAVE / 2) steps = 2;
   const int threads = row_threads(vecs, steps), rows = threads == WAVE ? 4 : 1;
   const dim3 block(threads, rows);
+  // STREAM of tensors beyond the Infinity Cache, us, as usual / so: 32768 rows of 7168 bf16 with fp32 residuals 510 / 503, 16384 of 4096 140 / 138, of bf16
+  // 96 / 93, 65536 of 1024 94 / 87; within it 16384 of 1024 23.3 / 24.9.  Hints on the residual stream cost up to a tenth.
+  const bool stream = (double)p.T_ * p.d * 2 * (sizeof(T) + sizeof(R)) > (double)(256ll << 20);
+  const auto of = [&](auto st) {
+    constexpr bool STREAM = decltype(st)::value != 0;
+    return steps == 1 ? layer_norm_fwd<T, R, 1, STREAM> : steps == 2 ? layer_norm_fwd<T, R, 2, STREAM> : layer_norm_fwd<T, R, 4, STREAM>;
+  };
+  const auto kernel = stream ? of(Int<1>{}) : of(Int<0>{});
   return in_launches(((long long)p.T_ + rows - 1) / rows, threads * rows, [&](long long first, unsigned blocks) {
     p.row0 = (int)first * rows;
-    if (steps == 1) hipLaunchKernelGGL((layer_norm_fwd<T, R, 1>), dim3(blocks), block, 0, s, p);
-    else if (steps == 2) hipLaunchKernelGGL((layer_norm_fwd<T, R, 2>), dim3(blocks), block, 0, s, p);
-    else hipLaunchKernelGGL((layer_norm_fwd<T, R, 4>), dim3(blocks), block, 0, s, p);
+    hipLaunchKernelGGL(kernel, dim3(blocks), block, 0, s, p);
   });
 }
 
 // The backward's launch: rows of up to 16 elements a lane in one wavefront, several of them in a block; longer rows in a block each.
 struct BwdPlan { int steps, threads, rows, most, blocks; bool wide; };
-inline BwdPlan bwd_plan(int T, int d, int vec) {
+// Nontemporal loads of more than the Infinity Cache holds, us, as usual / so: 16384 rows of 4096 bf16 107 / 93, of 7168 174 / 154, 65536 of 1024
+// 103 / 90; of less: 2047 of 2880 16.5 / 19.4, 16384 of 1024 30.0 / 30.9.  Fewer rows at a time then do: 16384 of 4096 bf16 in one block of 512
+// threads per CU 89, with fp32 residuals 206 -> 197 (but fp32, eight elements a thread less, 16384 of 2048 88 -> 106); 32768 of 2048 in two blocks of
+// 256 per CU for four 98 -> 92.
+inline bool streams(int T, int d, int element, int residual, bool through) {
+  return (double)T * d * (element + residual * (through ? 2 : 1)) > (double)(256ll << 20);
+}
+inline BwdPlan bwd_plan(int T, int d, int vec, bool stream) {
   constexpr int CUS = 256;
   const int vecs = d / vec, per = 16 / vec;          // steps of 16 elements
   BwdPlan b;
@@ -281,7 +297,7 @@ inline BwdPlan bwd_plan(int T, int d, int vec) {
   else if (b.wide || row_threads(vecs, per) == WAVE) b.steps = per;
   else b.steps = row_threads(vecs, 1) <= BWD_THREADS ? 1 : row_threads(vecs, 2) <= BWD_THREADS ? 2 : per;
   b.threads = row_threads(vecs, b.steps);
-  const int per_cu = b.steps * vec == 16 ? 1 : b.threads > WAVE && b.threads <= 256 && T >= 8192 ? 4 : 2;
+  const int per_cu = b.steps * vec == 16 || (stream && vec == 8 && b.threads > 256) ? 1 : !stream && b.threads > WAVE && b.threads <= 256 && T >= 8192 ? 4 : 2;
   b.most = T < per_cu * CUS ? T : per_cu * CUS;
   b.rows = b.threads > WAVE ? 1 : T >= per_cu * CUS * BWD_ROWS ? BWD_ROWS : T == 0 ? 1 : (T - 1) / (per_cu * CUS) + 1;
   const int units = T == 0 ? 0 : (T - 1) / b.rows + 1;
@@ -291,7 +307,8 @@ inline BwdPlan bwd_plan(int T, int d, int vec) {
 
 template <typename T, typename R>
 int backward(BwdArgs<T, R> p, T* dw, T* db, int accumulate, hipStream_t s) {
-  const BwdPlan plan = bwd_plan(p.T_, p.d, VEC<T>);
+  const bool stream = streams(p.T_, p.d, sizeof(T), sizeof(R), p.dh_out);
+  const BwdPlan plan = bwd_plan(p.T_, p.d, VEC<T>, stream);
   const int steps = plan.steps, blocks = plan.blocks;
   const dim3 grid(blocks), block(plan.threads, plan.rows);
   constexpr int PER = 16 / VEC<T>;
@@ -303,16 +320,19 @@ int backward(BwdArgs<T, R> p, T* dw, T* db, int accumulate, hipStream_t s) {
       int dev = 0;
       if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return MOE_EHIP;
       if (!attr_set[dev]) {
-        if (hipFuncSetAttribute(reinterpret_cast<const void*>(&layer_norm_bwd<T, R, PER, true>), hipFuncAttributeMaxDynamicSharedMemorySize,
-                                2 * sizeof(float) * 16 * WIDE_THREADS) != hipSuccess)
-          return MOE_EHIP;
+        for (const void* kernel : {reinterpret_cast<const void*>(&layer_norm_bwd<T, R, PER, true, false>), reinterpret_cast<const void*>(&layer_norm_bwd<T, R, PER, true, true>)})
+          if (hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, 2 * sizeof(float) * 16 * WIDE_THREADS) != hipSuccess) return MOE_EHIP;
         attr_set[dev] = true;
       }
-      hipLaunchKernelGGL((layer_norm_bwd<T, R, PER, true>), grid, block, lds, s, p);
+      const auto kernel = stream ? layer_norm_bwd<T, R, PER, true, true> : layer_norm_bwd<T, R, PER, true, false>;
+      hipLaunchKernelGGL(kernel, grid, block, lds, s, p);
+    } else {
+      const auto of = [&](auto st) {
+        constexpr bool STREAM = decltype(st)::value != 0;
+        return steps == 1 ? layer_norm_bwd<T, R, 1, false, STREAM> : steps == 2 ? layer_norm_bwd<T, R, 2, false, STREAM> : layer_norm_bwd<T, R, PER, false, STREAM>;
+      };
+      hipLaunchKernelGGL(stream ? of(Int<1>{}) : of(Int<0>{}), grid, block, 0, s, p);
     }
-    else if (steps == 1) hipLaunchKernelGGL((layer_norm_bwd<T, R, 1, false>), grid, block, 0, s, p);
-    else if (steps == 2) hipLaunchKernelGGL((layer_norm_bwd<T, R, 2, false>), grid, block, 0, s, p);
-    else hipLaunchKernelGGL((layer_norm_bwd<T, R, PER, false>), grid, block, 0, s, p);
     HIP_CHECK_LAUNCH();
   }
   if (dw || db) {
@@ -327,8 +347,10 @@ int backward(BwdArgs<T, R> p, T* dw, T* db, int accumulate, hipStream_t s) {
 
 // For T rows and fewer, of bf16 or fp32
 size_t layer_norm_ws_bytes(int T, int d) {
-  const int a = bwd_plan(T, d, 8).most, b = bwd_plan(T, d, 4).most;
-  return (size_t)(a > b ? a : b) * 2 * d * sizeof(float);
+  int most = 0;
+  for (int vec : {8, 4})
+    for (bool stream : {false, true}) most = std::max(most, bwd_plan(T, d, vec, stream).most);
+  return (size_t)most * 2 * d * sizeof(float);
 }
 
 int launch_layer_norm_fwd(const void* y, const void* h, const void* w, const void* b, int dtype, int res_dtype, int T, int d, float eps, void* h_out,

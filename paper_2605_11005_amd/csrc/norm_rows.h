@@ -15,9 +15,13 @@ template <typename T> constexpr int VEC = 16 / sizeof(T);
 template <typename T, int N>
 struct Raw {
   u32x4 w[N * sizeof(T) / 16];
+  template <bool STREAM = false>      // not used again
   __device__ __forceinline__ void load(const T* p, size_t i) {
 #pragma unroll
-    for (int j = 0; j < (int)(N * sizeof(T) / 16); ++j) w[j] = *reinterpret_cast<const u32x4*>(p + i + j * VEC<T>);
+    for (int j = 0; j < (int)(N * sizeof(T) / 16); ++j) {
+      const u32x4* const from = reinterpret_cast<const u32x4*>(p + i + j * VEC<T>);
+      w[j] = STREAM ? __builtin_nontemporal_load(from) : *from;
+    }
   }
   __device__ __forceinline__ void clear() {
 #pragma unroll
@@ -31,30 +35,35 @@ struct Raw {
     }
   }
 };
-template <int N, typename T>
+template <int N, bool STREAM = false, typename T>
 __device__ __forceinline__ void unpack(const T* p, size_t i, float (&v)[N]) {
   Raw<T, N> raw;
-  raw.load(p, i);
+  raw.template load<STREAM>(p, i);
   raw.values(v);
 }
-template <int N>
+template <bool STREAM>
+__device__ __forceinline__ void store_words(void* p, u32x4 w) {
+  if constexpr (STREAM) __builtin_nontemporal_store(w, reinterpret_cast<u32x4*>(p));
+  else *reinterpret_cast<u32x4*>(p) = w;
+}
+template <int N, bool STREAM = false>
 __device__ __forceinline__ void pack(bf16_t* p, size_t i, const float (&v)[N]) {
 #pragma unroll
   for (int j = 0; j < N / 8; ++j) {
     u32x4 w;
 #pragma unroll
     for (int k = 0; k < 4; ++k) w[k] = pack_bf16x2(v[8 * j + 2 * k], v[8 * j + 2 * k + 1]);
-    *reinterpret_cast<u32x4*>(p + i + 8 * j) = w;
+    store_words<STREAM>(p + i + 8 * j, w);
   }
 }
-template <int N>
+template <int N, bool STREAM = false>
 __device__ __forceinline__ void pack(float* p, size_t i, const float (&v)[N]) {
 #pragma unroll
   for (int j = 0; j < N / 4; ++j) {
     u32x4 w;
 #pragma unroll
     for (int k = 0; k < 4; ++k) w[k] = __float_as_uint(v[4 * j + k]);
-    *reinterpret_cast<u32x4*>(p + i + 4 * j) = w;
+    store_words<STREAM>(p + i + 4 * j, w);
   }
 }
 
