@@ -97,10 +97,6 @@ int gradients(const LinearArgs& l, const void* dy, void* dz, float* sums, int32_
 }
 
 enum Route { FEW_ROWS, TILES, LARGE };
-#ifndef FWD_ROUTE
-#define FWD_ROUTE -1
-#define BWD_ROUTE -1
-#endif
 // Time in us of the 256x256 tiles, with all experts alike: whole rounds of the chip, each tile by the length of its contraction
 struct Large {
   long long n;             // tiles
@@ -136,12 +132,10 @@ inline float large_bwd_time(const LinearArgs& l, bool dx, bool dw) {
   return 15.f + (at_early > at_late ? at_early : at_late);
 }
 Route forward_route(const LinearArgs& l) {
-  if (FWD_ROUTE >= 0) return (Route)FWD_ROUTE;
   if (l.rows <= 32ll * l.e_cnt) return FEW_ROWS;
   return linear_tiles_fwd_time(l) <= large_fwd_time(l) ? TILES : LARGE;
 }
 Route backward_route(const LinearArgs& l, bool dx, bool dw) {
-  if (BWD_ROUTE >= 0) return (Route)BWD_ROUTE;
   return linear_tiles_bwd_time(l, dx, dw) <= large_bwd_time(l, dx, dw) ? TILES : LARGE;
 }
 

@@ -236,9 +236,6 @@ __global__ __launch_bounds__(NT, 2) void linear_gradients(Gradients g) {
 }
 static_assert(NT == BIAS_THREADS, "");
 
-#ifndef TILE_PARTS
-#define TILE_PARTS 0
-#endif
 // Time in us of a k-tile on a CU: one workgroup alone, two beside each other (both of them), and of each of many when the whole chip multiplies.
 // Operands that come from memory and not from the caches take longer.
 struct KTile { float alone, two, many; };
@@ -258,12 +255,10 @@ inline float forward_time(long long tiles, long long k_tiles, double outputs, co
     const float t = 6.f + (float)((k_tiles + p - 1) / p) * k_tile(k, (float)(tiles * p) / 256.f) + join_time(p, outputs);
     if (p == 1 || t < best) { best = t; *parts = p; }
   }
-  if (TILE_PARTS) *parts = TILE_PARTS;
   return best;
 }
 // Parts of both gradients' products in one launch: as many as bring either's longest tile down to what the chip takes for all of them
 inline int chain_parts(long long tiles, long long k_tiles, float all) {
-  if (TILE_PARTS) return TILE_PARTS;
   const long long most = most_parts(tiles, k_tiles);
   const float goal = all > 5.f ? all : 5.f;
   long long p = 1;
