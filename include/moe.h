@@ -347,9 +347,10 @@ int moe_layer_norm_bwd(const void* h_out, const void* w, const float* mean, cons
  * Sums, bias, activation and residual are fp32; z and y are rounded once each (y from the unrounded z).
  *
  * moe_linear_bwd -- the gradient, at the saved x and z:
- *     dz = dy act'(z)        dx = dz W[e]^T        dw[e] (+)= sum_rows x^T dz        db[e] (+)= sum_rows dz        (residual's is dy)
+ *     dz = dy act'(z)        dx (+)= dz W[e]^T        dw[e] (+)= sum_rows x^T dz        db[e] (+)= sum_rows dz        (residual's is dy)
  *   z NULL where act is MOE_ACT_NONE.  dx [cap,K] out (rows past the last expert's left untouched), dw [e_cnt,K,N], db [e_cnt,N] out; each may be
- *   NULL: not formed.  accumulate == 1 adds to dw and db; with 0 an expert without rows gets zeros.
+ *   NULL: not formed.  accumulate == 1 adds to dw and db; with 0 an expert without rows gets zeros.  dx_accumulate == 1 adds to dx (an input that
+ *   something else reads as well).
  *   ws: moe_workspace_bytes(MOE_WS_LINEAR_BWD, dtype, 0, 0, K, N, e_cnt, cap) bytes, 256-byte aligned
  * All sums are fp32.  In bf16 the products take dz rounded to bf16; db sums it unrounded.  relu's slope at 0 is 0.
  * Results are bit-reproducible from run to run.  fp32 products are those of moe_expert_fwd and _bwd.
@@ -360,7 +361,7 @@ int moe_layer_norm_bwd(const void* h_out, const void* w, const float* mean, cons
 int moe_linear_fwd(const void* x, int dtype, int cap, int K, int N, int e_cnt, const int32_t* offsets, const void* w, const void* bias, int act,
                    const void* residual, void* z, void* y, void* ws, size_t ws_bytes, moe_stream_t stream);
 int moe_linear_bwd(const void* x, const void* z, const void* dy, int dtype, int cap, int K, int N, int e_cnt, const int32_t* offsets, const void* w,
-                   int act, void* dx, void* dw, void* db, int accumulate, void* ws, size_t ws_bytes, moe_stream_t stream);
+                   int act, void* dx, int dx_accumulate, void* dw, void* db, int accumulate, void* ws, size_t ws_bytes, moe_stream_t stream);
 
 /*
  * Microscaled 4-bit numbers (the OCP MX format of e2m1 elements with one e8m0 scale per 32): an element is 0, 1/2, 1, 3/2, 2, 3, 4, 6 or the

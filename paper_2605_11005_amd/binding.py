@@ -108,7 +108,7 @@ def load_library():
     lib.moe_linear_fwd.restype = c_int
     lib.moe_linear_fwd.argtypes = [c_void_p] + [c_int] * 5 + [c_void_p] * 3 + [c_int] + [c_void_p] * 4 + [c_size_t, c_void_p]
     lib.moe_linear_bwd.restype = c_int
-    lib.moe_linear_bwd.argtypes = [c_void_p] * 3 + [c_int] * 5 + [c_void_p] * 2 + [c_int] + [c_void_p] * 3 + [c_int, c_void_p, c_size_t, c_void_p]
+    lib.moe_linear_bwd.argtypes = [c_void_p] * 3 + [c_int] * 5 + [c_void_p] * 2 + [c_int, c_void_p, c_int] + [c_void_p] * 2 + [c_int, c_void_p, c_size_t, c_void_p]
     lib.moe_workspace_bytes.restype = c_size_t
     lib.moe_workspace_bytes.argtypes = [c_int] * 8
     lib.moe_error_string.restype = ctypes.c_char_p
@@ -438,9 +438,9 @@ def moe_linear_fwd(x, offsets, w, bias, act, residual, z, y, ws):
                                          _ptr(z), _ptr(y), _ptr(ws), ws.numel() * ws.element_size(), _stream()), "moe_linear_fwd")
 
 
-def moe_linear_bwd(x, z, dy, offsets, w, act, dx, dw, db, accumulate, ws):
+def moe_linear_bwd(x, z, dy, offsets, w, act, dx, dw, db, accumulate, ws, dx_accumulate=False):
     """Shapes as in moe_linear_fwd; z None where act is ACT_NONE; outputs may be None.  The gradient of a residual is dy."""
-    rc = _marshal().linear_bwd(x, z, dy, offsets, w, act, dx, dw, db, accumulate, ws)
+    rc = _marshal().linear_bwd(x, z, dy, offsets, w, act, dx, dw, db, accumulate, ws, dx_accumulate)
     if rc >= 0:
         return _check(rc, "moe_linear_bwd")
     import torch
@@ -450,7 +450,7 @@ def moe_linear_bwd(x, z, dy, offsets, w, act, dx, dw, db, accumulate, ws):
     _need(z, dt, (cap, N), "z"); _need(dy, dt, (cap, N), "dy"); _need(dx, dt, (cap, K), "dx"); _need(dw, dt, batch + (K, N), "dw")
     _need(db, dt, batch + (N,), "db"); _need(ws, name="ws")
     _check(load_library().moe_linear_bwd(_ptr(x), _ptr(z), _ptr(dy), _dtype_code(x), cap, K, N, e_cnt, _ptr(offsets), _ptr(w), int(act), _ptr(dx),
-                                         _ptr(dw), _ptr(db), int(accumulate), _ptr(ws), ws.numel() * ws.element_size(), _stream()), "moe_linear_bwd")
+                                         int(dx_accumulate), _ptr(dw), _ptr(db), int(accumulate), _ptr(ws), ws.numel() * ws.element_size(), _stream()), "moe_linear_bwd")
 
 
 def mx4_shapes(n, K):

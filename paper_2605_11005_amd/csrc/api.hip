@@ -452,16 +452,16 @@ int moe_linear_fwd(const void* x, int dtype, int cap, int K, int N, int e_cnt, c
 }
 
 int moe_linear_bwd(const void* x, const void* z, const void* dy, int dtype, int cap, int K, int N, int e_cnt, const int32_t* offsets, const void* w,
-                   int act, void* dx, void* dw, void* db, int accumulate, void* ws, size_t ws_bytes, moe_stream_t stream) {
+                   int act, void* dx, int dx_accumulate, void* dw, void* db, int accumulate, void* ws, size_t ws_bytes, moe_stream_t stream) {
   int rc = shape_check_linear(dtype, cap, K, N, e_cnt, offsets, act);
   if (rc) return rc;
-  if (accumulate != 0 && accumulate != 1) return MOE_EINVAL;
+  if ((accumulate != 0 && accumulate != 1) || (dx_accumulate != 0 && dx_accumulate != 1)) return MOE_EINVAL;
   if (cap > 0 && (!dy || (dw && !x) || (act != MOE_ACT_NONE && !z))) return MOE_EINVAL;
   if (cap > 0 && e_cnt > 0 && dx && !w) return MOE_EINVAL;
   if (misaligned(x, 16) || misaligned(z, 16) || misaligned(dy, 16) || misaligned(w, 16) || misaligned(dx, 16) || misaligned(dw, 16) || misaligned(db, 16))
     return MOE_EINVAL;
   if (!ws || misaligned(ws, 256) || ws_bytes < linear_bwd_ws_bytes(dtype, cap, K, N, e_cnt)) return MOE_EWORKSPACE;
-  return launch_linear_bwd(LinearArgs{x, w, nullptr, nullptr, (void*)z, nullptr, dtype, cap, K, N, e_cnt, act, offsets}, dy, dx, dw, db, accumulate, ws,
+  return launch_linear_bwd(LinearArgs{x, w, nullptr, nullptr, (void*)z, nullptr, dtype, cap, K, N, e_cnt, act, offsets}, dy, dx, dx_accumulate, dw, db, accumulate, ws,
                            (hipStream_t)stream);
 }
 

@@ -541,6 +541,14 @@ __device__ __forceinline__ void quarter_tiles(const GArgs& p, const Quarters& li
           pre1[sl][pass] = p.R0 ? load16_once(p.R0 + (size_t)grow * p.ldc + gcol) : make_uint4(0, 0, 0, 0);
         }
     }
+    if (MODE == LDX && p.accumulate) {     // and the old values
+      const int gcol = min(n0 + wn * 64 + c8 * 8, p.N - 8);
+#pragma unroll
+      for (int sl = 0; sl < 4; ++sl)
+#pragma unroll
+        for (int pass = 0; pass < 2; ++pass)
+          pre1[sl][pass] = load16_once(p.C0 + (size_t)min(row0 + wm * 64 + 16 * sl + pass * 8 + (lane >> 3), row_end - 1) * p.ldc + gcol);
+    }
     f32x16 acc[2][2];
 #pragma unroll
     for (int i = 0; i < 2; ++i)
@@ -614,7 +622,7 @@ __device__ __forceinline__ void quarter_tiles(const GArgs& p, const Quarters& li
     else if (rows_left > 0) k_loop(IntC<1>{});
     else k_loop(IntC<0>{});
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
-    if (MODE == DA || MODE == LIN) {      // these have arrived: the compiler is to wait for them here, not behind the next tile's first loads
+    if (MODE == DA || MODE == LIN || (MODE == LDX && p.accumulate)) {      // these have arrived: the compiler is to wait for them here, not behind the next tile's first loads
       u32x4_t ub = __builtin_bit_cast(u32x4_t, bias);
       asm volatile("" : "+v"(ub));
       bias = __builtin_bit_cast(uint4, ub);
@@ -703,7 +711,10 @@ __device__ __forceinline__ void quarter_tiles(const GArgs& p, const Quarters& li
           if (grow < ep_row_end && gcol < p.N) {
             const size_t idx = (size_t)grow * p.ldc + gcol;
             if (MODE == DA) finish_da(p, idx, xs[pass], pre1[sl][pass], pre3[sl][pass]);
-            else store16(p.C0 + idx, pack8(xs[pass]));
+            else {
+              if (MODE == LDX && p.accumulate) add8(xs[pass], pre1[sl][pass]);
+              store16(p.C0 + idx, pack8(xs[pass]));
+            }
           }
         }
       }
@@ -1439,7 +1450,7 @@ __device__ __forceinline__ void gg_body(const GArgs& p) {
         }
       };
       // WG and the router's dx adding to existing gradients: the same, with the old values
-      constexpr bool rmw = (MODE == WG || MODE == RX) && !PARTIAL && RMW_TAG;
+      constexpr bool rmw = (MODE == WG || MODE == RX || MODE == LDX) && !PARTIAL && RMW_TAG;
       auto old_fetch = [&](int sl) {
         const int mi = sl >> 2, h = (sl >> 1) & 1, np = sl & 1;
 #pragma unroll
@@ -1560,7 +1571,7 @@ __device__ __forceinline__ void gg_body(const GArgs& p) {
     }
     };
     if ((MODE == WG || MODE == WGD) && ep_piece >= 0) epilogue(IntC<1>{}, IntC<0>{});
-    else if (((MODE == WG || MODE == WGD || MODE == RX) && p.accumulate) || (MODE == LIN && p.R0)) epilogue(IntC<0>{}, IntC<1>{});
+    else if (((MODE == WG || MODE == WGD || MODE == RX || MODE == LDX) && p.accumulate) || (MODE == LIN && p.R0)) epilogue(IntC<0>{}, IntC<1>{});
     else epilogue(IntC<0>{}, IntC<0>{});
   }
   if constexpr (SPLIT) {
@@ -2016,14 +2027,16 @@ size_t linear_split_bytes(int K, int N) {
   return 32 * piece <= most ? 32 * piece : most / piece * piece;
 }
 
-// dx = dz W^T and dW (+)= x^T dz; either may be left out.  ws: plan of MOE_MAX_LOCAL words, then linear_split_bytes
-int launch_linear_bwd_large(const LinearArgs& l, const void* dz, void* dx, void* dw, int accumulate, int32_t* sched, void* ws, hipStream_t s) {
+// dx (+)= dz W^T and dW (+)= x^T dz; either may be left out.  ws: plan of MOE_MAX_LOCAL words, then linear_split_bytes
+int launch_linear_bwd_large(const LinearArgs& l, const void* dz, void* dx, int dx_accumulate, void* dw, int accumulate, int32_t* sched, void* ws,
+                            hipStream_t s) {
   const long mn = (long)l.K * l.N;
   GArgs x = {};
   x.A0 = x.A1 = (const bf16_t*)dz; x.lda = l.N;
   x.B0 = x.B1 = (const bf16_t*)l.w; x.ldb = l.N; x.b_es = mn;
   x.C0 = (bf16_t*)dx; x.ldc = l.K;
   x.off = l.offsets; x.rows = x.chunk = l.rows; x.sched = sched; x.e_cnt = l.e_cnt; x.N = l.K; x.K = l.N;
+  x.accumulate = dx_accumulate;
   GArgs w = {};
   w.A0 = w.A1 = (const bf16_t*)l.x; w.lda = l.K;
   w.B0 = w.B1 = (const bf16_t*)dz; w.ldb = l.N;

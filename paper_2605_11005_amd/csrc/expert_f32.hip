@@ -723,14 +723,14 @@ int launch_linear_fwd_f32(const LinearArgs& l, void* ws, hipStream_t s) {
 }
 
 // ws_dx: linear_f32_parts_bytes(rows, K), ws_dw: linear_f32_parts_bytes(e_cnt * K, N)
-int launch_linear_bwd_f32(const LinearArgs& l, const void* dz, void* dx, void* dw, int accumulate, const BiasGrad& db, void* ws_dx, void* ws_dw,
+int launch_linear_bwd_f32(const LinearArgs& l, const void* dz, void* dx, int dx_accumulate, void* dw, int accumulate, const BiasGrad& db, void* ws_dx, void* ws_dw,
                           hipStream_t s) {
   const bool have_dx = dx && l.rows > 0;
   Gradients g = {};
   g.db = db;
   Args& x = g.x;
   x.A[0] = (const float*)dz; x.lda = l.N; x.B[0] = (const float*)l.w; x.ldb = l.N; x.b_es = (long)l.K * l.N;
-  x.C[0] = (float*)dx; x.ldc = l.K; x.N = l.K; x.K = l.N; x.off = l.offsets; x.e_cnt = l.e_cnt; x.rows = l.rows;
+  x.C[0] = (float*)dx; x.ldc = l.K; x.N = l.K; x.K = l.N; x.off = l.offsets; x.e_cnt = l.e_cnt; x.rows = l.rows; x.beta = dx_accumulate;
   Args& w = g.w;
   w.A[0] = (const float*)l.x; w.lda = l.K; w.B[0] = (const float*)dz; w.ldb = l.N;
   w.C[0] = (float*)dw; w.ldc = l.N; w.c_es = (long)l.K * l.N; w.M = l.K; w.N = l.N; w.off = l.offsets; w.e_cnt = l.e_cnt; w.beta = accumulate;
@@ -751,5 +751,5 @@ int launch_linear_bwd_f32(const LinearArgs& l, const void* dz, void* dx, void* d
     hipLaunchKernelGGL(kernel, dim3(blocks), dim3(NT), 0, s, g);
     HIP_CHECK_LAUNCH();
   }
-  return launch_join_gradients<float>(l, x.parts, dx, w.parts, dw, accumulate, s);
+  return launch_join_gradients<float>(l, x.parts, dx, dx_accumulate, w.parts, dw, accumulate, s);
 }

@@ -1,6 +1,6 @@
 // A linear layer, grouped by expert or dense:
 //     z = x W[e] + b[e]        y = act(z) + residual
-//     dz = dy act'(z)          dx = dz W[e]^T        dW[e] (+)= x^T dz        db[e] (+)= sum_rows dz
+//     dz = dy act'(z)          dx (+)= dz W[e]^T     dW[e] (+)= x^T dz        db[e] (+)= sum_rows dz
 // The products are those of expert_bf16.hip and expert_f32.hip; here are what surrounds them, dz with the sums of its columns, and which
 // kernel a call takes.
 #include "activation.h"
@@ -177,7 +177,7 @@ int launch_linear_fwd(const LinearArgs& l, void* ws, hipStream_t s) {
   return launch_linear_fwd_large(l, (int32_t*)ws, s);
 }
 
-int launch_linear_bwd(const LinearArgs& l, const void* dy, void* dx, void* dw, void* db, int accumulate, void* ws, hipStream_t s) {
+int launch_linear_bwd(const LinearArgs& l, const void* dy, void* dx, int dx_accumulate, void* dw, void* db, int accumulate, void* ws, hipStream_t s) {
   if (l.e_cnt == 0) return MOE_OK;
   const BwdSpace space(l.dtype, l.rows, l.K, l.N, l.e_cnt);
   char* const base = (char*)ws;
@@ -195,12 +195,12 @@ int launch_linear_bwd(const LinearArgs& l, const void* dy, void* dx, void* dw, v
   }
   const void* const g = through ? dz : dy;
   const BiasGrad bias = {l.offsets, l.rows, l.N, accumulate, sums, db};
-  if (!bf16) return launch_linear_bwd_f32(l, g, dx, dw, accumulate, bias, base + space.products, base + space.dw_parts, s);
-  if (!large) return launch_linear_tiles_bwd(l, g, dx, dw, accumulate, bias, base + space.products, base + space.dw_parts, s);
+  if (!bf16) return launch_linear_bwd_f32(l, g, dx, dx_accumulate, dw, accumulate, bias, base + space.products, base + space.dw_parts, s);
+  if (!large) return launch_linear_tiles_bwd(l, g, dx, dx_accumulate, dw, accumulate, bias, base + space.products, base + space.dw_parts, s);
   if (db) {
     ProfScope prof(MOE_K_LINEAR_BIAS, s);
     hipLaunchKernelGGL(bias_grad, dim3(bias_blocks(l.N, l.e_cnt)), dim3(BIAS_THREADS), 0, s, bias);
     HIP_CHECK_LAUNCH();
   }
-  return launch_linear_bwd_large(l, g, dx, dw, accumulate, setup, base + space.products, s);
+  return launch_linear_bwd_large(l, g, dx, dx_accumulate, dw, accumulate, setup, base + space.products, s);
 }

@@ -103,7 +103,8 @@ int launch_join_forward(const LinearArgs& l, const Parts& p, hipStream_t s) {
 
 // dx of all rows of all experts, and dW of all matrices; what was not cut has no part in it
 template <typename T>
-__global__ __launch_bounds__(JOIN_THREADS) void join_gradients(LinearArgs l, Parts px, T* dx, Parts pw, T* dw, int accumulate) {
+__global__ __launch_bounds__(JOIN_THREADS) void join_gradients(LinearArgs l, Parts px, T* dx, int dx_accumulate, Parts pw, T* dw,
+                                                            int accumulate) {
   constexpr int V = VEC<T>;
   const size_t rows = l.offsets ? (size_t)l.offsets[l.e_cnt] : (size_t)l.rows;
   const size_t n_dx = px.n > 1 ? rows * l.K / V : 0, n_dw = pw.n > 1 ? (size_t)l.e_cnt * l.K * l.N / V : 0;
@@ -111,6 +112,7 @@ __global__ __launch_bounds__(JOIN_THREADS) void join_gradients(LinearArgs l, Par
     float y[V];
     if (v < n_dx) {
       add_parts(px, V * v, y);
+      if (dx_accumulate) add_from<T>(dx, V * v, y);
       store_to<T>(dx, V * v, y);
     } else {
       const size_t at = V * (v - n_dx);
@@ -121,12 +123,13 @@ __global__ __launch_bounds__(JOIN_THREADS) void join_gradients(LinearArgs l, Par
   }
 }
 template <typename T>
-int launch_join_gradients(const LinearArgs& l, const Parts& px, void* dx, const Parts& pw, void* dw, int accumulate, hipStream_t s) {
+int launch_join_gradients(const LinearArgs& l, const Parts& px, void* dx, int dx_accumulate, const Parts& pw, void* dw, int accumulate, hipStream_t s) {
   if (px.n <= 1 && pw.n <= 1) return MOE_OK;
   const long long n = ((px.n > 1 ? (long long)l.rows * l.K : 0) + (pw.n > 1 ? (long long)l.e_cnt * l.K * l.N : 0)) / VEC<T>;
   const long long blocks = (n + JOIN_THREADS - 1) / JOIN_THREADS, most = 8ll * device_cu_count();
   ProfScope prof(MOE_K_WGRAD_REDUCE, s);
-  hipLaunchKernelGGL(join_gradients<T>, dim3((unsigned)(blocks < most ? blocks : most)), dim3(JOIN_THREADS), 0, s, l, px, (T*)dx, pw, (T*)dw, accumulate);
+  hipLaunchKernelGGL(join_gradients<T>, dim3((unsigned)(blocks < most ? blocks : most)), dim3(JOIN_THREADS), 0, s, l, px, (T*)dx, dx_accumulate, pw, (T*)dw,
+                     accumulate);
   HIP_CHECK_LAUNCH();
   return MOE_OK;
 }

@@ -1,7 +1,7 @@
 // The linear layer's products in bf16 where the large tiles of expert_bf16.hip would leave most of the chip idle: 128x128 tiles, as many workgroups as
 // it takes, contractions in parts.
 //     FWD  y  = act(x W + b) + residual    ragged rows, W read transposed
-//     DX   dx = dz W^T                     ragged rows, both operands contiguous along the contraction
+//     DX   dx (+)= dz W^T                  ragged rows, both operands contiguous along the contraction
 //     DW   dW (+)= x^T dz                  contraction over an expert's rows, both operands read transposed
 // Four wavefronts of 64x64 each, k-tiles 64 deep in two stages of 32 KB, two workgroups per CU: while one waits for its barrier or its operands
 // or finishes its outputs, the other multiplies.  A k-tile's fragments are read as a whole, so that its stage is free for the k-tile after the
@@ -80,7 +80,7 @@ __device__ __forceinline__ bool tile_of(const LinearArgs& l, const Product& p, i
 template <int OP>
 __device__ __forceinline__ void finish(const LinearArgs& l, const Product& p, int e, size_t at, int col, float (&y)[8]) {
   if (OP == FWD) return finish_forward<bf16_t>(l, e, at, col, y);
-  if (OP == DW && p.accumulate) add_from<bf16_t>(p.C, at, y);
+  if (p.accumulate) add_from<bf16_t>(p.C, at, y);
   store_to<bf16_t>(p.C, at, y);
 }
 
@@ -286,8 +286,8 @@ Product forward_of(const LinearArgs& l, void* ws, float* time) {
   p.parts.n = whole_parts(p.parts.n, k_tiles);
   return p;
 }
-Product dx_of(const LinearArgs& l, const void* dz, void* dx, void* ws) {
-  Product p = {(const bf16_t*)dz, (const bf16_t*)l.w, l.N, l.N, (long)l.K * l.N, (bf16_t*)dx, 0, l.K, l.N, {(float*)ws, (size_t)l.rows * l.K, 1}, 0};
+Product dx_of(const LinearArgs& l, const void* dz, void* dx, int accumulate, void* ws) {
+  Product p = {(const bf16_t*)dz, (const bf16_t*)l.w, l.N, l.N, (long)l.K * l.N, (bf16_t*)dx, 0, l.K, l.N, {(float*)ws, (size_t)l.rows * l.K, 1}, accumulate};
   p.tiles = row_tiles(l) * column_tiles(l.K);
   return p;
 }
@@ -331,7 +331,7 @@ float linear_tiles_fwd_time(const LinearArgs& l) {
 }
 float linear_tiles_bwd_time(const LinearArgs& l, bool dx, bool dw) {
   void* const some = (void*)1;
-  Product x = dx_of(l, nullptr, dx && l.rows > 0 ? some : nullptr, nullptr), w = dw_of(l, nullptr, dw ? some : nullptr, 0, nullptr);
+  Product x = dx_of(l, nullptr, dx && l.rows > 0 ? some : nullptr, 0, nullptr), w = dw_of(l, nullptr, dw ? some : nullptr, 0, nullptr);
   return plan_gradients(l, x, w);
 }
 
@@ -348,9 +348,9 @@ int launch_linear_tiles_fwd(const LinearArgs& l, void* ws, hipStream_t s) {
 }
 
 // ws_dx: linear_parts_bytes(rows, K), ws_dw: linear_parts_bytes(e_cnt * K, N)
-int launch_linear_tiles_bwd(const LinearArgs& l, const void* dz, void* dx, void* dw, int accumulate, const BiasGrad& db, void* ws_dx, void* ws_dw,
+int launch_linear_tiles_bwd(const LinearArgs& l, const void* dz, void* dx, int dx_accumulate, void* dw, int accumulate, const BiasGrad& db, void* ws_dx, void* ws_dw,
                             hipStream_t s) {
-  Product x = dx_of(l, dz, l.rows > 0 ? dx : nullptr, ws_dx), w = dw_of(l, dz, dw, accumulate, ws_dw);
+  Product x = dx_of(l, dz, l.rows > 0 ? dx : nullptr, dx_accumulate, ws_dx), w = dw_of(l, dz, dw, accumulate, ws_dw);
   plan_gradients(l, x, w);
   Gradients g = {l, x, w, db, (int)blocks_of(x.tiles), l.offsets ? (int)((w.tiles + 255) / 256 * 256) : (int)blocks_of(w.tiles), 0, 0};
   if (x.C) g.dx_total = g.dx_blocks * x.parts.n;
@@ -361,5 +361,5 @@ int launch_linear_tiles_bwd(const LinearArgs& l, const void* dz, void* dx, void*
     hipLaunchKernelGGL(linear_gradients, dim3(blocks), dim3(NT), 0, s, g);
     HIP_CHECK_LAUNCH();
   }
-  return launch_join_gradients<bf16_t>(l, x.parts, dx, w.parts, dw, accumulate, s);
+  return launch_join_gradients<bf16_t>(l, x.parts, dx, dx_accumulate, w.parts, dw, accumulate, s);
 }

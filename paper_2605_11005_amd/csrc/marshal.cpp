@@ -578,6 +578,7 @@ PyObject* linear_bwd(PyObject*, PyObject* const* v, Py_ssize_t n) {
     const Buf dx = any(a, true), dw = any(a, true), db = any(a, true);
     const int accumulate = a.flag();
     const Buf ws = any(a);
+    const int dx_accumulate = a.flag();
     const Linear l(x, off, w);
     for (const Buf* m : {&z, &dy}) l.rows(*m, l.N);
     l.rows(dx, l.K);
@@ -586,8 +587,8 @@ PyObject* linear_bwd(PyObject*, PyObject* const* v, Py_ssize_t n) {
     const int dt = dtype_code(x);
     const size_t ws_bytes = (size_t)ws.bytes();
     return [=, s = stream()] {
-      return entry.linear_bwd(x.ptr, z.ptr, dy.ptr, dt, l.cap, l.K, l.N, l.e_cnt, (const int32_t*)off.ptr, w.ptr, act, dx.ptr, dw.ptr, db.ptr,
-                              accumulate, ws.ptr, ws_bytes, s);
+      return entry.linear_bwd(x.ptr, z.ptr, dy.ptr, dt, l.cap, l.K, l.N, l.e_cnt, (const int32_t*)off.ptr, w.ptr, act, dx.ptr, dx_accumulate,
+                              dw.ptr, db.ptr, accumulate, ws.ptr, ws_bytes, s);
     };
   });
 }

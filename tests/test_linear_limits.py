@@ -16,8 +16,9 @@ def fwd(x=P, dtype=B.MOE_BF16, cap=4, K=16, N=8, e_cnt=2, offsets=P, w=P, bias=P
     return B.load_library().moe_linear_fwd(x, dtype, cap, K, N, e_cnt, offsets, w, bias, act, residual, z, y, ws, ws_bytes, None)
 
 
-def bwd(x=P, z=P, dy=P, dtype=B.MOE_BF16, cap=4, K=16, N=8, e_cnt=2, offsets=P, w=P, act=2, dx=P, dw=P, db=P, accumulate=0, ws=P, ws_bytes=MB):
-    return B.load_library().moe_linear_bwd(x, z, dy, dtype, cap, K, N, e_cnt, offsets, w, act, dx, dw, db, accumulate, ws, ws_bytes, None)
+def bwd(x=P, z=P, dy=P, dtype=B.MOE_BF16, cap=4, K=16, N=8, e_cnt=2, offsets=P, w=P, act=2, dx=P, dw=P, db=P, accumulate=0, ws=P, ws_bytes=MB,
+        dx_accumulate=0):
+    return B.load_library().moe_linear_bwd(x, z, dy, dtype, cap, K, N, e_cnt, offsets, w, act, dx, dx_accumulate, dw, db, accumulate, ws, ws_bytes, None)
 
 
 @pytest.mark.parametrize("call", (fwd, bwd))
@@ -34,7 +35,7 @@ def test_linear_refuses(call, args, code):
 
 def test_linear_refuses_one_way():
     assert fwd(y=None) == EINVAL and fwd(y=ODD) == EINVAL and fwd(bias=ODD) == EINVAL and fwd(residual=ODD) == EINVAL
-    assert bwd(dy=None) == EINVAL and bwd(z=None) == EINVAL and bwd(accumulate=2) == EINVAL and bwd(dx=ODD) == EINVAL and bwd(dw=ODD) == EINVAL
+    assert bwd(dy=None) == EINVAL and bwd(z=None) == EINVAL and bwd(accumulate=2) == EINVAL and bwd(dx_accumulate=-1) == EINVAL and bwd(dx=ODD) == EINVAL and bwd(dw=ODD) == EINVAL
     # nothing to do: no launch
     assert fwd(cap=0, x=None, y=None) == 0 and fwd(e_cnt=0, w=None) == 0 and bwd(e_cnt=0) == 0
 
