@@ -8,41 +8,12 @@
 // A CU takes in about 33 GB/s of weights however many of its wavefronts ask for them (4 rows of 4096 to 14336: 31 to 33 us with 4, 8 and 16 wavefronts
 // for each of 112 strips), so what counts is how many CUs ask: narrower strips, or strips cut along the contraction, whose parts store fp32 sums
 // that a second launch adds in order and finishes (plan_of).
-#include "few_rows.h"
 #include "linear_finish.h"
+#include "linear_piece.h"
 
 namespace {
 
-constexpr int DEPTH = 2, W = 4, TM = 64;
-
-// A wavefront's piece of a weight matrix: a lane holds C columns of each of eight rows.
-template <int C>
-struct FewPiece {
-  unsigned int w[8][C / 2];
-  template <bool STREAM>
-  __device__ __forceinline__ void load(const bf16_t* base, bool in, int row, int voff) {
-    constexpr int NT = STREAM ? 2 : 0;
-    const __amdgpu_buffer_rsrc_t d = descriptor(base, in);
-#pragma unroll
-    for (int r = 0; r < 8; ++r) {
-      if constexpr (C == 8) {
-        const u32x4 v = __builtin_amdgcn_raw_buffer_load_b128(d, voff, r * row, NT);
-#pragma unroll
-        for (int q = 0; q < 4; ++q) w[r][q] = v[q];
-      } else {
-        const u32x2 v = __builtin_amdgcn_raw_buffer_load_b64(d, voff, r * row, NT);
-        w[r][0] = v[0];
-        w[r][1] = v[1];
-      }
-    }
-  }
-  __device__ __forceinline__ bf16x8 operand(int j) const {      // column j of the block, its eight k
-    u32x4 f;
-#pragma unroll
-    for (int q = 0; q < 4; ++q) f[q] = __builtin_amdgcn_perm(w[2 * q + 1][j >> 1], w[2 * q][j >> 1], (j & 1) ? 0x07060302u : 0x05040100u);
-    return __builtin_bit_cast(bf16x8, f);
-  }
-};
+constexpr int DEPTH = 2, W = 4, TM = 64, KP = 32;
 
 struct FewArgs {
   LinearArgs l;
@@ -91,7 +62,7 @@ __device__ __forceinline__ void few_tile(const FewArgs& p, const Place& at, int 
   int xrow[TG];
 #pragma unroll
   for (int t = 0; t < TG; ++t) xrow[t] = 2 * min(16 * t + i, rows - 1) * K;
-  FewPiece<C> piece[DEPTH];
+  ColumnPiece<C> piece[DEPTH];
   u32x4 xs[DEPTH][TG];
   auto load = [&](auto slot, int step) {
     constexpr int S = decltype(slot)::value;

@@ -10,6 +10,7 @@
 // Every output is one chain of sums over ascending k per part.
 #include "bias_grad.h"
 #include "linear_finish.h"
+#include "linear_piece.h"
 #include "tile128.h"
 
 namespace {
@@ -84,7 +85,7 @@ __device__ __forceinline__ void finish(const LinearArgs& l, const Product& p, in
   store_to<bf16_t>(p.C, at, y);
 }
 
-// STREAM (FWD): weights that one tile reads are loaded as such
+// STREAM (FWD, DX): weights that one tile reads are loaded as such
 template <int OP, bool STREAM = false>
 __device__ __forceinline__ void multiply_tile(const LinearArgs& l, const Product& p, int b, int part, char* lds) {
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -117,7 +118,7 @@ __device__ __forceinline__ void multiply_tile(const LinearArgs& l, const Product
       const uint32_t back = OP != DW && last < QK - 1 ? past_end((int)k0 + 8 * QuarterKc::chunk(j, lane), depth) : 0;
       if (OP == DW) a_tr.template issue1<true>(j, st, wave, lane, k0, last);
       else a_kc.issue1(j, st, wave, k0, back);
-      if (OP == DX) b_kc.issue1(j, st + QOPER_BYTES, wave, k0, back);
+      if (OP == DX) b_kc.template issue1<STREAM>(j, st + QOPER_BYTES, wave, k0, back);
       else b_tr.template issue1<true, STREAM>(j, st + QOPER_BYTES, wave, lane, k0, last);
     }
   };
@@ -213,26 +214,83 @@ __device__ __forceinline__ void multiply_tile(const LinearArgs& l, const Product
   }
 }
 
+// dW where the experts have few rows, bound by writing it: every wavefront forms 64 x 128 of a matrix by itself, 32 rows at a time, both operands through
+// registers (linear_piece.h).  Element r of acc[i][j] is row 4 (4 (lane / 16) + r) + i, column 8 (lane % 16) + j.
+constexpr int OUTER_M = 64, OUTER_N = 128, OUTER_ROWS = 64;
+__device__ __forceinline__ void outer_tile(const LinearArgs& l, const Product& p, int b) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), i = lane & 15, g = lane >> 4;
+  const int mt = (p.M + OUTER_M - 1) / OUTER_M, nt = (p.N + OUTER_N - 1) / OUTER_N, at = b * (NT / WAVE) + wave;
+  if (at >= l.e_cnt * mt * nt) return;
+  const int e = at / (mt * nt), in_e = at - e * mt * nt, m0 = in_e / nt * OUTER_M, n0 = in_e % nt * OUTER_N;
+  const int first = __builtin_amdgcn_readfirstlane(l.offsets ? l.offsets[e] : 0), end = __builtin_amdgcn_readfirstlane(l.offsets ? l.offsets[e + 1] : l.rows);
+  const int xcol = 2 * min(4 * i, p.M - m0 - 4), zcol = 2 * min(8 * i, p.N - n0 - 8);        // columns past the end repeat the last ones
+  const int xrow = 2 * (int)p.lda, zrow = 2 * (int)p.ldb;
+  f32x4 acc[4][8];
+#pragma unroll
+  for (int a = 0; a < 4; ++a)
+#pragma unroll
+    for (int c = 0; c < 8; ++c) acc[a][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+  for (int row = first; row < end; row += 32) {
+    ColumnPiece<4> x;
+    ColumnPiece<8> z;
+    const bf16_t* const xb = p.A + (size_t)row * p.lda + m0;
+    const bf16_t* const zb = p.B + (size_t)row * p.ldb + n0;
+    if (end - row >= 32) {
+      x.load<false>(xb, true, xrow, 8 * g * xrow + xcol);
+      z.load<false>(zb, true, zrow, 8 * g * zrow + zcol);
+    } else {
+      x.load_end(xb, xrow, 8 * g, end - row, xcol);
+      z.load_end(zb, zrow, 8 * g, end - row, zcol);
+    }
+#pragma unroll
+    for (int c = 0; c < 8; ++c) {
+      const bf16x8 f = z.operand(c);
+#pragma unroll
+      for (int a = 0; a < 4; ++a) acc[a][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x.operand(a), f, acc[a][c], 0, 0, 0);
+    }
+  }
+  const int col = n0 + 8 * i;
+  if (col >= p.N) return;
+#pragma unroll
+  for (int r = 0; r < 4; ++r)
+#pragma unroll
+    for (int a = 0; a < 4; ++a) {
+      const int m = m0 + 4 * (4 * g + r) + a;
+      if (m >= p.M) continue;
+      float y[8];
+#pragma unroll
+      for (int c = 0; c < 8; ++c) y[c] = acc[a][c][r];
+      finish<DW>(l, p, e, ((size_t)e * p.M + m) * p.N + col, col, y);
+    }
+}
+
 template <int OP, bool STREAM = false>
 __global__ __launch_bounds__(NT, 2) void linear_tiles(TileArgs a) {
   __shared__ __align__(1024) char lds[TILE_LDS];
   multiply_tile<OP, STREAM>(a.l, a.p, blockIdx.x, blockIdx.y, lds);
 }
 
-// The gradients in one launch: dW's blocks, dx's, db's.  (dx_blocks, dw_blocks: of one part; multiples of 8)
+// The gradients in one launch: dW's blocks and dx's, the longer ones first, and db's.  (dx_blocks, dw_blocks: of one part; multiples of 8)
 struct Gradients {
   LinearArgs l;
   Product dx, dw;
   BiasGrad db;
   int dx_blocks, dw_blocks, dx_total, dw_total;
+  int outer;               // dW by outer_tile
+  int dx_first;
 };
+template <bool STREAM>
 __global__ __launch_bounds__(NT, 2) void linear_gradients(Gradients g) {
   __shared__ __align__(1024) char lds[TILE_LDS];
   int b = blockIdx.x;
-  if (b < g.dw_total) return multiply_tile<DW>(g.l, g.dw, b % g.dw_blocks, b / g.dw_blocks, lds);
-  b -= g.dw_total;
-  if (b < g.dx_total) return multiply_tile<DX>(g.l, g.dx, b % g.dx_blocks, b / g.dx_blocks, lds);
-  bias_columns<bf16_t>(g.db, b - g.dx_total, reinterpret_cast<float*>(lds));
+  const int dw = g.dx_first ? b - g.dx_total : b, dx = g.dx_first ? b : b - g.dw_total;
+  if (dx >= 0 && dx < g.dx_total) return multiply_tile<DX, STREAM>(g.l, g.dx, dx % g.dx_blocks, dx / g.dx_blocks, lds);
+  if (dw >= 0 && dw < g.dw_total) {
+    if (g.outer) return outer_tile(g.l, g.dw, dw);
+    return multiply_tile<DW>(g.l, g.dw, dw % g.dw_blocks, dw / g.dw_blocks, lds);
+  }
+  b -= g.dx_total + g.dw_total;
+  bias_columns<bf16_t>(g.db, b, reinterpret_cast<float*>(lds));
 }
 static_assert(NT == BIAS_THREADS, "");
 
@@ -297,19 +355,26 @@ Product dw_of(const LinearArgs& l, const void* dz, void* dw, int accumulate, voi
   return p;
 }
 // parts of both; returns the time of their launch and of the one that adds the parts up
-float plan_gradients(const LinearArgs& l, Product& x, Product& w) {
+inline long long outer_waves(const LinearArgs& l) {
+  return (long long)l.e_cnt * ((l.K + OUTER_M - 1) / OUTER_M) * ((l.N + OUTER_N - 1) / OUTER_N);
+}
+float plan_gradients(const LinearArgs& l, Product& x, Product& w, bool* outer, bool* dx_first) {
   const long long kx = (l.N + QK - 1) / QK, kw = ((long long)l.rows / l.e_cnt + QK - 1) / QK;
-  const float all = CACHED.many / 256.f * (float)((x.C ? x.tiles * kx : 0) + (w.C ? w.tiles * kw : 0));
+  *outer = w.C && (long long)OUTER_ROWS * l.e_cnt >= l.rows;
+  const float all = CACHED.many / 256.f * (float)((x.C ? x.tiles * kx : 0) + (w.C && !*outer ? w.tiles * kw : 0)) +
+                    (*outer ? (float)outer_waves(l) * (1.5f / 2048.f) * (float)(1 + (l.rows / l.e_cnt + 31) / 32) : 0.f);
   float chain = 0.f, join = 0.f;
+  *dx_first = true;
   double parts = 0;
   if (x.C) {
     x.parts.n = whole_parts(chain_parts(x.tiles, kx, all), kx);
     chain = (float)((kx + x.parts.n - 1) / x.parts.n) * CACHED.alone;
     if (x.parts.n > 1) { join = 3.f; parts += (double)x.parts.n * l.rows * l.K; }
   }
-  if (w.C) {
+  if (w.C && !*outer) {
     w.parts.n = chain_parts(w.tiles, kw, all);             // (experts' rows differ: parts of some may be empty)
     const float c = (float)((kw + w.parts.n - 1) / w.parts.n) * CACHED.alone;
+    *dx_first = chain >= c;
     chain = c > chain ? c : chain;
     if (w.parts.n > 1) { join = 3.f; parts += (double)w.parts.n * l.e_cnt * l.K * l.N; }
   }
@@ -332,7 +397,8 @@ float linear_tiles_fwd_time(const LinearArgs& l) {
 float linear_tiles_bwd_time(const LinearArgs& l, bool dx, bool dw) {
   void* const some = (void*)1;
   Product x = dx_of(l, nullptr, dx && l.rows > 0 ? some : nullptr, 0, nullptr), w = dw_of(l, nullptr, dw ? some : nullptr, 0, nullptr);
-  return plan_gradients(l, x, w);
+  bool outer, dx_first;
+  return plan_gradients(l, x, w, &outer, &dx_first);
 }
 
 int launch_linear_tiles_fwd(const LinearArgs& l, void* ws, hipStream_t s) {
@@ -351,14 +417,16 @@ int launch_linear_tiles_fwd(const LinearArgs& l, void* ws, hipStream_t s) {
 int launch_linear_tiles_bwd(const LinearArgs& l, const void* dz, void* dx, int dx_accumulate, void* dw, int accumulate, const BiasGrad& db, void* ws_dx, void* ws_dw,
                             hipStream_t s) {
   Product x = dx_of(l, dz, l.rows > 0 ? dx : nullptr, dx_accumulate, ws_dx), w = dw_of(l, dz, dw, accumulate, ws_dw);
-  plan_gradients(l, x, w);
-  Gradients g = {l, x, w, db, (int)blocks_of(x.tiles), l.offsets ? (int)((w.tiles + 255) / 256 * 256) : (int)blocks_of(w.tiles), 0, 0};
+  bool outer, dx_first;
+  plan_gradients(l, x, w, &outer, &dx_first);
+  Gradients g = {l, x, w, db, (int)blocks_of(x.tiles), l.offsets ? (int)((w.tiles + 255) / 256 * 256) : (int)blocks_of(w.tiles), 0, 0, outer, dx_first};
   if (x.C) g.dx_total = g.dx_blocks * x.parts.n;
-  if (w.C) g.dw_total = g.dw_blocks * w.parts.n;
+  if (w.C) g.dw_total = outer ? (int)((outer_waves(l) + 3) / 4) : g.dw_blocks * w.parts.n;
   const unsigned blocks = g.dx_total + g.dw_total + (db.db ? bias_blocks(l.N, l.e_cnt) : 0);
   if (blocks > 0) {
     ProfScope prof(x.C && w.C ? MOE_K_LINEAR_DX_DW : w.C ? MOE_K_LINEAR_DW : x.C ? MOE_K_LINEAR_DX : MOE_K_LINEAR_BIAS, s);
-    hipLaunchKernelGGL(linear_gradients, dim3(blocks), dim3(NT), 0, s, g);
+    const bool stream = l.rows <= (long long)QT * l.e_cnt && 2ll * l.K * l.N * l.e_cnt > (256ll << 20);
+    hipLaunchKernelGGL(stream ? linear_gradients<true> : linear_gradients<false>, dim3(blocks), dim3(NT), 0, s, g);
     HIP_CHECK_LAUNCH();
   }
   return launch_join_gradients<bf16_t>(l, x.parts, dx, dx_accumulate, w.parts, dw, accumulate, s);

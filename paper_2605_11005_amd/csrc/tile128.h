@@ -31,8 +31,9 @@ struct QuarterKc {         // load j of a wavefront: rows 8*(4w+j) + lane/8, who
       voff[j] = (uint32_t)(min(rl, rows_valid - 1) * ld * 2 + c * 16);
     }
   }
+  template <bool STREAM = false>
   __device__ __forceinline__ void issue1(int j, uint32_t oper_lds, int wave, long kofs, uint32_t back = 0) const {
-    lds_load16(base + kofs, voff[j] - back, oper_lds + (4 * wave + j) * 1024);
+    lds_load16<STREAM>(base + kofs, voff[j] - back, oper_lds + (4 * wave + j) * 1024);
   }
   static __device__ __forceinline__ int chunk(int j, int lane) { return (lane & 7) ^ (4 * (j & 1) + (lane >> 4)); }
 };
