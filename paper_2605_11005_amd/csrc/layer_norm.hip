@@ -257,14 +257,132 @@ __global__ __launch_bounds__(WIDE ? WIDE_THREADS : BWD_THREADS) void layer_norm_
   }
 }
 
+// The backward of few rows in one launch: blocks of rows as in the forward, and blocks that sum 64 columns over all rows, for which dw and db need the saved
+// mean and 1/deviation alone.  What the latter read again comes from the caches.
+constexpr int SUM_COLUMNS = 64;
+template <typename T, typename R>
+struct OneLaunch {
+  BwdArgs<T, R> p;
+  T* dw; T* db;
+  int accumulate, row_blocks;
+};
+template <typename T, typename R>
+__device__ __forceinline__ void sum_columns(const OneLaunch<T, R>& a, int c0) {
+  constexpr int N = VEC<T>, LANES = SUM_COLUMNS / N, AT_ONCE = WAVE / LANES;      // lanes and rows of a wavefront's load
+  __shared__ float part[2][MOST_WAVES][SUM_COLUMNS];
+  const BwdArgs<T, R>& p = a.p;
+  const int tid = threadIdx.y * blockDim.x + threadIdx.x, waves = blockDim.x * blockDim.y >> 6, wave = tid >> 6, lane = tid & 63;
+  const int c = c0 + lane % LANES * N;
+  float dw[N], db[N];
+#pragma unroll
+  for (int j = 0; j < N; ++j) dw[j] = db[j] = 0.f;
+  if (c < p.d)
+#pragma unroll 4
+    for (int row = wave * AT_ONCE + lane / LANES; row < p.T_; row += waves * AT_ONCE) {
+      float h[N], dn[N];
+      unpack(p.h, (size_t)row * p.d + c, h);
+      unpack(p.dn, (size_t)row * p.d + c, dn);
+      const float mean = p.mean[row], rstd = p.rstd[row];
+#pragma unroll
+      for (int j = 0; j < N; ++j) {
+        dw[j] += dn[j] * ((h[j] - mean) * rstd);
+        db[j] += dn[j];
+      }
+    }
+#pragma unroll
+  for (int j = 0; j < N; ++j)
+#pragma unroll
+    for (int m = LANES; m < WAVE; m *= 2) {
+      dw[j] += __shfl_xor(dw[j], m);
+      db[j] += __shfl_xor(db[j], m);
+    }
+  if (lane < LANES)
+#pragma unroll
+    for (int j = 0; j < N; ++j) { part[0][wave][lane * N + j] = dw[j]; part[1][wave][lane * N + j] = db[j]; }
+  __syncthreads();
+  for (int i = tid; i < 2 * SUM_COLUMNS; i += 64 * waves) {        // (a block may be a single wavefront)
+    const int which = i / SUM_COLUMNS, col = i % SUM_COLUMNS;
+    T* const out = which ? a.db : a.dw;
+    if (!out || c0 + col >= p.d) continue;
+    float s = 0.f;
+    for (int w = 0; w < waves; ++w) s += part[which][w][col];
+    T& to = out[c0 + col];
+    if constexpr (sizeof(T) == 2) to = (bf16_t)pack_bf16x2(a.accumulate ? bf16_to_f32(to) + s : s, 0.f);      // (the hardware's conversion keeps every NaN)
+    else to = a.accumulate ? to + s : s;
+  }
+}
+template <typename T, typename R, int STEPS>
+__global__ __launch_bounds__((MOST_THREADS<T, STEPS>)) void layer_norm_bwd_few(OneLaunch<T, R> a) {
+  constexpr int N = VEC<T>;
+  __shared__ float2 red[MOST_WAVES];       // of the block's wavefronts, a row's one after the other
+  const BwdArgs<T, R>& p = a.p;
+  if ((int)blockIdx.x >= a.row_blocks) return sum_columns(a, ((int)blockIdx.x - a.row_blocks) * SUM_COLUMNS);
+  const int row = blockIdx.x * blockDim.y + threadIdx.y;
+  const bool in = row < p.T_;
+  const size_t at = (size_t)row * p.d;
+  const float mean = in ? p.mean[row] : 0.f, rstd = in ? p.rstd[row] : 0.f, inv_d = 1.f / (float)p.d;
+  float xh[STEPS][N], t[STEPS][N], g[STEPS][N], s1 = 0.f, s2 = 0.f;
+#pragma unroll
+  for (int i = 0; i < STEPS; ++i) {
+    const int c = (i * blockDim.x + threadIdx.x) * N;
+    float w[N];
+#pragma unroll
+    for (int j = 0; j < N; ++j) { xh[i][j] = mean; t[i][j] = g[i][j] = 0.f; w[j] = 1.f; }
+    if (in && c < p.d) {
+      unpack(p.h, at + c, xh[i]);
+      unpack(p.dn, at + c, t[i]);
+      if (p.dh_out) unpack(p.dh_out, at + c, g[i]);
+      if (p.w) unpack(p.w, c, w);
+    }
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      xh[i][j] = (xh[i][j] - mean) * rstd;
+      t[i][j] *= w[j];
+      s1 += t[i][j];
+      s2 += t[i][j] * xh[i][j];
+    }
+  }
+  s1 = wave_total(s1);
+  s2 = wave_total(s2);
+  const int waves = blockDim.x >> 6;
+  if (waves > 1) {
+    float2* const mine = red + threadIdx.y * waves;
+    if ((threadIdx.x & 63) == 0) mine[threadIdx.x >> 6] = make_float2(s1, s2);
+    __syncthreads();
+    s1 = s2 = 0.f;
+    for (int k = 0; k < waves; ++k) { s1 += mine[k].x; s2 += mine[k].y; }
+  }
+  s1 *= inv_d;
+  s2 *= inv_d;
+#pragma unroll
+  for (int i = 0; i < STEPS; ++i) {
+    const int c = (i * blockDim.x + threadIdx.x) * N;
+    if (!in || c >= p.d) continue;
+#pragma unroll
+    for (int j = 0; j < N; ++j) g[i][j] += rstd * (t[i][j] - s1 - xh[i][j] * s2);
+    if (p.dh) pack(p.dh, at + c, g[i]);
+    if (p.dy) pack(p.dy, at + c, g[i]);
+  }
+}
+
+// Threads and steps of a row, rows of a block
+struct Shape {
+  int steps, threads, rows;
+  Shape(int d, int vec) {
+    const int vecs = d / vec;
+    steps = 1;
+    while (row_threads(vecs, steps) > 512 && steps < 4) steps *= 2;
+    if (vecs > WAVE && vecs <= 3 * WAVE / 2) steps = 2;
+    threads = row_threads(vecs, steps);
+    rows = threads == WAVE ? 4 : 1;
+  }
+  dim3 block() const { return dim3(threads, rows); }
+};
 template <typename T, typename R>
 int forward(FwdArgs<T, R> p, hipStream_t s) {
-  const int vecs = p.d / VEC<T>;
-  int steps = 1;
-  while (row_threads(vecs, steps) > 512 && steps < 4) steps *= 2;
-  if (vecs > WAVE && vecs <= 3 * WAVE / 2) steps = 2;
-  const int threads = row_threads(vecs, steps), rows = threads == WAVE ? 4 : 1;
-  const dim3 block(threads, rows);
+  const Shape shape(p.d, VEC<T>);
+  const int steps = shape.steps, threads = shape.threads, rows = shape.rows;
+  const dim3 block = shape.block();
   // STREAM of tensors beyond the Infinity Cache, us, as usual / so: 32768 rows of 7168 bf16 with fp32 residuals 510 / 503, 16384 of 4096 140 / 138, of bf16
   // 96 / 93, 65536 of 1024 94 / 87; within it 16384 of 1024 23.3 / 24.9.  Hints on the residual stream cost up to a tenth.
   const bool stream = (double)p.T_ * p.d * 2 * (sizeof(T) + sizeof(R)) > (double)(256ll << 20);
@@ -305,8 +423,26 @@ inline BwdPlan bwd_plan(int T, int d, int vec, bool stream) {
   return b;
 }
 
+// Two launches / one, us: 256 rows of 2880 bf16 9.5 / 5.2, of 16384 21.8 / 12.5, 512 of 7168 17.2 / 11.6, 1024 of 520 12.9 / 6.8, of 4096 16.3 / 12.6, of
+// 7168 19.1 / 18.8, with fp32 residuals of 4096 19.5 / 20.6; 2047 of 2880 16.7 / 22.3.
+inline bool one_launch(int T, int d, int element, int residual) {
+  return T <= 512 || (T <= 1024 && (long long)T * d * (element + residual) <= (24ll << 20));
+}
+
 template <typename T, typename R>
 int backward(BwdArgs<T, R> p, T* dw, T* db, int accumulate, hipStream_t s) {
+  if (p.T_ > 0 && one_launch(p.T_, p.d, sizeof(T), sizeof(R))) {
+    Shape shape(p.d, VEC<T>);
+    if (shape.threads < 512) shape.rows = 512 / shape.threads;      // (the blocks that sum columns want wavefronts)
+    const OneLaunch<T, R> a = {p, dw, db, accumulate, p.dh || p.dy ? (p.T_ + shape.rows - 1) / shape.rows : 0};
+    const unsigned blocks = a.row_blocks + (dw || db ? (p.d + SUM_COLUMNS - 1) / SUM_COLUMNS : 0);
+    if (blocks == 0) return MOE_OK;
+    ProfScope prof(MOE_K_LAYER_NORM_BWD, s);
+    const auto kernel = shape.steps == 1 ? layer_norm_bwd_few<T, R, 1> : shape.steps == 2 ? layer_norm_bwd_few<T, R, 2> : layer_norm_bwd_few<T, R, 4>;
+    hipLaunchKernelGGL(kernel, dim3(blocks), shape.block(), 0, s, a);
+    HIP_CHECK_LAUNCH();
+    return MOE_OK;
+  }
   const bool stream = streams(p.T_, p.d, sizeof(T), sizeof(R), p.dh_out);
   const BwdPlan plan = bwd_plan(p.T_, p.d, VEC<T>, stream);
   const int steps = plan.steps, blocks = plan.blocks;

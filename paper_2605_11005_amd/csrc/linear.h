@@ -9,12 +9,15 @@ struct LinearArgs {
   int dtype, rows, K, N, e_cnt, act;
   const int32_t* offsets;                 // NULL: one matrix, all rows
 };
-// db[e] (+)= the sums of expert e's row tiles of LINEAR_SUM_ROWS rows: lines off[e] / LINEAR_SUM_ROWS + e and on of sums (bias_grad.h); db NULL: none
+// db[e] (+)= the sums of expert e's row tiles of LINEAR_SUM_ROWS rows: lines off[e] / LINEAR_SUM_ROWS + e and on of sums (bias_grad.h), or of its rows
+// themselves, dy act'(z); db NULL: none
 constexpr int LINEAR_SUM_ROWS = 64;
 struct BiasGrad {
   const int32_t* off;                     // NULL: one expert, all rows
   int rows, N, accumulate;
   const float* sums;
+  const void *dy, *z;                     // dy NULL: sums
+  int act;
   void* db;
 };
 size_t linear_fwd_ws_bytes(int dtype, int rows, int K, int N, int e_cnt);

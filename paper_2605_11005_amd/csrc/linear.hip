@@ -77,17 +77,41 @@ __global__ __launch_bounds__(GRAD_WAVES * WAVE) void act_grad(const int32_t* __r
   }
 }
 
+// dz alone, 16 bytes a thread, for few rows, whose sums the products' launch forms by itself
+constexpr int DZ_THREADS = 256, FEW_SUM_ROWS = 1024;
+template <typename T>
+__global__ __launch_bounds__(DZ_THREADS) void act_grad_few(const int32_t* __restrict__ off, int rows, int e_cnt, int N, int act,
+                                                           const T* __restrict__ dy, const T* __restrict__ z, T* __restrict__ dz) {
+  constexpr int V = VEC<T>;
+  const size_t at = ((size_t)blockIdx.x * DZ_THREADS + threadIdx.x) * V;
+  if (at >= (size_t)(off ? off[e_cnt] : rows) * N) return;
+  float g[V], v[V];
+  values(*reinterpret_cast<const u32x4*>(dy + at), g);
+  values(*reinterpret_cast<const u32x4*>(z + at), v);
+  with_activation(act, [&](auto a) {
+#pragma unroll
+    for (int j = 0; j < V; ++j) g[j] = act_slope<decltype(a)::value, sizeof(T) == 2>(v[j], g[j]);
+  });
+  *reinterpret_cast<u32x4*>(dz + at) = words(g);
+}
+
 // db, where no launch of the products takes it along
 __global__ __launch_bounds__(BIAS_THREADS) void bias_grad(BiasGrad p) {
   __shared__ float part[BIAS_THREADS];
   bias_columns<bf16_t>(p, blockIdx.x, part);
 }
 
+// few: sums by the launch behind
 template <typename T>
-int gradients(const LinearArgs& l, const void* dy, void* dz, float* sums, int32_t* setup, hipStream_t s) {
+int gradients(const LinearArgs& l, const void* dy, void* dz, float* sums, bool few, int32_t* setup, hipStream_t s) {
   constexpr int WIDTH = WAVE * VEC<T>;
-  {
-    ProfScope prof(MOE_K_LINEAR_ACT, s);
+  ProfScope prof(MOE_K_LINEAR_ACT, s);
+  if (few) {
+    const long long n = (long long)l.rows * l.N / VEC<T>;
+    hipLaunchKernelGGL(act_grad_few<T>, dim3((unsigned)((n + DZ_THREADS - 1) / DZ_THREADS)), dim3(DZ_THREADS), 0, s, l.offsets, l.rows, l.e_cnt, l.N, l.act,
+                       (const T*)dy, (const T*)l.z, (T*)dz);
+    HIP_CHECK_LAUNCH();
+  } else {
     const long long tiles = ((long long)(l.rows + SUM_ROWS - 1) / SUM_ROWS + l.e_cnt) * ((l.N + WIDTH - 1) / WIDTH);
     hipLaunchKernelGGL(act_grad<T>, dim3((unsigned)((tiles + 7) / 8 * 8)), dim3(GRAD_WAVES * WAVE), 0, s, l.offsets, l.rows, l.e_cnt, l.N, l.act, (const T*)dy,
                        (const T*)l.z, (T*)dz, sums, setup);
@@ -186,15 +210,18 @@ int launch_linear_bwd(const LinearArgs& l, const void* dy, void* dx, int dx_accu
   float* const sums = (float*)(base + space.sums);
   int32_t* const setup = large ? (int32_t*)ws : nullptr;
   int rc;
-  if (l.rows > 0 && (db || (through && (dx || dw)))) {
-    rc = bf16 ? gradients<bf16_t>(l, dy, dz, db ? sums : nullptr, setup, s) : gradients<float>(l, dy, dz, db ? sums : nullptr, setup, s);
+  // Few rows: the products' launch sums dy act'(z) by itself, so that without an activation there is no launch in front of it, and with one a short one.  us,
+  // before / so: 16 rows of 1024 to 1024 without 14.3 / 11.2, with silu 14.5 / 13.5, 300 rows 21.5 / 13.1 and 21.9 / 16.0.
+  const bool few = !large && l.rows <= FEW_SUM_ROWS;
+  if (l.rows > 0 && ((db && !few) || (through && (dx || dw)))) {
+    rc = bf16 ? gradients<bf16_t>(l, dy, dz, db ? sums : nullptr, few, setup, s) : gradients<float>(l, dy, dz, db ? sums : nullptr, few, setup, s);
     if (rc) return rc;
   } else if (large) {
     hipLaunchKernelGGL(linear_setup, dim3(1), dim3(SETUP_WORDS), 0, s, setup);
     HIP_CHECK_LAUNCH();
   }
   const void* const g = through ? dz : dy;
-  const BiasGrad bias = {l.offsets, l.rows, l.N, accumulate, sums, db};
+  const BiasGrad bias = {l.offsets, l.rows, l.N, accumulate, sums, few ? dy : nullptr, l.z, l.act, db};
   if (!bf16) return launch_linear_bwd_f32(l, g, dx, dx_accumulate, dw, accumulate, bias, base + space.products, base + space.dw_parts, s);
   if (!large) return launch_linear_tiles_bwd(l, g, dx, dx_accumulate, dw, accumulate, bias, base + space.products, base + space.dw_parts, s);
   if (db) {
