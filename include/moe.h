@@ -321,7 +321,8 @@ int moe_block_norm_bwd(const void* y, const float* gate, const void* w_post, int
  *   dh [T,d] res_dtype out, may be dh_out itself; dy [T,d] dtype out, the same in the type of y, may be dn itself; dw, db [d] dtype out, added to
  *   their contents with accumulate == 1.  Each may be NULL: not formed.
  *   ws: moe_workspace_bytes(MOE_WS_LAYER_NORM, dtype, T, 0, d, 0, 0, 0) bytes, 256-byte aligned.
- * The column sums are fp32, formed over rows that T, d and dtype decide and added in a fixed order: results are bit-reproducible.
+ * The column sums are fp32, formed over rows that T, d, the types and whether dy or dh lies over dn decide and added in a fixed order: results are
+ * bit-reproducible.
  * Errors of both: EINVAL (NULL, negative sizes, unknown types, res_dtype neither dtype nor MOE_F32, eps not a positive number, h_out without y),
  * EUNSUPPORTED (bf16 with d % 8 != 0, fp32 with d % 4 != 0, d > MOE_MAX_NORM_D, T > 2^31 - 2^16), EWORKSPACE.
  */

@@ -431,7 +431,10 @@ inline bool one_launch(int T, int d, int element, int residual) {
 
 template <typename T, typename R>
 int backward(BwdArgs<T, R> p, T* dw, T* db, int accumulate, hipStream_t s) {
-  if (p.T_ > 0 && one_launch(p.T_, p.d, sizeof(T), sizeof(R))) {
+  // (in place, the rows would write over what the column sums still read)
+  const auto over = [&](const void* out) { return out && (out == p.dn || out == p.h); };
+  const bool in_place = (dw || db) && (over(p.dh) || over(p.dy));
+  if (p.T_ > 0 && !in_place && one_launch(p.T_, p.d, sizeof(T), sizeof(R))) {
     Shape shape(p.d, VEC<T>);
     if (shape.threads < 512) shape.rows = 512 / shape.threads;      // (the blocks that sum columns want wavefronts)
     const OneLaunch<T, R> a = {p, dw, db, accumulate, p.dh || p.dy ? (p.T_ + shape.rows - 1) / shape.rows : 0};

@@ -148,6 +148,76 @@ def test_in_place():
         assert torch.equal(dh, c.out["dh"]) and torch.equal(dn, c.out["dy"])
 
 
+@pytest.mark.parametrize("dt,rt", TYPES)
+@pytest.mark.parametrize("T,d", [(2, 16384), (70, 520), (500, 4096), (1024, 1032), (1400, 264)])
+def test_in_place_beside_the_column_sums(T, d, dt, rt):
+    """dy over dn and dh over dh_out where dw and db are formed too."""
+    c = Case(T, d, dt, rt, seed=T)
+    c.forward()
+    c.backward()
+    ws = torch.empty(B.moe_workspace_bytes(B.WS_LAYER_NORM, 0, T, 0, d, 0, 0, 0), dtype=torch.uint8, device="cuda")
+    for _ in range(3):
+        dh, dn = c.dh_out.clone(), c.dn.clone()
+        dw, db = (torch.full_like(c.w, float("nan")) for _ in range(2))
+        B.moe_layer_norm_bwd(c.h_out, c.w, c.mean, c.rstd, dh, dn, dh, dn, dw, db, False, ws)
+        c.out = {"dh": dh, "dy": dn, "dw": dw, "db": db}       # (the sums may take rows in other groups than out of place: held to the oracle)
+        c.check_backward()
+
+
+@pytest.mark.parametrize("T", (511, 512, 513, 1023, 1024, 1025))
+@pytest.mark.parametrize("d", (264, 3080))
+def test_one_launch_and_two(T, d):
+    """Around the row counts that one launch takes."""
+    for dt, rt in TYPES:
+        c = Case(T, d, dt, rt, seed=T)
+        c.forward()
+        c.check_forward()
+        for accumulate, want in ((True, ("dh", "dy", "dw", "db")), (False, ("dw",)), (False, ("dy",))):
+            c.backward(accumulate, want)
+            c.check_backward(accumulate)
+
+
+@pytest.mark.parametrize("dt,rt,T,d", [(BF16, BF16, 66000, 1032), (BF16, BF16, 16500, 4104), (BF16, F32, 33000, 2056), (BF16, F32, 9000, 9000),
+                                       (F32, F32, 66000, 520), (F32, F32, 20000, 2052), (F32, F32, 4200, 16384), (BF16, BF16, 131000, 520)])
+def test_tensors_beyond_the_infinity_cache(dt, rt, T, d):
+    """The same bounds, in float64 on the device."""
+    print(f"case layer norm {T} {d} {dt} {rt}", flush=True)
+    g = torch.Generator(device="cuda").manual_seed(d)
+    r = lambda *s, dtype: torch.randn(s, generator=g, device="cuda").to(dtype)  # noqa: E731
+    y, h, dn, dh_out, w, b = r(T, d, dtype=dt), r(T, d, dtype=rt), r(T, d, dtype=dt), r(T, d, dtype=rt), r(d, dtype=dt), r(d, dtype=dt)
+    h_out, n, mean, rstd = torch.empty_like(h), torch.empty_like(y), torch.empty(T, device="cuda"), torch.empty(T, device="cuda")
+    B.moe_layer_norm_fwd(y, h, w, b, EPS, h_out, n, mean, rstd)
+    dh, dy, dw, db = torch.empty_like(h), torch.empty_like(y), torch.empty_like(w), torch.empty_like(b)
+    ws = torch.empty(B.moe_workspace_bytes(B.WS_LAYER_NORM, 0, T, 0, d, 0, 0, 0), dtype=torch.uint8, device="cuda")
+    B.moe_layer_norm_bwd(h_out, w, mean, rstd, dh_out, dn, dh, dy, dw, db, False, ws)
+
+    def held(got, ref, mag, steps=100):
+        half = HALF_ULP[got.dtype]
+        assert ((got.double() - ref).abs() <= half * (1 + 2.0 ** -7) * ref.abs() + steps * 2.0 ** -24 * mag).all()
+
+    W, Bb, sums, mags = w.double(), b.double(), torch.zeros(2, d, dtype=torch.float64, device="cuda"), torch.zeros(2, d, dtype=torch.float64, device="cuda")
+    for at in torch.arange(T).split(8192):
+        at = slice(int(at[0]), int(at[-1]) + 1)
+        x, size = y[at].double() + h[at].double(), y[at].double().abs() + h[at].double().abs()
+        m = x.mean(1, keepdim=True)
+        rs = ((x - m).square().mean(1, keepdim=True) + EPS).rsqrt()
+        held(h_out[at], x, size)
+        held(mean[at], m[:, 0], size.mean(1))
+        held(rstd[at], rs[:, 0], rs[:, 0])
+        held(n[at], (x - m) * rs * W + Bb, (size + size.mean(1, keepdim=True)) * rs * W.abs() + Bb.abs())
+        m, rs, dN, through = mean[at, None].double(), rstd[at, None].double(), dn[at].double(), dh_out[at].double()
+        x, size = (h_out[at].double() - m) * rs, (h_out[at].double().abs() + m.abs()) * rs
+        t = W * dN
+        want = through + rs * (t - t.mean(1, keepdim=True) - x * (t * x).mean(1, keepdim=True))
+        mag = through.abs() + rs * (t.abs() + t.abs().mean(1, keepdim=True) + size * (t.abs() * size).mean(1, keepdim=True))
+        held(dh[at], want, mag)
+        held(dy[at], want, mag)
+        sums += torch.stack([(dN * x).sum(0), dN.sum(0)])
+        mags += torch.stack([(dN.abs() * size).sum(0), dN.abs().sum(0)])
+    held(dw, sums[0], mags[0], T / 512 + 160)
+    held(db, sums[1], mags[1], T / 512 + 160)
+
+
 def test_gradient_against_differences():
     c = Case(4, 24, F32, F32)
     c.forward()

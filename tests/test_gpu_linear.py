@@ -90,8 +90,9 @@ class Case:
         dz_err = np.zeros_like(z) if exact else (1 + np.abs(z)) * 2.0 ** -20 * np.abs(host(self.dy[:R]))     # |slope| has |z| in it
         rounded = dz_err + (0 if exact or self.dt == F32 else half * (np.abs(ref["dz"]) + dz_err))
         add = 1.0 if accumulate else 0.0
+        weights = self.weights()
         for e, at in L.segments(self.ref_off):
-            w, x, n = np.abs(self.weights()[e]), np.abs(host(self.x[at])), at.stop - at.start
+            w, x, n = np.abs(weights[e]), np.abs(host(self.x[at])), at.stop - at.start
             pick = (lambda t: t) if self.dense else (lambda t: t[e])
             if self.dx is not None:
                 err = rounded[at] @ w.T + (self.N + 4) * 2.0 ** -23 * mag["dx"][at] + 2.0 ** -23 * add
@@ -174,6 +175,46 @@ def test_weight_gradient_of_many_rows(rows, dt):
     """One heavy expert, whose gradient is summed in pieces."""
     c = Case(rows, 72, 136, "silu", dt, seed=5)
     c.check_both(accumulate=True)
+
+
+@pytest.mark.parametrize("dt", (BF16, F32))
+@pytest.mark.parametrize("rows", [31, 32, 33, 63, 65, 127, 128, 129, 1023, 1024, 1025, [32] * 3, [97, 0, 0], [64, 1, 128], [500, 24, 501]], ids=str)
+def test_row_counts_around_the_kernels_limits(rows, dt):
+    print(f"case linear {rows} {dt}", flush=True)
+    Case(rows, 264, 200, "gelu", dt, slack=0, seed=3).check_both(accumulate=True)
+
+
+@pytest.mark.parametrize("dt", (BF16, F32))
+@pytest.mark.parametrize("rows,K,N", [([i % 3 for i in range(1024)], 16, 24), ([0] * 700 + [150] + [0] * 323, 72, 136), ([(7 * i) % 41 for i in range(130)], 40, 72)],
+                         ids=["1024 experts", "one of 1024", "130 experts"])
+def test_many_experts(rows, K, N, dt):
+    print(f"case linear {len(rows)} experts {dt}", flush=True)
+    Case(rows, K, N, "silu", dt, seed=len(rows)).check_both()
+
+
+@pytest.mark.parametrize("rows,K,N", [(4, 8200, 16392), (100, 8200, 16392), (50, 16392, 8200), ([3, 0, 40, 1, 2], 4104, 6664), ([100, 0, 128, 1, 60], 4104, 6664)],
+                         ids=str)
+def test_weights_beyond_the_infinity_cache(rows, K, N):
+    """The bounds of the other tests, in float64 on the device."""
+    print(f"case linear {rows} {K} {N}", flush=True)
+    c = Case(rows, 8, 8, "none", slack=0)
+    g = torch.Generator(device="cuda").manual_seed(K)
+    r = lambda *s: torch.randn(s, generator=g, device="cuda").to(BF16)  # noqa: E731
+    c.K, c.N = K, N
+    c.x, c.w, c.bias, c.residual, c.dy = r(c.cap, K), r(*c.lead, K, N), r(*c.lead, N), r(c.cap, N), r(c.cap, N)
+    c.forward()
+    c.backward()
+    for e, at in L.segments(c.ref_off):
+        pick = (lambda t: t) if c.dense else (lambda t: t[e])
+        w, x, dy = pick(c.w).double(), c.x[at].double(), c.dy[at].double()
+        for name, got, ref, mag, terms in (
+                ("y", c.y[at], x @ w + pick(c.bias).double() + c.residual[at].double(),
+                 x.abs() @ w.abs() + pick(c.bias).double().abs() + c.residual[at].double().abs(), K + 5),
+                ("dx", c.dx[at], dy @ w.T, dy.abs() @ w.T.abs(), N + 4),
+                ("dw", pick(c.dw), x.T @ dy, x.T.abs() @ dy.abs(), at.stop - at.start + 40),
+                ("db", pick(c.db), dy.sum(0), dy.abs().sum(0), at.stop - at.start + 4)):
+            err = terms * 2.0 ** -23 * mag
+            assert ((got.double() - ref).abs() <= err + 2.0 ** -8 * (ref.abs() + err)).all(), (name, e)
 
 
 @pytest.mark.parametrize("dt", (BF16, F32))
@@ -305,6 +346,33 @@ def test_on_another_stream():
         c.forward()
     s.synchronize()
     assert torch.equal(want[:c.R], c.y[:c.R])
+
+
+def test_two_calls_at_once():
+    """Two streams, each with its own workspace, in the kernels for few rows, for tiles and for the largest."""
+    for rows, K, N in ((8, 520, 1032), (300, 264, 520), ([300, 0, 100], 136, 264), (4096, 2056, 4088)):
+        print(f"case linear {rows} {K} {N}", flush=True)
+        cases = [Case(rows, K, N, "gelu", seed=i) for i in range(2)]
+        first = []
+        for c in cases:
+            c.forward()
+            c.backward()
+            first.append([t.clone() for t in (c.z, c.y, c.dx, c.dw, c.db)])
+        torch.cuda.synchronize()
+        spaces = [(c.ws(B.WS_LINEAR_FWD), c.ws(B.WS_LINEAR_BWD)) for c in cases]
+        outs = [[torch.full_like(t, float("nan")) for t in f] for f in first]
+        streams = [torch.cuda.Stream() for _ in cases]
+        for s in streams:
+            s.wait_stream(torch.cuda.current_stream())
+        for _ in range(4):
+            for c, s, (fws, bws), (z, y, dx, dw, db) in zip(cases, streams, spaces, outs):
+                with torch.cuda.stream(s):
+                    B.moe_linear_fwd(c.x, c.off, c.w, c.bias, B.ACT_GELU, c.residual, z, y, fws)
+                    B.moe_linear_bwd(c.x, z, c.dy, c.off, c.w, B.ACT_GELU, dx, dw, db, False, bws)
+        torch.cuda.synchronize()
+        for want, got in zip(first, outs):
+            for a, b in zip(want, got):
+                assert torch.equal(torch.nan_to_num(a), torch.nan_to_num(b))
 
 
 def test_the_marshalling_makes_the_calls(monkeypatch):
