@@ -403,10 +403,13 @@ struct BwdPlan { int steps, threads, rows, most, blocks; bool wide; };
 // 103 / 90; of less: 2047 of 2880 16.5 / 19.4, 16384 of 1024 30.0 / 30.9.  Fewer rows at a time then do: 16384 of 4096 bf16 in one block of 512
 // threads per CU 89, with fp32 residuals 206 -> 197 (but fp32, eight elements a thread less, 16384 of 2048 88 -> 106); 32768 of 2048 in two blocks of
 // 256 per CU for four 98 -> 92.
+// Within the cache too one block per CU does where its loads alone keep the CU busy, and where rows are so few that the blocks' sums count, us, two / one:
+// 8192 of 4096 bf16 54.0 / 48.4, 2047 19.6 / 17.9 (of 3584 45.2 / 46.4 and 18.5 / 17.5), with fp32 residuals 12000 of 2048 85 / 73, 4096 of 2880 37.3 / 35.3
+// (of 1536 22.0 / 24.3); 1100 of 1536 12.1 / 11.4, of 2880 15.4 / 13.6 (4096 of 2880 23.0 / 25.1).
 inline bool streams(int T, int d, int element, int residual, bool through) {
   return (double)T * d * (element + residual * (through ? 2 : 1)) > (double)(256ll << 20);
 }
-inline BwdPlan bwd_plan(int T, int d, int vec, bool stream) {
+inline BwdPlan bwd_plan(int T, int d, int vec, bool fp32_residual, bool stream) {
   constexpr int CUS = 256;
   const int vecs = d / vec, per = 16 / vec;          // steps of 16 elements
   BwdPlan b;
@@ -415,7 +418,8 @@ inline BwdPlan bwd_plan(int T, int d, int vec, bool stream) {
   else if (b.wide || row_threads(vecs, per) == WAVE) b.steps = per;
   else b.steps = row_threads(vecs, 1) <= BWD_THREADS ? 1 : row_threads(vecs, 2) <= BWD_THREADS ? 2 : per;
   b.threads = row_threads(vecs, b.steps);
-  const int per_cu = b.steps * vec == 16 || (stream && vec == 8 && b.threads > 256) ? 1 : !stream && b.threads > WAVE && b.threads <= 256 && T >= 8192 ? 4 : 2;
+  const bool fills = vec == 8 && (b.threads > 448 || (b.threads > 256 && stream) || (b.threads >= 256 && fp32_residual));
+  const int per_cu = b.steps * vec == 16 || fills || (b.threads > 2 * WAVE && T <= 6 * CUS) ? 1 : !stream && b.threads > WAVE && b.threads <= 256 && T >= 8192 ? 4 : 2;
   b.most = T < per_cu * CUS ? T : per_cu * CUS;
   b.rows = b.threads > WAVE ? 1 : T >= per_cu * CUS * BWD_ROWS ? BWD_ROWS : T == 0 ? 1 : (T - 1) / (per_cu * CUS) + 1;
   const int units = T == 0 ? 0 : (T - 1) / b.rows + 1;
@@ -447,7 +451,7 @@ int backward(BwdArgs<T, R> p, T* dw, T* db, int accumulate, hipStream_t s) {
     return MOE_OK;
   }
   const bool stream = streams(p.T_, p.d, sizeof(T), sizeof(R), p.dh_out);
-  const BwdPlan plan = bwd_plan(p.T_, p.d, VEC<T>, stream);
+  const BwdPlan plan = bwd_plan(p.T_, p.d, VEC<T>, sizeof(R) == 4, stream);
   const int steps = plan.steps, blocks = plan.blocks;
   const dim3 grid(blocks), block(plan.threads, plan.rows);
   constexpr int PER = 16 / VEC<T>;
@@ -488,7 +492,8 @@ int backward(BwdArgs<T, R> p, T* dw, T* db, int accumulate, hipStream_t s) {
 size_t layer_norm_ws_bytes(int T, int d) {
   int most = 0;
   for (int vec : {8, 4})
-    for (bool stream : {false, true}) most = std::max(most, bwd_plan(T, d, vec, stream).most);
+    for (bool fp32 : {false, true})
+      for (bool stream : {false, true}) most = std::max(most, bwd_plan(T, d, vec, fp32, stream).most);
   return (size_t)most * 2 * d * sizeof(float);
 }
 
