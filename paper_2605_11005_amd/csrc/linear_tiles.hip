@@ -18,7 +18,10 @@ namespace {
 enum { FWD, DX, DW };
 constexpr int NT = 256, TILE_PITCH = 68;
 constexpr int STAGE = 2 * QOPER_BYTES, SLAB = 64 * TILE_PITCH * 4;
-constexpr int TILE_LDS = 4 * SLAB > 2 * STAGE ? 4 * SLAB : 2 * STAGE;
+// tiles of up to 64 rows
+constexpr int SHORT = 64, SHORT_A = SHORT * QK * 2, SHORT_STAGE = SHORT_A + QOPER_BYTES, SHORT_DEPTH = 3, SHORT_PITCH = 36;
+constexpr int most(int a, int b) { return a > b ? a : b; }
+constexpr int TILE_LDS = most(most(4 * SLAB, 2 * STAGE), SHORT_DEPTH * SHORT_STAGE);
 static_assert(TILE_LDS <= 80 * 1024, "two workgroups per CU");
 
 // one product: rows [rows of an expert] x N columns (DW: M x N per expert), contraction K (DW: the expert's rows)
@@ -85,6 +88,108 @@ __device__ __forceinline__ void finish(const LinearArgs& l, const Product& p, in
   store_to<bf16_t>(p.C, at, y);
 }
 
+// eight columns of a row of a part
+template <int OP>
+__device__ __forceinline__ void store_out(const LinearArgs& l, const Product& p, int e, int part, size_t at, int col, const float* from) {
+  const f32x4 lo = *reinterpret_cast<const f32x4*>(from), hi = *reinterpret_cast<const f32x4*>(from + 4);
+  if (p.parts.n > 1) {
+    float* const to = p.parts.sums + part * p.parts.stride + at;
+    *reinterpret_cast<f32x4*>(to) = lo;
+    *reinterpret_cast<f32x4*>(to + 4) = hi;
+  } else {
+    float y[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+    finish<OP>(l, p, e, at, col, y);
+  }
+}
+
+// Matrices with up to 64 rows, bound by reading the weights: four wavefronts of 64 x 32 and three stages of 24 KB, so that more weights are on their
+// way and none are read into registers twice.  Forwards, us, as the other tiles / so: 40 rows of 14336 to 4096 37.0 / 31.5, of 4096 to 14336 36.2 / 32.0,
+// eight experts' 20 to 180 rows of 2048 to 1408 24.6 / 22.5, 16 experts' 20 to 306 of 2880 to 2880 75 / 68.  (What an expert of more rows has left over
+// past whole tiles reads weights that its other tiles read, from L2: 300 rows each 31.2, so 35.5.)
+template <int OP, bool STREAM>
+__device__ __forceinline__ void multiply_short(const LinearArgs& l, const Product& p, const Tile& t, int part, char* lds) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int n0 = t.nt * QT, row0 = t.first + t.mt * QT, rows = t.end - row0;
+  const int depth = p.K, all = (depth + QK - 1) / QK, per = (all + p.parts.n - 1) / p.parts.n, kt0 = min(all, part * per), kt1 = min(all, kt0 + per);
+  const uint32_t base = lds_addr(lds);
+  const bf16_t* const A = p.A + (size_t)row0 * p.lda;
+  uint32_t a_from[2];                              // load j of a wavefront: rows 8 (2 wave + j) + lane / 8
+#pragma unroll
+  for (int j = 0; j < 2; ++j) a_from[j] = (uint32_t)(min(8 * (2 * wave + j) + (lane >> 3), rows - 1) * p.lda * 2 + 16 * QuarterKc::chunk(j, lane));
+  QuarterKc b_kc;
+  QuarterTr b_tr;
+  if (OP == FWD) b_tr.setup(p.B + (size_t)t.e * p.b_es, nullptr, false, p.ldb, n0, p.N, wave, lane);
+  else b_kc.setup(p.B + (size_t)t.e * p.b_es + (size_t)n0 * p.ldb, p.ldb, p.N - n0, wave, lane);
+  auto issue = [&](int kt, int slot) {
+    const uint32_t st = base + slot * SHORT_STAGE;
+    const long k0 = (long)kt * QK;
+    const int last = depth - 1 - (int)k0;          // >= 0
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const uint32_t back = last < QK - 1 ? past_end((int)k0 + 8 * QuarterKc::chunk(j, lane), depth) : 0;
+      if (j < 2) lds_load16(A + k0, a_from[j] - back, st + (2 * wave + j) * 1024);
+      if (OP == DX) b_kc.template issue1<STREAM>(j, st + SHORT_A, wave, k0, back);
+      else b_tr.template issue1<true, STREAM>(j, st + SHORT_A, wave, lane, k0, last);
+    }
+  };
+  int a_off[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int row = i * 32 + (lane & 31);
+    a_off[i] = row * 128 + (((lane >> 5) ^ ((row >> 1) & 7)) << 4);
+  }
+  const int col = wave * 32 + (lane & 31);
+  const int b_off = SHORT_A + (OP == DX ? col * 128 + (((lane >> 5) ^ ((col >> 1) & 7)) << 4) : quarter_tr_off(wave >> 1, (wave & 1) * 32, lane));
+  f32x16 acc[2];
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) acc[i][r] = 0.f;
+#pragma unroll
+  for (int q = 0; q < SHORT_DEPTH; ++q)
+    if (kt0 + q < kt1) issue(kt0 + q, q);
+  int slot = 0;
+  for (int kt = kt0; kt < kt1; ++kt) {
+    if (kt + 2 < kt1) asm volatile("s_waitcnt vmcnt(12)" ::: "memory");
+    else if (kt + 1 < kt1) asm volatile("s_waitcnt vmcnt(6)" ::: "memory");
+    else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    const char* st = lds + slot * SHORT_STAGE;
+    bf16x8 fa[4][2], fb[4];
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      fb[s] = OP == DX ? lds_frag_kc(st + (b_off ^ (s * 32))) : quarter_frag_tr(st + b_off + s * 2048);
+#pragma unroll
+      for (int i = 0; i < 2; ++i) fa[s][i] = lds_frag_kc(st + (a_off[i] ^ (s * 32)));
+    }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    __builtin_amdgcn_s_barrier();                  // every wavefront has its fragments: the stage is free
+    if (kt + SHORT_DEPTH < kt1) issue(kt + SHORT_DEPTH, slot);
+    slot = slot == SHORT_DEPTH - 1 ? 0 : slot + 1;
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      if ((kt + 1) * QK > depth && kt * QK + 16 * s + 8 * (lane >> 5) >= depth) fa[s][0] = fa[s][1] = fb[s] = bf16x8{};
+#pragma unroll
+      for (int i = 0; i < 2; ++i) acc[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(fa[s][i], fb[s], acc[i], 0, 0, 0);
+    }
+  }
+  float* const slab = reinterpret_cast<float*>(lds) + wave * (SHORT * SHORT_PITCH);
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) slab[(32 * i + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3)) * SHORT_PITCH + (lane & 31)] = acc[i][r];
+  __builtin_amdgcn_wave_barrier();
+  const int out_col = n0 + wave * 32 + (lane & 3) * 8;
+  if (out_col >= p.N) return;
+#pragma unroll
+  for (int q = 0; q < 4; ++q) {
+    const int in = 16 * q + (lane >> 2);
+    if (in >= rows) break;
+    const float* const from = slab + in * SHORT_PITCH + (lane & 3) * 8;
+    store_out<OP>(l, p, t.e, part, (size_t)(row0 + in) * p.N + out_col, out_col, from);
+  }
+}
+
 // STREAM (FWD, DX): weights that one tile reads are loaded as such
 template <int OP, bool STREAM = false>
 __device__ __forceinline__ void multiply_tile(const LinearArgs& l, const Product& p, int b, int part, char* lds) {
@@ -92,6 +197,8 @@ __device__ __forceinline__ void multiply_tile(const LinearArgs& l, const Product
   const int wm = wave >> 1, wn = wave & 1;
   Tile t;
   if (!tile_of<OP>(l, p, b, lane, t)) return;
+  if constexpr (OP != DW)
+    if (t.end - t.first <= SHORT) return multiply_short<OP, STREAM>(l, p, t, part, lds);
   const int n0 = t.nt * QT;
   const int row0 = OP == DW ? t.mt * QT : t.first + t.mt * QT, row_end = OP == DW ? p.M : t.end;      // of the output
   // k-tiles [kt, kt1) of 64, of the whole contraction [0, depth)
@@ -201,16 +308,7 @@ __device__ __forceinline__ void multiply_tile(const LinearArgs& l, const Product
     const int in = 8 * q + (lane >> 3), row = row0 + wm * 64 + in;
     if (row >= row_end) break;
     const float* from = slab + in * TILE_PITCH + (lane & 7) * 8;
-    const f32x4 lo = *reinterpret_cast<const f32x4*>(from), hi = *reinterpret_cast<const f32x4*>(from + 4);
-    const size_t at = ((size_t)(OP == DW ? t.e : 0) * p.M + row) * p.N + col;
-    if (p.parts.n > 1) {
-      float* const to = p.parts.sums + part * p.parts.stride + at;
-      *reinterpret_cast<f32x4*>(to) = lo;
-      *reinterpret_cast<f32x4*>(to + 4) = hi;
-    } else {
-      float y[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-      finish<OP>(l, p, t.e, at, col, y);
-    }
+    store_out<OP>(l, p, t.e, part, ((size_t)(OP == DW ? t.e : 0) * p.M + row) * p.N + col, col, from);
   }
 }
 
