@@ -14,6 +14,7 @@
 namespace {
 
 constexpr int DEPTH = 2, W = 4, TM = 64, KP = 32;
+constexpr long long PART_SUMS = 4 << 20;       // of all parts together, at most
 
 struct FewArgs {
   LinearArgs l;
@@ -149,27 +150,39 @@ __global__ __launch_bounds__(W * WAVE, 2) void linear_few(FewArgs p) {
   else few_tile<C, 4, STREAM>(p, at, blockIdx.y, sums);
 }
 
-// tiles of 64 rows by a strip, at most
-inline long long tiles_of(int rows, int N, int e_cnt, int strip) {
-  return (((long long)rows + TM - 1) / TM + (e_cnt < rows ? e_cnt : rows) - 1) * ((N + strip - 1) / strip);
+// tiles of 64 rows by a strip, at most, where `active` experts have rows
+inline long long tiles_of(int rows, int N, int active, int strip) {
+  return (((long long)rows + TM - 1) / TM + active - 1) * ((N + strip - 1) / strip);
 }
-// Columns of a lane and parts of the contraction, by their time in us: weights at what memory delivers (rows of 128 bytes a little less) or at what
-// the CU with the most strips takes in, and the launch that adds the parts up.  One row, us, strips of 128 whole / of 64 whole / of 128 in two parts / in
-// eight: 4096 to 14336 31.9 / 26.8 / 25.8 / 26.0; 14336 to 4096 82.8 / 61.1 / 48.4 / 26.6; 4096 to 1536 17.3 / 13.4 / 12.6 / 8.4; 768 to 4096 5.6 / 5.2 / 7.6
-// / 7.7; 8 experts of 4096 to 1536 32.8 / 23.5 / 25.7 / 24.6; 32 experts of 7168 to 2048 145 / 157 / 152 / 151.
+// Time in us of strips of `bytes` each: rounds of the chip at what memory delivers, the last one by the CU's own intake where that is longer, and the first
+// loads of each
+inline float strips_time(long long strips, float bytes, float chip, float cu) {
+  const float rest = (float)(strips % 256) * bytes / chip, own = strips % 256 ? bytes / cu : 0.f;
+  return (float)((strips + 255) / 256) + (float)(strips / 256) * 256.f * bytes / chip + (rest > own ? rest : own);
+}
+// Columns of a lane and parts of the contraction, by their time and that of the launch that adds the parts up.  How many experts have rows is not
+// known here: the mean over counts from half of what may to all.  Rows of 64 columns come a little slower, from memory and into a CU.
+// One row, us, strips of 128 whole / of 64 whole / of 128 in two parts / in eight: 4096 to 14336 31.9 / 26.8 / 25.8 / 26.0; 14336 to 4096 82.8 / 61.1 / 48.4
+// / 26.6; 4096 to 1536 17.3 / 13.4 / 12.6 / 8.4; 768 to 4096 5.6 / 5.2 / 7.6 / 7.7.  128 rows of 32 experts of 7168 to 2048, strips of 128 whole / in two /
+// in four: 14 of them with rows 70.7 / 75.9 / 77.8, 16 75.9 / 77.4 / 81.3, 17 119.9 / 98.2 / 91.6, 20 119.6 / 102.1 / 99.7, 24 126 / 114 / 117, 32
+// 147 / 146 / 150.
 struct Plan { int c, parts; };
 inline Plan plan_of(int rows, int K, int N, int e_cnt) {
-  const int steps = (K + KP - 1) / KP;
-  const double bytes = 2.0 * (e_cnt < rows ? e_cnt : rows) * K * N;
-  double best = 0;
+  const int steps = (K + KP - 1) / KP, all = e_cnt < rows ? e_cnt : rows, half = (all + 1) / 2, samples = all - half < 7 ? all - half + 1 : 8;
+  float best = 0;
   Plan plan = {0, 0};
   for (int c = 8; c >= 4; c -= 4) {
-    const long long tiles = tiles_of(rows, N, e_cnt, 16 * c);
-    const double memory = bytes / (c == 8 ? 6.5e6 : 5.5e6), rate = c == 8 ? 40e3 : 30e3;
-    for (int p = 1; p <= MOST_PARTS && p <= steps / (2 * W) && (p == 1 || p * tiles <= CUT_WORKGROUPS); ++p) {
-      const double cu = (double)((p * tiles + 255) / 256) * ((steps + p - 1) / p) * (KP * 32 * c / rate);
-      const double t = (cu > memory ? cu : memory) + join_time(p, (double)rows * N);
-      if (plan.c == 0 || t < 0.97 * best) { best = t; plan = {c, p}; }
+    const int strip = 16 * c;
+    const float chip = c == 8 ? 6.5e6f : 5.5e6f, cu = c == 8 ? 45e3f : 33e3f;
+    for (int p = 1; p <= MOST_PARTS && p <= steps / (2 * W) && (p == 1 || (long long)p * rows * N <= PART_SUMS); ++p) {
+      const float bytes = (float)((steps + p - 1) / p) * (float)(KP * 2 * strip);
+      float t = 0.f;
+      for (int i = 0; i < samples; ++i) {
+        const int active = samples > 1 ? half + (int)((long long)i * (all - half) / (samples - 1)) : all;
+        t += strips_time(p * tiles_of(rows, N, active, strip), bytes, chip, cu);
+      }
+      t = t / (float)samples + join_time(p, (double)rows * N);
+      if (plan.c == 0 || t < 0.97f * best) { best = t; plan = {c, p}; }
     }
     if (plan.c == 0) { plan = {8, 1}; break; }             // (a contraction too short to be cut)
   }
@@ -178,17 +191,17 @@ inline Plan plan_of(int rows, int K, int N, int e_cnt) {
 
 }  // namespace
 
-// parts * rows * N floats for any number of rows up to this one: parts is at most MOST_PARTS, and CUT_WORKGROUPS strips of 64 rows
+// parts * rows * N floats for any number of rows up to this one
 size_t linear_few_ws_bytes(int rows, int N) {
-  const size_t all = (size_t)MOST_PARTS * rows * N * 4, most = (size_t)CUT_WORKGROUPS * TM * 128 * 4;
-  return all < most ? all : most;
+  const size_t all = (size_t)MOST_PARTS * rows * N;
+  return 4 * (all < PART_SUMS ? all : PART_SUMS);
 }
 
 int launch_linear_few(const LinearArgs& l, void* ws, hipStream_t s) {
   const Plan plan = plan_of(l.rows, l.K, l.N, l.e_cnt);
   const int steps = (l.K + KP - 1) / KP, per = (steps + plan.parts - 1) / plan.parts;
   const FewArgs p = {l, {(float*)ws, (size_t)l.rows * l.N, (steps + per - 1) / per}, per};
-  const dim3 grid((unsigned)((tiles_of(l.rows, l.N, l.e_cnt, 16 * plan.c) + 7) / 8 * 8), p.parts.n);
+  const dim3 grid((unsigned)((tiles_of(l.rows, l.N, l.e_cnt < l.rows ? l.e_cnt : l.rows, 16 * plan.c) + 7) / 8 * 8), p.parts.n);
   ProfScope prof(MOE_K_LINEAR, s);
   const bool stream = 2ll * l.K * l.N * l.e_cnt > (256ll << 20);       // (stream_rule.h: weights that the Infinity Cache does not keep)
   const auto kernel = plan.c == 8 ? (stream ? linear_few<8, true> : linear_few<8, false>) : (stream ? linear_few<4, true> : linear_few<4, false>);
