@@ -34,6 +34,9 @@
 namespace {
 
 constexpr int TM = 64, TN = 64, TK = 32, NT = 256;
+// LWG: consecutive tiles that an XCD takes in turn, where experts differ in rows.  Backward of 16 experts, 38 to 887 rows each, 520 to 776, us, an eighth of
+// the list each / 128 / 64 / 32 / 16: 96 / 89 / 80 / 72 / 70 (200 rows each 66 / 68 / 68 / 68 / 67).
+constexpr int CHUNK = 16;
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 
 enum { UP, DOWN, DA, DX, WG, WGD, LIN, LDX, LWG };
@@ -250,24 +253,25 @@ struct Args {
 };
 
 // LDS of one k-tile: the three bf16 terms of each operand, or the operands themselves
-template <int MODE> struct Traits {
+// WIDE (LINEAR): two tiles of 64 columns beside each other, which share what A takes
+template <int MODE, bool WIDE = false> struct Traits {
   static constexpr bool RAGGED_K = MODE == WG || MODE == WGD || MODE == LWG, LINEAR = MODE >= LIN;
   static constexpr bool DUAL = MODE == UP || MODE == WGD;
-  static constexpr int NB = DUAL ? 2 : 1;
+  static constexpr int NB = DUAL || WIDE ? 2 : 1;
   typedef typename Pick<RAGGED_K, OperMN, OperKC>::type OperA;
   typedef typename Pick<MODE == DA || MODE == DX || MODE == LDX, OperKC, OperMN>::type OperB;
   static constexpr int SPLIT_BYTES = (1 + NB) * 3 * PLANE_BYTES, PLAIN_BYTES = (OperA::WORDS + NB * OperB::WORDS) * 4;
   static constexpr int BUFFER = SPLIT_BYTES > PLAIN_BYTES ? SPLIT_BYTES : PLAIN_BYTES;
-  static constexpr int BLOCKS = DUAL ? 3 : 4;      // per CU, with one LDS buffer
+  static constexpr int BLOCKS = NB == 2 ? 3 : 4;      // per CU, with one LDS buffer
 };
 
 // Block `block` of one GEMM, a 1-D list of tiles: RaggedTiles' for the ragged-M shapes, the same with a fixed number of row tiles
 // per expert for the ragged-K ones.
 // BUFS: LDS buffers, two in launches of few blocks (use_two()).
 // part (LINEAR): of the contraction, whose sums go to p.parts.
-template <int MODE, int BUFS>
+template <int MODE, int BUFS, bool WIDE = false>
 __device__ __forceinline__ void gemm_tile(const Args& p, int block, char* lds, int part = 0) {
-  using TR = Traits<MODE>;
+  using TR = Traits<MODE, WIDE>;
   constexpr bool RAGGED_K = TR::RAGGED_K, DUAL = TR::DUAL;
   constexpr int NB = TR::NB, BUFFER = TR::BUFFER;
   typedef typename TR::OperA OperA;
@@ -275,7 +279,8 @@ __device__ __forceinline__ void gemm_tile(const Args& p, int block, char* lds, i
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int n_tiles = (p.N + TN - 1) / TN, m_tiles = (p.M + TM - 1) / TM;
+  constexpr int COLS = WIDE ? 2 * TN : TN;
+  const int n_tiles = (p.N + COLS - 1) / COLS, m_tiles = (p.M + TM - 1) / TM;
   int e, mt, nt, row0, row_end, K;                       // output rows [row0, row_end)
   int k_from = 0;
   if (TR::LINEAR && !p.off) {                            // one expert: the tiles are known
@@ -290,8 +295,8 @@ __device__ __forceinline__ void gemm_tile(const Args& p, int block, char* lds, i
     K = RAGGED_K ? p.rows : p.K;
   } else if (RAGGED_K) {
     const int total = p.e_cnt * m_tiles * n_tiles, share = (total + 7) / 8;
-    const int tile = (block % 8) * share + block / 8;
-    if (block / 8 >= share || tile >= total) return;
+    const int tile = TR::LINEAR ? (block / (8 * CHUNK) * 8 + block % 8) * CHUNK + block / 8 % CHUNK : block / 8 < share ? (block % 8) * share + block / 8 : total;
+    if (tile >= total) return;
     e = tile / (m_tiles * n_tiles);
     mt = (tile - e * m_tiles * n_tiles) / n_tiles;
     nt = tile % n_tiles;
@@ -304,7 +309,8 @@ __device__ __forceinline__ void gemm_tile(const Args& p, int block, char* lds, i
     row_end = p.off[e + 1];
     K = p.K;
   }
-  const int col0 = nt * TN;
+  const int col0 = nt * COLS;
+  const auto col_of = [&](int i) { return WIDE && i && col0 + TN < p.N ? col0 + TN : col0; };        // (past the last column: the first tile again)
   if (TR::LINEAR && p.parts.n > 1) {                     // whole k-tiles
     const int per = ((K + TK - 1) / TK + p.parts.n - 1) / p.parts.n * TK;
     k_from = min(K, part * per);
@@ -318,14 +324,14 @@ __device__ __forceinline__ void gemm_tile(const Args& p, int block, char* lds, i
       const size_t first = (TR::LINEAR && !p.off ? 0 : p.off[e]) + k_from;
       a.setup(p.A[0] + first * p.lda + row0, p.lda, p.M - row0, K, tid);
 #pragma unroll
-      for (int i = 0; i < NB; ++i) b[i].setup(p.B[i] + first * p.ldb + col0, p.ldb, p.N - col0, K, tid);
+      for (int i = 0; i < NB; ++i) b[i].setup(p.B[WIDE ? 0 : i] + first * p.ldb + col_of(i), p.ldb, p.N - col_of(i), K, tid);
     } else {
       a.setup(p.A[seg] + (size_t)row0 * p.lda + k_from, p.lda, row_end - row0, K, tid);
 #pragma unroll
       for (int i = 0; i < NB; ++i) {
         const float* w = p.B[DUAL ? i : seg] + (size_t)e * p.b_es;
-        if constexpr (MODE == DA || MODE == DX || MODE == LDX) b[i].setup(w + (size_t)col0 * p.ldb + k_from, p.ldb, p.N - col0, K, tid);
-        else b[i].setup(w + (size_t)k_from * p.ldb + col0, p.ldb, p.N - col0, K, tid);
+        if constexpr (MODE == DA || MODE == DX || MODE == LDX) b[i].setup(w + (size_t)col_of(i) * p.ldb + k_from, p.ldb, p.N - col_of(i), K, tid);
+        else b[i].setup(w + (size_t)k_from * p.ldb + col_of(i), p.ldb, p.N - col_of(i), K, tid);
       }
     }
   };
@@ -455,15 +461,16 @@ __device__ __forceinline__ void gemm_tile(const Args& p, int block, char* lds, i
   };
   // The outputs of the accumulator elements in todo (bit r: element r).  Element 4g + i of a lane is row 8g + 4*(lane/32) + i,
   // column lane%32 of its wavefront's block.
-  auto finish = [&](uint32_t todo, float scale) {
-    const int col = col0 + wn * 32 + (lane & 31);
+  auto finish_tile = [&](uint32_t todo, float scale, auto which) {
+    constexpr int I = decltype(which)::value;        // WIDE: of the two
+    const int col = col0 + TN * I + wn * 32 + (lane & 31);
     if (col >= p.N) return;
     if (TR::LINEAR && p.parts.n > 1) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         const int row = row0 + wm * 32 + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3);
         if (row < row_end && (todo >> r & 1))
-          p.parts.sums[part * p.parts.stride + (size_t)e * p.c_es + (size_t)row * p.ldc + col] = (acc[0][0][r] + acc[0][1][r]) * scale;
+          p.parts.sums[part * p.parts.stride + (size_t)e * p.c_es + (size_t)row * p.ldc + col] = (acc[I][0][r] + acc[I][1][r]) * scale;
       }
       return;
     }
@@ -475,7 +482,7 @@ __device__ __forceinline__ void gemm_tile(const Args& p, int block, char* lds, i
           const int row = row0 + wm * 32 + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3);
           if (row >= row_end || !(todo >> r & 1)) continue;
           const size_t idx = (size_t)row * p.ldc + col;
-          const float z = (acc[0][0][r] + acc[0][1][r]) * scale + bias;
+          const float z = (acc[I][0][r] + acc[I][1][r]) * scale + bias;
           const float v = act_value<decltype(a)::value, false>(z);
           if (p.C[1]) p.C[1][idx] = z;
           p.C[0][idx] = p.R ? v + p.R[idx] : v;
@@ -499,7 +506,7 @@ __device__ __forceinline__ void gemm_tile(const Args& p, int block, char* lds, i
       for (int i = 0; i < 4; ++i) {
         if (r0 + i >= row_end || !(todo >> (4 * g + i) & 1)) continue;
         const size_t idx = (size_t)e * p.c_es + (size_t)(r0 + i) * p.ldc + col;
-        const float x = (acc[0][0][4 * g + i] + acc[0][1][4 * g + i]) * scale;
+        const float x = (acc[I][0][4 * g + i] + acc[I][1][4 * g + i]) * scale;
         const float x3 = (acc[NB - 1][0][4 * g + i] + acc[NB - 1][1][4 * g + i]) * scale;      // second output of a dual tile
         if (MODE == UP) {
           if (p.C[0]) { p.C[0][idx] = x; p.C[1][idx] = x3; }
@@ -515,6 +522,10 @@ __device__ __forceinline__ void gemm_tile(const Args& p, int block, char* lds, i
         }
       }
     }
+  };
+  auto finish = [&](uint32_t todo, float scale) {
+    finish_tile(todo, scale, Int<0>{});
+    if constexpr (WIDE) finish_tile(todo, scale, Int<1>{});
   };
   // Outputs with an infinity, a NaN, a number beyond 2^96 or a sum beyond 2^64 in them have sums that are no numbers.  Those, and no
   // others of their tile, come from the operands as they are: what a row or column holds does not show in its neighbours' bits.
@@ -659,10 +670,10 @@ int launch_expert_bwd_f32(const float* xp, const float* h1, const float* h3, con
 namespace {
 
 // (tile, part) of one product, and of both gradients
-template <int MODE, int BUFS>
-__global__ __launch_bounds__(NT, BUFS == 2 ? 2 : Traits<MODE>::BLOCKS) void linear_f32(Args p) {
-  __shared__ __align__(16) char lds[BUFS * Traits<MODE>::BUFFER];
-  gemm_tile<MODE, BUFS>(p, blockIdx.x, lds, blockIdx.y);
+template <int MODE, int BUFS, bool WIDE>
+__global__ __launch_bounds__(NT, (BUFS == 2 ? 2 : Traits<MODE, WIDE>::BLOCKS)) void linear_f32(Args p) {
+  __shared__ __align__(16) char lds[BUFS * Traits<MODE, WIDE>::BUFFER];
+  gemm_tile<MODE, BUFS, WIDE>(p, blockIdx.x, lds, blockIdx.y);
 }
 struct Gradients {
   Args x, w;
@@ -670,37 +681,51 @@ struct Gradients {
   int x_blocks, w_blocks, x_total, w_total;      // of one part (multiples of 8); of all
   int w_first;
 };
-template <int BUFS>
-__global__ __launch_bounds__(NT, BUFS == 2 ? 2 : Traits<LDX>::BLOCKS) void gradients_f32(Gradients g) {
-  __shared__ __align__(16) char lds[BUFS * (Traits<LDX>::BUFFER > Traits<LWG>::BUFFER ? Traits<LDX>::BUFFER : Traits<LWG>::BUFFER)];
+template <int BUFS, bool WIDE>
+__global__ __launch_bounds__(NT, (BUFS == 2 ? 2 : Traits<LDX, WIDE>::BLOCKS)) void gradients_f32(Gradients g) {
+  __shared__ __align__(16) char lds[BUFS * (Traits<LDX, WIDE>::BUFFER > Traits<LWG, WIDE>::BUFFER ? Traits<LDX, WIDE>::BUFFER : Traits<LWG, WIDE>::BUFFER)];
   int b = blockIdx.x;
   if (b >= g.x_total + g.w_total) return bias_columns<float>(g.db, b - g.x_total - g.w_total, reinterpret_cast<float*>(lds));
   const int first = g.w_first ? g.w_total : g.x_total;
   const bool in_first = b < first;
   if (!in_first) b -= first;
-  if (in_first == (g.w_first != 0)) gemm_tile<LWG, BUFS>(g.w, b % g.w_blocks, lds, b / g.w_blocks);
-  else gemm_tile<LDX, BUFS>(g.x, b % g.x_blocks, lds, b / g.x_blocks);
+  if (in_first == (g.w_first != 0)) gemm_tile<LWG, BUFS, WIDE>(g.w, b % g.w_blocks, lds, b / g.w_blocks);
+  else gemm_tile<LDX, BUFS, WIDE>(g.x, b % g.x_blocks, lds, b / g.x_blocks);
 }
 static_assert(NT == BIAS_THREADS, "");
 
-// A k-tile takes 0.65 us while its workgroup has a CU for itself, and the chip multiplies 140 TFLOP/s: a contraction is cut until its tiles end
+// A k-tile takes 0.65 us (WIDE: 1.2) while its workgroup has a CU for itself, and the chip multiplies 140 TFLOP/s: a contraction is cut until its tiles end
 // with everything, or in 6 us, while there are workgroups to take the parts.  1, 64 and 1000 rows of 2048 to 2048 fp32 forward 45, 50, 77 us uncut.
-constexpr float K_TILE = 0.65f;
-int f32_parts(long long tiles, long long k_tiles, float all) {
+constexpr float K_TILE = 0.65f, WIDE_K_TILE = 1.2f;
+int f32_parts(long long tiles, long long k_tiles, float all, bool wide) {
   const float goal = all > 6.f ? all : 6.f;
   int p = 1;
-  while (p < MOST_PARTS && (p + 1) * tiles <= 4 * CUT_WORKGROUPS && 4 * (p + 1) <= k_tiles && (float)((k_tiles + p - 1) / p) * K_TILE > goal) ++p;
+  while (p < MOST_PARTS && (p + 1) * tiles <= (wide ? 2 : 4) * CUT_WORKGROUPS && 4 * (p + 1) <= k_tiles && (float)((k_tiles + p - 1) / p) * (wide ? WIDE_K_TILE : K_TILE) > goal) ++p;
   return p;
 }
 long long f32_row_tiles(const LinearArgs& l) {
   return ((long long)l.rows + TM - 1) / TM + (l.offsets ? (l.e_cnt < l.rows ? l.e_cnt : l.rows) - 1 : 0);
 }
+// Two LDS buffers (see use_two) while three blocks share a CU: the linear layer's kernels have the registers.  Backward, us, up to two / three: 500 rows
+// of 1024 to 1024 34.8 / 30.0, 700 of 520 to 776 46.6 / 38.7.
+inline bool few_f32(long long blocks) { return blocks <= 3 * device_cu_count(); }
+inline long long f32_columns(int n, bool wide) { const int w = wide ? 2 * TN : TN; return (n + w - 1) / w; }
+// WIDE tiles, half as many that split A's operands half as often, where they fill the chip all the same and leave little of their columns empty.
+// us, 64 / 128 columns: forward, 16000 rows of 2048 to 2048 930 / 815 (165 TFLOP/s), 4000 of them 245 / 224, of 1024 to 1024 (504 tiles) 65.0 / 63.9, of
+// 1408 to 768 (378) 69 / 75, 1000 of 2048 to 2048 (256) 70 / 66 to 91; 16000 of 520 to 776 (896 columns for 832) 115 / 118.  Backward: 16000 rows of
+// 2048 to 2048 1830 / 1600, of 1024 to 1024 544 / 450, 1000 of them 55 / 48 (700 33 / 37), 32 experts' 1000 of 768 to 768 569 / 522, 8 experts' 300 of 1024
+// to 512 51 / 58.
+bool wide_fwd(const LinearArgs& l) {
+  const long long tiles = f32_columns(l.N, true);
+  return f32_row_tiles(l) * tiles >= 1000 && 20 * tiles * 2 <= 21 * f32_columns(l.N, false);
+}
+bool wide_bwd(const LinearArgs& l) { return l.rows >= 600ll * l.e_cnt && (double)l.rows * l.K * l.N >= 1e9; }
 float f32_time(double products) { return (float)(2 * products / 140e6); }
 inline long long blocks8(long long tiles) { return (tiles + 7) / 8 * 8; }
 
 }  // namespace
 
-// rows * columns floats times the parts of at most 4 CUT_WORKGROUPS tiles of 64x64
+// rows * columns floats times the parts of at most 4 CUT_WORKGROUPS tiles of 64x64 (2 of 64x128)
 size_t linear_f32_parts_bytes(long long rows, int columns) {
   const size_t all = (size_t)MOST_PARTS * rows * columns * 4, most = (size_t)4 * CUT_WORKGROUPS * TM * TN * 4;
   return all < most ? all : most;
@@ -711,11 +736,12 @@ int launch_linear_fwd_f32(const LinearArgs& l, void* ws, hipStream_t s) {
   u.A[0] = (const float*)l.x; u.lda = l.K; u.B[0] = (const float*)l.w; u.ldb = l.N; u.b_es = (long)l.K * l.N;
   u.C[0] = (float*)l.y; u.C[1] = (float*)l.z; u.ldc = l.N; u.N = l.N; u.K = l.K; u.off = l.offsets; u.e_cnt = l.e_cnt; u.rows = l.rows;
   u.bias = (const float*)l.bias; u.R = (const float*)l.residual; u.act = l.act;
-  const long long tiles = f32_row_tiles(l) * ((l.N + TN - 1) / TN), blocks = blocks8(tiles);
-  u.parts = {(float*)ws, (size_t)l.rows * l.N, f32_parts(tiles, (l.K + TK - 1) / TK, f32_time((double)l.rows * l.K * l.N))};
+  const bool wide = wide_fwd(l);
+  const long long tiles = f32_row_tiles(l) * f32_columns(l.N, wide), blocks = blocks8(tiles);
+  u.parts = {(float*)ws, (size_t)l.rows * l.N, f32_parts(tiles, (l.K + TK - 1) / TK, f32_time((double)l.rows * l.K * l.N), wide)};
   {
     ProfScope prof(MOE_K_LINEAR, s);
-    const auto kernel = use_two(blocks * u.parts.n) ? linear_f32<LIN, 2> : linear_f32<LIN, 1>;
+    const auto kernel = wide ? linear_f32<LIN, 1, true> : few_f32(blocks * u.parts.n) ? linear_f32<LIN, 2, false> : linear_f32<LIN, 1, false>;
     hipLaunchKernelGGL(kernel, dim3((unsigned)blocks, u.parts.n), dim3(NT), 0, s, u);
     HIP_CHECK_LAUNCH();
   }
@@ -735,19 +761,20 @@ int launch_linear_bwd_f32(const LinearArgs& l, const void* dz, void* dx, int dx_
   w.A[0] = (const float*)l.x; w.lda = l.K; w.B[0] = (const float*)dz; w.ldb = l.N;
   w.C[0] = (float*)dw; w.ldc = l.N; w.c_es = (long)l.K * l.N; w.M = l.K; w.N = l.N; w.off = l.offsets; w.e_cnt = l.e_cnt; w.beta = accumulate;
   w.rows = l.rows;
-  const long long x_tiles = f32_row_tiles(l) * ((l.K + TN - 1) / TN), w_tiles = (long long)l.e_cnt * ((l.K + TM - 1) / TM) * ((l.N + TN - 1) / TN);
+  const bool wide = wide_bwd(l);
+  const long long x_tiles = f32_row_tiles(l) * f32_columns(l.K, wide), w_tiles = (long long)l.e_cnt * ((l.K + TM - 1) / TM) * f32_columns(l.N, wide);
   const float all = f32_time((double)l.rows * l.K * l.N * ((have_dx ? 1 : 0) + (dw ? 1 : 0)));
-  x.parts = {(float*)ws_dx, (size_t)l.rows * l.K, have_dx ? f32_parts(x_tiles, (l.N + TK - 1) / TK, all) : 1};
-  w.parts = {(float*)ws_dw, (size_t)l.e_cnt * l.K * l.N, dw ? f32_parts(w_tiles, (l.rows / l.e_cnt + TK - 1) / TK, all) : 1};
+  x.parts = {(float*)ws_dx, (size_t)l.rows * l.K, have_dx ? f32_parts(x_tiles, (l.N + TK - 1) / TK, all, wide) : 1};
+  w.parts = {(float*)ws_dw, (size_t)l.e_cnt * l.K * l.N, dw ? f32_parts(w_tiles, (l.rows / l.e_cnt + TK - 1) / TK, all, wide) : 1};
   g.x_blocks = (int)blocks8(x_tiles);
-  g.w_blocks = (int)blocks8(w_tiles);
+  g.w_blocks = l.offsets ? (int)((w_tiles + 8 * CHUNK - 1) / (8 * CHUNK) * 8 * CHUNK) : (int)blocks8(w_tiles);
   g.x_total = have_dx ? g.x_blocks * x.parts.n : 0;
   g.w_total = dw ? g.w_blocks * w.parts.n : 0;
   g.w_first = 5ll * l.rows / w.parts.n > 6ll * l.e_cnt * l.N / x.parts.n;      // the longer tiles (see the experts' backward)
   const unsigned blocks = g.x_total + g.w_total + (db.db ? bias_blocks(l.N, l.e_cnt) : 0);
   if (blocks > 0) {
     ProfScope prof(have_dx && dw ? MOE_K_LINEAR_DX_DW : dw ? MOE_K_LINEAR_DW : have_dx ? MOE_K_LINEAR_DX : MOE_K_LINEAR_BIAS, s);
-    const auto kernel = use_two(blocks) ? gradients_f32<2> : gradients_f32<1>;
+    const auto kernel = wide ? gradients_f32<1, true> : few_f32(blocks) ? gradients_f32<2, false> : gradients_f32<1, false>;
     hipLaunchKernelGGL(kernel, dim3(blocks), dim3(NT), 0, s, g);
     HIP_CHECK_LAUNCH();
   }

@@ -217,6 +217,30 @@ def test_weights_beyond_the_infinity_cache(rows, K, N):
             assert ((got.double() - ref).abs() <= err + 2.0 ** -8 * (ref.abs() + err)).all(), (name, e)
 
 
+@pytest.mark.parametrize("rows,K,N", [(2100, 1032, 2012), (7000, 260, 1220), ([1800, 0, 1300, 900, 40], 516, 1092), ([5, 700, 0, 30, 200, 1, 64, 90], 260, 388)], ids=str)
+def test_fp32_of_many_tiles(rows, K, N):
+    """Pairs of tiles beside each other whose second one is narrow or missing, and experts whose rows differ, tiles in chunks."""
+    print(f"case linear {rows} {K} {N} fp32", flush=True)
+    Case(rows, K, N, "gelu_tanh", F32, seed=N).check_both(accumulate=isinstance(rows, list))
+
+
+def test_fp32_infinities_in_pairs_of_tiles():
+    """Sums that are no numbers are formed again from the operands: in both tiles of a pair, and in no others."""
+    c = Case(2100, 520, 2060, "none", F32, residual=False, bias=False)
+    c.x.abs_().add_(0.5)
+    c.w.abs_().add_(0.01)
+    for col in (3, 70, 2047, 2059):
+        c.w[519, col] = float("inf")
+    c.w[0, 130] = 2.0 ** 100
+    c.forward()
+    y = host(c.y)
+    assert (y[:, [3, 70, 2047, 2059]] == np.inf).all()
+    rest = np.delete(y, (3, 70, 2047, 2059), axis=1)
+    assert np.isfinite(rest).all()
+    ref = host(c.x) @ np.delete(host(c.w), (3, 70, 2047, 2059), axis=1)
+    assert (np.abs(rest - ref) <= (520 + 4) * 2.0 ** -23 * ref).all()               # (all terms positive: their sum is their sizes')
+
+
 @pytest.mark.parametrize("dt", (BF16, F32))
 @pytest.mark.parametrize("K", (64, 72))
 def test_infinities_and_nan_stay_where_they_belong(K, dt):
