@@ -169,6 +169,14 @@ def test_long_contractions(rows, dt, K, N):
     Case(rows, K, N, "gelu", dt, seed=K).check_both(accumulate=rows in (33, [130, 0, 70, 1, 5]))
 
 
+@pytest.mark.parametrize("dt,N", [(BF16, 4104), (F32, 2052)])
+@pytest.mark.parametrize("rows", [8300, [5000, 3, 0, 3300]], ids=str)
+def test_gradients_of_large_activations(rows, dt, N):
+    """dy and z beyond half of the Infinity Cache."""
+    print(f"case linear {rows} 16 {N} {dt}", flush=True)
+    Case(rows, 16, N, "gelu", dt, residual=False, seed=7).check_both()
+
+
 @pytest.mark.parametrize("dt", (BF16, F32))
 @pytest.mark.parametrize("rows", [20000, [18000, 12, 0, 300]], ids=str)
 def test_weight_gradient_of_many_rows(rows, dt):
