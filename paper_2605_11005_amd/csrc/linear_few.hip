@@ -150,15 +150,16 @@ __global__ __launch_bounds__(W * WAVE, 2) void linear_few(FewArgs p) {
   else few_tile<C, 4, STREAM>(p, at, blockIdx.y, sums);
 }
 
-// tiles of 64 rows by a strip, at most, where `active` experts have rows
-inline long long tiles_of(int rows, int N, int active, int strip) {
-  return (((long long)rows + TM - 1) / TM + active - 1) * ((N + strip - 1) / strip);
+inline long long strips_of(int N, int strip) { return (N + strip - 1) / strip; }
+// tiles of 64 rows by a strip, at most
+inline long long most_tiles(int rows, int N, int e_cnt, int strip) {
+  return (((long long)rows + TM - 1) / TM + (e_cnt < rows ? e_cnt : rows) - 1) * strips_of(N, strip);
 }
-// Time in us of strips of `bytes` each: rounds of the chip at what memory delivers, the last one by the CU's own intake where that is longer, and the first
+// Time in us of strips of `bytes` each: what memory delivers, or what the CU with the most strips takes in, less of it while all CUs ask; and the first
 // loads of each
 inline float strips_time(long long strips, float bytes, float chip, float cu) {
-  const float rest = (float)(strips % 256) * bytes / chip, own = strips % 256 ? bytes / cu : 0.f;
-  return (float)((strips + 255) / 256) + (float)(strips / 256) * 256.f * bytes / chip + (rest > own ? rest : own);
+  const float rounds = (float)((strips + 255) / 256), memory = (float)strips * bytes / chip, own = rounds * bytes / (strips > 256 ? 0.71f * cu : cu);
+  return 0.5f * rounds + (memory > own ? memory : own);
 }
 // Columns of a lane and parts of the contraction, by their time and that of the launch that adds the parts up.  How many experts have rows is not
 // known here: the mean over counts from half of what may to all.  Rows of 64 columns come a little slower, from memory and into a CU.
@@ -169,6 +170,7 @@ inline float strips_time(long long strips, float bytes, float chip, float cu) {
 struct Plan { int c, parts; };
 inline Plan plan_of(int rows, int K, int N, int e_cnt) {
   const int steps = (K + KP - 1) / KP, all = e_cnt < rows ? e_cnt : rows, half = (all + 1) / 2, samples = all - half < 7 ? all - half + 1 : 8;
+  const long long row_tiles = ((long long)rows + TM - 1) / TM;
   float best = 0;
   Plan plan = {0, 0};
   for (int c = 8; c >= 4; c -= 4) {
@@ -179,7 +181,7 @@ inline Plan plan_of(int rows, int K, int N, int e_cnt) {
       float t = 0.f;
       for (int i = 0; i < samples; ++i) {
         const int active = samples > 1 ? half + (int)((long long)i * (all - half) / (samples - 1)) : all;
-        t += strips_time(p * tiles_of(rows, N, active, strip), bytes, chip, cu);
+        t += strips_time(p * (active > row_tiles ? active : row_tiles) * strips_of(N, strip), bytes, chip, cu);
       }
       t = t / (float)samples + join_time(p, (double)rows * N);
       if (plan.c == 0 || t < 0.97f * best) { best = t; plan = {c, p}; }
@@ -201,7 +203,7 @@ int launch_linear_few(const LinearArgs& l, void* ws, hipStream_t s) {
   const Plan plan = plan_of(l.rows, l.K, l.N, l.e_cnt);
   const int steps = (l.K + KP - 1) / KP, per = (steps + plan.parts - 1) / plan.parts;
   const FewArgs p = {l, {(float*)ws, (size_t)l.rows * l.N, (steps + per - 1) / per}, per};
-  const dim3 grid((unsigned)((tiles_of(l.rows, l.N, l.e_cnt < l.rows ? l.e_cnt : l.rows, 16 * plan.c) + 7) / 8 * 8), p.parts.n);
+  const dim3 grid((unsigned)((most_tiles(l.rows, l.N, l.e_cnt, 16 * plan.c) + 7) / 8 * 8), p.parts.n);
   ProfScope prof(MOE_K_LINEAR, s);
   const bool stream = 2ll * l.K * l.N * l.e_cnt > (256ll << 20);       // (stream_rule.h: weights that the Infinity Cache does not keep)
   const auto kernel = plan.c == 8 ? (stream ? linear_few<8, true> : linear_few<8, false>) : (stream ? linear_few<4, true> : linear_few<4, false>);
