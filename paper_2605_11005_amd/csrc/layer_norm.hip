@@ -258,16 +258,18 @@ __global__ __launch_bounds__(WIDE ? WIDE_THREADS : BWD_THREADS) void layer_norm_
 }
 
 // The backward of few rows in one launch: blocks of rows as in the forward, and blocks that sum 64 columns over all rows, for which dw and db need the saved
-// mean and 1/deviation alone.  What the latter read again comes from the caches.
-constexpr int SUM_COLUMNS = 64;
+// mean and 1/deviation alone.  What the latter read again comes from the caches.  DEEP, from several hundred rows on: the blocks that sum begin first and have
+// eight rows a thread on their way, and may sum a part of the rows each, which a second launch adds up.
+constexpr int SUM_COLUMNS = 64, SUM_AHEAD = 8, PART_ROWS = 256;
 template <typename T, typename R>
 struct OneLaunch {
   BwdArgs<T, R> p;
   T* dw; T* db;
   int accumulate, row_blocks;
+  int parts;                               // DEEP: of the rows; more than one leave their sums in p.sums
 };
-template <typename T, typename R>
-__device__ __forceinline__ void sum_columns(const OneLaunch<T, R>& a, int c0) {
+template <bool DEEP, typename T, typename R>
+__device__ __forceinline__ void sum_columns(const OneLaunch<T, R>& a, int c0, int row_part) {
   constexpr int N = VEC<T>, LANES = SUM_COLUMNS / N, AT_ONCE = WAVE / LANES;      // lanes and rows of a wavefront's load
   __shared__ float part[2][MOST_WAVES][SUM_COLUMNS];
   const BwdArgs<T, R>& p = a.p;
@@ -276,7 +278,35 @@ __device__ __forceinline__ void sum_columns(const OneLaunch<T, R>& a, int c0) {
   float dw[N], db[N];
 #pragma unroll
   for (int j = 0; j < N; ++j) dw[j] = db[j] = 0.f;
-  if (c < p.d)
+  if constexpr (DEEP) {
+    const int share = (p.T_ + a.parts - 1) / a.parts, end = min(p.T_, (row_part + 1) * share), stride = waves * AT_ONCE;
+    if (c < p.d)
+      for (int first = row_part * share + wave * AT_ONCE + lane / LANES; first < end; first += SUM_AHEAD * stride) {
+        Raw<R, N> h[SUM_AHEAD];
+        Raw<T, N> dn[SUM_AHEAD];
+        float mean[SUM_AHEAD], rstd[SUM_AHEAD];
+#pragma unroll
+        for (int u = 0; u < SUM_AHEAD; ++u) {              // (rows past the end: the first one again, and left out)
+          const int row = first + u * stride < end ? first + u * stride : first;
+          h[u].load(p.h, (size_t)row * p.d + c);
+          dn[u].load(p.dn, (size_t)row * p.d + c);
+          mean[u] = p.mean[row];
+          rstd[u] = p.rstd[row];
+        }
+#pragma unroll
+        for (int u = 0; u < SUM_AHEAD; ++u) {
+          const bool in = first + u * stride < end;
+          float x[N], g[N];
+          h[u].values(x);
+          dn[u].values(g);
+#pragma unroll
+          for (int j = 0; j < N; ++j) {
+            dw[j] += in ? g[j] * ((x[j] - mean[u]) * rstd[u]) : 0.f;
+            db[j] += in ? g[j] : 0.f;
+          }
+        }
+      }
+  } else if (c < p.d)
 #pragma unroll 4
     for (int row = wave * AT_ONCE + lane / LANES; row < p.T_; row += waves * AT_ONCE) {
       float h[N], dn[N];
@@ -306,18 +336,27 @@ __device__ __forceinline__ void sum_columns(const OneLaunch<T, R>& a, int c0) {
     if (!out || c0 + col >= p.d) continue;
     float s = 0.f;
     for (int w = 0; w < waves; ++w) s += part[which][w][col];
+    if (DEEP && a.parts > 1) {
+      p.sums[((size_t)row_part * 2 + which) * p.d + c0 + col] = s;
+      continue;
+    }
     T& to = out[c0 + col];
     if constexpr (sizeof(T) == 2) to = (bf16_t)pack_bf16x2(a.accumulate ? bf16_to_f32(to) + s : s, 0.f);      // (the hardware's conversion keeps every NaN)
     else to = a.accumulate ? to + s : s;
   }
 }
-template <typename T, typename R, int STEPS>
+template <typename T, typename R, int STEPS, bool DEEP>
 __global__ __launch_bounds__((MOST_THREADS<T, STEPS>)) void layer_norm_bwd_few(OneLaunch<T, R> a) {
   constexpr int N = VEC<T>;
   __shared__ float2 red[MOST_WAVES];       // of the block's wavefronts, a row's one after the other
   const BwdArgs<T, R>& p = a.p;
-  if ((int)blockIdx.x >= a.row_blocks) return sum_columns(a, ((int)blockIdx.x - a.row_blocks) * SUM_COLUMNS);
-  const int row = blockIdx.x * blockDim.y + threadIdx.y;
+  int block = blockIdx.x;
+  if constexpr (DEEP) {
+    const int sums = (int)gridDim.x - a.row_blocks;
+    if (block < sums) return sum_columns<true>(a, block / a.parts * SUM_COLUMNS, block % a.parts);
+    block -= sums;
+  } else if (block >= a.row_blocks) return sum_columns<false>(a, (block - a.row_blocks) * SUM_COLUMNS, 0);
+  const int row = block * blockDim.y + threadIdx.y;
   const bool in = row < p.T_;
   const size_t at = (size_t)row * p.d;
   const float mean = in ? p.mean[row] : 0.f, rstd = in ? p.rstd[row] : 0.f, inv_d = 1.f / (float)p.d;
@@ -427,28 +466,49 @@ inline BwdPlan bwd_plan(int T, int d, int vec, bool fp32_residual, bool stream) 
   return b;
 }
 
-// Two launches / one, us: 256 rows of 2880 bf16 9.5 / 5.2, of 16384 21.8 / 12.5, 512 of 7168 17.2 / 11.6, 1024 of 520 12.9 / 6.8, of 4096 16.3 / 12.6, of
-// 7168 19.1 / 18.8, with fp32 residuals of 4096 19.5 / 20.6; 2047 of 2880 16.7 / 22.3.
-inline bool one_launch(int T, int d, int element, int residual) {
-  return T <= 512 || (T <= 1024 && (long long)T * d * (element + residual) <= (24ll << 20));
+// Two launches / one / one, DEEP, us: 256 rows of 2880 bf16 9.5 / 5.2 / 5.8, of 16384 21.8 / 12.5 / 12.2, 512 of 7168 17.2 / 11.7 / 10.4, 700 of 520 - / 5.2 / 6.4,
+// 1000 of 2880 - / 12.5 / 10.0, of 4096 16.3 / 12.7 / 10.7, with fp32 residuals 19.5 / 20.1 / 16.2, of 7168 18.9 / - / 15.9 (27.4 / - / 28.8).  Two / DEEP, in
+// parts: 1100 of 520 15.1 / 7.6, 4096 13.2 / 10.3, 2047 of 1032 13.3 / 11.5 (4096 of 1032 16.9 / 18.5, 2047 of 2880 16.6 / 20.7, 10000
+// of 128 with fp32 residuals 12.4 / 14.5).
+enum class FewRows { NO, SHALLOW, DEEP };
+inline FewRows few_rows(int T, int d, int element, int residual) {
+  const long long n = (long long)T * d;
+  if (T > 1024) return T <= 4096 && n * residual <= (8ll << 20) ? FewRows::DEEP : FewRows::NO;
+  if (T > 512 && n * (element + residual) > (30ll << 20)) return FewRows::NO;
+  return T >= 700 && n >= 1600000 ? FewRows::DEEP : FewRows::SHALLOW;
 }
 
+template <typename T, typename R>
+int add_columns(const BwdArgs<T, R>& p, int blocks, T* dw, T* db, int accumulate, hipStream_t s) {
+  if (!dw && !db) return MOE_OK;
+  ProfScope prof(MOE_K_LAYER_NORM_SUMS, s);
+  hipLaunchKernelGGL(column_sums<T>, dim3((p.d + WAVE - 1) / WAVE, 2), dim3(SUM_WAVES * WAVE), 0, s, p.sums, blocks, p.d, accumulate, dw, db);
+  HIP_CHECK_LAUNCH();
+  return MOE_OK;
+}
 template <typename T, typename R>
 int backward(BwdArgs<T, R> p, T* dw, T* db, int accumulate, hipStream_t s) {
   // (in place, the rows would write over what the column sums still read)
   const auto over = [&](const void* out) { return out && (out == p.dn || out == p.h); };
   const bool in_place = (dw || db) && (over(p.dh) || over(p.dy));
-  if (p.T_ > 0 && !in_place && one_launch(p.T_, p.d, sizeof(T), sizeof(R))) {
+  const FewRows few = p.T_ == 0 || in_place ? FewRows::NO : few_rows(p.T_, p.d, sizeof(T), sizeof(R));
+  if (few != FewRows::NO) {
     Shape shape(p.d, VEC<T>);
     if (shape.threads < 512) shape.rows = 512 / shape.threads;      // (the blocks that sum columns want wavefronts)
-    const OneLaunch<T, R> a = {p, dw, db, accumulate, p.dh || p.dy ? (p.T_ + shape.rows - 1) / shape.rows : 0};
-    const unsigned blocks = a.row_blocks + (dw || db ? (p.d + SUM_COLUMNS - 1) / SUM_COLUMNS : 0);
+    const int parts = p.T_ <= 1024 ? 1 : (p.T_ + PART_ROWS - 1) / PART_ROWS;       // at most 16
+    const OneLaunch<T, R> a = {p, dw, db, accumulate, p.dh || p.dy ? (p.T_ + shape.rows - 1) / shape.rows : 0, parts};
+    const unsigned blocks = a.row_blocks + (dw || db ? parts * ((p.d + SUM_COLUMNS - 1) / SUM_COLUMNS) : 0);
     if (blocks == 0) return MOE_OK;
-    ProfScope prof(MOE_K_LAYER_NORM_BWD, s);
-    const auto kernel = shape.steps == 1 ? layer_norm_bwd_few<T, R, 1> : shape.steps == 2 ? layer_norm_bwd_few<T, R, 2> : layer_norm_bwd_few<T, R, 4>;
-    hipLaunchKernelGGL(kernel, dim3(blocks), shape.block(), 0, s, a);
-    HIP_CHECK_LAUNCH();
-    return MOE_OK;
+    {
+      ProfScope prof(MOE_K_LAYER_NORM_BWD, s);
+      const auto of = [&](auto deep) {
+        constexpr bool DEEP = decltype(deep)::value != 0;
+        return shape.steps == 1 ? layer_norm_bwd_few<T, R, 1, DEEP> : shape.steps == 2 ? layer_norm_bwd_few<T, R, 2, DEEP> : layer_norm_bwd_few<T, R, 4, DEEP>;
+      };
+      hipLaunchKernelGGL(few == FewRows::DEEP ? of(Int<1>{}) : of(Int<0>{}), dim3(blocks), shape.block(), 0, s, a);
+      HIP_CHECK_LAUNCH();
+    }
+    return parts > 1 ? add_columns(p, parts, dw, db, accumulate, s) : MOE_OK;
   }
   const bool stream = streams(p.T_, p.d, sizeof(T), sizeof(R), p.dh_out);
   const BwdPlan plan = bwd_plan(p.T_, p.d, VEC<T>, sizeof(R) == 4, stream);
@@ -478,12 +538,7 @@ int backward(BwdArgs<T, R> p, T* dw, T* db, int accumulate, hipStream_t s) {
     }
     HIP_CHECK_LAUNCH();
   }
-  if (dw || db) {
-    ProfScope prof(MOE_K_LAYER_NORM_SUMS, s);
-    hipLaunchKernelGGL(column_sums<T>, dim3((p.d + WAVE - 1) / WAVE, 2), dim3(SUM_WAVES * WAVE), 0, s, p.sums, blocks, p.d, accumulate, dw, db);
-    HIP_CHECK_LAUNCH();
-  }
-  return MOE_OK;
+  return add_columns(p, blocks, dw, db, accumulate, s);
 }
 
 }  // namespace

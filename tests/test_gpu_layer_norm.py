@@ -164,8 +164,7 @@ def test_in_place_beside_the_column_sums(T, d, dt, rt):
         c.check_backward()
 
 
-@pytest.mark.parametrize("T", (511, 512, 513, 1023, 1024, 1025))
-@pytest.mark.parametrize("d", (264, 3080))
+@pytest.mark.parametrize("T,d", [(T, d) for T in (511, 512, 513, 1023, 1024, 1025) for d in (264, 3080)] + [(699, 4096), (700, 4096), (2100, 1032), (140000, 8), (65000, 64)])
 def test_one_launch_and_two(T, d):
     """Around the row counts that one launch takes."""
     for dt, rt in TYPES:
