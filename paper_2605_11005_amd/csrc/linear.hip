@@ -83,7 +83,7 @@ __global__ __launch_bounds__(GRAD_WAVES * WAVE) void act_grad(const int32_t* __r
 }
 
 // dz alone, 16 bytes a thread, for few rows, whose sums the products' launch forms by itself
-constexpr int DZ_THREADS = 256, FEW_SUM_ROWS = 1024;
+constexpr int DZ_THREADS = 256;
 template <typename T>
 __global__ __launch_bounds__(DZ_THREADS) void act_grad_few(const int32_t* __restrict__ off, int rows, int e_cnt, int N, int act,
                                                            const T* __restrict__ dy, const T* __restrict__ z, T* __restrict__ dz) {
@@ -221,9 +221,10 @@ int launch_linear_bwd(const LinearArgs& l, const void* dy, void* dx, int dx_accu
   float* const sums = (float*)(base + space.sums);
   int32_t* const setup = large ? (int32_t*)ws : nullptr;
   int rc;
-  // Few rows: the products' launch sums dy act'(z) by itself, so that without an activation there is no launch in front of it, and with one a short one.  us,
-  // before / so: 16 rows of 1024 to 1024 without 14.3 / 11.2, with silu 14.5 / 13.5, 300 rows 21.5 / 13.1 and 21.9 / 16.0.
-  const bool few = !large && l.rows <= FEW_SUM_ROWS;
+  // Few rows: the products' launch sums dy act'(z) by itself, so that without an activation there is no launch in front of it, and with one a short one.
+  // fp32's dz is not rounded: its columns are what db sums.  us, sums in front / so, gelu: bf16 200 rows of 1024 to 1024 22.7 / 15.7, 500 rows 25 / 19, 800
+  // rows 28 / 24, 1000 rows 29 / 30, of 520 to 776 27 / 34, 800 rows of 64 to 72 20 / 30; fp32 1000 rows of 1024 to 1024 53 / 47, of 520 to 776 41 / 32.
+  const bool few = !large && l.rows <= (bf16 ? 640 : 1024), of_dz = !bf16 && through && (dx || dw);
   if (l.rows > 0 && ((db && !few) || (through && (dx || dw)))) {
     rc = bf16 ? gradients<bf16_t>(l, dy, dz, db ? sums : nullptr, few, setup, s) : gradients<float>(l, dy, dz, db ? sums : nullptr, few, setup, s);
     if (rc) return rc;
@@ -232,7 +233,7 @@ int launch_linear_bwd(const LinearArgs& l, const void* dy, void* dx, int dx_accu
     HIP_CHECK_LAUNCH();
   }
   const void* const g = through ? dz : dy;
-  const BiasGrad bias = {l.offsets, l.rows, l.N, accumulate, sums, few ? dy : nullptr, l.z, l.act, db};
+  const BiasGrad bias = {l.offsets, l.rows, l.N, accumulate, sums, !few ? nullptr : of_dz ? dz : dy, l.z, of_dz ? MOE_ACT_NONE : l.act, db};
   if (!bf16) return launch_linear_bwd_f32(l, g, dx, dx_accumulate, dw, accumulate, bias, base + space.products, base + space.dw_parts, s);
   if (!large) return launch_linear_tiles_bwd(l, g, dx, dx_accumulate, dw, accumulate, bias, base + space.products, base + space.dw_parts, s);
   if (db) {
