@@ -26,6 +26,8 @@
 // two LDS buffers and two blocks per CU 87 + 176; splitting between the matrix instructions of one wavefront, which takes more
 // registers, 104 + 181; tiles of 128x64 95 + 199 (better only for a thousand rows and more per expert: 145 for 176 at 3000, d = f =
 // 1024).
+#include <algorithm>
+
 #include "bias_grad.h"
 #include "common.h"
 #include "kernels.h"
@@ -295,7 +297,7 @@ __device__ __forceinline__ void gemm_tile(const Args& p, int block, char* lds, i
     K = RAGGED_K ? p.rows : p.K;
   } else if (RAGGED_K) {
     const int total = p.e_cnt * m_tiles * n_tiles, share = (total + 7) / 8;
-    const int tile = TR::LINEAR ? (block / (8 * CHUNK) * 8 + block % 8) * CHUNK + block / 8 % CHUNK : block / 8 < share ? (block % 8) * share + block / 8 : total;
+    const int tile = TR::LINEAR ? (block / (8 * CHUNK) * 8 + (block + part) % 8) * CHUNK + block / 8 % CHUNK : block / 8 < share ? (block % 8) * share + block / 8 : total;
     if (tile >= total) return;
     e = tile / (m_tiles * n_tiles);
     mt = (tile - e * m_tiles * n_tiles) / n_tiles;
@@ -311,8 +313,13 @@ __device__ __forceinline__ void gemm_tile(const Args& p, int block, char* lds, i
   }
   const int col0 = nt * COLS;
   const auto col_of = [&](int i) { return WIDE && i && col0 + TN < p.N ? col0 + TN : col0; };        // (past the last column: the first tile again)
-  if (TR::LINEAR && p.parts.n > 1) {                     // whole k-tiles
-    const int per = ((K + TK - 1) / TK + p.parts.n - 1) / p.parts.n * TK;
+  int parts = p.parts.n;
+  if (MODE == LWG) {
+    parts = parts_of_expert<float>(p.off, K, parts);
+    if (part >= parts) return;
+  }
+  if (TR::LINEAR && parts > 1) {                         // whole k-tiles
+    const int per = ((K + TK - 1) / TK + parts - 1) / parts * TK;
     k_from = min(K, part * per);
     K = min(K - k_from, per);
   }
@@ -465,7 +472,7 @@ __device__ __forceinline__ void gemm_tile(const Args& p, int block, char* lds, i
     constexpr int I = decltype(which)::value;        // WIDE: of the two
     const int col = col0 + TN * I + wn * 32 + (lane & 31);
     if (col >= p.N) return;
-    if (TR::LINEAR && p.parts.n > 1) {
+    if (TR::LINEAR && parts > 1) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         const int row = row0 + wm * 32 + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3);
@@ -766,15 +773,22 @@ int launch_linear_bwd_f32(const LinearArgs& l, const void* dz, void* dx, int dx_
   const float all = f32_time((double)l.rows * l.K * l.N * ((have_dx ? 1 : 0) + (dw ? 1 : 0)));
   x.parts = {(float*)ws_dx, (size_t)l.rows * l.K, have_dx ? f32_parts(x_tiles, (l.N + TK - 1) / TK, all, wide) : 1};
   w.parts = {(float*)ws_dw, (size_t)l.e_cnt * l.K * l.N, dw ? f32_parts(w_tiles, (l.rows / l.e_cnt + TK - 1) / TK, all, wide) : 1};
+  // experts whose rows differ: parts, where one of six times the mean rows would take 14 us longer than all of them otherwise
+  const int mean_parts = w.parts.n;
+  const float longest = (float)((longest_rows(l) + TK - 1) / TK) * (wide ? WIDE_K_TILE : K_TILE);
+  if (dw && l.offsets && longest > all + 14.f) {
+    const long long most = (wide ? 2 : 4) * CUT_WORKGROUPS / w_tiles;
+    w.parts.n = std::max(mean_parts, (int)std::min<long long>(most, MOST_PARTS));
+  }
   g.x_blocks = (int)blocks8(x_tiles);
   g.w_blocks = l.offsets ? (int)((w_tiles + 8 * CHUNK - 1) / (8 * CHUNK) * 8 * CHUNK) : (int)blocks8(w_tiles);
   g.x_total = have_dx ? g.x_blocks * x.parts.n : 0;
   g.w_total = dw ? g.w_blocks * w.parts.n : 0;
-  g.w_first = 5ll * l.rows / w.parts.n > 6ll * l.e_cnt * l.N / x.parts.n;      // the longer tiles (see the experts' backward)
+  g.w_first = 5ll * l.rows / mean_parts > 6ll * l.e_cnt * l.N / x.parts.n;      // the longer tiles (see the experts' backward)
   const unsigned blocks = g.x_total + g.w_total + (db.db ? bias_blocks(l.N, l.e_cnt) : 0);
   if (blocks > 0) {
     ProfScope prof(have_dx && dw ? MOE_K_LINEAR_DX_DW : dw ? MOE_K_LINEAR_DW : have_dx ? MOE_K_LINEAR_DX : MOE_K_LINEAR_BIAS, s);
-    const auto kernel = wide ? gradients_f32<1, true> : few_f32(blocks) ? gradients_f32<2, false> : gradients_f32<1, false>;
+    const auto kernel = wide ? gradients_f32<1, true> : few_f32(blocks - (w.parts.n - mean_parts) * g.w_blocks) ? gradients_f32<2, false> : gradients_f32<1, false>;
     hipLaunchKernelGGL(kernel, dim3(blocks), dim3(NT), 0, s, g);
     HIP_CHECK_LAUNCH();
   }

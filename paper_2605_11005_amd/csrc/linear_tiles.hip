@@ -8,6 +8,8 @@
 // next half-way through its multiplication.  Where the tiles alone would not fill the chip the contraction is cut; a part's sums are stored
 // in fp32 and added in order by a launch behind (linear_join_*).
 // Every output is one chain of sums over ascending k per part.
+#include <algorithm>
+
 #include "bias_grad.h"
 #include "linear_finish.h"
 #include "linear_piece.h"
@@ -44,16 +46,16 @@ struct Tile { int e, mt, nt, first, end; };      // rows [first, end) of expert 
 // tile b of a part's list: an expert's tiles in bands of 8 row tiles, column tile next, row tile inside the band fastest, so that what an XCD
 // multiplies at a time shares panels
 template <int OP>
-__device__ __forceinline__ bool tile_of(const LinearArgs& l, const Product& p, int b, int lane, Tile& t) {
+__device__ __forceinline__ bool tile_of(const LinearArgs& l, const Product& p, int b, int part, int lane, Tile& t) {
   const int n_tiles = (p.N + QT - 1) / QT;
   int e = 0, at, m;
   t.first = 0;
   t.end = l.rows;
   if (OP == DW) {
     m = (p.M + QT - 1) / QT;
-    // an XCD takes an eighth of the list; where experts differ in rows, every eighth chunk of 32 tiles
+    // an XCD takes an eighth of the list; where experts differ in rows, every eighth chunk of 32 tiles, of the next part the XCD beside it
     const int total = l.e_cnt * m * n_tiles, share = (total + 7) / 8;
-    at = l.offsets ? (b / 256 * 8 + b % 8) * 32 + b / 8 % 32 : b / 8 < share ? b % 8 * share + b / 8 : total;
+    at = l.offsets ? (b / 256 * 8 + (b + part) % 8) * 32 + b / 8 % 32 : b / 8 < share ? b % 8 * share + b / 8 : total;
     if (at >= total) return false;
     e = at / (m * n_tiles);
     at -= e * m * n_tiles;
@@ -90,9 +92,9 @@ __device__ __forceinline__ void finish(const LinearArgs& l, const Product& p, in
 
 // eight columns of a row of a part
 template <int OP>
-__device__ __forceinline__ void store_out(const LinearArgs& l, const Product& p, int e, int part, size_t at, int col, const float* from) {
+__device__ __forceinline__ void store_out(const LinearArgs& l, const Product& p, int e, int parts, int part, size_t at, int col, const float* from) {
   const f32x4 lo = *reinterpret_cast<const f32x4*>(from), hi = *reinterpret_cast<const f32x4*>(from + 4);
-  if (p.parts.n > 1) {
+  if (parts > 1) {
     float* const to = p.parts.sums + part * p.parts.stride + at;
     *reinterpret_cast<f32x4*>(to) = lo;
     *reinterpret_cast<f32x4*>(to + 4) = hi;
@@ -186,7 +188,7 @@ __device__ __forceinline__ void multiply_short(const LinearArgs& l, const Produc
     const int in = 16 * q + (lane >> 2);
     if (in >= rows) break;
     const float* const from = slab + in * SHORT_PITCH + (lane & 3) * 8;
-    store_out<OP>(l, p, t.e, part, (size_t)(row0 + in) * p.N + out_col, out_col, from);
+    store_out<OP>(l, p, t.e, p.parts.n, part, (size_t)(row0 + in) * p.N + out_col, out_col, from);
   }
 }
 
@@ -196,14 +198,15 @@ __device__ __forceinline__ void multiply_tile(const LinearArgs& l, const Product
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = wave >> 1, wn = wave & 1;
   Tile t;
-  if (!tile_of<OP>(l, p, b, lane, t)) return;
+  if (!tile_of<OP>(l, p, b, part, lane, t)) return;
   if constexpr (OP != DW)
     if (t.end - t.first <= SHORT) return multiply_short<OP, STREAM>(l, p, t, part, lds);
   const int n0 = t.nt * QT;
   const int row0 = OP == DW ? t.mt * QT : t.first + t.mt * QT, row_end = OP == DW ? p.M : t.end;      // of the output
   // k-tiles [kt, kt1) of 64, of the whole contraction [0, depth)
-  const int depth = OP == DW ? t.end - t.first : p.K, all = (depth + QK - 1) / QK, per = (all + p.parts.n - 1) / p.parts.n;
-  const int kt0 = min(all, part * per), kt1 = min(all, kt0 + per);
+  const int depth = OP == DW ? t.end - t.first : p.K, parts = OP == DW ? parts_of_expert<bf16_t>(l.offsets, depth, p.parts.n) : p.parts.n;
+  if (OP == DW && part >= parts) return;
+  const int all = (depth + QK - 1) / QK, per = (all + parts - 1) / parts, kt0 = min(all, part * per), kt1 = min(all, kt0 + per);
 
   const uint32_t base = lds_addr(lds);
   QuarterKc a_kc, b_kc;
@@ -308,7 +311,7 @@ __device__ __forceinline__ void multiply_tile(const LinearArgs& l, const Product
     const int in = 8 * q + (lane >> 3), row = row0 + wm * 64 + in;
     if (row >= row_end) break;
     const float* from = slab + in * TILE_PITCH + (lane & 7) * 8;
-    store_out<OP>(l, p, t.e, part, ((size_t)(OP == DW ? t.e : 0) * p.M + row) * p.N + col, col, from);
+    store_out<OP>(l, p, t.e, parts, part, ((size_t)(OP == DW ? t.e : 0) * p.M + row) * p.N + col, col, from);
   }
 }
 
@@ -470,11 +473,15 @@ float plan_gradients(const LinearArgs& l, Product& x, Product& w, bool* outer, b
     if (x.parts.n > 1) { join = 3.f; parts += (double)x.parts.n * l.rows * l.K; }
   }
   if (w.C && !*outer) {
-    w.parts.n = chain_parts(w.tiles, kw, all);             // (experts' rows differ: parts of some may be empty)
-    const float c = (float)((kw + w.parts.n - 1) / w.parts.n) * CACHED.alone;
+    w.parts.n = chain_parts(w.tiles, kw, all);
+    // experts whose rows differ: parts, where one of six times the mean rows would take 14 us longer than all of them otherwise
+    const long long longest = (longest_rows(l) + QK - 1) / QK;
+    if (l.offsets && (float)longest * CACHED.alone > all + 14.f) w.parts.n = (int)most_parts(w.tiles, longest);
+    const int mean_parts = l.offsets ? (int)std::max(1ll, std::min<long long>(w.parts.n, kw / 8)) : w.parts.n;
+    const float c = (float)((kw + mean_parts - 1) / mean_parts) * CACHED.alone;
     *dx_first = chain >= c;
     chain = c > chain ? c : chain;
-    if (w.parts.n > 1) { join = 3.f; parts += (double)w.parts.n * l.e_cnt * l.K * l.N; }
+    if (w.parts.n > 1) { join = 3.f; parts += (double)mean_parts * l.e_cnt * l.K * l.N; }
   }
   return 6.f + (all > chain ? all : chain) + join + (float)(parts * (8.0 / 9e6));
 }

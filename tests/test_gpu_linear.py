@@ -169,6 +169,15 @@ def test_long_contractions(rows, dt, K, N):
     Case(rows, K, N, "gelu", dt, seed=K).check_both(accumulate=rows in (33, [130, 0, 70, 1, 5]))
 
 
+@pytest.mark.parametrize("dt", (BF16, F32))
+@pytest.mark.parametrize("rows", [[3000, 0, 511, 512, 1024, 1], [0, 0, 5000, 255, 256, 700, 1023], [40] * 20 + [6000]], ids=str)
+def test_weight_gradients_of_experts_that_differ(rows, dt):
+    """Some experts' rows are cut in parts in a launch where others' are not."""
+    print(f"case linear {rows} {dt}", flush=True)
+    for accumulate in (False, True):
+        Case(rows, 136, 72, "gelu", dt, seed=11).check_both(accumulate)
+
+
 @pytest.mark.parametrize("dt,N", [(BF16, 4104), (F32, 2052)])
 @pytest.mark.parametrize("rows", [8300, [5000, 3, 0, 3300]], ids=str)
 def test_gradients_of_large_activations(rows, dt, N):
