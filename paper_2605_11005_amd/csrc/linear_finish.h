@@ -39,13 +39,17 @@ __device__ __forceinline__ void store_to(void* p, size_t at, const float (&y)[VE
 
 // The forward's outputs at element `at`, columns col and on, of expert e from the sums: z, activation, residual
 template <typename T>
-__device__ __forceinline__ void finish_forward(const LinearArgs& l, int e, size_t at, int col, float (&y)[VEC<T>]) {
-  if (l.bias) add_from<T>(l.bias, (size_t)e * l.N + col, y);
+__device__ __forceinline__ void activate_forward(const LinearArgs& l, size_t at, float (&y)[VEC<T>]) {
   if (l.z) store_to<T>(l.z, at, y);
   with_activation(l.act, [&](auto a) {
 #pragma unroll
     for (int j = 0; j < VEC<T>; ++j) y[j] = act_value<decltype(a)::value, sizeof(T) == 2>(y[j]);
   });
+}
+template <typename T>
+__device__ __forceinline__ void finish_forward(const LinearArgs& l, int e, size_t at, int col, float (&y)[VEC<T>]) {
+  if (l.bias) add_from<T>(l.bias, (size_t)e * l.N + col, y);
+  activate_forward<T>(l, at, y);
   if (l.residual) add_from<T>(l.residual, at, y);
   store_to<T>(l.y, at, y);
 }

@@ -294,6 +294,22 @@ __device__ __forceinline__ void multiply_tile(const LinearArgs& l, const Product
     step(2);
     step(3);
   }
+  // FWD: residual and bias are on their way while the sums change places: one load after the other behind the stores takes 8192 rows of 256 to 8192
+  // with z and residual from 128 to 160 us.  (The gradients, 4096 rows of 2880 to 2880, so: 162 -> 178.)
+  const int col = n0 + wn * 64 + (lane & 7) * 8, first_row = row0 + wm * 64 + (lane >> 3);
+  const auto at_row = [&](int row) { return ((size_t)(OP == DW ? t.e : 0) * p.M + row) * p.N + col; };
+  const bf16_t* const old = parts > 1 ? nullptr : (const bf16_t*)l.residual;
+  u32x4 pre[8];
+  float bias[8];
+#pragma unroll
+  for (int j = 0; j < 8; ++j) bias[j] = 0.f;
+  if (OP == FWD && col < p.N) {
+    if (parts == 1 && l.bias) values(*reinterpret_cast<const u32x4*>((const bf16_t*)l.bias + (size_t)t.e * l.N + col), bias);
+    if (old)
+#pragma unroll
+      for (int q = 0; q < 8; ++q)
+        if (first_row + 8 * q < row_end) pre[q] = *reinterpret_cast<const u32x4*>(old + at_row(first_row + 8 * q));
+  }
   // Element 4 g + q of a lane's block is row 8 g + 4 (lane / 32) + q, column lane % 32: through the wavefront's own slab to eight columns a lane.
   float* const slab = reinterpret_cast<float*>(lds) + wave * (SLAB / 4);
 #pragma unroll
@@ -304,14 +320,35 @@ __device__ __forceinline__ void multiply_tile(const LinearArgs& l, const Product
       for (int r = 0; r < 16; ++r)
         slab[(32 * i + 8 * (r >> 2) + 4 * (lane >> 5) + (r & 3)) * TILE_PITCH + 32 * j + (lane & 31)] = acc[i][j][r];
   __builtin_amdgcn_wave_barrier();
-  const int col = n0 + wn * 64 + (lane & 7) * 8;
   if (col >= p.N) return;
+  if constexpr (OP == FWD) {
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+      const int row = first_row + 8 * q;
+      if (row >= row_end) break;
+      const float* const from = slab + (8 * q + (lane >> 3)) * TILE_PITCH + (lane & 7) * 8;
+      if (parts > 1) {
+        store_out<OP>(l, p, t.e, parts, part, at_row(row), col, from);
+        continue;
+      }
+      float y[8], add[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) y[j] = from[j] + bias[j];
+      activate_forward<bf16_t>(l, at_row(row), y);
+      if (old) {
+        values(pre[q], add);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) y[j] += add[j];
+      }
+      store_to<bf16_t>(l.y, at_row(row), y);
+    }
+  } else {
 #pragma unroll 2
-  for (int q = 0; q < 8; ++q) {
-    const int in = 8 * q + (lane >> 3), row = row0 + wm * 64 + in;
-    if (row >= row_end) break;
-    const float* from = slab + in * TILE_PITCH + (lane & 7) * 8;
-    store_out<OP>(l, p, t.e, parts, part, ((size_t)(OP == DW ? t.e : 0) * p.M + row) * p.N + col, col, from);
+    for (int q = 0; q < 8; ++q) {
+      const int row = first_row + 8 * q;
+      if (row >= row_end) break;
+      store_out<OP>(l, p, t.e, parts, part, at_row(row), col, slab + (8 * q + (lane >> 3)) * TILE_PITCH + (lane & 7) * 8);
+    }
   }
 }
 
