@@ -37,7 +37,7 @@ __device__ __forceinline__ void store_to(void* p, size_t at, const float (&y)[VE
   *reinterpret_cast<u32x4*>((T*)p + at) = words(y);
 }
 
-// The forward's outputs at element `at`, columns col and on, of expert e from the sums: z, activation, residual
+// From sums with their bias: z is stored, and they become act(z)
 template <typename T>
 __device__ __forceinline__ void activate_forward(const LinearArgs& l, size_t at, float (&y)[VEC<T>]) {
   if (l.z) store_to<T>(l.z, at, y);
@@ -46,6 +46,7 @@ __device__ __forceinline__ void activate_forward(const LinearArgs& l, size_t at,
     for (int j = 0; j < VEC<T>; ++j) y[j] = act_value<decltype(a)::value, sizeof(T) == 2>(y[j]);
   });
 }
+// The forward's outputs at element `at`, columns col and on, of expert e from the sums
 template <typename T>
 __device__ __forceinline__ void finish_forward(const LinearArgs& l, int e, size_t at, int col, float (&y)[VEC<T>]) {
   if (l.bias) add_from<T>(l.bias, (size_t)e * l.N + col, y);
