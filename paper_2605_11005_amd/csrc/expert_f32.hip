@@ -530,31 +530,28 @@ __device__ __forceinline__ void gemm_tile(const Args& p, int block, char* lds, i
       }
     }
   };
-  auto finish = [&](uint32_t todo, float scale) {
-    finish_tile(todo, scale, Int<0>{});
-    if constexpr (WIDE) finish_tile(todo, scale, Int<1>{});
-  };
   // Outputs with an infinity, a NaN, a number beyond 2^96 or a sum beyond 2^64 in them have sums that are no numbers.  Those, and no
   // others of their tile, come from the operands as they are: what a row or column holds does not show in its neighbours' bits.
   // (With one in every tile the six GEMMs of 3000 rows, d = 520, f = 776, take 178 + 360 us for 90 + 175.)
   // So do all weight gradients of an expert with one or two rows, which the terms would not round as well (EXACT_ROWS).
+  // (The two outputs of a dual tile, of the same row and column, come again together; the two tiles of a WIDE one each for itself.)
   const bool exact = RAGGED_K && K <= EXACT_ROWS;
-  uint32_t lost = exact ? 0xFFFFu : 0u;
+  constexpr int TILES = WIDE ? 2 : 1;
+  uint32_t lost[TILES];
+#pragma unroll
+  for (int w = 0; w < TILES; ++w) lost[w] = exact ? 0xFFFFu : 0u;
   if (!exact) {
     sums(Int<1>{});
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      bool whole = true;
+    for (int r = 0; r < 16; ++r)
 #pragma unroll
-      for (int i = 0; i < NB; ++i) whole &= fabsf(acc[i][0][r] + acc[i][1][r]) <= 3.402823466e38f;
-      lost |= whole ? 0u : 1u << r;
-    }
+      for (int i = 0; i < NB; ++i) lost[WIDE ? i : 0] |= fabsf(acc[i][0][r] + acc[i][1][r]) <= 3.402823466e38f ? 0u : 1u << r;
   }
-  const bool again = __syncthreads_or(lost != 0);
-  finish(~lost, UNSCALE);
+  const bool again = __syncthreads_or((lost[0] | lost[TILES - 1]) != 0);
+  static_for<TILES>([&](auto w) { finish_tile(~lost[decltype(w)::value], UNSCALE, w); });
   if (again) {
     sums(Int<0>{});
-    finish(lost, 1.f);
+    static_for<TILES>([&](auto w) { finish_tile(lost[decltype(w)::value], 1.f, w); });
   }
 }
 

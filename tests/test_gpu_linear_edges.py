@@ -31,3 +31,34 @@ def test_gelu_far_below_zero_keeps_its_digits(rows):
     off = np.abs(y - ref)
     bad = ~(off <= (2.0 ** -8 + 2.0 ** -13 + 2.0 ** -21) * np.abs(ref))
     assert not bad.any(), (z[bad.any(0)], (off / np.maximum(np.abs(ref), 1e-300)).max())
+
+
+def fp32_products(x, w, dy):
+    rows, K, N = *x.shape, w.shape[1]
+    new = lambda *s: torch.full(s, float("nan"), device="cuda")  # noqa: E731
+    y, dx, dw = new(rows, N), new(rows, K), new(K, N)
+    ws = torch.empty(max(B.moe_workspace_bytes(which, B.MOE_F32, 0, 0, K, N, 1, rows) for which in (B.WS_LINEAR_FWD, B.WS_LINEAR_BWD)), dtype=torch.uint8,
+                     device="cuda")
+    B.moe_linear_fwd(x, None, w, None, B.ACT_NONE, None, None, y, ws)
+    B.moe_linear_bwd(x, None, dy, None, w, B.ACT_NONE, dx, dw, None, False, ws)
+    return y, dx, dw
+
+
+def test_fp32_infinities_do_not_show_in_the_other_tile_of_a_pair():
+    """4200 rows of 136 to 2060 take tiles of 128 columns, two of 64 beside each other.  What an infinite weight or gradient makes infinite is formed again
+    from the operands: all other outputs keep their bits."""
+    g = torch.Generator().manual_seed(2)
+    r = lambda *s: (torch.rand(s, generator=g) + 0.5).cuda()  # noqa: E731
+    x, w, dy = r(4200, 136), r(136, 2060), r(4200, 2060)
+    y, dx, dw = fp32_products(x, w, dy)
+    infinite = w.clone()
+    infinite[5, 3] = float("inf")             # column 3 of y, column 5 of dx
+    y2, dx2, _ = fp32_products(x, infinite, dy)
+    others = lambda t, at: torch.cat([t[:, :at], t[:, at + 1:]], 1)  # noqa: E731
+    assert torch.isposinf(y2[:, 3]).all() and torch.equal(others(y, 3), others(y2, 3))
+    assert torch.isposinf(dx2[:, 5]).all() and torch.equal(others(dx, 5), others(dx2, 5))
+    infinite = dy.clone()
+    infinite[7, 100] = float("inf")           # column 100 of dw, row 7 of dx
+    _, dx3, dw3 = fp32_products(x, w, infinite)
+    assert torch.isposinf(dw3[:, 100]).all() and torch.equal(others(dw, 100), others(dw3, 100))
+    assert torch.isposinf(dx3[7]).all() and torch.equal(dx[:7], dx3[:7]) and torch.equal(dx[8:], dx3[8:])
