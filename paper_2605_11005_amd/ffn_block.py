@@ -8,7 +8,7 @@ x is the block's input, the normalised residual stream h; x' is the next block's
 y = None, and its gradient moe_layer_norm_bwd with the stream itself.
 
 training: run_ffn_forward, and run_ffn_backward from the last block to the first: its `dh` and `dx` are the `dh_out` and `dn` of the block before.
-serving : run_ffn_forward with buffers without gradients.
+serving : run_ffn_forward with buffers without gradients, of as many tokens as these are for, or fewer.
 Nothing synchronises with the host between the calls.
 """
 from __future__ import annotations
@@ -21,7 +21,7 @@ from .layer import torch_dtype
 
 class FfnBlockBuffers:
     """All outputs, saved activations and scratch of one block's step, allocated once.  shared_f: width of the dense expert.  residual: the type of the
-    residual stream, the tokens' own or fp32."""
+    residual stream, the tokens' own or fp32.  Without gradients they serve up to wl.T tokens; a training step takes wl.T."""
 
     def __init__(self, wl, cap: int, shared_f: int, act: str = "gelu", residual=None, grads: bool = True, device="cuda"):
         dt, T, d, k, f, ec = torch_dtype(wl), wl.T, wl.d, wl.k, wl.f, wl.e_cnt
@@ -48,8 +48,14 @@ class FfnBlockBuffers:
                            ws2=new(shared_f, d), bs2=new(d), w=new(d), b=new(d))
             uses += [ws(B.WS_LINEAR_BWD, 0, 0, K, N, n, rows) for K, N, n, rows in self._products(wl, cap, shared_f)]
             uses.append(ws(B.WS_LAYER_NORM, T, 0, d, 0, 0, 0))
-        uses += [ws(B.WS_DISPATCH, T, k, d, f, ec, cap), ws(B.WS_ROUTER, T, k, d, f, wl.E, cap)]
+        # (what the router's logits take is not monotonic in the tokens: of all numbers of them that may come the largest)
+        uses += [ws(B.WS_DISPATCH, T, k, d, f, ec, cap)] + [ws(B.WS_ROUTER, t, k, d, f, wl.E, cap) for t in ((T,) if grads else range(T + 1))]
         self.ws = new(max(uses), dtype=torch.uint8)        # one after the other on a stream: the calls take turns
+
+    def of_tokens(self, T):
+        """What the forward writes per token; without gradients T rows of each (refused by the calls where there are fewer)."""
+        per_token = self.logits, self.topk_idx, self.topk_w, self.inv, self.sa, self.y, self.h, self.x
+        return per_token if self.grads or len(self.y) == T else tuple(t[:T] for t in per_token)
 
     @staticmethod
     def _products(wl, cap, shared_f):
@@ -57,16 +63,18 @@ class FfnBlockBuffers:
 
 
 def run_ffn_forward(wl, w, h, x, buf: FfnBlockBuffers, eps: float = 1e-5):
-    """w: "wr", "w1", "b1", "w2", "b2" of the experts, "ws1", "bs1", "ws2", "bs2" of the dense one, "w", "b" of the norm.  -> buf.h, buf.x"""
-    B.moe_router_fwd(x, w["wr"], buf.logits, buf.ws)
-    B.moe_route(buf.logits, wl.k, wl.gate_mode, wl.e_lo, wl.e_cnt, buf.topk_idx, buf.topk_w, buf.counts)
-    B.moe_dispatch(x, wl.k, buf.topk_idx, None, wl.e_lo, wl.e_cnt, buf.offsets, buf.perm, buf.inv, False, buf.xp, buf.ws)
+    """w: "wr", "w1", "b1", "w2", "b2" of the experts, "ws1", "bs1", "ws2", "bs2" of the dense one, "w", "b" of the norm.  -> buf.h, buf.x, of which fewer
+    tokens than the buffers are for (without gradients) take the first rows"""
+    logits, topk_idx, topk_w, inv, sa, y, h_out, x_out = buf.of_tokens(x.shape[0])
+    B.moe_router_fwd(x, w["wr"], logits, buf.ws)
+    B.moe_route(logits, wl.k, wl.gate_mode, wl.e_lo, wl.e_cnt, topk_idx, topk_w, buf.counts)
+    B.moe_dispatch(x, wl.k, topk_idx, None, wl.e_lo, wl.e_cnt, buf.offsets, buf.perm, inv, False, buf.xp, buf.ws)
     B.moe_linear_fwd(buf.xp, buf.offsets, w["w1"], w["b1"], buf.act, None, buf.z, buf.a, buf.ws)
     B.moe_linear_fwd(buf.a, buf.offsets, w["w2"], w["b2"], B.ACT_NONE, None, None, buf.o, buf.ws)
-    B.moe_combine(buf.o, buf.inv, buf.topk_w, buf.y)
-    B.moe_linear_fwd(x, None, w["ws1"], w["bs1"], buf.act, None, buf.sz, buf.sa, buf.ws)
-    B.moe_linear_fwd(buf.sa, None, w["ws2"], w["bs2"], B.ACT_NONE, buf.y, None, buf.y, buf.ws)      # onto what the experts gave
-    B.moe_layer_norm_fwd(buf.y, h, w["w"], w["b"], eps, buf.h, buf.x, buf.mean, buf.rstd)
+    B.moe_combine(buf.o, inv, topk_w, y)
+    B.moe_linear_fwd(x, None, w["ws1"], w["bs1"], buf.act, None, buf.sz, sa, buf.ws)
+    B.moe_linear_fwd(sa, None, w["ws2"], w["bs2"], B.ACT_NONE, y, None, y, buf.ws)      # onto what the experts gave
+    B.moe_layer_norm_fwd(y, h, w["w"], w["b"], eps, h_out, x_out, buf.mean, buf.rstd)
 
 
 def run_ffn_backward(wl, w, x, buf: FfnBlockBuffers, dh_out, dn, accumulate: bool = False):
