@@ -353,7 +353,8 @@ int moe_layer_norm_bwd(const void* h_out, const void* w, const float* mean, cons
  *   NULL: not formed.  accumulate == 1 adds to dw and db; with 0 an expert without rows gets zeros.  dx_accumulate == 1 adds to dx (an input that
  *   something else reads as well).
  *   ws: moe_workspace_bytes(MOE_WS_LINEAR_BWD, dtype, 0, 0, K, N, e_cnt, cap) bytes, 256-byte aligned
- * All sums are fp32.  In bf16 the products take dz rounded to bf16; db sums it unrounded.  relu's slope at 0 is 0.
+ * All sums are fp32.  In bf16 the products take dz rounded to bf16, as a bf16 tensor would hold it (with an activation dx and dw are off by 2.35e-3 of their
+ * root mean square for the 1.66e-3 of their own rounding; an fp32 layer keeps all of dz); db sums it unrounded.  relu's slope at 0 is 0.
  * Results are bit-reproducible from run to run.  fp32 products are those of moe_expert_fwd and _bwd.
  * Errors of both: EINVAL (NULL, negative sizes, unknown dtype or act, offsets NULL with e_cnt != 1, pointers not 16-byte aligned), EUNSUPPORTED (bf16
  * with K % 8 != 0 or N % 8 != 0, fp32 with % 4, K or N > MOE_MAX_LINEAR, e_cnt > MOE_MAX_LOCAL, 2^22 tiles of 64 x 64 or more in y, x or the

@@ -5,9 +5,9 @@
 // through registers alone: a lane loads C = 8 (or 4) columns of each of eight rows, and column j of that block is its operand of the j-th of C
 // 16x16x32 instructions, in which row i of the instruction stands for column C i + j of the strip.  The sums of a lane's C instructions
 // are then C consecutive columns of one row of x.
-// A CU takes in about 33 GB/s of weights however many of its wavefronts ask for them (4 rows of 4096 to 14336: 31 to 33 us with 4, 8 and 16 wavefronts
-// for each of 112 strips), so what counts is how many CUs ask: narrower strips, or strips cut along the contraction, whose parts store fp32 sums
-// that a second launch adds in order and finishes (plan_of).
+// What a CU takes in of weights does not go by how many of its wavefronts ask for them: 33 GB/s with 4, 8 and 16 wavefronts for each of 112 strips (4 rows of
+// 4096 to 14336, 31 to 33 us), 44 GB/s where 32 CUs have a strip each (14336 to 4096, 83 us).  So what counts is how many CUs ask: narrower strips, or
+// strips cut along the contraction, whose parts store fp32 sums that a second launch adds in order and finishes (plan_of).
 #include "linear_finish.h"
 #include "linear_piece.h"
 
@@ -162,7 +162,8 @@ inline float strips_time(long long strips, float bytes, float chip, float cu) {
   return 0.5f * rounds + (memory > own ? memory : own);
 }
 // Columns of a lane and parts of the contraction, by their time and that of the launch that adds the parts up.  How many experts have rows is not
-// known here: the mean over counts from half of what may to all.  Rows of 64 columns come a little slower, from memory and into a CU.
+// known here: the mean over counts from half of what may to all.  Rows of 64 columns come a little slower, from memory and into a CU.  (45 GB/s into a CU
+// is what few strips get; for 112 whole ones the model says 24 us where 32 are measured, and cuts them all the same.)
 // One row, us, strips of 128 whole / of 64 whole / of 128 in two parts / in eight: 4096 to 14336 31.9 / 26.8 / 25.8 / 26.0; 14336 to 4096 82.8 / 61.1 / 48.4
 // / 26.6; 4096 to 1536 17.3 / 13.4 / 12.6 / 8.4; 768 to 4096 5.6 / 5.2 / 7.6 / 7.7.  128 rows of 32 experts of 7168 to 2048, strips of 128 whole / in two /
 // in four: 14 of them with rows 70.7 / 75.9 / 77.8, 16 75.9 / 77.4 / 81.3, 17 119.9 / 98.2 / 91.6, 20 119.6 / 102.1 / 99.7, 24 126 / 114 / 117, 32
