@@ -17,9 +17,10 @@ __device__ __forceinline__ void clear(int32_t* words) {
 __global__ void linear_setup(int32_t* words) { clear(words); }
 
 // dz = dy act'(z), rounded to the type that the products take, and the column sums of what it was before, over 64 rows of an expert by
-// 64 lanes' 16 bytes.  (In bf16 the matrix instruction takes both operands so, and dz's rest as a second operand would double both products.  Behind an
-// activation dx and dw are then off by 2.35e-3 of their root mean square, where the rounding of their own values takes 1.66e-3: 16384 rows of 7168 to 2048,
-// gelu, against 64 bits.  Without one dz is dy, and nothing is rounded.)  Eight wavefronts take every eighth row each; their sums meet in ascending order.  HBM bound: dy and z in, dz out.
+// 64 lanes' 16 bytes.  Eight wavefronts take every eighth row each; their sums meet in ascending order.  HBM bound: dy and z in, dz out.
+// (The bf16 matrix instruction takes both operands in bf16, and dz's rest as a second operand would double both products.  Behind an activation dx and dw
+// are then off by 2.35e-3 of their root mean square, where the rounding of their own values takes 1.66e-3: 16384 rows of 7168 to 2048, gelu, against
+// 64 bits.  Without one dz is dy, and nothing is rounded.)
 // STREAM: with an activation neither dy nor z is read again, and dz is.  Where they take half of the Infinity Cache and more, loads that leave no trace
 // there bring a whole backward of 16384 rows of 256 to 4096 from 176 to 158 us, of 2048 to 7168 from 952 to 926; tensors that lie in the cache already are
 // not kept by them: 4096 rows of 1024 to 4096 101 -> 93 us from memory, but 90 -> 93 in a loop over the same ones.
